@@ -398,6 +398,117 @@ GS_API gs_status gs_attention_scores(const void* Yq, const void* Yk, int in_dtyp
                               unsigned flags, void* stream);
 
 /*
+ * Cross attention: queries read the keys and values of an encoder's states, a
+ * sequence of another length (Sec. 2.2 attention score with the weights applied to
+ * values; Sec. 3.2: on Gram-loc rows the scores, and so the weights, are those of the
+ * full vectors).  For sequence b, query head h and key head g = h / (Hq / Hkv):
+ *     s_ij = scale * <Q[b,i,h], K[b,j,g]>,   j valid:  j < key_lens[b] and key_mask[b,j] != 0
+ *     lse_i = log sum_{j valid} exp(s_ij),   O[b,i,h] = sum_{j valid} exp(s_ij - lse_i) V[b,j,g]
+ * A row without a valid key (or whose valid logits are all -inf) is O = 0, lse = -inf; a
+ * row with a valid logit that is NaN or +inf is NaN.  Keys and values that are not
+ * valid are never used, whatever they hold.
+ */
+typedef struct gs_heads { /* element (b, l, h, c) of a B x L x H x width array           */
+    void* data;           /* device pointer (data = NULL: an empty array)                */
+    long long batch, row, head; /* element strides >= 0 of b, l, h; c has stride 1.  Inputs
+                             may repeat memory (stride 0: states that all sequences
+                             share); outputs may not.                                 */
+} gs_heads;
+
+typedef struct gs_attn {
+    int dtype;            /* GS_F32 or GS_BF16: every array but lse                      */
+    int B, Lq, Lk;        /* sequences, query rows and keys of each (0 allowed)           */
+    int Hq, Hkv;          /* query heads and key heads, Hkv divides Hq                   */
+    int dk, dv;           /* widths of a head's queries / keys and values, 1 to 128       */
+    float scale;          /* finite and > 0                                              */
+    const int* key_lens;  /* B keys to read of each sequence (NULL: Lk); values outside
+                             [0, Lk] count as the nearer end                             */
+    const unsigned char* key_mask; /* B x Lk, 0 = not read (NULL: all)                   */
+    long long ld_mask;    /* row stride >= Lk, or 0: one row for every sequence          */
+    unsigned flags;       /* GS_PATH_*                                                   */
+} gs_attn;
+
+/*
+ * Bytes of workspace that gs_cross_attention (backward = 0) or
+ * gs_cross_attention_backward (backward != 0) needs on the current device for a
+ * problem of these sizes, types and flags (0: none).  The pointers in *a are not read.
+ */
+GS_API gs_status gs_cross_attention_workspace(const gs_attn* a, int backward, long long* bytes);
+
+/*
+ * O (B x Lq x Hq x dv) and, when lse is not NULL, lse (B x Hq x Lq fp32, dense: the
+ * natural logarithm above, which the backward pass reads).  O must not overlap an input.
+ * workspace: a 16-byte aligned device buffer of gs_cross_attention_workspace's
+ * size, overwritten; calls that may run at the same time (on two streams, or in two graphs that
+ * may be launched together) need one each.
+ * Tensor-core path: GS_BF16 with data on 16-byte boundaries and strides that are
+ * multiples of 8 elements; logits, statistics and sums in fp32, weights rounded to
+ * bf16 for the product with the values.  Otherwise fp32 CUDA cores.  Results do not depend on
+ * what else runs, and a call repeated gives the same bits.
+ * Errors: GS_ERR_INVALID_ARG (null pointer, unknown type or path, scale), GS_ERR_SHAPE
+ * (sizes, strides, workspace too small), GS_ERR_ALIGNMENT (a forced
+ * tensor-core path with unaligned data; a workspace off a 16-byte boundary),
+ * GS_ERR_UNSUPPORTED (a width above 128; a forced tensor-core path with GS_F32 or more than 128 query
+ * heads to a key head), GS_ERR_CUDA.
+ */
+GS_API gs_status gs_cross_attention(const gs_attn* a, const gs_heads* Q, const gs_heads* K, const gs_heads* V,
+                                    const gs_heads* O, float* lse, void* workspace, long long workspace_bytes,
+                                    void* stream);
+
+/*
+ * Gradient of gs_cross_attention: with P_ij = exp(s_ij - lse_i) and
+ * D_i = <dO_i, O_i>, dS_ij = P_ij (<dO_i, V_j> - D_i),
+ *     dV_j = sum_i P_ij dO_i,  dK_j = scale sum_i dS_ij Q_i,  dQ_i = scale sum_j dS_ij K_j,
+ * the sums over i running over the query heads that share the key head.  O and
+ * lse are the forward call's.  dQ, dK, dV have the shapes of Q, K, V and type dtype; keys
+ * that are not valid get zeros, rows without a valid key zeros in dQ.  Where inputs repeat
+ * memory (stride 0), the gradients still come one per index: the caller sums them.
+ * Deterministic: no atomics.  Workspace, paths and errors as gs_cross_attention.
+ */
+GS_API gs_status gs_cross_attention_backward(const gs_attn* a, const gs_heads* Q, const gs_heads* K,
+                                             const gs_heads* V, const gs_heads* O, const float* lse,
+                                             const gs_heads* dO, const gs_heads* dQ, const gs_heads* dK,
+                                             const gs_heads* dV, void* workspace, long long workspace_bytes,
+                                             void* stream);
+
+/*
+ * Draws one entry of each score row (Sec. 2.2: the hard decision on scores, taken at
+ * random in proportion to their softmax; argmax when temperature = 0).  S is N x M
+ * (s_dtype GS_F32 or GS_BF16, row stride lds >= M, or 0: N draws from one row), U holds N numbers of
+ * [0, 1), the randomness.  With T the row's temperature, m its largest score and
+ * w_i = exp((s_i - m) / T):
+ *   1. top_k: only the k largest scores (1 <= k < M; other k: all), equal scores by
+ *      lowest index first;
+ *   2. top_p: of these, in the same order, the shortest run whose weight is at least
+ *      top_p times their whole weight (top_p >= 1 or NaN: all; never none);
+ *   3. min_p: of these, the ones with w_i >= min_p (min_p <= 0 or NaN: all; the largest
+ *      always stays);
+ *   4. index[n] = the first i, in index order, whose running kept weight exceeds
+ *      U[n] times the kept weight; prob[n] = w_i / the kept weight.
+ * Scores that are -inf or NaN are never drawn (a row of nothing else: index -1,
+ * prob 0); beside a +inf only +infs are.  T = 0 (or negative or NaN): index = the first of the
+ * largest scores, prob 1.  U is taken as 0 where it is negative or NaN, and as the largest fp32
+ * below 1 from 1 on.
+ * Weights are 64-bit fixed point numbers: exp to a relative error below 2^-38 of the largest
+ * weight's scale, sums exact in any order, so that a draw differs from exact arithmetic's
+ * only where U lies that close to a border.
+ * The four settings come as one number for all rows or, where the pointer is not
+ * NULL, one per row (device arrays of N).  index (N int32) and prob (N fp32) are
+ * optional, not both NULL.  N = 0 is a no-op.  No workspace.
+ * Errors: GS_ERR_INVALID_ARG, GS_ERR_SHAPE (N < 0, M < 1 or above 2^19, 0 < lds < M),
+ * GS_ERR_CUDA.
+ */
+typedef struct gs_sampling {
+    float temperature, top_p, min_p;
+    int top_k;
+    const float *temperature_rows, *top_p_rows, *min_p_rows; /* N each or NULL */
+    const int* top_k_rows;
+} gs_sampling;
+
+GS_API gs_status gs_sample_scores(const void* S, int s_dtype, long long N, int M, long long lds,
+                                  const gs_sampling* how, const float* U, int* index, float* prob, void* stream);
+
+/*
  * Project + similarity that allocates nothing (the paper has no counterpart;
  * this is a deployment variant).  For callers that cannot call cudaMalloc:
  * code running under a CUDA graph capture that forbids allocation, plugins

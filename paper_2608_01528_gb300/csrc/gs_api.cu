@@ -9,6 +9,7 @@
 #include <algorithm>
 
 #include "gs_internal.h"
+#include "gs_xattn.h"
 
 namespace {
 
@@ -176,7 +177,7 @@ bool big_gemm(long long m, long long n, long long k) { return m >= 512 && 2.0 * 
 
 extern "C" {
 
-int gs_version(void) { return 100; }
+int gs_version(void) { return 200; }
 
 const char* gs_status_string(gs_status s) {
     switch (s) {
@@ -862,6 +863,145 @@ gs_status gs_attention_scores(const void* Yq, const void* Yk, int in_dtype, int 
         if (e != cudaSuccess) return from_cuda(e);
     }
     return GS_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+// Strides of an array of B x L x H x w elements: non-negative, and (outputs) no two elements alike as far as
+// a stride of 0 tells.
+bool valid_heads(const gs_heads* v, int B, int L, int H, bool output) {
+    if (!v || v->batch < 0 || v->row < 0 || v->head < 0) return false;
+    return !output || ((v->batch > 0 || B <= 1) && (v->row > 0 || L <= 1) && (v->head > 0 || H <= 1));
+}
+gs::HeadView view_of(const gs_heads* v) { return {(char*)v->data, v->batch, v->row, v->head}; }
+
+// The checks that both calls and the workspace query share; fills what the kernels take.
+gs_status attn_args(const gs_attn* p, gs::XattnArgs& a) {
+    if (!p || !valid_path(p->flags)) return GS_ERR_INVALID_ARG;
+    if (p->dtype != GS_F32 && p->dtype != GS_BF16) return GS_ERR_INVALID_ARG;
+    if (!isfinite(p->scale) || !(p->scale > 0.f)) return GS_ERR_INVALID_ARG;
+    if (p->B < 0 || p->Lq < 0 || p->Lk < 0 || p->Hq < 1 || p->Hkv < 1 || p->Hq % p->Hkv || p->dk < 1 || p->dv < 1)
+        return GS_ERR_SHAPE;
+    if (p->dk > 128 || p->dv > 128) return GS_ERR_UNSUPPORTED;
+    if (p->key_mask && p->ld_mask != 0 && p->ld_mask < p->Lk) return GS_ERR_SHAPE;
+    // block and row numbers are 32-bit, positions stay clear of that limit when a tile is added
+    const long long limit = 0x7fffffffLL, far = limit - 1024;
+    if (p->Lk > far || (long long)p->Lq * (p->Hq / p->Hkv) > far || (long long)p->B * p->Hq > limit) return GS_ERR_SHAPE;
+    if ((long long)p->B * p->Hq * p->Lq > limit || (long long)p->B * p->Hkv * p->Lk > limit) return GS_ERR_SHAPE;
+    a = gs::XattnArgs{};
+    a.dtype = p->dtype;
+    a.B = p->B; a.Lq = p->Lq; a.Lk = p->Lk; a.Hq = p->Hq; a.Hkv = p->Hkv; a.G = p->Hq / p->Hkv;
+    a.dk = p->dk; a.dv = p->dv;
+    a.rows = (long long)a.Lq * a.G;
+    a.scale = p->scale;
+    a.lens = p->key_lens;
+    a.mask = p->key_mask;
+    a.ldm = p->ld_mask;
+    a.splits = a.rsplits = 1;
+    return GS_OK;
+}
+
+gs_status attn_device(int& dev, int& sms) {
+    if (cudaGetDevice(&dev) != cudaSuccess) return GS_ERR_CUDA;
+    if (!device_supported(dev)) return GS_ERR_UNSUPPORTED;
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1) return GS_ERR_CUDA;
+    return GS_OK;
+}
+
+gs_status attn_workspace(const float* ws, long long bytes, long long floats) {
+    if (floats == 0) return GS_OK;
+    if (!ws) return GS_ERR_INVALID_ARG;
+    if ((uintptr_t)ws % 16) return GS_ERR_ALIGNMENT;
+    return bytes < 4 * floats ? GS_ERR_SHAPE : GS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+gs_status gs_cross_attention_workspace(const gs_attn* p, int backward, long long* bytes) {
+    if (!bytes) return GS_ERR_INVALID_ARG;
+    *bytes = 0;
+    gs::XattnArgs a;
+    gs_status st = attn_args(p, a);
+    if (st != GS_OK) return st;
+    int dev = 0, sms = 0;
+    if ((st = attn_device(dev, sms)) != GS_OK) return st;
+    gs::xattn_simt_plan(a, backward != 0, sms);
+    *bytes = 4 * (backward ? gs::xattn_ws_backward(a) : gs::xattn_ws_forward(a));
+    return GS_OK;
+}
+
+gs_status gs_cross_attention(const gs_attn* p, const gs_heads* Q, const gs_heads* K, const gs_heads* V,
+                             const gs_heads* O, float* lse, void* workspace, long long workspace_bytes,
+                             void* stream) {
+    gs::XattnArgs a;
+    gs_status st = attn_args(p, a);
+    if (st != GS_OK) return st;
+    if (!Q || !K || !V || !O) return GS_ERR_INVALID_ARG;
+    if (!valid_heads(Q, a.B, a.Lq, a.Hq, false) || !valid_heads(K, a.B, a.Lk, a.Hkv, false) ||
+        !valid_heads(V, a.B, a.Lk, a.Hkv, false) || !valid_heads(O, a.B, a.Lq, a.Hq, true))
+        return GS_ERR_SHAPE;
+    if (a.B == 0 || a.Lq == 0) return GS_OK;
+    if (!Q->data || !O->data || (a.Lk > 0 && (!K->data || !V->data))) return GS_ERR_INVALID_ARG;
+    int dev = 0, sms = 0;
+    if ((st = attn_device(dev, sms)) != GS_OK) return st;
+    a.q = view_of(Q); a.k = view_of(K); a.v = view_of(V); a.o = view_of(O);
+    a.lse = lse;
+    a.ws = (float*)workspace;
+    cudaStream_t s = (cudaStream_t)stream;
+    if (p->flags == GS_PATH_TENSOR) return GS_ERR_UNSUPPORTED;
+    gs::xattn_simt_plan(a, false, sms);
+    if ((st = attn_workspace(a.ws, workspace_bytes, gs::xattn_ws_forward(a))) != GS_OK) return st;
+    return from_cuda(gs::launch_xattn_simt(a, s));
+}
+
+gs_status gs_cross_attention_backward(const gs_attn* p, const gs_heads* Q, const gs_heads* K, const gs_heads* V,
+                                      const gs_heads* O, const float* lse, const gs_heads* dO, const gs_heads* dQ,
+                                      const gs_heads* dK, const gs_heads* dV, void* workspace,
+                                      long long workspace_bytes, void* stream) {
+    gs::XattnArgs a;
+    gs_status st = attn_args(p, a);
+    if (st != GS_OK) return st;
+    if (!Q || !K || !V || !O || !dO || !dQ || !dK || !dV) return GS_ERR_INVALID_ARG;
+    if (!valid_heads(Q, a.B, a.Lq, a.Hq, false) || !valid_heads(K, a.B, a.Lk, a.Hkv, false) ||
+        !valid_heads(V, a.B, a.Lk, a.Hkv, false) || !valid_heads(O, a.B, a.Lq, a.Hq, false) ||
+        !valid_heads(dO, a.B, a.Lq, a.Hq, false) || !valid_heads(dQ, a.B, a.Lq, a.Hq, true) ||
+        !valid_heads(dK, a.B, a.Lk, a.Hkv, true) || !valid_heads(dV, a.B, a.Lk, a.Hkv, true))
+        return GS_ERR_SHAPE;
+    if (a.B == 0 || (a.Lq == 0 && a.Lk == 0)) return GS_OK;
+    if (a.Lq > 0 && (!Q->data || !O->data || !dO->data || !dQ->data || !lse)) return GS_ERR_INVALID_ARG;
+    if (a.Lk > 0 && (!K->data || !V->data || !dK->data || !dV->data)) return GS_ERR_INVALID_ARG;
+    int dev = 0, sms = 0;
+    if ((st = attn_device(dev, sms)) != GS_OK) return st;
+    a.q = view_of(Q); a.k = view_of(K); a.v = view_of(V); a.o = view_of(O);
+    a.dO = view_of(dO); a.dQ = view_of(dQ); a.dK = view_of(dK); a.dV = view_of(dV);
+    a.lse = const_cast<float*>(lse);
+    a.ws = (float*)workspace;
+    cudaStream_t s = (cudaStream_t)stream;
+    if (p->flags == GS_PATH_TENSOR) return GS_ERR_UNSUPPORTED;
+    gs::xattn_simt_plan(a, true, sms);
+    if ((st = attn_workspace(a.ws, workspace_bytes, gs::xattn_ws_backward(a))) != GS_OK) return st;
+    return from_cuda(gs::launch_xattn_simt_backward(a, s));
+}
+
+gs_status gs_sample_scores(const void* S, int s_dtype, long long N, int M, long long lds, const gs_sampling* how,
+                           const float* U, int* index, float* prob, void* stream) {
+    if (s_dtype != GS_F32 && s_dtype != GS_BF16) return GS_ERR_INVALID_ARG;
+    if (!how) return GS_ERR_INVALID_ARG;
+    if (N < 0 || N > 0x7fffffffLL || M < 1 || M > (1 << 19) || lds < 0 || (lds > 0 && lds < M)) return GS_ERR_SHAPE;
+    if (N == 0) return GS_OK;
+    if (!S || !U || (!index && !prob)) return GS_ERR_INVALID_ARG;
+    int dev = 0, sms = 0;
+    gs_status st = attn_device(dev, sms);
+    if (st != GS_OK) return st;
+    gs::SampleArgs a{};
+    a.S = S; a.bf16 = s_dtype == GS_BF16; a.N = N; a.M = M; a.lds = lds;
+    a.how = *how;
+    a.U = U; a.index = index; a.prob = prob;
+    return from_cuda(gs::launch_sample(a, sms, (cudaStream_t)stream));
 }
 
 gs_status gs_selftest_wait_timeout(void* stream) {

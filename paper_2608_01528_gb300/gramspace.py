@@ -10,7 +10,8 @@ Names follow the C ABI (gs_ prefix dropped): build_basis, build_basis_grouped,
 basis_groups, import_basis, project_similarity, project_similarity_host (with
 reserve_staging), project_similarity_static, similarity_coeffs, group_argmax,
 prob_vectorize, reconstruct, reconstruct_bind, bind, attention_scores,
-stream_status, selftest_wait_timeout.
+cross_attention, cross_attention_backward, sample_scores, stream_status,
+selftest_wait_timeout.
 """
 from __future__ import annotations
 
@@ -36,13 +37,32 @@ EXPORTS = ("gs_build_basis", "gs_basis_info", "gs_basis_destroy", "gs_project_si
            "gs_status_string", "gs_version", "gs_project_similarity_static", "gs_similarity_coeffs",
            "gs_selftest_wait_timeout", "gs_basis_import", "gs_basis_reserve_staging",
            "gs_project_similarity_host", "gs_build_basis_grouped", "gs_basis_groups", "gs_group_argmax",
-           "gs_bind", "gs_reconstruct_bind")
+           "gs_bind", "gs_reconstruct_bind", "gs_cross_attention_workspace", "gs_cross_attention",
+           "gs_cross_attention_backward", "gs_sample_scores")
 
 
 class GramSpaceError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
         super().__init__(f"{where}: {status_string(status)} ({status})")
+
+
+class _Heads(ctypes.Structure):  # gs_heads
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_longlong), ("row", ctypes.c_longlong),
+                ("head", ctypes.c_longlong)]
+
+
+class _Attn(ctypes.Structure):  # gs_attn
+    _fields_ = [("dtype", ctypes.c_int), ("B", ctypes.c_int), ("Lq", ctypes.c_int), ("Lk", ctypes.c_int),
+                ("Hq", ctypes.c_int), ("Hkv", ctypes.c_int), ("dk", ctypes.c_int), ("dv", ctypes.c_int),
+                ("scale", ctypes.c_float), ("key_lens", ctypes.c_void_p), ("key_mask", ctypes.c_void_p),
+                ("ld_mask", ctypes.c_longlong), ("flags", ctypes.c_uint)]
+
+
+class _Sampling(ctypes.Structure):  # gs_sampling
+    _fields_ = [("temperature", ctypes.c_float), ("top_p", ctypes.c_float), ("min_p", ctypes.c_float),
+                ("top_k", ctypes.c_int), ("temperature_rows", ctypes.c_void_p), ("top_p_rows", ctypes.c_void_p),
+                ("min_p_rows", ctypes.c_void_p), ("top_k_rows", ctypes.c_void_p)]
 
 
 _lib = None
@@ -74,6 +94,11 @@ def load_library(path=LIB_PATH):
     L.gs_prob_vectorize.argtypes = [vp, vp, i64, ip, vp, ip, ip, u32, vp]
     L.gs_reconstruct.argtypes = [vp, vp, ip, i64, ip, vp, ip, u32, vp]
     L.gs_attention_scores.argtypes = [vp, vp, ip, ip, ip, ip, ip, ip, f32, ip, vp, u32, vp]
+    hp, ap = ctypes.POINTER(_Heads), ctypes.POINTER(_Attn)
+    L.gs_cross_attention_workspace.argtypes = [ap, ip, ctypes.POINTER(i64)]
+    L.gs_cross_attention.argtypes = [ap, hp, hp, hp, hp, vp, vp, i64, vp]
+    L.gs_cross_attention_backward.argtypes = [ap, hp, hp, hp, hp, vp, hp, hp, hp, hp, vp, i64, vp]
+    L.gs_sample_scores.argtypes = [vp, ip, i64, ip, i64, ctypes.POINTER(_Sampling), vp, vp, vp, vp]
     L.gs_stream_status.argtypes = [vp]
     L.gs_selftest_wait_timeout.argtypes = [vp]
     L.gs_project_similarity_static.argtypes = [vp, ip, ip, vp, ip, vp, vp, i64, ip, ip, f32, vp, vp, vp]
@@ -85,7 +110,9 @@ def load_library(path=LIB_PATH):
                  "gs_similarity_coeffs", "gs_prob_vectorize", "gs_reconstruct", "gs_attention_scores",
                  "gs_stream_status", "gs_selftest_wait_timeout", "gs_basis_import",
                  "gs_basis_reserve_staging", "gs_project_similarity_host", "gs_build_basis_grouped",
-                 "gs_basis_groups", "gs_group_argmax", "gs_bind", "gs_reconstruct_bind"):
+                 "gs_basis_groups", "gs_group_argmax", "gs_bind", "gs_reconstruct_bind",
+                 "gs_cross_attention_workspace", "gs_cross_attention", "gs_cross_attention_backward",
+                 "gs_sample_scores"):
         getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L
@@ -453,6 +480,156 @@ def attention_scores(Yq, Yk, scale, apply_softmax=True, path="auto", out=None, s
                                    1 if apply_softmax else 0, _ptr(A), PATHS[path], _stream(stream, Yq.device))
     _check(st, "gs_attention_scores")
     return A
+
+
+def _launch_stream(stream, device):
+    """The context in which a call that runs on `stream` allocates: memory from torch's allocator belongs to the
+    stream that is current when it is taken, so outputs and workspaces are taken under the launch stream."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _heads(t, name, L, H, w, like):
+    """gs_heads of a B x L x H x w tensor with a dense last axis."""
+    if t.dim() != 4 or tuple(t.shape) != (like.shape[0], L, H, w):
+        raise ValueError(f"{name} must be {like.shape[0]} x {L} x {H} x {w}, got {tuple(t.shape)}")
+    if t.dtype != like.dtype or t.device != like.device:
+        raise TypeError(f"{name} must be {like.dtype} on {like.device}, got {t.dtype} on {t.device}")
+    s = t.stride()
+    if w > 1 and s[3] != 1:
+        raise ValueError(f"{name} must have unit stride along its last axis")
+    return _Heads(t.data_ptr(), s[0], s[1], s[2])
+
+
+def _attn(Q, K, V, scale, key_lens, key_mask, path):
+    """gs_attn and the gs_heads of the inputs, after the checks that need no device."""
+    for name, t in (("Q", Q), ("K", K), ("V", V)):
+        if t.dim() != 4:
+            raise ValueError(f"{name} must be 4-D (batch, length, heads, width), got {tuple(t.shape)}")
+    code = _dtype_code(Q)
+    B, Lq, Hq, dk = Q.shape
+    Lk, Hkv, dv = K.shape[1], K.shape[2], V.shape[3]
+    hs = [_heads(Q, "Q", Lq, Hq, dk, Q), _heads(K, "K", Lk, Hkv, dk, Q), _heads(V, "V", Lk, Hkv, dv, Q)]
+    a = _Attn(code, B, Lq, Lk, Hq, Hkv, dk, dv, dk ** -0.5 if scale is None and dk else scale or 0.0, None, None, 0,
+              PATHS[path])
+    if key_lens is not None:
+        if key_lens.dtype != torch.int32 or tuple(key_lens.shape) != (B,) or not key_lens.is_contiguous():
+            raise ValueError(f"key_lens must be a contiguous int32 vector of {B} lengths")
+        if key_lens.device != Q.device:
+            raise TypeError(f"key_lens must be on {Q.device}")
+        a.key_lens = key_lens.data_ptr()
+    if key_mask is not None:
+        if key_mask.dtype not in (torch.bool, torch.uint8) or tuple(key_mask.shape) != (B, Lk) \
+                or (Lk > 1 and key_mask.stride(1) != 1):
+            raise ValueError(f"key_mask must be a {B} x {Lk} bool (or uint8) tensor with unit column stride")
+        if key_mask.device != Q.device:
+            raise TypeError(f"key_mask must be on {Q.device}")
+        a.key_mask = key_mask.data_ptr()
+        a.ld_mask = key_mask.stride(0) if B > 1 else Lk
+    if not Q.is_cuda:
+        raise TypeError("Q, K and V must be CUDA tensors")
+    return a, hs
+
+
+def _attn_workspace(L, a, backward, device):
+    n = ctypes.c_longlong()
+    _check(L.gs_cross_attention_workspace(ctypes.byref(a), int(backward), ctypes.byref(n)), "gs_cross_attention_workspace")
+    return torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
+
+
+def _attn_lse(lse, B, Hq, Lq, device):
+    if lse.dtype != torch.float32 or tuple(lse.shape) != (B, Hq, Lq) or not lse.is_contiguous() or lse.device != device:
+        raise ValueError(f"lse must be a contiguous float32 {B} x {Hq} x {Lq} tensor on {device}")
+    return lse
+
+
+def cross_attention(Q, K, V, scale=None, key_lens=None, key_mask=None, want_lse=False, path="auto", out=None,
+                    stream=None):
+    """softmax(scale * Q K^T over the valid keys) V per head; see gs_cross_attention.
+
+    Q: B x Lq x Hq x dk, K: B x Lk x Hkv x dk, V: B x Lk x Hkv x dv (float32 or bfloat16, any
+    strides with a dense last axis; Hkv divides Hq, head h reads key head h // (Hq // Hkv)).
+    scale: dk ** -0.5 by default.  key_lens: int32 [B], keys to read of each sequence.  key_mask:
+    bool B x Lk, False = not read.  Returns {"O": B x Lq x Hq x dv, "lse": B x Hq x Lq float32 with want_lse};
+    `out` may supply them."""
+    a, hs = _attn(Q, K, V, scale, key_lens, key_mask, path)
+    L = load_library()
+    out = dict(out or {})
+    with _on(Q.device), _launch_stream(stream, Q.device):
+        if "O" not in out:
+            out["O"] = torch.empty((a.B, a.Lq, a.Hq, a.dv), dtype=Q.dtype, device=Q.device)
+        if want_lse and "lse" not in out:
+            out["lse"] = torch.empty((a.B, a.Hq, a.Lq), dtype=torch.float32, device=Q.device)
+        o = _heads(out["O"], "O", a.Lq, a.Hq, a.dv, Q)
+        lse = _ptr(_attn_lse(out["lse"], a.B, a.Hq, a.Lq, Q.device)) if out.get("lse") is not None else None
+        ws = _attn_workspace(L, a, False, Q.device)
+        st = L.gs_cross_attention(ctypes.byref(a), *map(ctypes.byref, hs), ctypes.byref(o), lse, _ptr(ws),
+                                  ws.numel() if ws is not None else 0, _stream(stream, Q.device))
+    _check(st, "gs_cross_attention")
+    return out
+
+
+def cross_attention_backward(Q, K, V, O, lse, dO, scale=None, key_lens=None, key_mask=None, path="auto", out=None,
+                             stream=None):
+    """The gradient of cross_attention; see gs_cross_attention_backward.  O and lse are the forward
+    call's (want_lse=True), dO the gradient of O; the other arguments as there.  Returns {"dQ", "dK", "dV"} with
+    the shapes and type of Q, K and V; `out` may supply them."""
+    a, hs = _attn(Q, K, V, scale, key_lens, key_mask, path)
+    L = load_library()
+    out = dict(out or {})
+    o, do = _heads(O, "O", a.Lq, a.Hq, a.dv, Q), _heads(dO, "dO", a.Lq, a.Hq, a.dv, Q)
+    _attn_lse(lse, a.B, a.Hq, a.Lq, Q.device)
+    with _on(Q.device), _launch_stream(stream, Q.device):
+        for name, t in (("dQ", Q), ("dK", K), ("dV", V)):
+            if name not in out:
+                out[name] = torch.empty(t.shape, dtype=t.dtype, device=t.device)
+        gh = [_heads(out["dQ"], "dQ", a.Lq, a.Hq, a.dk, Q), _heads(out["dK"], "dK", a.Lk, a.Hkv, a.dk, Q),
+              _heads(out["dV"], "dV", a.Lk, a.Hkv, a.dv, Q)]
+        ws = _attn_workspace(L, a, True, Q.device)
+        st = L.gs_cross_attention_backward(ctypes.byref(a), *map(ctypes.byref, hs), ctypes.byref(o), _ptr(lse),
+                                           ctypes.byref(do), *map(ctypes.byref, gh), _ptr(ws),
+                                           ws.numel() if ws is not None else 0, _stream(stream, Q.device))
+    _check(st, "gs_cross_attention_backward")
+    return out
+
+
+def sample_scores(S, U, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, want_prob=True, out=None, stream=None):
+    """One random entry of each row of the scores S (N x M, float32 or bfloat16, CUDA) from the numbers
+    U (N float32 of [0, 1)); see gs_sample_scores for the rules.  temperature, top_k, top_p and min_p are
+    numbers or, for one setting per row, contiguous CUDA vectors of N (float32; top_k int32).  Returns
+    {"index": N int32, "prob": N float32}."""
+    ld = _ld(S)
+    N, M = S.shape
+    code = _dtype_code(S)
+    how = _Sampling()
+    rows = (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
+            ("min_p", min_p, torch.float32))
+    for name, v, dt in rows + (("U", U, torch.float32),):
+        if isinstance(v, torch.Tensor) or name == "U":
+            if v.dtype != dt or tuple(v.shape) != (N,) or not v.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous {dt} vector of N = {N} entries")
+            if v.device != S.device:
+                raise TypeError(f"{name} must be on {S.device}")
+            if name != "U":
+                setattr(how, name + "_rows", v.data_ptr())
+        else:
+            setattr(how, name, int(v) if dt == torch.int32 else float(v))
+    out = dict(out or {})
+    for name, dt in (("index", torch.int32), ("prob", torch.float32)):
+        t = out.get(name)
+        if t is not None and (t.dtype != dt or tuple(t.shape) != (N,) or not t.is_contiguous() or t.device != S.device):
+            raise ValueError(f"out[{name!r}] must be a contiguous {dt} vector of N = {N} entries on {S.device}")
+    if not S.is_cuda:
+        raise TypeError("S must be a CUDA tensor")
+    L = load_library()
+    with _on(S.device), _launch_stream(stream, S.device):
+        if "index" not in out:
+            out["index"] = torch.empty(N, dtype=torch.int32, device=S.device)
+        if want_prob and "prob" not in out:
+            out["prob"] = torch.empty(N, dtype=torch.float32, device=S.device)
+        st = L.gs_sample_scores(_ptr(S), code, N, M, ld if N > 1 else M, ctypes.byref(how), _ptr(U), _ptr(out.get("index")),
+                                _ptr(out.get("prob")), _stream(stream, S.device))
+    _check(st, "gs_sample_scores")
+    return out
 
 
 def project_similarity_static(Q, R, cnorm, X, mode="raw", scale=1.0, want_argmax=True, want_maxval=True,

@@ -1,0 +1,101 @@
+"""Refusals of cross attention and sampling that need no device."""
+import ctypes
+
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def g():
+    from paper_2608_01528_gb300 import build, gramspace
+    build.build()
+    gramspace.load_library()
+    return gramspace
+
+
+def attn(g, **kw):
+    d = dict(dtype=0, B=1, Lq=2, Lk=3, Hq=4, Hkv=2, dk=8, dv=8, scale=1.0, key_lens=None, key_mask=None, ld_mask=0, flags=0)
+    d.update(kw)
+    return g._Attn(*(d[k] for k, _ in g._Attn._fields_))
+
+
+def heads(g, data=None, batch=1000, row=100, head=10):
+    return g._Heads(data, batch, row, head)
+
+
+def forward(g, a, q=None, k=None, v=None, o=None):
+    hs = [x if x is not None else heads(g) for x in (q, k, v, o)]
+    return g.load_library().gs_cross_attention(ctypes.byref(a), *map(ctypes.byref, hs), None, None, 0, None)
+
+
+def test_attention_arguments(g):
+    for kw in (dict(dtype=2), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(flags=3)):
+        assert forward(g, attn(g, **kw)) == g.GS_ERR_INVALID_ARG, kw
+    for kw in (dict(B=-1), dict(Lq=-1), dict(Lk=-1), dict(Hq=0), dict(Hkv=0), dict(Hq=3), dict(dk=0), dict(dv=0),
+               dict(Lk=2 ** 31 - 1), dict(Lq=2 ** 30), dict(B=2 ** 20, Lq=2 ** 12), dict(B=2 ** 20, Lk=2 ** 12),
+               dict(key_mask=16, ld_mask=2)):
+        assert forward(g, attn(g, **kw)) == g.GS_ERR_SHAPE, kw
+    for kw in (dict(dk=129), dict(dv=129)):
+        assert forward(g, attn(g, **kw)) == g.GS_ERR_UNSUPPORTED, kw
+    bad = heads(g, batch=-1)
+    assert forward(g, attn(g), q=bad) == g.GS_ERR_SHAPE and forward(g, attn(g), o=bad) == g.GS_ERR_SHAPE
+    assert forward(g, attn(g), o=heads(g, row=0)) == g.GS_ERR_SHAPE  # rows of the output on one another
+    assert forward(g, attn(g)) == g.GS_ERR_INVALID_ARG               # null data
+    assert forward(g, attn(g, B=0)) == g.GS_OK and forward(g, attn(g, Lq=0)) == g.GS_OK
+    L = g.load_library()
+    n = ctypes.c_longlong(7)
+    assert L.gs_cross_attention_workspace(ctypes.byref(attn(g, dk=129)), 0, ctypes.byref(n)) == g.GS_ERR_UNSUPPORTED
+    assert n.value == 0
+    assert L.gs_cross_attention_workspace(None, 0, ctypes.byref(n)) == g.GS_ERR_INVALID_ARG
+    assert L.gs_cross_attention_workspace(ctypes.byref(attn(g)), 0, None) == g.GS_ERR_INVALID_ARG
+    h = [heads(g) for _ in range(8)]
+    back = lambda a, hs, lse=None: L.gs_cross_attention_backward(  # noqa: E731
+        ctypes.byref(a), *map(ctypes.byref, hs[:4]), lse, *map(ctypes.byref, hs[4:]), None, 0, None)
+    assert back(attn(g), h) == g.GS_ERR_INVALID_ARG
+    assert back(attn(g, B=0), h) == g.GS_OK
+    assert back(attn(g), h[:5] + [heads(g, head=0)] + h[6:]) == g.GS_ERR_SHAPE
+
+
+def test_attention_wrapper(g):
+    q, k, v = torch.zeros(2, 5, 4, 8), torch.zeros(2, 7, 2, 8), torch.zeros(2, 7, 2, 6)
+    for bad in ((q[0], k, v), (q, k[:1], v), (q, k, v[:, :3]), (q, torch.zeros(2, 7, 2, 9), v), (q, k, v[:, :, :1]),
+                (q, torch.zeros(2, 7, 8, 2).transpose(2, 3), v)):
+        with pytest.raises(ValueError):
+            g.cross_attention(*bad)
+    for bad in ((q.double(), k, v), (q, k.bfloat16(), v), (q.half(), k.half(), v.half())):
+        with pytest.raises(TypeError):
+            g.cross_attention(*bad)
+    with pytest.raises(TypeError):  # host tensors
+        g.cross_attention(q, k, v)
+    for kw in (dict(key_lens=torch.zeros(2)), dict(key_lens=torch.zeros(3, dtype=torch.int32)),
+               dict(key_mask=torch.zeros(2, 7)), dict(key_mask=torch.zeros(2, 6, dtype=torch.bool)),
+               dict(key_mask=torch.zeros(7, 2, dtype=torch.bool).t())):
+        with pytest.raises(ValueError):
+            g.cross_attention(q, k, v, **kw)
+
+
+def test_sampling_arguments(g):
+    L = g.load_library()
+    how = g._Sampling(1.0, 1.0, 0.0, 0)
+    d = 16  # never dereferenced: every call below returns before touching memory
+
+    def call(S=d, dt=0, N=4, M=10, ld=10, h=how, U=d, index=d, prob=d):
+        return L.gs_sample_scores(S, dt, N, M, ld, ctypes.byref(h) if h is not None else None, U, index, prob, None)
+
+    assert call(dt=2) == g.GS_ERR_INVALID_ARG and call(h=None) == g.GS_ERR_INVALID_ARG
+    for kw in (dict(N=-1), dict(N=2 ** 31), dict(M=0), dict(M=2 ** 19 + 1, ld=2 ** 20), dict(ld=9)):
+        assert call(**kw) == g.GS_ERR_SHAPE, kw
+    for kw in (dict(S=None), dict(U=None), dict(index=None, prob=None)):
+        assert call(**kw) == g.GS_ERR_INVALID_ARG, kw
+    assert call(N=0, S=None, U=None) == g.GS_OK
+    S, U = torch.zeros(3, 5), torch.zeros(3)
+    for kw in (dict(U=torch.zeros(2)), dict(U=torch.zeros(3, dtype=torch.float64)), dict(temperature=torch.zeros(4)),
+               dict(top_k=torch.zeros(3)), dict(out={"index": torch.zeros(3)}), dict(out={"prob": torch.zeros(2)})):
+        with pytest.raises(ValueError):
+            g.sample_scores(**{"S": S, "U": U, **kw})
+    with pytest.raises(TypeError):
+        g.sample_scores(S.double(), U)
+    with pytest.raises(TypeError):
+        g.sample_scores(S, U)
+    with pytest.raises(ValueError):
+        g.sample_scores(S.t(), torch.zeros(5))
