@@ -929,8 +929,14 @@ gs_status gs_cross_attention_workspace(const gs_attn* p, int backward, long long
     if (st != GS_OK) return st;
     int dev = 0, sms = 0;
     if ((st = attn_device(dev, sms)) != GS_OK) return st;
+    // the arrays' alignment, not known here, decides between the paths: room for either
     gs::xattn_simt_plan(a, backward != 0, sms);
-    *bytes = 4 * (backward ? gs::xattn_ws_backward(a) : gs::xattn_ws_forward(a));
+    long long floats = backward ? gs::xattn_ws_backward(a) : gs::xattn_ws_forward(a);
+    if (!backward && a.dtype == GS_BF16 && a.G <= 128) {
+        gs::xattn_tc_plan(a, sms);
+        floats = std::max(floats, gs::xattn_ws_forward(a));
+    }
+    *bytes = 4 * floats;
     return GS_OK;
 }
 
@@ -952,7 +958,14 @@ gs_status gs_cross_attention(const gs_attn* p, const gs_heads* Q, const gs_heads
     a.lse = lse;
     a.ws = (float*)workspace;
     cudaStream_t s = (cudaStream_t)stream;
-    if (p->flags == GS_PATH_TENSOR) return GS_ERR_UNSUPPORTED;
+    const bool tc_ok = gs::tc_available(dev) && gs::xattn_tc_supported(a);
+    if (p->flags == GS_PATH_TENSOR && !tc_ok)
+        return a.dtype != GS_BF16 || a.G > 128 ? GS_ERR_UNSUPPORTED : GS_ERR_ALIGNMENT;
+    if (tc_ok && p->flags != GS_PATH_SIMT && a.Lk > 0) {
+        gs::xattn_tc_plan(a, sms);
+        if ((st = attn_workspace(a.ws, workspace_bytes, gs::xattn_ws_forward(a))) != GS_OK) return st;
+        return from_cuda(gs::launch_xattn_tc(a, sms, dev, s));
+    }
     gs::xattn_simt_plan(a, false, sms);
     if ((st = attn_workspace(a.ws, workspace_bytes, gs::xattn_ws_forward(a))) != GS_OK) return st;
     return from_cuda(gs::launch_xattn_simt(a, s));
@@ -1015,7 +1028,8 @@ gs_status gs_stream_status(void* stream) {
     cudaError_t e = stream ? cudaStreamSynchronize((cudaStream_t)stream) : cudaDeviceSynchronize();
     if (e != cudaSuccess) return GS_ERR_CUDA;
     const unsigned w = gs::take_device_error_build() | gs::take_device_error_tc() | gs::take_device_error_gemm() |
-                       gs::take_device_error_attn() | gs::take_device_error_rbind() | gs::take_device_error_x3();
+                       gs::take_device_error_attn() | gs::take_device_error_rbind() | gs::take_device_error_x3() |
+                       gs::take_device_error_xattn();
     if (w & GS_DEV_ERR_TIMEOUT) return GS_ERR_TIMEOUT;
     if (w & GS_DEV_ERR_RANGE) return GS_ERR_RANGE;
     if (w & GS_DEV_ERR_LAYOUT) return GS_ERR_UNSUPPORTED;

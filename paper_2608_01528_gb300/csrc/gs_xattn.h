@@ -63,6 +63,13 @@ cudaError_t launch_xattn_join(const XattnArgs& a, cudaStream_t s);
 cudaError_t launch_xattn_join_dq(const XattnArgs& a, cudaStream_t s);
 cudaError_t launch_xattn_join_dkv(const XattnArgs& a, cudaStream_t s);
 
+// ----------------------------------------------------------------- tcgen05 (gs_xattn_tc.cu)
+// bf16, at most 128 query heads to a key head, Q, K, V on 16-byte boundaries with strides in multiples of 8
+bool xattn_tc_supported(const XattnArgs& a);
+void xattn_tc_plan(XattnArgs& a, int sms);
+cudaError_t launch_xattn_tc(const XattnArgs& a, int sms, int device, cudaStream_t s);
+unsigned take_device_error_xattn();
+
 // ----------------------------------------------------------------- sampling (gs_sample.cu)
 struct SampleArgs {
     const void* S;

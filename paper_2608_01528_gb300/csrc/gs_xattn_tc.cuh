@@ -1,0 +1,152 @@
+// gs_xattn_tc.cuh -- what the tensor-core cross-attention kernels share: 4-D TMA tiles of
+// (B, L, H, width) arrays, MN-major operands, packed arithmetic, valid-key words.
+#pragma once
+
+#include "gs_tc_ptx.cuh"
+#include "gs_xattn.h"
+
+namespace gs {
+namespace xtc {
+
+using namespace ptx;
+
+constexpr int kTile = 128;                  // packed rows / keys of a tile: the MMA's M, and TMEM's lanes
+constexpr int kChunk = 64;                  // width of a 128-byte-swizzled chunk (bf16)
+constexpr int kChunkBytes = kTile * kChunk * 2;  // 16 KB
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+static __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, uint64_t* bar, int x, int y, int z,
+                                                   int w) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(
+            smem_u32(dst)),
+        "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
+        : "memory");
+}
+static __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+
+// Descriptor of an MN-major B operand: rows of the tile are the K dimension (128 bytes apart), its 64-column
+// chunks the N dimension.  128-byte swizzle; 8-row groups 1,024 bytes apart (stride offset), chunks 16 KB
+// apart (leading offset).
+static __device__ __forceinline__ uint64_t sdesc_mn(uint32_t saddr) {
+    uint64_t d = (uint64_t)((saddr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)(kChunkBytes >> 4) << 16;
+    d |= (uint64_t)(1024 >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+__host__ __device__ constexpr uint32_t idesc_bf16_bmn(int n) { return idesc_bf16_f32(n) | (1u << 16); }
+
+// D[tmem] (+)= A[smem] B[smem]^T over `ksteps` steps of 16: both K-major, in chunks of 64 columns
+static __device__ __forceinline__ void mma_tile_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, int ksteps) {
+    for (int k = 0; k < ksteps; ++k) {
+        const uint32_t off = (uint32_t)((k >> 2) * kChunkBytes + (k & 3) * 32);
+        mma_f16_ss(d, sdesc_sw128(a + off), sdesc_sw128(b + off), idesc, k != 0 ? 1u : 0u);
+    }
+}
+// D[tmem] (+)= A[tmem: bf16 pairs] B over 128 rows of B: A's K-step k lies 8 columns after the last, its second
+// half (rows 64 on) `half` columns after the first
+static __device__ __forceinline__ void mma_tile_ts(uint32_t d, uint32_t a, uint32_t half, uint32_t b, uint32_t idesc,
+                                                   bool accumulate) {
+#pragma unroll
+    for (int k = 0; k < kTile / 16; ++k)
+        mma_bf16_ts(d, a + (uint32_t)(k & 3) * 8 + (k >= 4 ? half : 0u), sdesc_mn(b + (uint32_t)k * 2048), idesc,
+                    accumulate || k != 0 ? 1u : 0u);
+}
+
+static __device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+static __device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// (a0, a1) * (b, b) + (c, c)
+static __device__ __forceinline__ void fma2(float& a0, float& a1, float b, float c) {
+    asm("{\n\t.reg .b64 x, y, z;\n\t"
+        "mov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %2};\n\tmov.b64 z, {%3, %3};\n\t"
+        "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "+f"(a0), "+f"(a1)
+        : "f"(b), "f"(c));
+}
+// (a0, a1) + (b0, b1)
+static __device__ __forceinline__ void add2(float& a0, float& a1, float b0, float b1) {
+    asm("{\n\t.reg .b64 x, y;\n\t"
+        "mov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\t"
+        "add.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "+f"(a0), "+f"(a1)
+        : "f"(b0), "f"(b1));
+}
+// (a0, a1) * (b0, b1)
+static __device__ __forceinline__ void mul2(float& a0, float& a1, float b0, float b1) {
+    asm("{\n\t.reg .b64 x, y;\n\t"
+        "mov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\t"
+        "mul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "+f"(a0), "+f"(a1)
+        : "f"(b0), "f"(b1));
+}
+
+static __device__ __forceinline__ int keys_of(const XattnArgs& a, int b) {
+    return a.lens ? min(max(__ldg(a.lens + b), 0), a.Lk) : a.Lk;
+}
+// bit l of word i: key j0 + 32 i + l may be read (taken by a whole warp)
+static __device__ __forceinline__ void valid_words(uint32_t (&w)[4], const XattnArgs& a, int b, int j0, int n) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int j = j0 + 32 * i + lane;
+        const bool ok = j < n && (!a.mask || __ldg(a.mask + (long long)b * a.ldm + j) != 0);
+        w[i] = __ballot_sync(0xffffffffu, ok);
+    }
+}
+// zeroes the rows of a tile of `chunks` chunks whose bit is clear (a whole warp; generic-proxy writes)
+static __device__ __forceinline__ void zero_rows(uint8_t* tile, int chunks, const uint32_t (&w)[4]) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t bad = ~w[i];
+        while (bad) {
+            const int r = 32 * i + __ffs(bad) - 1;
+            bad &= bad - 1;
+            if (lane < 8 * chunks)
+                *reinterpret_cast<uint4*>(tile + (size_t)(lane >> 3) * kChunkBytes + r * 128 + (lane & 7) * 16) =
+                    make_uint4(0, 0, 0, 0);
+        }
+    }
+}
+
+// A tensor map over a (B, L, H, width) bf16 array, axes (width, H, L, B), box {64, bh, bl, 1}.  A batch (or head) stride of 0
+// becomes an axis of one, indexed by 0 * coordinate.
+struct HeadMap {
+    CUtensorMap map;
+    int bmul, hmul;
+};
+// whether every row of the array starts on a 16-byte boundary and the strides fit a tensor map
+inline bool map_supported(const HeadView& v, int B, int L, int H) {
+    auto ok = [](long long s, int n) { return n <= 1 || (s % 8 == 0 && s < (1LL << 38)); };
+    return (uintptr_t)v.p % 16 == 0 && ok(v.b, B) && ok(v.l, L) && ok(v.h, H) && (L <= 1 || v.l > 0);
+}
+inline bool make_head_map(HeadMap* m, const HeadView& v, int B, int L, int H, int w, int bh, int bl) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    m->bmul = B > 1 && v.b == 0 ? 0 : 1;
+    m->hmul = H > 1 && v.h == 0 ? 0 : 1;
+    cuuint64_t dims[4] = {(cuuint64_t)w, (cuuint64_t)(m->hmul ? H : 1), (cuuint64_t)L, (cuuint64_t)(m->bmul ? B : 1)};
+    // the strides of axes of one element are never used: any legal value
+    cuuint64_t strides[3] = {(cuuint64_t)(dims[1] > 1 ? v.h * 2 : 256), (cuuint64_t)(L > 1 ? v.l * 2 : 256),
+                             (cuuint64_t)(dims[3] > 1 ? v.b * 2 : 256)};
+    cuuint32_t box[4] = {(cuuint32_t)kChunk, (cuuint32_t)bh, (cuuint32_t)bl, 1};
+    cuuint32_t es[4] = {1, 1, 1, 1};
+    return fn(&m->map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, v.p, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace xtc
+}  // namespace gs

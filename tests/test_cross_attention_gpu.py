@@ -303,3 +303,36 @@ def test_decoding_step_end_to_end(gs):
         j = int(d["index"][i])
         # a score off by 1e-3 moves a weight by 2e-3 of itself at this temperature: so far the borders may lie apart
         assert run[j] - p[j] - 5e-3 <= float(u[i]) <= run[j] + 5e-3
+
+
+TENSOR_SHAPES = [
+    (1, 1, 1, 1, 1, 8, 8),
+    (1, 1, 128, 8, 8, 64, 64),
+    (2, 1, 5000, 8, 2, 128, 64),
+    (1, 5, 40000, 4, 1, 64, 128),        # keys in parts
+    (1, 130, 1100, 1, 1, 72, 40),
+    (3, 260, 517, 8, 2, 128, 128),
+    (2, 3, 700, 128, 1, 64, 64),         # 128 query heads on one key head
+    (4, 600, 300, 16, 16, 64, 64),       # pairs of row tiles
+    (20, 129, 129, 8, 8, 40, 72),        # pairs, the second tile one row
+    (8, 300, 200, 28, 4, 128, 128),      # pairs, groups of seven: 126 rows a tile
+    (40, 128, 257, 4, 4, 128, 64),
+]
+
+
+@pytest.mark.parametrize("kind", ["none", "lens", "holes", "both"])
+@pytest.mark.parametrize("shape", TENSOR_SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_tensor_cores(gs, shape, kind):
+    Q, K, V, dO = make(*shape, "bf16")
+    lens, mask = masks(kind, shape[0], shape[2])
+    check_forward(gs, Q, K, V, 1.0 / math.sqrt(shape[5]), lens, mask, "tensor", True)
+
+
+def test_growing_maxima(gs):
+    """Keys whose logits grow along the sequence by far more than the running maximum lags, and fall again."""
+    for B, H in ((1, 2), (16, 16)):
+        Q, K, V, dO = make(B, 200, 1000, H, H, 64, 64, "bf16", peak=1.0)
+        up = torch.cat([torch.linspace(0, 12, 700), torch.linspace(12, -12, 300)]).cuda()
+        K[..., 0] = up[None, :, None].bfloat16()
+        Q[..., 0] = (torch.arange(200) % 7 - 3).cuda()[None, :, None].bfloat16() * 4
+        check_forward(gs, Q, K, V, 0.5, None, None, "tensor", True)
