@@ -932,9 +932,9 @@ gs_status gs_cross_attention_workspace(const gs_attn* p, int backward, long long
     // the arrays' alignment, not known here, decides between the paths: room for either
     gs::xattn_simt_plan(a, backward != 0, sms);
     long long floats = backward ? gs::xattn_ws_backward(a) : gs::xattn_ws_forward(a);
-    if (!backward && a.dtype == GS_BF16 && a.G <= 128) {
-        gs::xattn_tc_plan(a, sms);
-        floats = std::max(floats, gs::xattn_ws_forward(a));
+    if (a.dtype == GS_BF16 && a.G <= 128) {
+        backward ? gs::xattn_bwd_tc_plan(a, sms) : gs::xattn_tc_plan(a, sms);
+        floats = std::max(floats, backward ? gs::xattn_ws_backward(a) : gs::xattn_ws_forward(a));
     }
     *bytes = 4 * floats;
     return GS_OK;
@@ -994,7 +994,14 @@ gs_status gs_cross_attention_backward(const gs_attn* p, const gs_heads* Q, const
     a.lse = const_cast<float*>(lse);
     a.ws = (float*)workspace;
     cudaStream_t s = (cudaStream_t)stream;
-    if (p->flags == GS_PATH_TENSOR) return GS_ERR_UNSUPPORTED;
+    const bool tc_ok = gs::tc_available(dev) && gs::xattn_bwd_tc_supported(a);
+    if (p->flags == GS_PATH_TENSOR && !tc_ok)
+        return a.dtype != GS_BF16 || a.G > 128 ? GS_ERR_UNSUPPORTED : GS_ERR_ALIGNMENT;
+    if (tc_ok && p->flags != GS_PATH_SIMT && a.Lq > 0 && a.Lk > 0) {
+        gs::xattn_bwd_tc_plan(a, sms);
+        if ((st = attn_workspace(a.ws, workspace_bytes, gs::xattn_ws_backward(a))) != GS_OK) return st;
+        return from_cuda(gs::launch_xattn_bwd_tc(a, dev, s));
+    }
     gs::xattn_simt_plan(a, true, sms);
     if ((st = attn_workspace(a.ws, workspace_bytes, gs::xattn_ws_backward(a))) != GS_OK) return st;
     return from_cuda(gs::launch_xattn_simt_backward(a, s));
@@ -1029,7 +1036,7 @@ gs_status gs_stream_status(void* stream) {
     if (e != cudaSuccess) return GS_ERR_CUDA;
     const unsigned w = gs::take_device_error_build() | gs::take_device_error_tc() | gs::take_device_error_gemm() |
                        gs::take_device_error_attn() | gs::take_device_error_rbind() | gs::take_device_error_x3() |
-                       gs::take_device_error_xattn();
+                       gs::take_device_error_xattn() | gs::take_device_error_xbwd();
     if (w & GS_DEV_ERR_TIMEOUT) return GS_ERR_TIMEOUT;
     if (w & GS_DEV_ERR_RANGE) return GS_ERR_RANGE;
     if (w & GS_DEV_ERR_LAYOUT) return GS_ERR_UNSUPPORTED;

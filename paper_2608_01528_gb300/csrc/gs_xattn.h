@@ -38,18 +38,26 @@ inline int xattn_parts(long long base, long long tiles, int want, int least) {
     return s < 1 ? 1 : (int)s;
 }
 
-// Workspace in floats.  Forward: per part and row dv sums, the row's maximum (base 2) and sum.
-// Backward: D_i per row, then the parts of dQ (splits > 1) and of dK, dV (rsplits > 1).
-inline long long xattn_ws_forward(const XattnArgs& a) {
-    return a.splits > 1 ? (long long)a.splits * a.B * a.Hq * a.Lq * (a.dv + 2) : 0;
+// Workspace in floats; every section starts on a 16-byte boundary.
+// Forward (splits > 1): per part and row dv sums, then the row's maximum (base 2) and sum.
+// Backward: D_i per row, then the parts of dQ (splits > 1), of dK and of dV (rsplits > 1).
+#define GS_XWS __host__ __device__ inline long long
+GS_XWS xattn_round4(long long n) { return (n + 3) / 4 * 4; }
+GS_XWS xattn_rows(const XattnArgs& a) { return (long long)a.B * a.Hq * a.Lq; }
+GS_XWS xattn_keys(const XattnArgs& a) { return (long long)a.B * a.Hkv * a.Lk; }
+GS_XWS xattn_ws_ml(const XattnArgs& a) { return xattn_round4(a.splits * xattn_rows(a) * a.dv); }
+GS_XWS xattn_ws_forward(const XattnArgs& a) { return a.splits > 1 ? xattn_ws_ml(a) + a.splits * xattn_rows(a) * 2 : 0; }
+GS_XWS xattn_ws_dq(const XattnArgs& a) { return xattn_round4(xattn_rows(a)); }
+GS_XWS xattn_ws_dk(const XattnArgs& a) {
+    return xattn_ws_dq(a) + (a.splits > 1 ? xattn_round4(a.splits * xattn_rows(a) * a.dk) : 0);
 }
-__host__ __device__ inline long long xattn_ws_delta(const XattnArgs& a) { return ((long long)a.B * a.Hq * a.Lq + 3) / 4 * 4; }
-inline long long xattn_ws_backward(const XattnArgs& a) {
-    long long n = xattn_ws_delta(a);
-    if (a.splits > 1) n += (long long)a.splits * a.B * a.Hq * a.Lq * a.dk;
-    if (a.rsplits > 1) n += (long long)a.rsplits * a.B * a.Hkv * a.Lk * (a.dk + a.dv);
-    return n;
+GS_XWS xattn_ws_dv(const XattnArgs& a) {
+    return xattn_ws_dk(a) + (a.rsplits > 1 ? xattn_round4(a.rsplits * xattn_keys(a) * a.dk) : 0);
 }
+GS_XWS xattn_ws_backward(const XattnArgs& a) {
+    return xattn_ws_dv(a) + (a.rsplits > 1 ? a.rsplits * xattn_keys(a) * a.dv : 0);
+}
+#undef GS_XWS
 
 // ----------------------------------------------------------------- CUDA cores (gs_xattn_simt.cu)
 // the parts (splits, rsplits) that the CUDA-core kernels take on `sms` multiprocessors
@@ -69,6 +77,11 @@ bool xattn_tc_supported(const XattnArgs& a);
 void xattn_tc_plan(XattnArgs& a, int sms);
 cudaError_t launch_xattn_tc(const XattnArgs& a, int sms, int device, cudaStream_t s);
 unsigned take_device_error_xattn();
+// the gradient (gs_xattn_bwd_tc.cu); dO as Q
+bool xattn_bwd_tc_supported(const XattnArgs& a);
+void xattn_bwd_tc_plan(XattnArgs& a, int sms);
+cudaError_t launch_xattn_bwd_tc(const XattnArgs& a, int device, cudaStream_t s);
+unsigned take_device_error_xbwd();
 
 // ----------------------------------------------------------------- sampling (gs_sample.cu)
 struct SampleArgs {

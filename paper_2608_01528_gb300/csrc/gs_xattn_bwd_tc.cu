@@ -1,0 +1,704 @@
+// gs_xattn_bwd_tc.cu -- the gradient of cross attention on tcgen05 (bf16 inputs).
+//
+// Two kernels, each with its own sums in TMEM, so that nothing meets in atomics and results repeat bit for bit:
+//   k_xattn_dkv_tc: a CTA keeps a tile of 128 keys (K, V) and walks the packed rows of the key head in tiles of 128:
+//     S^T = K Q^T, P^T = 2^(c s - lse log2 e), dV += P^T dO, dP^T = V dO^T, dS^T = P^T (dP^T - D), dK += dS^T Q.
+//   k_xattn_dq_tc: a CTA keeps a tile of 128 packed rows (Q, dO) and walks the keys:
+//     S = Q K^T, dP = dO V^T, dS = P (dP - D), dQ += dS K.
+// S and dP are computed in both (7 products of the tile instead of 5); the alternative, dQ summed from the first
+// kernel, needs fp32 atomics on 4 bytes per product of 128 x 128 x dk, and their order changes results.
+//
+// P and dS go from TMEM to registers and back as bf16, where they are the A operand (lanes are keys in the first kernel,
+// rows in the second, so neither needs a transpose); the B operands Q, dO, K are read as they lie (MN-major).
+// Eight softmax warps: warp w reads lanes 32 (w % 4)..+31 and columns 64 (w / 4)..+63.  While they work on S the tensor
+// core runs dP or the sums, and the other way round.
+//
+// Keys that are not read: P = dS = 0, and in the second kernel their rows of K are zeroed in shared memory before
+// the MMA reads them (0 * NaN).  Rows past the end have lse = +inf: P = 0.
+
+#include <stddef.h>
+
+#include <algorithm>
+
+#include "gs_xattn_tc.cuh"
+
+namespace gs {
+namespace {
+
+using namespace xtc;
+
+__device__ unsigned g_err_xbwd = 0;
+
+constexpr int kMmaWarp = 8, kTmaWarp = 9, kAuxWarp = 10;
+constexpr int kThreads = 11 * 32;
+constexpr int kSoftWarps = 8;
+
+struct Ctl {
+    uint64_t own_full;                               // the tiles that stay
+    uint64_t a_full[4], a_empty[4], a_ready[4];      // Q (dkv) or K (dq) stages
+    uint64_t b_full[4], b_empty[4];                  // dO (dkv) or V (dq) stages
+    uint64_t st_full[4], st_empty[4];                // dkv: row statistics
+    uint64_t s_full, p_full, dp_full, ds_full;       // MMA <-> softmax
+    uint64_t s_free, dp_free, ds_free;               // dq
+    uint64_t done;
+    alignas(16) float nlse[4][kTile];                // -lse log2 e (-inf: no weight); read 16 bytes at a time
+    alignas(16) float ndelta[4][kTile];              // -D
+    uint32_t tmem_base;
+    int abort_flag;
+};
+static_assert(offsetof(Ctl, nlse) % 16 == 0 && offsetof(Ctl, ndelta) % 16 == 0, "float4 reads");
+
+struct Params {
+    XattnArgs a;
+    int qmul, omul, kmul, khmul, vmul, vhmul;  // HeadMap multipliers: q, dO (batch), k and v (batch, head)
+    int nl;
+    long long rtiles;
+    int ktiles, ksteps, vsteps;
+    int vec_q, vec_k, vec_v;  // outputs on 16-byte boundaries
+};
+
+// stages of the streamed operands
+template <int DKC, int DVC>
+struct Cfg {
+    static constexpr int kOwn = (DKC + DVC) * kChunkBytes;
+    static constexpr int kRoom = (227 * 1024 - 1024 - (int)sizeof(Ctl) - kOwn) / kOwn;
+    static constexpr int kStages = kRoom < 4 ? kRoom : 4;
+    static constexpr size_t kSmem = 1024 + (size_t)kOwn * (1 + kStages) + sizeof(Ctl);
+    static_assert(kStages >= 2, "ring too short");
+};
+
+// -lse log2 e of a row: -inf where the row has no weight (P = 0); a NaN or +inf lse gives NaN, as the forward result is
+__device__ __forceinline__ float neg_lse2(float lse) {
+    return lse == -INFINITY ? -INFINITY : lse == INFINITY ? NAN : -lse * kLog2e;
+}
+
+// 32 fp32 columns of this thread's lane as bf16 to global (or zeros)
+__device__ __forceinline__ void store32(__nv_bfloat16* dst, const float* v, int left, bool vec) {
+    if (vec) {
+#pragma unroll
+        for (int e = 0; e < 32; e += 8)
+            if (e < left)
+                *reinterpret_cast<uint4*>(dst + e) = make_uint4(pack_bf16(v[e], v[e + 1]), pack_bf16(v[e + 2], v[e + 3]),
+                                                                pack_bf16(v[e + 4], v[e + 5]), pack_bf16(v[e + 6], v[e + 7]));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+            if (e < left) dst[e] = __float2bfloat16_rn(v[e]);
+    }
+}
+__device__ __forceinline__ void store32(float* dst, const float* v, int left, bool vec) {
+    if (vec) {
+#pragma unroll
+        for (int e = 0; e < 32; e += 4)
+            if (e < left) *reinterpret_cast<float4*>(dst + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+            if (e < left) dst[e] = v[e];
+    }
+}
+// `cols` columns of an accumulator (a whole warp), times mul, zeros where !keep, to out (bf16) or part (fp32)
+__device__ __forceinline__ void drain_acc(uint32_t taddr, int cols, bool any, bool keep, bool mine, float mul,
+                                          __nv_bfloat16* out, bool vec, float* part) {
+    for (int q = 0; q < cols; q += 32) {
+        __syncwarp();
+        float v[32];
+        if (any) {
+            tmem_ld32(taddr + (uint32_t)q, v);
+        }
+#pragma unroll
+        for (int e = 0; e < 32; ++e) v[e] = any && keep ? v[e] * mul : 0.f;
+        if (mine) {
+            if (part)
+                store32(part + q, v, cols - q, cols % 4 == 0);
+            else
+                store32(out + q, v, cols - q, vec);
+        }
+    }
+}
+
+template <int DKC, int DVC>
+__global__ void __launch_bounds__(kThreads, 1)
+    k_xattn_dkv_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mo,
+                   const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const Params p) {
+    using C = Cfg<DKC, DVC>;
+    constexpr int ST = C::kStages;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    uint8_t* base = smem_raw + (((raw + 1023u) & ~1023u) - raw);
+    uint8_t* Ks = base;
+    uint8_t* Vs = Ks + DKC * kChunkBytes;
+    uint8_t* Qr = Vs + DVC * kChunkBytes;                 // ring of Q tiles
+    uint8_t* Or = Qr + (size_t)ST * DKC * kChunkBytes;    // ring of dO tiles
+    Ctl& c = *reinterpret_cast<Ctl*>(Or + (size_t)ST * DVC * kChunkBytes);
+    volatile int* abort_flag = &c.abort_flag;
+    unsigned* err = &g_err_xbwd;
+    const XattnArgs& a = p.a;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    long long i = blockIdx.x;
+    const int kt = (int)(i % p.ktiles);
+    i /= p.ktiles;
+    const int part = (int)(i % a.rsplits);
+    i /= a.rsplits;
+    const int hk = (int)(i % a.Hkv), b = (int)(i / a.Hkv);
+    const int tile_rows = p.nl * a.G;
+    const int n = keys_of(a, b), j0 = kt * kTile;
+    const long long t0 = p.rtiles * part / a.rsplits, t1 = p.rtiles * (part + 1) / a.rsplits;
+    const int nt = j0 < n ? (int)(t1 - t0) : 0;  // row tiles
+
+    if (threadIdx.x == 0) {
+        mbar_init(&c.own_full, 1);
+        for (int s = 0; s < ST; ++s) {
+            mbar_init(&c.a_full[s], 1);
+            mbar_init(&c.a_empty[s], 1);
+            mbar_init(&c.b_full[s], 1);
+            mbar_init(&c.b_empty[s], 1);
+            mbar_init(&c.st_full[s], 1);
+            mbar_init(&c.st_empty[s], kSoftWarps);
+        }
+        mbar_init(&c.s_full, 1);
+        mbar_init(&c.dp_full, 1);
+        mbar_init(&c.p_full, kSoftWarps);
+        mbar_init(&c.ds_full, kSoftWarps);
+        mbar_init(&c.done, 1);
+        c.abort_flag = 0;
+        fence_barrier_init();
+    }
+    if (warp == kMmaWarp) {
+        tmem_alloc(&c.tmem_base, 512);
+        tmem_relinquish();
+    }
+    // rows of a tile that its box does not write (128 % G != 0) are summed over all the same: zeros
+    if (tile_rows < kTile) {
+        const int words = (kTile - tile_rows) * 8;  // 16-byte words per chunk
+        for (int e = threadIdx.x; e < ST * (DKC + DVC) * words; e += kThreads)
+            *reinterpret_cast<uint4*>(Qr + (size_t)(e / words) * kChunkBytes + tile_rows * 128 + (e % words) * 16) =
+                make_uint4(0, 0, 0, 0);
+        fence_proxy_async();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = c.tmem_base;
+    const uint32_t t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 256 + DVC * kChunk;
+
+    if (warp == kTmaWarp) {
+        if (lane == 0 && nt > 0) {
+            mbar_arrive_expect_tx(&c.own_full, (uint32_t)C::kOwn);
+            for (int k = 0; k < DKC; ++k)
+                tma_load_4d(Ks + (size_t)k * kChunkBytes, &mk, &c.own_full, k * kChunk, hk * p.khmul, j0, b * p.kmul);
+            for (int k = 0; k < DVC; ++k)
+                tma_load_4d(Vs + (size_t)k * kChunkBytes, &mv, &c.own_full, k * kChunk, hk * p.vhmul, j0, b * p.vmul);
+            RingPos rp;
+            int sa = 0, sb = 0;
+            for (int t = 0; t < nt; ++t, rp.next(ST)) {
+                const int s = rp.idx, l0 = (int)(t0 + t) * p.nl;
+                if (!mbar_wait_1t(&c.a_empty[s], rp.phase ^ 1u, abort_flag, err)) break;
+                mbar_arrive_expect_tx(&c.a_full[s], (uint32_t)(DKC * kChunk * 2 * tile_rows));
+                for (int k = 0; k < DKC; ++k)
+                    tma_load_4d(Qr + (size_t)(s * DKC + k) * kChunkBytes, &mq, &c.a_full[s], k * kChunk, hk * a.G, l0,
+                                b * p.qmul);
+                ++sa;
+                if (!mbar_wait_1t(&c.b_empty[s], rp.phase ^ 1u, abort_flag, err)) break;
+                mbar_arrive_expect_tx(&c.b_full[s], (uint32_t)(DVC * kChunk * 2 * tile_rows));
+                for (int k = 0; k < DVC; ++k)
+                    tma_load_4d(Or + (size_t)(s * DVC + k) * kChunkBytes, &mo, &c.b_full[s], k * kChunk, hk * a.G, l0,
+                                b * p.omul);
+                ++sb;
+            }
+            mbar_drain(&c.own_full, 0, err);
+            for (int j = std::max(0, sa - ST); j < sa; ++j) mbar_drain(&c.a_full[j % ST], (uint32_t)(j / ST) & 1u, err);
+            for (int j = std::max(0, sb - ST); j < sb; ++j) mbar_drain(&c.b_full[j % ST], (uint32_t)(j / ST) & 1u, err);
+        }
+    } else if (warp == kAuxWarp) {
+        // ------------------------------------------------------------- the rows' statistics
+        RingPos rp;
+        for (int t = 0; t < nt; ++t, rp.next(ST)) {
+            if (!mbar_wait_warp(&c.st_empty[rp.idx], rp.phase ^ 1u, abort_flag, err)) break;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int r = 32 * e + lane;
+                const long long pr = (t0 + t) * tile_rows + r;
+                float L = -INFINITY, D = 0.f;
+                if (r < tile_rows && pr < a.rows) {
+                    const long long ql = pr / a.G;
+                    const long long at = ((long long)b * a.Hq + hk * a.G + (int)(pr - ql * a.G)) * a.Lq + ql;
+                    L = neg_lse2(__ldg(a.lse + at));
+                    D = L == -INFINITY ? 0.f : -a.ws[at];
+                }
+                c.nlse[rp.idx][r] = L;
+                c.ndelta[rp.idx][r] = D;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&c.st_full[rp.idx]);
+        }
+    } else if (warp == kMmaWarp) {
+        if (lane == 0 && nt > 0) {
+            const uint32_t id_s = idesc_bf16_f32(kTile), id_v = idesc_bf16_bmn(DVC * kChunk), id_k = idesc_bf16_bmn(DKC * kChunk);
+            const uint32_t ka = smem_u32(Ks), va = smem_u32(Vs), qa = smem_u32(Qr), oa = smem_u32(Or);
+            RingPos cur, nxt;  // stages of this row tile and of the next
+            auto scores = [&](const RingPos& r) {
+                if (!mbar_wait_1t(&c.a_full[r.idx], r.phase, abort_flag, err)) return false;
+                tc_fence_after();
+                mma_tile_ss(t_s, ka, qa + (uint32_t)(r.idx * DKC * kChunkBytes), id_s, p.ksteps);
+                mma_commit(&c.s_full);
+                return true;
+            };
+            auto dprod = [&](const RingPos& r) {
+                if (!mbar_wait_1t(&c.b_full[r.idx], r.phase, abort_flag, err)) return false;
+                tc_fence_after();
+                mma_tile_ss(t_dp, va, oa + (uint32_t)(r.idx * DVC * kChunkBytes), id_s, p.vsteps);
+                mma_commit(&c.dp_full);
+                return true;
+            };
+            bool ok = mbar_wait_1t(&c.own_full, 0, abort_flag, err) && scores(cur) && dprod(cur);
+            for (int t = 0; t < nt && ok; ++t) {
+                nxt = cur;
+                nxt.next(ST);
+                if (!(ok = mbar_wait_1t(&c.p_full, (uint32_t)t & 1u, abort_flag, err))) break;
+                tc_fence_after();
+                mma_tile_ts(t_dv, t_s, 64u, oa + (uint32_t)(cur.idx * DVC * kChunkBytes), id_v, t != 0);
+                mma_commit(&c.b_empty[cur.idx]);
+                if (t + 1 < nt && !(ok = scores(nxt))) break;
+                if (!(ok = mbar_wait_1t(&c.ds_full, (uint32_t)t & 1u, abort_flag, err))) break;
+                tc_fence_after();
+                mma_tile_ts(t_dk, t_dp, 64u, qa + (uint32_t)(cur.idx * DKC * kChunkBytes), id_k, t != 0);
+                mma_commit(&c.a_empty[cur.idx]);
+                if (t + 1 < nt && !(ok = dprod(nxt))) break;
+                cur = nxt;
+            }
+            mma_commit(&c.done);
+            mbar_drain(&c.done, 0, err);
+        }
+    } else {
+        // ------------------------------------------------------------- softmax warps: a lane is a key
+        const int half = warp >> 2, quad = warp & 3;
+        const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
+        const uint32_t ts = t_s + lane_base + 64u * half, td = t_dp + lane_base + 64u * half;
+        const int j = j0 + quad * 32 + lane;
+        const bool valid = j < n && (!a.mask || __ldg(a.mask + (long long)b * a.ldm + j) != 0);
+        const bool whole = __all_sync(0xffffffffu, valid);
+        const float cs = a.scale * kLog2e;
+        RingPos rp;
+        bool ok = true;
+        for (int t = 0; t < nt; ++t, rp.next(ST)) {
+            const uint32_t ph = (uint32_t)t & 1u;
+            if (!mbar_wait_warp_inline(&c.st_full[rp.idx], rp.phase, abort_flag, err) ||
+                !mbar_wait_warp_inline(&c.s_full, ph, abort_flag, err)) {
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+            uint32_t sr[64], pk[32];
+            float* s = reinterpret_cast<float*>(sr);
+            tmem_ld32_issue(ts, sr);
+            tmem_ld32_issue(ts + 32u, sr + 32);
+            tmem_wait_ld32(sr);
+            tmem_wait_ld32(sr + 32);
+            const float4* nl = reinterpret_cast<const float4*>(&c.nlse[rp.idx][64 * half]);
+            const float4* nd = reinterpret_cast<const float4*>(&c.ndelta[rp.idx][64 * half]);
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+                const float4 L = nl[q];
+                float* x = s + 4 * q;
+                x[0] = ex2(fmaf(x[0], cs, L.x));
+                x[1] = ex2(fmaf(x[1], cs, L.y));
+                x[2] = ex2(fmaf(x[2], cs, L.z));
+                x[3] = ex2(fmaf(x[3], cs, L.w));
+            }
+            if (!whole) {
+#pragma unroll
+                for (int q = 0; q < 64; ++q) s[q] = valid ? s[q] : 0.f;
+            }
+#pragma unroll
+            for (int q = 0; q < 32; ++q) pk[q] = pack_bf16(s[2 * q], s[2 * q + 1]);
+            tmem_st32(ts, pk);
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&c.p_full);
+            if (!mbar_wait_warp_inline(&c.dp_full, ph, abort_flag, err)) {
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t dr[32];
+                float* d = reinterpret_cast<float*>(dr);
+                tmem_ld32_issue(td + 32u * h, dr);
+                tmem_wait_ld32(dr);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const float4 D = nd[8 * h + q];
+                    float* x = d + 4 * q;
+                    const float* w = s + 32 * h + 4 * q;
+                    add2(x[0], x[1], D.x, D.y);
+                    add2(x[2], x[3], D.z, D.w);
+                    mul2(x[0], x[1], w[0], w[1]);
+                    mul2(x[2], x[3], w[2], w[3]);
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int q = 0; q < 32; ++q) d[q] = valid ? d[q] : 0.f;
+                }
+#pragma unroll
+                for (int q = 0; q < 16; ++q) pk[16 * h + q] = pack_bf16(d[2 * q], d[2 * q + 1]);
+            }
+            tmem_st32(td, pk);
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(&c.ds_full);
+                mbar_arrive(&c.st_empty[rp.idx]);
+            }
+        }
+        if (ok && nt > 0) ok = mbar_wait_warp_inline(&c.done, 0, abort_flag, err);
+        tc_fence_after();
+        if (ok) {  // group 0 writes dV, group 1 dK
+            const bool mine = j < a.Lk;
+            const long long jj = mine ? j : 0;
+            const long long nk = (long long)a.B * a.Hkv * a.Lk;
+            const long long at = ((long long)part * nk + ((long long)b * a.Hkv + hk) * a.Lk + jj);
+            const bool parts = a.rsplits > 1;
+            if (half == 0)
+                drain_acc(t_dv + lane_base, a.dv, nt > 0, valid, mine, 1.f,
+                          reinterpret_cast<__nv_bfloat16*>(a.dV.p) + b * a.dV.b + jj * a.dV.l + hk * a.dV.h, p.vec_v != 0,
+                          parts ? a.ws + xattn_ws_dv(a) + at * a.dv : nullptr);
+            else
+                drain_acc(t_dk + lane_base, a.dk, nt > 0, valid, mine, parts ? 1.f : a.scale,
+                          reinterpret_cast<__nv_bfloat16*>(a.dK.p) + b * a.dK.b + jj * a.dK.l + hk * a.dK.h, p.vec_k != 0,
+                          parts ? a.ws + xattn_ws_dk(a) + at * a.dk : nullptr);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+template <int DKC, int DVC>
+__global__ void __launch_bounds__(kThreads, 1)
+    k_xattn_dq_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mo,
+                  const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const Params p) {
+    using C = Cfg<DKC, DVC>;
+    constexpr int ST = C::kStages;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    uint8_t* base = smem_raw + (((raw + 1023u) & ~1023u) - raw);
+    uint8_t* Qs = base;
+    uint8_t* Os = Qs + DKC * kChunkBytes;
+    uint8_t* Kr = Os + DVC * kChunkBytes;               // ring of K tiles
+    uint8_t* Vr = Kr + (size_t)ST * DKC * kChunkBytes;  // ring of V tiles
+    Ctl& c = *reinterpret_cast<Ctl*>(Vr + (size_t)ST * DVC * kChunkBytes);
+    volatile int* abort_flag = &c.abort_flag;
+    unsigned* err = &g_err_xbwd;
+    const XattnArgs& a = p.a;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    long long i = blockIdx.x;
+    const long long rt = i % p.rtiles;
+    i /= p.rtiles;
+    const int part = (int)(i % a.splits);
+    i /= a.splits;
+    const int hk = (int)(i % a.Hkv), b = (int)(i / a.Hkv);
+    const int tile_rows = p.nl * a.G;
+    const int n = keys_of(a, b);
+    const int t0 = (int)((long long)p.ktiles * part / a.splits);
+    const int t1 = min((int)((long long)p.ktiles * (part + 1) / a.splits), (n + kTile - 1) / kTile);
+    const int nt = max(0, t1 - t0);  // key tiles
+    const bool fix = a.lens != nullptr || a.mask != nullptr;
+
+    if (threadIdx.x == 0) {
+        mbar_init(&c.own_full, 1);
+        for (int s = 0; s < ST; ++s) {
+            mbar_init(&c.a_full[s], 1);
+            mbar_init(&c.a_empty[s], 1);
+            mbar_init(&c.a_ready[s], 1);
+            mbar_init(&c.b_full[s], 1);
+            mbar_init(&c.b_empty[s], 1);
+        }
+        mbar_init(&c.s_full, 1);
+        mbar_init(&c.dp_full, 1);
+        mbar_init(&c.ds_full, kSoftWarps);
+        mbar_init(&c.s_free, kSoftWarps);
+        mbar_init(&c.dp_free, kSoftWarps);
+        mbar_init(&c.ds_free, 1);
+        mbar_init(&c.done, 1);
+        c.abort_flag = 0;
+        fence_barrier_init();
+    }
+    if (warp == kMmaWarp) {
+        tmem_alloc(&c.tmem_base, 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = c.tmem_base;
+    const uint32_t t_s = tmem, t_dp = tmem + 128, t_dq = tmem + 256, t_ds = tmem + 384;  // dS: 64 columns of bf16 pairs
+
+    if (warp == kTmaWarp) {
+        if (lane == 0 && nt > 0) {
+            mbar_arrive_expect_tx(&c.own_full, (uint32_t)((DKC + DVC) * kChunk * 2 * tile_rows));
+            for (int k = 0; k < DKC; ++k)
+                tma_load_4d(Qs + (size_t)k * kChunkBytes, &mq, &c.own_full, k * kChunk, hk * a.G, (int)rt * p.nl, b * p.qmul);
+            for (int k = 0; k < DVC; ++k)
+                tma_load_4d(Os + (size_t)k * kChunkBytes, &mo, &c.own_full, k * kChunk, hk * a.G, (int)rt * p.nl, b * p.omul);
+            RingPos rp;
+            int sa = 0, sb = 0;
+            for (int t = 0; t < nt; ++t, rp.next(ST)) {
+                const int s = rp.idx;
+                if (!mbar_wait_1t(&c.a_empty[s], rp.phase ^ 1u, abort_flag, err)) break;
+                mbar_arrive_expect_tx(&c.a_full[s], (uint32_t)(DKC * kChunkBytes));
+                for (int k = 0; k < DKC; ++k)
+                    tma_load_4d(Kr + (size_t)(s * DKC + k) * kChunkBytes, &mk, &c.a_full[s], k * kChunk, hk * p.khmul,
+                                (t0 + t) * kTile, b * p.kmul);
+                ++sa;
+                if (!mbar_wait_1t(&c.b_empty[s], rp.phase ^ 1u, abort_flag, err)) break;
+                mbar_arrive_expect_tx(&c.b_full[s], (uint32_t)(DVC * kChunkBytes));
+                for (int k = 0; k < DVC; ++k)
+                    tma_load_4d(Vr + (size_t)(s * DVC + k) * kChunkBytes, &mv, &c.b_full[s], k * kChunk, hk * p.vhmul,
+                                (t0 + t) * kTile, b * p.vmul);
+                ++sb;
+            }
+            mbar_drain(&c.own_full, 0, err);
+            for (int j = std::max(0, sa - ST); j < sa; ++j) mbar_drain(&c.a_full[j % ST], (uint32_t)(j / ST) & 1u, err);
+            for (int j = std::max(0, sb - ST); j < sb; ++j) mbar_drain(&c.b_full[j % ST], (uint32_t)(j / ST) & 1u, err);
+        }
+    } else if (warp == kAuxWarp) {
+        // ------------------------------------------------------------- rows of K that are not read
+        RingPos rp;
+        for (int t = 0; t < nt && fix; ++t, rp.next(ST)) {
+            uint32_t w[4];
+            valid_words(w, a, b, (t0 + t) * kTile, n);
+            if (!mbar_wait_warp(&c.a_full[rp.idx], rp.phase, abort_flag, err)) break;
+            if ((w[0] & w[1] & w[2] & w[3]) != 0xffffffffu) {
+                zero_rows(Kr + (size_t)rp.idx * DKC * kChunkBytes, DKC, w);
+                fence_proxy_async();
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&c.a_ready[rp.idx]);
+        }
+    } else if (warp == kMmaWarp) {
+        if (lane == 0 && nt > 0) {
+            const uint32_t id_s = idesc_bf16_f32(kTile), id_q = idesc_bf16_bmn(DKC * kChunk);
+            const uint32_t qa = smem_u32(Qs), oa = smem_u32(Os), ka = smem_u32(Kr), va = smem_u32(Vr);
+            RingPos cur, nxt;
+            auto scores = [&](const RingPos& r) {
+                if (!mbar_wait_1t(fix ? &c.a_ready[r.idx] : &c.a_full[r.idx], r.phase, abort_flag, err)) return false;
+                tc_fence_after();
+                mma_tile_ss(t_s, qa, ka + (uint32_t)(r.idx * DKC * kChunkBytes), id_s, p.ksteps);
+                mma_commit(&c.s_full);
+                return true;
+            };
+            auto dprod = [&](const RingPos& r) {
+                if (!mbar_wait_1t(&c.b_full[r.idx], r.phase, abort_flag, err)) return false;
+                tc_fence_after();
+                mma_tile_ss(t_dp, oa, va + (uint32_t)(r.idx * DVC * kChunkBytes), id_s, p.vsteps);
+                mma_commit(&c.dp_full);
+                mma_commit(&c.b_empty[r.idx]);
+                return true;
+            };
+            bool ok = mbar_wait_1t(&c.own_full, 0, abort_flag, err) && scores(cur) && dprod(cur);
+            for (int t = 0; t < nt && ok; ++t) {
+                const uint32_t ph = (uint32_t)t & 1u;
+                nxt = cur;
+                nxt.next(ST);
+                if (t + 1 < nt && !(ok = mbar_wait_1t(&c.s_free, ph, abort_flag, err) && scores(nxt))) break;
+                if (t + 1 < nt && !(ok = mbar_wait_1t(&c.dp_free, ph, abort_flag, err) && dprod(nxt))) break;
+                if (!(ok = mbar_wait_1t(&c.ds_full, ph, abort_flag, err))) break;
+                tc_fence_after();
+                mma_tile_ts(t_dq, t_ds, 32u, ka + (uint32_t)(cur.idx * DKC * kChunkBytes), id_q, t != 0);
+                mma_commit(&c.ds_free);
+                mma_commit(&c.a_empty[cur.idx]);
+                cur = nxt;
+            }
+            mma_commit(&c.done);
+            mbar_drain(&c.done, 0, err);
+        }
+    } else {
+        // ------------------------------------------------------------- softmax warps: a lane is a row
+        const int half = warp >> 2, quad = warp & 3;
+        const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
+        const uint32_t ts = t_s + lane_base + 64u * half, td = t_dp + lane_base + 64u * half;
+        const int r = quad * 32 + lane;
+        const long long pr = rt * tile_rows + r;
+        const bool mine = r < tile_rows && pr < a.rows;
+        const long long ql = mine ? pr / a.G : 0;
+        const int h = hk * a.G + (mine ? (int)(pr - ql * a.G) : 0);
+        const long long at = ((long long)b * a.Hq + h) * a.Lq + ql;
+        const float cs = a.scale * kLog2e;
+        const float nl = mine ? neg_lse2(__ldg(a.lse + at)) : -INFINITY;
+        const bool none = nl == -INFINITY;
+        const float nd = none ? 0.f : -a.ws[at];
+        bool ok = true;
+        for (int t = 0; t < nt; ++t) {
+            const uint32_t ph = (uint32_t)t & 1u;
+            const int j0 = (t0 + t) * kTile;
+            const bool whole = j0 + kTile <= n && !a.mask;
+            uint32_t w[4];
+            if (!whole) valid_words(w, a, b, j0, n);
+            if (!mbar_wait_warp_inline(&c.s_full, ph, abort_flag, err)) {
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+            uint32_t sr[64], pk[32];
+            float* s = reinterpret_cast<float*>(sr);
+            tmem_ld32_issue(ts, sr);
+            tmem_ld32_issue(ts + 32u, sr + 32);
+            tmem_wait_ld32(sr);
+            tmem_wait_ld32(sr + 32);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&c.s_free);
+#pragma unroll
+            for (int q = 0; q < 64; q += 2) {
+                fma2(s[q], s[q + 1], cs, nl);
+                s[q] = ex2(s[q]);
+                s[q + 1] = ex2(s[q + 1]);
+            }
+            if (!mbar_wait_warp_inline(&c.dp_full, ph, abort_flag, err)) {
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+                uint32_t dr[32];
+                float* d = reinterpret_cast<float*>(dr);
+                tmem_ld32_issue(td + 32u * hh, dr);
+                tmem_wait_ld32(dr);
+#pragma unroll
+                for (int q = 0; q < 32; q += 2) {
+                    add2(d[q], d[q + 1], nd, nd);
+                    mul2(d[q], d[q + 1], s[32 * hh + q], s[32 * hh + q + 1]);
+                }
+                if (!whole) {
+                    const uint32_t ww = half == 0 ? w[hh] : w[2 + hh];
+#pragma unroll
+                    for (int q = 0; q < 32; ++q) d[q] = (ww >> q) & 1u ? d[q] : 0.f;
+                }
+#pragma unroll
+                for (int q = 0; q < 16; ++q) pk[16 * hh + q] = pack_bf16(d[2 * q], d[2 * q + 1]);
+            }
+            if (none) {  // (NaN in dO of a row without weight stays out)
+#pragma unroll
+                for (int q = 0; q < 32; ++q) pk[q] = 0u;
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&c.dp_free);
+            if (t > 0 && !mbar_wait_warp_inline(&c.ds_free, (uint32_t)(t - 1) & 1u, abort_flag, err)) {
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+            tmem_st32(t_ds + lane_base + 32u * half, pk);
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&c.ds_full);
+        }
+        if (ok && nt > 0) ok = mbar_wait_warp_inline(&c.done, 0, abort_flag, err);
+        tc_fence_after();
+        if (ok && half == 0)
+            drain_acc(t_dq + lane_base, a.dk, nt > 0, !none, mine, a.splits > 1 ? 1.f : a.scale,
+                      reinterpret_cast<__nv_bfloat16*>(a.dQ.p) + b * a.dQ.b + ql * a.dQ.l + h * a.dQ.h, p.vec_q != 0,
+                      a.splits > 1 ? a.ws + xattn_ws_dq(a) + ((long long)part * a.B * a.Hq * a.Lq + at) * a.dk : nullptr);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+bool g_attr[64][4];
+
+template <int DKC, int DVC>
+cudaError_t launch(const HeadMap& q, const HeadMap& o, const HeadMap& k, const HeadMap& v, const Params& p, int device,
+                   cudaStream_t s) {
+    using C = Cfg<DKC, DVC>;
+    const XattnArgs& a = p.a;
+    bool& set = g_attr[device][(DKC - 1) * 2 + DVC - 1];
+    cudaError_t e = cudaSuccess;
+    if (!set) {
+        e = cudaFuncSetAttribute(k_xattn_dkv_tc<DKC, DVC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
+        if (e == cudaSuccess)
+            e = cudaFuncSetAttribute(k_xattn_dq_tc<DKC, DVC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
+        if (e != cudaSuccess) return e;
+        set = true;
+    }
+    k_xattn_dkv_tc<DKC, DVC><<<(unsigned)((long long)p.ktiles * a.rsplits * a.Hkv * a.B), kThreads, C::kSmem, s>>>(
+        q.map, o.map, k.map, v.map, p);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if (a.rsplits > 1 && (e = launch_xattn_join_dkv(a, s)) != cudaSuccess) return e;
+    k_xattn_dq_tc<DKC, DVC><<<(unsigned)(p.rtiles * a.splits * a.Hkv * a.B), kThreads, C::kSmem, s>>>(q.map, o.map, k.map,
+                                                                                                      v.map, p);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    return a.splits > 1 ? launch_xattn_join_dq(a, s) : cudaSuccess;
+}
+
+bool on_vectors(const HeadView& v, int B, int L, int H, int w) {
+    return w % 8 == 0 && (uintptr_t)v.p % 16 == 0 && (B <= 1 || v.b % 8 == 0) && (L <= 1 || v.l % 8 == 0) &&
+           (H <= 1 || v.h % 8 == 0);
+}
+
+}  // namespace
+
+unsigned take_device_error_xbwd() {
+    unsigned v = 0, z = 0;
+    cudaMemcpyFromSymbol(&v, g_err_xbwd, sizeof(v));
+    if (v) cudaMemcpyToSymbol(g_err_xbwd, &z, sizeof(z));
+    return v;
+}
+
+bool xattn_bwd_tc_supported(const XattnArgs& a) {
+    return xattn_tc_supported(a) && map_supported(a.dO, a.B, a.Lq, a.Hq) && (a.Hq <= 1 || a.dO.h > 0);
+}
+
+void xattn_bwd_tc_plan(XattnArgs& a, int sms) {
+    const long long nl = kTile / a.G;
+    const long long kt = (a.Lk + kTile - 1) / kTile, rt = (a.Lq + nl - 1) / nl;
+    // the keys (rows) are cut into parts of two tiles or more where one CTA per row (key) tile leaves multiprocessors idle
+    a.splits = xattn_parts(rt * a.Hkv * a.B, kt, sms, 2);
+    a.rsplits = xattn_parts(kt * a.Hkv * a.B, rt, sms, 2);
+}
+
+cudaError_t launch_xattn_bwd_tc(const XattnArgs& a, int device, cudaStream_t s) {
+    if (device < 0 || device >= 64) return cudaErrorInvalidDevice;
+    Params p{};
+    p.a = a;
+    p.nl = kTile / a.G;
+    p.rtiles = (a.Lq + p.nl - 1) / p.nl;
+    p.ktiles = (a.Lk + kTile - 1) / kTile;
+    p.ksteps = (a.dk + 15) / 16;
+    p.vsteps = (a.dv + 15) / 16;
+    p.vec_q = on_vectors(a.dQ, a.B, a.Lq, a.Hq, a.dk);
+    p.vec_k = on_vectors(a.dK, a.B, a.Lk, a.Hkv, a.dk);
+    p.vec_v = on_vectors(a.dV, a.B, a.Lk, a.Hkv, a.dv);
+    HeadMap q, o, k, v;
+    if (!make_head_map(&q, a.q, a.B, a.Lq, a.Hq, a.dk, a.G, p.nl) || !make_head_map(&o, a.dO, a.B, a.Lq, a.Hq, a.dv, a.G, p.nl) ||
+        !make_head_map(&k, a.k, a.B, a.Lk, a.Hkv, a.dk, 1, kTile) || !make_head_map(&v, a.v, a.B, a.Lk, a.Hkv, a.dv, 1, kTile))
+        return cudaErrorInvalidValue;
+    p.qmul = q.bmul;
+    p.omul = o.bmul;
+    p.kmul = k.bmul;
+    p.khmul = k.hmul;
+    p.vmul = v.bmul;
+    p.vhmul = v.hmul;
+    cudaError_t e = launch_xattn_delta(a, s);
+    if (e != cudaSuccess) return e;
+    const bool k2 = a.dk > kChunk, v2 = a.dv > kChunk;
+    return k2 ? (v2 ? launch<2, 2>(q, o, k, v, p, device, s) : launch<2, 1>(q, o, k, v, p, device, s))
+              : (v2 ? launch<1, 2>(q, o, k, v, p, device, s) : launch<1, 1>(q, o, k, v, p, device, s));
+}
+
+}  // namespace gs

@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(kThreads) k_xattn(const XattnArgs a, long long
                 if (col < a.dv) po[col] = o[i][q];
             }
             if (tx == 0) {
-                float* ml = a.ws + (long long)a.splits * nrows * a.dv + ((long long)bl.part * nrows + at) * 2;
+                float* ml = a.ws + xattn_ws_ml(a) + ((long long)bl.part * nrows + at) * 2;
                 ml[0] = m[i];
                 ml[1] = l[i];
             }
@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(256) k_xattn_join(const XattnArgs a) {
     const long long at = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
     const int lane = threadIdx.x & 31;
     if (at >= nrows) return;
-    const float* ml = a.ws + (long long)a.splits * nrows * a.dv;
+    const float* ml = a.ws + xattn_ws_ml(a);
     float m = -INFINITY;
     for (int s = lane; s < a.splits; s += 32) m = fmaxf(m, ml[((long long)s * nrows + at) * 2]);
 #pragma unroll
@@ -396,7 +396,7 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long l
             const int col = 64 * (q / 4) + 4 * tx + q % 4;
             if (col >= a.dk) continue;
             if (a.splits > 1)
-                a.ws[xattn_ws_delta(a) + ((long long)bl.part * nrows + row_index(a, bl.b, bl.hk, r)) * a.dk + col] = o[i][q];
+                a.ws[xattn_ws_dq(a) + ((long long)bl.part * nrows + row_index(a, bl.b, bl.hk, r)) * a.dk + col] = o[i][q];
             else
                 row_at<T>(a, a.dQ, bl.b, bl.hk, r)[col] = from_f32<T>(o[i][q] * a.scale);
         }
@@ -450,8 +450,6 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dkv(const XattnArgs a, int k
         weigh<DK>(ok_, Ws, Qs);
     }
     const long long nk = (long long)a.B * a.Hkv * a.Lk;
-    float* parts = a.ws + xattn_ws_delta(a);
-    if (a.splits > 1) parts += (long long)a.splits * a.B * a.Hq * a.Lq * a.dk;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int j = j0 + ty + 16 * i;
@@ -462,7 +460,7 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dkv(const XattnArgs a, int k
             const int col = 64 * (q / 4) + 4 * tx + q % 4;
             if (col >= a.dk) continue;
             if (a.rsplits > 1)
-                parts[((long long)bl.part * nk + at) * a.dk + col] = ok_[i][q];
+                a.ws[xattn_ws_dk(a) + ((long long)bl.part * nk + at) * a.dk + col] = ok_[i][q];
             else
                 (reinterpret_cast<T*>(a.dK.p) + bl.b * a.dK.b + j * a.dK.l + bl.hk * a.dK.h)[col] =
                     from_f32<T>(ok_[i][q] * a.scale);
@@ -472,7 +470,7 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dkv(const XattnArgs a, int k
             const int col = 64 * (q / 4) + 4 * tx + q % 4;
             if (col >= a.dv) continue;
             if (a.rsplits > 1)
-                parts[(long long)a.rsplits * nk * a.dk + ((long long)bl.part * nk + at) * a.dv + col] = ov[i][q];
+                a.ws[xattn_ws_dv(a) + ((long long)bl.part * nk + at) * a.dv + col] = ov[i][q];
             else
                 (reinterpret_cast<T*>(a.dV.p) + bl.b * a.dV.b + j * a.dV.l + bl.hk * a.dV.h)[col] = from_f32<T>(ov[i][q]);
         }
@@ -584,7 +582,7 @@ cudaError_t launch_xattn_join(const XattnArgs& a, cudaStream_t s) {
 
 cudaError_t launch_xattn_join_dq(const XattnArgs& a, cudaStream_t s) {
     const long long n = (long long)a.B * a.Hq * a.Lq * a.dk;
-    const float* src = a.ws + xattn_ws_delta(a);
+    const float* src = a.ws + xattn_ws_dq(a);
     if (a.dtype == GS_F32)
         k_xattn_sum<float><<<sum_grid(n), 256, 0, s>>>(src, a.splits, n, a.dQ, a.Hq, a.Lq, a.dk, a.scale);
     else
@@ -594,9 +592,7 @@ cudaError_t launch_xattn_join_dq(const XattnArgs& a, cudaStream_t s) {
 
 cudaError_t launch_xattn_join_dkv(const XattnArgs& a, cudaStream_t s) {
     const long long rows = (long long)a.B * a.Hkv * a.Lk;
-    const float* src = a.ws + xattn_ws_delta(a);
-    if (a.splits > 1) src += (long long)a.splits * a.B * a.Hq * a.Lq * a.dk;
-    const float* srcv = src + (long long)a.rsplits * rows * a.dk;
+    const float *src = a.ws + xattn_ws_dk(a), *srcv = a.ws + xattn_ws_dv(a);
     const long long nk = rows * a.dk, nv = rows * a.dv;
     if (a.dtype == GS_F32) {
         k_xattn_sum<float><<<sum_grid(nk), 256, 0, s>>>(src, a.rsplits, nk, a.dK, a.Hkv, a.Lk, a.dk, a.scale);

@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (mine) {
                 if (a.splits > 1) {
-                    float2* ml = reinterpret_cast<float2*>(a.ws + (long long)a.splits * all * a.dv) + (long long)part * all + at;
+                    float2* ml = reinterpret_cast<float2*>(a.ws + xattn_ws_ml(a)) + (long long)part * all + at;
                     *ml = make_float2(m2, l);
                 } else if (a.lse) {
                     a.lse[at] = l == 0.f ? -INFINITY : (m2 + log2f(l)) * kLn2;

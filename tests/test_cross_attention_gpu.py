@@ -328,6 +328,21 @@ def test_tensor_cores(gs, shape, kind):
     check_forward(gs, Q, K, V, 1.0 / math.sqrt(shape[5]), lens, mask, "tensor", True)
 
 
+BACKWARD_SHAPES = TENSOR_SHAPES + [
+    (1, 3000, 100, 2, 1, 64, 64),        # rows in parts
+    (1, 700, 900, 2, 2, 128, 64),        # both in parts
+    (2, 1, 300, 7, 1, 64, 128),
+]
+
+
+@pytest.mark.parametrize("kind", ["none", "lens", "holes", "both"])
+@pytest.mark.parametrize("shape", BACKWARD_SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_tensor_cores_backward(gs, shape, kind):
+    Q, K, V, dO = make(*shape, "bf16")
+    lens, mask = masks(kind, shape[0], shape[2])
+    check_grad(gs, Q, K, V, dO, 1.0 / math.sqrt(shape[5]), lens, mask, "tensor", True)
+
+
 def test_growing_maxima(gs):
     """Keys whose logits grow along the sequence by far more than the running maximum lags, and fall again."""
     for B, H in ((1, 2), (16, 16)):
