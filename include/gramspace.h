@@ -489,9 +489,9 @@ GS_API gs_status gs_cross_attention_backward(const gs_attn* a, const gs_heads* Q
  * prob 0); beside a +inf only +infs are.  T = 0 (or negative or NaN): index = the first of the
  * largest scores, prob 1.  U is taken as 0 where it is negative or NaN, and as the largest fp32
  * below 1 from 1 on.
- * Weights are 64-bit fixed point numbers: exp to a relative error below 2^-38 of the largest
- * weight's scale, sums exact in any order, so that a draw differs from exact arithmetic's
- * only where U lies that close to a border.
+ * Weights are 64-bit fixed point numbers (2^41 for the largest), exact to a relative 2^-34 and
+ * to half a unit, their sums exact in any order, so that a draw differs from exact
+ * arithmetic's only where U lies that close to a border.
  * The four settings come as one number for all rows or, where the pointer is not
  * NULL, one per row (device arrays of N).  index (N int32) and prob (N fp32) are
  * optional, not both NULL.  N = 0 is a no-op.  No workspace.

@@ -1021,7 +1021,7 @@ gs_status gs_sample_scores(const void* S, int s_dtype, long long N, int M, long 
     a.S = S; a.bf16 = s_dtype == GS_BF16; a.N = N; a.M = M; a.lds = lds;
     a.how = *how;
     a.U = U; a.index = index; a.prob = prob;
-    return from_cuda(gs::launch_sample(a, sms, (cudaStream_t)stream));
+    return from_cuda(gs::launch_sample(a, dev, (cudaStream_t)stream));
 }
 
 gs_status gs_selftest_wait_timeout(void* stream) {

@@ -94,6 +94,6 @@ struct SampleArgs {
     int* index;
     float* prob;
 };
-cudaError_t launch_sample(const SampleArgs& a, int sms, cudaStream_t s);
+cudaError_t launch_sample(const SampleArgs& a, int device, cudaStream_t s);
 
 }  // namespace gs

@@ -9,7 +9,7 @@ DT = {"f32": torch.float32, "bf16": torch.bfloat16}
 
 def reference(s, u, T, k, p, mp):
     """(the indices that exact arithmetic may draw, {index: probability}): two where u ends within 2^-35 of the kept
-    weight from a border (the call's exponentials are exact to 2^-38 of the largest weight, each)."""
+    weight from a border (weights exact to a relative e = 2^-34 move a share p by at most 2 p (1 - p) e <= 2^-35)."""
     s = np.asarray(s, dtype=np.longdouble)
     M = s.size
     live = ~np.isnan(s) & (s != -np.inf)
@@ -58,7 +58,7 @@ def check(gs, S, U, T=1.0, k=0, p=1.0, mp=0.0, **kw):
     for n in range(N):
         cand, pr = reference(s[n], *(c[n] for c in cols))
         assert int(idx[n]) in cand, (n, int(idx[n]), cand)
-        # two conversions and one division in fp32, weights exact to 2^-38
+        # two conversions and one division in fp32, weights exact to 2^-34
         assert abs(prob[n] - pr[int(idx[n])]) <= 4 * 2.0 ** -24 * pr[int(idx[n])] + 2.0 ** -37, n
     return out
 
