@@ -26,6 +26,7 @@ struct XattnArgs {
     float* ws;     // workspace
     int splits;    // forward, dQ: parts of the key axis
     int rsplits;   // dK / dV: parts of the packed rows
+    long long stats;  // backward: floats of the rows' statistics at the start of the workspace
 };
 
 // How many parts a kernel cuts its long axis into, so that about `want` blocks run: `base` blocks
@@ -40,14 +41,14 @@ inline int xattn_parts(long long base, long long tiles, int want, int least) {
 
 // Workspace in floats; every section starts on a 16-byte boundary.
 // Forward (splits > 1): per part and row dv sums, then the row's maximum (base 2) and sum.
-// Backward: D_i per row, then the parts of dQ (splits > 1), of dK and of dV (rsplits > 1).
+// Backward: the rows' statistics (a.stats), then the parts of dQ (splits > 1), of dK and of dV (rsplits > 1).
 #define GS_XWS __host__ __device__ inline long long
 GS_XWS xattn_round4(long long n) { return (n + 3) / 4 * 4; }
 GS_XWS xattn_rows(const XattnArgs& a) { return (long long)a.B * a.Hq * a.Lq; }
 GS_XWS xattn_keys(const XattnArgs& a) { return (long long)a.B * a.Hkv * a.Lk; }
 GS_XWS xattn_ws_ml(const XattnArgs& a) { return xattn_round4(a.splits * xattn_rows(a) * a.dv); }
 GS_XWS xattn_ws_forward(const XattnArgs& a) { return a.splits > 1 ? xattn_ws_ml(a) + a.splits * xattn_rows(a) * 2 : 0; }
-GS_XWS xattn_ws_dq(const XattnArgs& a) { return xattn_round4(xattn_rows(a)); }
+GS_XWS xattn_ws_dq(const XattnArgs& a) { return a.stats; }
 GS_XWS xattn_ws_dk(const XattnArgs& a) {
     return xattn_ws_dq(a) + (a.splits > 1 ? xattn_round4(a.splits * xattn_rows(a) * a.dk) : 0);
 }
@@ -64,8 +65,6 @@ GS_XWS xattn_ws_backward(const XattnArgs& a) {
 void xattn_simt_plan(XattnArgs& a, bool backward, int sms);
 cudaError_t launch_xattn_simt(const XattnArgs& a, cudaStream_t s);
 cudaError_t launch_xattn_simt_backward(const XattnArgs& a, cudaStream_t s);
-// D_i = <dO_i, O_i> into ws
-cudaError_t launch_xattn_delta(const XattnArgs& a, cudaStream_t s);
 // O and lse from a.splits parts; dQ, dK, dV from theirs
 cudaError_t launch_xattn_join(const XattnArgs& a, cudaStream_t s);
 cudaError_t launch_xattn_join_dq(const XattnArgs& a, cudaStream_t s);

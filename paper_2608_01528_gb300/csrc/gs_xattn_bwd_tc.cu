@@ -10,8 +10,9 @@
 //
 // P and dS go from TMEM to registers and back as bf16, where they are the A operand (lanes are keys in the first kernel,
 // rows in the second, so neither needs a transpose); the B operands Q, dO, K are read as they lie (MN-major).
-// Eight softmax warps: warp w reads lanes 32 (w % 4)..+31 and columns 64 (w / 4)..+63.  While they work on S the tensor
-// core runs dP or the sums, and the other way round.
+// Sixteen softmax warps: warp w reads lanes 32 (w % 4)..+31 and columns 32 (w / 4)..+31.  While they work on S the tensor
+// core runs dP or the sums, and the other way round.  The rows' statistics (-lse log2 e, -D) are laid out
+// per row tile by k_xattn_stats, so that a tile's come with one copy.
 //
 // Keys that are not read: P = dS = 0, and in the second kernel their rows of K are zeroed in shared memory before
 // the MMA reads them (0 * NaN).  Rows past the end have lse = +inf: P = 0.
@@ -29,9 +30,11 @@ using namespace xtc;
 
 __device__ unsigned g_err_xbwd = 0;
 
-constexpr int kMmaWarp = 8, kTmaWarp = 9, kAuxWarp = 10;
-constexpr int kThreads = 11 * 32;
-constexpr int kSoftWarps = 8;
+constexpr int kSoftWarps = 16;
+constexpr int kMmaWarp = 16, kTmaWarp = 17, kMaskWarp = 18;
+constexpr int kThreads = 19 * 32;
+constexpr int kCols = 32;        // of a softmax warp
+constexpr int kStats = 2 * kTile;  // floats of a row tile: -lse log2 e (-inf: no weight), then -D
 
 struct Ctl {
     uint64_t own_full;                               // the tiles that stay
@@ -41,12 +44,11 @@ struct Ctl {
     uint64_t s_full, p_full, dp_full, ds_full;       // MMA <-> softmax
     uint64_t s_free, dp_free, ds_free;               // dq
     uint64_t done;
-    alignas(16) float nlse[4][kTile];                // -lse log2 e (-inf: no weight); read 16 bytes at a time
-    alignas(16) float ndelta[4][kTile];              // -D
+    alignas(16) float stats[4][kStats];              // dkv; read 16 bytes at a time
     uint32_t tmem_base;
     int abort_flag;
 };
-static_assert(offsetof(Ctl, nlse) % 16 == 0 && offsetof(Ctl, ndelta) % 16 == 0, "float4 reads");
+static_assert(offsetof(Ctl, stats) % 16 == 0, "bulk copies, float4 reads");
 
 struct Params {
     XattnArgs a;
@@ -97,15 +99,13 @@ __device__ __forceinline__ void store32(float* dst, const float* v, int left, bo
             if (e < left) dst[e] = v[e];
     }
 }
-// `cols` columns of an accumulator (a whole warp), times mul, zeros where !keep, to out (bf16) or part (fp32)
-__device__ __forceinline__ void drain_acc(uint32_t taddr, int cols, bool any, bool keep, bool mine, float mul,
+// Columns [c0, c1) of an accumulator of `cols` (a whole warp), times mul, zeros where !keep, to out (bf16) or part (fp32)
+__device__ __forceinline__ void drain_acc(uint32_t taddr, int c0, int c1, int cols, bool any, bool keep, bool mine, float mul,
                                           __nv_bfloat16* out, bool vec, float* part) {
-    for (int q = 0; q < cols; q += 32) {
+    for (int q = c0; q < min(c1, cols); q += 32) {
         __syncwarp();
         float v[32];
-        if (any) {
-            tmem_ld32(taddr + (uint32_t)q, v);
-        }
+        if (any) tmem_ld32(taddr + (uint32_t)q, v);
 #pragma unroll
         for (int e = 0; e < 32; ++e) v[e] = any && keep ? v[e] * mul : 0.f;
         if (mine) {
@@ -113,6 +113,54 @@ __device__ __forceinline__ void drain_acc(uint32_t taddr, int cols, bool any, bo
                 store32(part + q, v, cols - q, cols % 4 == 0);
             else
                 store32(out + q, v, cols - q, vec);
+        }
+    }
+}
+
+// Statistics of every row tile of a key head: slots without a row get (-inf, 0).  16 threads a row, 8 columns each.
+// Bound by reading O and dO once.
+__global__ void __launch_bounds__(256) k_xattn_stats(const XattnArgs a, int nl, long long rtiles, int vec) {
+    long long i = blockIdx.x;
+    const long long rt = i % rtiles;
+    i /= rtiles;
+    const int hk = (int)(i % a.Hkv), b = (int)(i / a.Hkv);
+    const int grp = threadIdx.x >> 4, ln = threadIdx.x & 15, c0 = ln * 8;
+    float* dst = a.ws + (long long)blockIdx.x * kStats;
+    float acc[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int r = grp + 16 * k, l = r / a.G, h = hk * a.G + r - l * a.G;
+        const long long ql = rt * nl + l;
+        acc[k] = 0.f;
+        if (l >= nl || ql >= a.Lq || c0 >= a.dv) continue;
+        const __nv_bfloat16* o = reinterpret_cast<const __nv_bfloat16*>(a.o.p) + b * a.o.b + ql * a.o.l + h * a.o.h + c0;
+        const __nv_bfloat16* d = reinterpret_cast<const __nv_bfloat16*>(a.dO.p) + b * a.dO.b + ql * a.dO.l + h * a.dO.h + c0;
+        if (vec) {
+            const uint4 x = __ldg(reinterpret_cast<const uint4*>(o)), y = __ldg(reinterpret_cast<const uint4*>(d));
+            const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                acc[k] = fmaf(__uint_as_float(xs[e] << 16), __uint_as_float(ys[e] << 16), acc[k]);
+                acc[k] = fmaf(__uint_as_float(xs[e] & 0xffff0000u), __uint_as_float(ys[e] & 0xffff0000u), acc[k]);
+            }
+        } else {
+            for (int e = 0; e < 8 && c0 + e < a.dv; ++e) acc[k] = fmaf(__bfloat162float(o[e]), __bfloat162float(d[e]), acc[k]);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+#pragma unroll
+        for (int o = 8; o; o >>= 1) acc[k] += __shfl_xor_sync(0xffffffffu, acc[k], o);
+        const int r = grp + 16 * k, l = r / a.G, h = hk * a.G + r - l * a.G;
+        const long long ql = rt * nl + l;
+        if (ln == 0) {
+            float L = -INFINITY, D = 0.f;
+            if (l < nl && ql < a.Lq) {
+                L = neg_lse2(a.lse[((long long)b * a.Hq + h) * a.Lq + ql]);
+                if (L != -INFINITY) D = -acc[k];
+            }
+            dst[r] = L;
+            dst[kTile + r] = D;
         }
     }
 }
@@ -191,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int k = 0; k < DVC; ++k)
                 tma_load_4d(Vs + (size_t)k * kChunkBytes, &mv, &c.own_full, k * kChunk, hk * p.vhmul, j0, b * p.vmul);
             RingPos rp;
-            int sa = 0, sb = 0;
+            int sa = 0, sb = 0, ss = 0;
             for (int t = 0; t < nt; ++t, rp.next(ST)) {
                 const int s = rp.idx, l0 = (int)(t0 + t) * p.nl;
                 if (!mbar_wait_1t(&c.a_empty[s], rp.phase ^ 1u, abort_flag, err)) break;
@@ -200,6 +248,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                     tma_load_4d(Qr + (size_t)(s * DKC + k) * kChunkBytes, &mq, &c.a_full[s], k * kChunk, hk * a.G, l0,
                                 b * p.qmul);
                 ++sa;
+                if (!mbar_wait_1t(&c.st_empty[s], rp.phase ^ 1u, abort_flag, err)) break;
+                mbar_arrive_expect_tx(&c.st_full[s], (uint32_t)sizeof(c.stats[0]));
+                bulk_load(c.stats[s], a.ws + (((long long)b * a.Hkv + hk) * p.rtiles + t0 + t) * kStats, sizeof(c.stats[0]),
+                          &c.st_full[s]);
+                ++ss;
                 if (!mbar_wait_1t(&c.b_empty[s], rp.phase ^ 1u, abort_flag, err)) break;
                 mbar_arrive_expect_tx(&c.b_full[s], (uint32_t)(DVC * kChunk * 2 * tile_rows));
                 for (int k = 0; k < DVC; ++k)
@@ -209,29 +262,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             mbar_drain(&c.own_full, 0, err);
             for (int j = std::max(0, sa - ST); j < sa; ++j) mbar_drain(&c.a_full[j % ST], (uint32_t)(j / ST) & 1u, err);
+            for (int j = std::max(0, ss - ST); j < ss; ++j) mbar_drain(&c.st_full[j % ST], (uint32_t)(j / ST) & 1u, err);
             for (int j = std::max(0, sb - ST); j < sb; ++j) mbar_drain(&c.b_full[j % ST], (uint32_t)(j / ST) & 1u, err);
-        }
-    } else if (warp == kAuxWarp) {
-        // ------------------------------------------------------------- the rows' statistics
-        RingPos rp;
-        for (int t = 0; t < nt; ++t, rp.next(ST)) {
-            if (!mbar_wait_warp(&c.st_empty[rp.idx], rp.phase ^ 1u, abort_flag, err)) break;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int r = 32 * e + lane;
-                const long long pr = (t0 + t) * tile_rows + r;
-                float L = -INFINITY, D = 0.f;
-                if (r < tile_rows && pr < a.rows) {
-                    const long long ql = pr / a.G;
-                    const long long at = ((long long)b * a.Hq + hk * a.G + (int)(pr - ql * a.G)) * a.Lq + ql;
-                    L = neg_lse2(__ldg(a.lse + at));
-                    D = L == -INFINITY ? 0.f : -a.ws[at];
-                }
-                c.nlse[rp.idx][r] = L;
-                c.ndelta[rp.idx][r] = D;
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&c.st_full[rp.idx]);
         }
     } else if (warp == kMmaWarp) {
         if (lane == 0 && nt > 0) {
@@ -258,12 +290,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                 nxt.next(ST);
                 if (!(ok = mbar_wait_1t(&c.p_full, (uint32_t)t & 1u, abort_flag, err))) break;
                 tc_fence_after();
-                mma_tile_ts(t_dv, t_s, 64u, oa + (uint32_t)(cur.idx * DVC * kChunkBytes), id_v, t != 0);
+                mma_tile_ts(t_dv, t_s, 32u, oa + (uint32_t)(cur.idx * DVC * kChunkBytes), id_v, t != 0);
                 mma_commit(&c.b_empty[cur.idx]);
                 if (t + 1 < nt && !(ok = scores(nxt))) break;
                 if (!(ok = mbar_wait_1t(&c.ds_full, (uint32_t)t & 1u, abort_flag, err))) break;
                 tc_fence_after();
-                mma_tile_ts(t_dk, t_dp, 64u, qa + (uint32_t)(cur.idx * DKC * kChunkBytes), id_k, t != 0);
+                mma_tile_ts(t_dk, t_dp, 32u, qa + (uint32_t)(cur.idx * DKC * kChunkBytes), id_k, t != 0);
                 mma_commit(&c.a_empty[cur.idx]);
                 if (t + 1 < nt && !(ok = dprod(nxt))) break;
                 cur = nxt;
@@ -271,11 +303,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             mma_commit(&c.done);
             mbar_drain(&c.done, 0, err);
         }
-    } else {
+    } else if (warp < kSoftWarps) {
         // ------------------------------------------------------------- softmax warps: a lane is a key
-        const int half = warp >> 2, quad = warp & 3;
+        const int quarter = warp >> 2, quad = warp & 3;
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
-        const uint32_t ts = t_s + lane_base + 64u * half, td = t_dp + lane_base + 64u * half;
+        const uint32_t ts = t_s + lane_base + (uint32_t)(kCols * quarter), td = t_dp + lane_base + (uint32_t)(kCols * quarter);
         const int j = j0 + quad * 32 + lane;
         const bool valid = j < n && (!a.mask || __ldg(a.mask + (long long)b * a.ldm + j) != 0);
         const bool whole = __all_sync(0xffffffffu, valid);
@@ -290,16 +322,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                 break;
             }
             tc_fence_after();
-            uint32_t sr[64], pk[32];
+            uint32_t sr[kCols], pk[kCols / 2];
             float* s = reinterpret_cast<float*>(sr);
             tmem_ld32_issue(ts, sr);
-            tmem_ld32_issue(ts + 32u, sr + 32);
             tmem_wait_ld32(sr);
-            tmem_wait_ld32(sr + 32);
-            const float4* nl = reinterpret_cast<const float4*>(&c.nlse[rp.idx][64 * half]);
-            const float4* nd = reinterpret_cast<const float4*>(&c.ndelta[rp.idx][64 * half]);
+            const float4* nl = reinterpret_cast<const float4*>(&c.stats[rp.idx][kCols * quarter]);
+            const float4* nd = reinterpret_cast<const float4*>(&c.stats[rp.idx][kTile + kCols * quarter]);
 #pragma unroll
-            for (int q = 0; q < 16; ++q) {
+            for (int q = 0; q < kCols / 4; ++q) {
                 const float4 L = nl[q];
                 float* x = s + 4 * q;
                 x[0] = ex2(fmaf(x[0], cs, L.x));
@@ -309,11 +339,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (!whole) {
 #pragma unroll
-                for (int q = 0; q < 64; ++q) s[q] = valid ? s[q] : 0.f;
+                for (int q = 0; q < kCols; ++q) s[q] = valid ? s[q] : 0.f;
             }
 #pragma unroll
-            for (int q = 0; q < 32; ++q) pk[q] = pack_bf16(s[2 * q], s[2 * q + 1]);
-            tmem_st32(ts, pk);
+            for (int q = 0; q < kCols / 2; ++q) pk[q] = pack_bf16(s[2 * q], s[2 * q + 1]);
+            tmem_st16(ts, pk);
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
@@ -323,30 +353,26 @@ __global__ void __launch_bounds__(kThreads, 1)
                 break;
             }
             tc_fence_after();
+            uint32_t dr[kCols];
+            float* d = reinterpret_cast<float*>(dr);
+            tmem_ld32_issue(td, dr);
+            tmem_wait_ld32(dr);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t dr[32];
-                float* d = reinterpret_cast<float*>(dr);
-                tmem_ld32_issue(td + 32u * h, dr);
-                tmem_wait_ld32(dr);
-#pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const float4 D = nd[8 * h + q];
-                    float* x = d + 4 * q;
-                    const float* w = s + 32 * h + 4 * q;
-                    add2(x[0], x[1], D.x, D.y);
-                    add2(x[2], x[3], D.z, D.w);
-                    mul2(x[0], x[1], w[0], w[1]);
-                    mul2(x[2], x[3], w[2], w[3]);
-                }
-                if (!whole) {
-#pragma unroll
-                    for (int q = 0; q < 32; ++q) d[q] = valid ? d[q] : 0.f;
-                }
-#pragma unroll
-                for (int q = 0; q < 16; ++q) pk[16 * h + q] = pack_bf16(d[2 * q], d[2 * q + 1]);
+            for (int q = 0; q < kCols / 4; ++q) {
+                const float4 D = nd[q];
+                float* x = d + 4 * q;
+                add2(x[0], x[1], D.x, D.y);
+                add2(x[2], x[3], D.z, D.w);
+                mul2(x[0], x[1], s[4 * q], s[4 * q + 1]);
+                mul2(x[2], x[3], s[4 * q + 2], s[4 * q + 3]);
             }
-            tmem_st32(td, pk);
+            if (!whole) {
+#pragma unroll
+                for (int q = 0; q < kCols; ++q) d[q] = valid ? d[q] : 0.f;
+            }
+#pragma unroll
+            for (int q = 0; q < kCols / 2; ++q) pk[q] = pack_bf16(d[2 * q], d[2 * q + 1]);
+            tmem_st16(td, pk);
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
@@ -357,18 +383,18 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (ok && nt > 0) ok = mbar_wait_warp_inline(&c.done, 0, abort_flag, err);
         tc_fence_after();
-        if (ok) {  // group 0 writes dV, group 1 dK
+        if (ok) {  // quarters 0 and 1 write dV, 2 and 3 dK
             const bool mine = j < a.Lk;
             const long long jj = mine ? j : 0;
-            const long long nk = (long long)a.B * a.Hkv * a.Lk;
-            const long long at = ((long long)part * nk + ((long long)b * a.Hkv + hk) * a.Lk + jj);
+            const long long at = (long long)part * xattn_keys(a) + ((long long)b * a.Hkv + hk) * a.Lk + jj;
             const bool parts = a.rsplits > 1;
-            if (half == 0)
-                drain_acc(t_dv + lane_base, a.dv, nt > 0, valid, mine, 1.f,
+            const int c0 = (quarter & 1) * 64;
+            if (quarter < 2)
+                drain_acc(t_dv + lane_base, c0, c0 + 64, a.dv, nt > 0, valid, mine, 1.f,
                           reinterpret_cast<__nv_bfloat16*>(a.dV.p) + b * a.dV.b + jj * a.dV.l + hk * a.dV.h, p.vec_v != 0,
                           parts ? a.ws + xattn_ws_dv(a) + at * a.dv : nullptr);
             else
-                drain_acc(t_dk + lane_base, a.dk, nt > 0, valid, mine, parts ? 1.f : a.scale,
+                drain_acc(t_dk + lane_base, c0, c0 + 64, a.dk, nt > 0, valid, mine, parts ? 1.f : a.scale,
                           reinterpret_cast<__nv_bfloat16*>(a.dK.p) + b * a.dK.b + jj * a.dK.l + hk * a.dK.h, p.vec_k != 0,
                           parts ? a.ws + xattn_ws_dk(a) + at * a.dk : nullptr);
         }
@@ -470,7 +496,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int j = std::max(0, sa - ST); j < sa; ++j) mbar_drain(&c.a_full[j % ST], (uint32_t)(j / ST) & 1u, err);
             for (int j = std::max(0, sb - ST); j < sb; ++j) mbar_drain(&c.b_full[j % ST], (uint32_t)(j / ST) & 1u, err);
         }
-    } else if (warp == kAuxWarp) {
+    } else if (warp == kMaskWarp) {
         // ------------------------------------------------------------- rows of K that are not read
         RingPos rp;
         for (int t = 0; t < nt && fix; ++t, rp.next(ST)) {
@@ -513,7 +539,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (t + 1 < nt && !(ok = mbar_wait_1t(&c.dp_free, ph, abort_flag, err) && dprod(nxt))) break;
                 if (!(ok = mbar_wait_1t(&c.ds_full, ph, abort_flag, err))) break;
                 tc_fence_after();
-                mma_tile_ts(t_dq, t_ds, 32u, ka + (uint32_t)(cur.idx * DKC * kChunkBytes), id_q, t != 0);
+                mma_tile_ts(t_dq, t_ds, 16u, ka + (uint32_t)(cur.idx * DKC * kChunkBytes), id_q, t != 0);
                 mma_commit(&c.ds_free);
                 mma_commit(&c.a_empty[cur.idx]);
                 cur = nxt;
@@ -523,42 +549,38 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
     } else {
         // ------------------------------------------------------------- softmax warps: a lane is a row
-        const int half = warp >> 2, quad = warp & 3;
+        const int quarter = warp >> 2, quad = warp & 3;
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
-        const uint32_t ts = t_s + lane_base + 64u * half, td = t_dp + lane_base + 64u * half;
+        const uint32_t ts = t_s + lane_base + (uint32_t)(kCols * quarter), td = t_dp + lane_base + (uint32_t)(kCols * quarter);
         const int r = quad * 32 + lane;
-        const long long pr = rt * tile_rows + r;
-        const bool mine = r < tile_rows && pr < a.rows;
-        const long long ql = mine ? pr / a.G : 0;
-        const int h = hk * a.G + (mine ? (int)(pr - ql * a.G) : 0);
-        const long long at = ((long long)b * a.Hq + h) * a.Lq + ql;
         const float cs = a.scale * kLog2e;
-        const float nl = mine ? neg_lse2(__ldg(a.lse + at)) : -INFINITY;
-        const bool none = nl == -INFINITY;
-        const float nd = none ? 0.f : -a.ws[at];
+        const float* stats = a.ws + (((long long)b * a.Hkv + hk) * p.rtiles + rt) * kStats;
+        const float nl = stats[r], nd = stats[kTile + r];
+        const bool none = nl == -INFINITY;  // no row, or one without weight
         bool ok = true;
         for (int t = 0; t < nt; ++t) {
             const uint32_t ph = (uint32_t)t & 1u;
             const int j0 = (t0 + t) * kTile;
             const bool whole = j0 + kTile <= n && !a.mask;
-            uint32_t w[4];
-            if (!whole) valid_words(w, a, b, j0, n);
+            uint32_t w = 0xffffffffu;
+            if (!whole) {
+                const int j = j0 + kCols * quarter + lane;
+                w = __ballot_sync(0xffffffffu, j < n && (!a.mask || __ldg(a.mask + (long long)b * a.ldm + j) != 0));
+            }
             if (!mbar_wait_warp_inline(&c.s_full, ph, abort_flag, err)) {
                 ok = false;
                 break;
             }
             tc_fence_after();
-            uint32_t sr[64], pk[32];
+            uint32_t sr[kCols], pk[kCols / 2];
             float* s = reinterpret_cast<float*>(sr);
             tmem_ld32_issue(ts, sr);
-            tmem_ld32_issue(ts + 32u, sr + 32);
             tmem_wait_ld32(sr);
-            tmem_wait_ld32(sr + 32);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&c.s_free);
 #pragma unroll
-            for (int q = 0; q < 64; q += 2) {
+            for (int q = 0; q < kCols; q += 2) {
                 fma2(s[q], s[q + 1], cs, nl);
                 s[q] = ex2(s[q]);
                 s[q + 1] = ex2(s[q + 1]);
@@ -568,38 +590,30 @@ __global__ void __launch_bounds__(kThreads, 1)
                 break;
             }
             tc_fence_after();
-#pragma unroll
-            for (int hh = 0; hh < 2; ++hh) {
-                uint32_t dr[32];
-                float* d = reinterpret_cast<float*>(dr);
-                tmem_ld32_issue(td + 32u * hh, dr);
-                tmem_wait_ld32(dr);
-#pragma unroll
-                for (int q = 0; q < 32; q += 2) {
-                    add2(d[q], d[q + 1], nd, nd);
-                    mul2(d[q], d[q + 1], s[32 * hh + q], s[32 * hh + q + 1]);
-                }
-                if (!whole) {
-                    const uint32_t ww = half == 0 ? w[hh] : w[2 + hh];
-#pragma unroll
-                    for (int q = 0; q < 32; ++q) d[q] = (ww >> q) & 1u ? d[q] : 0.f;
-                }
-#pragma unroll
-                for (int q = 0; q < 16; ++q) pk[16 * hh + q] = pack_bf16(d[2 * q], d[2 * q + 1]);
-            }
-            if (none) {  // (NaN in dO of a row without weight stays out)
-#pragma unroll
-                for (int q = 0; q < 32; ++q) pk[q] = 0u;
-            }
+            uint32_t dr[kCols];
+            float* d = reinterpret_cast<float*>(dr);
+            tmem_ld32_issue(td, dr);
+            tmem_wait_ld32(dr);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&c.dp_free);
+#pragma unroll
+            for (int q = 0; q < kCols; q += 2) {
+                add2(d[q], d[q + 1], nd, nd);
+                mul2(d[q], d[q + 1], s[q], s[q + 1]);
+            }
+            if (w != 0xffffffffu) {
+#pragma unroll
+                for (int q = 0; q < kCols; ++q) d[q] = (w >> q) & 1u ? d[q] : 0.f;
+            }
+#pragma unroll
+            for (int q = 0; q < kCols / 2; ++q) pk[q] = none ? 0u : pack_bf16(d[2 * q], d[2 * q + 1]);
             if (t > 0 && !mbar_wait_warp_inline(&c.ds_free, (uint32_t)(t - 1) & 1u, abort_flag, err)) {
                 ok = false;
                 break;
             }
             tc_fence_after();
-            tmem_st32(t_ds + lane_base + 32u * half, pk);
+            tmem_st16(t_ds + lane_base + (uint32_t)(kCols / 2 * quarter), pk);
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
@@ -607,10 +621,18 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (ok && nt > 0) ok = mbar_wait_warp_inline(&c.done, 0, abort_flag, err);
         tc_fence_after();
-        if (ok && half == 0)
-            drain_acc(t_dq + lane_base, a.dk, nt > 0, !none, mine, a.splits > 1 ? 1.f : a.scale,
+        if (ok) {  // 32 columns of dQ a quarter
+            const long long pr = rt * tile_rows + r;
+            const bool mine = r < tile_rows && pr < a.rows;
+            const int l = r / a.G;
+            const long long ql = mine ? rt * p.nl + l : 0;
+            const int h = hk * a.G + (mine ? r - l * a.G : 0);
+            const long long at = ((long long)b * a.Hq + h) * a.Lq + ql;
+            drain_acc(t_dq + lane_base, kCols * quarter, kCols * quarter + kCols, a.dk, nt > 0, !none, mine,
+                      a.splits > 1 ? 1.f : a.scale,
                       reinterpret_cast<__nv_bfloat16*>(a.dQ.p) + b * a.dQ.b + ql * a.dQ.l + h * a.dQ.h, p.vec_q != 0,
-                      a.splits > 1 ? a.ws + xattn_ws_dq(a) + ((long long)part * a.B * a.Hq * a.Lq + at) * a.dk : nullptr);
+                      a.splits > 1 ? a.ws + xattn_ws_dq(a) + ((long long)part * xattn_rows(a) + at) * a.dk : nullptr);
+        }
     }
     tc_fence_before();
     __syncthreads();
@@ -670,6 +692,7 @@ void xattn_bwd_tc_plan(XattnArgs& a, int sms) {
     // the keys (rows) are cut into parts of two tiles or more where one CTA per row (key) tile leaves multiprocessors idle
     a.splits = xattn_parts(rt * a.Hkv * a.B, kt, sms, 2);
     a.rsplits = xattn_parts(kt * a.Hkv * a.B, rt, sms, 2);
+    a.stats = rt * a.Hkv * a.B * kStats;
 }
 
 cudaError_t launch_xattn_bwd_tc(const XattnArgs& a, int device, cudaStream_t s) {
@@ -694,7 +717,9 @@ cudaError_t launch_xattn_bwd_tc(const XattnArgs& a, int device, cudaStream_t s) 
     p.khmul = k.hmul;
     p.vmul = v.bmul;
     p.vhmul = v.hmul;
-    cudaError_t e = launch_xattn_delta(a, s);
+    const int vec = on_vectors(a.o, a.B, a.Lq, a.Hq, a.dv) && on_vectors(a.dO, a.B, a.Lq, a.Hq, a.dv);
+    k_xattn_stats<<<(unsigned)(p.rtiles * a.Hkv * a.B), 256, 0, s>>>(a, p.nl, p.rtiles, vec);
+    cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     const bool k2 = a.dk > kChunk, v2 = a.dv > kChunk;
     return k2 ? (v2 ? launch<2, 2>(q, o, k, v, p, device, s) : launch<2, 1>(q, o, k, v, p, device, s))

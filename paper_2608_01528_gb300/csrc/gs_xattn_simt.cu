@@ -540,6 +540,16 @@ cudaError_t backward_t(const XattnArgs& a, cudaStream_t s) {
 
 unsigned sum_grid(long long n) { return (unsigned)std::min<long long>((n + 255) / 256, 152 * 16); }
 
+cudaError_t launch_delta(const XattnArgs& a, cudaStream_t s) {
+    const long long rows = (long long)a.B * a.Hq * a.Lq;
+    if (rows == 0) return cudaSuccess;
+    if (a.dtype == GS_F32)
+        k_xattn_delta<float><<<(unsigned)((rows + 7) / 8), 256, 0, s>>>(a);
+    else
+        k_xattn_delta<__nv_bfloat16><<<(unsigned)((rows + 7) / 8), 256, 0, s>>>(a);
+    return cudaGetLastError();
+}
+
 }  // namespace
 
 void xattn_simt_plan(XattnArgs& a, bool backward, int sms) {
@@ -547,6 +557,7 @@ void xattn_simt_plan(XattnArgs& a, bool backward, int sms) {
     // two blocks a multiprocessor where they fit, and parts of four tiles or more
     a.splits = xattn_parts(rt * a.Hkv * a.B, kt, 2 * sms, 4);
     a.rsplits = backward ? xattn_parts(kt * a.Hkv * a.B, rt, 2 * sms, 4) : 1;
+    a.stats = xattn_round4(xattn_rows(a));  // D_i
 }
 
 cudaError_t launch_xattn_simt(const XattnArgs& a, cudaStream_t s) {
@@ -556,19 +567,9 @@ cudaError_t launch_xattn_simt(const XattnArgs& a, cudaStream_t s) {
 }
 
 cudaError_t launch_xattn_simt_backward(const XattnArgs& a, cudaStream_t s) {
-    cudaError_t e = launch_xattn_delta(a, s);
+    cudaError_t e = launch_delta(a, s);
     if (e != cudaSuccess) return e;
     return a.dtype == GS_F32 ? backward_t<float>(a, s) : backward_t<__nv_bfloat16>(a, s);
-}
-
-cudaError_t launch_xattn_delta(const XattnArgs& a, cudaStream_t s) {
-    const long long rows = (long long)a.B * a.Hq * a.Lq;
-    if (rows == 0) return cudaSuccess;
-    if (a.dtype == GS_F32)
-        k_xattn_delta<float><<<(unsigned)((rows + 7) / 8), 256, 0, s>>>(a);
-    else
-        k_xattn_delta<__nv_bfloat16><<<(unsigned)((rows + 7) / 8), 256, 0, s>>>(a);
-    return cudaGetLastError();
 }
 
 cudaError_t launch_xattn_join(const XattnArgs& a, cudaStream_t s) {

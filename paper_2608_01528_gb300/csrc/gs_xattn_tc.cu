@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             auto values = [&](int t, uint32_t k, uint32_t v) {  // weights of group t's k-th key tile
                 if (!mbar_wait_1t(&c.p_full[t], k & 1u, abort_flag, err)) return false;
                 tc_fence_after();
-                mma_tile_ts(tmem + o_col[t], tmem + s_col[t], 32u, v, id_o, k != 0);
+                mma_tile_ts(tmem + o_col[t], tmem + s_col[t], 16u, v, id_o, k != 0);
                 mma_commit(&c.o_done[t]);
                 return true;
             };

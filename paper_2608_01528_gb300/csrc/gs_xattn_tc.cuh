@@ -47,14 +47,20 @@ static __device__ __forceinline__ void mma_tile_ss(uint32_t d, uint32_t a, uint3
         mma_f16_ss(d, sdesc_sw128(a + off), sdesc_sw128(b + off), idesc, k != 0 ? 1u : 0u);
     }
 }
-// D[tmem] (+)= A[tmem: bf16 pairs] B over 128 rows of B: A's K-step k lies 8 columns after the last, its second
-// half (rows 64 on) `half` columns after the first
-static __device__ __forceinline__ void mma_tile_ts(uint32_t d, uint32_t a, uint32_t half, uint32_t b, uint32_t idesc,
+// D[tmem] (+)= A[tmem: bf16 pairs] B over 128 rows of B: 32 rows of A's K axis (two steps of 8 columns) every `gap`
+// columns
+static __device__ __forceinline__ void mma_tile_ts(uint32_t d, uint32_t a, uint32_t gap, uint32_t b, uint32_t idesc,
                                                    bool accumulate) {
 #pragma unroll
     for (int k = 0; k < kTile / 16; ++k)
-        mma_bf16_ts(d, a + (uint32_t)(k & 3) * 8 + (k >= 4 ? half : 0u), sdesc_mn(b + (uint32_t)k * 2048), idesc,
+        mma_bf16_ts(d, a + (uint32_t)(k >> 1) * gap + (uint32_t)(k & 1) * 8, sdesc_mn(b + (uint32_t)k * 2048), idesc,
                     accumulate || k != 0 ? 1u : 0u);
+}
+// Untiled copy of `bytes` (a multiple of 16, both addresses on 16-byte boundaries) to shared memory.
+static __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+                 "l"(src), "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
 }
 
 static __device__ __forceinline__ float ex2(float x) {
