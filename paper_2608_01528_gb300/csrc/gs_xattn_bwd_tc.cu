@@ -55,7 +55,7 @@ struct Params {
     int qmul, omul, kmul, khmul, vmul, vhmul;  // HeadMap multipliers: q, dO (batch), k and v (batch, head)
     int nl;
     long long rtiles;
-    int ktiles, ksteps, vsteps;
+    int ktiles;
     int vec_q, vec_k, vec_v;  // outputs on 16-byte boundaries
 };
 
@@ -273,14 +273,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             auto scores = [&](const RingPos& r) {
                 if (!mbar_wait_1t(&c.a_full[r.idx], r.phase, abort_flag, err)) return false;
                 tc_fence_after();
-                mma_tile_ss(t_s, ka, qa + (uint32_t)(r.idx * DKC * kChunkBytes), id_s, p.ksteps);
+                mma_tile_ss<DKC>(t_s, ka, qa + (uint32_t)(r.idx * DKC * kChunkBytes), id_s);
                 mma_commit(&c.s_full);
                 return true;
             };
             auto dprod = [&](const RingPos& r) {
                 if (!mbar_wait_1t(&c.b_full[r.idx], r.phase, abort_flag, err)) return false;
                 tc_fence_after();
-                mma_tile_ss(t_dp, va, oa + (uint32_t)(r.idx * DVC * kChunkBytes), id_s, p.vsteps);
+                mma_tile_ss<DVC>(t_dp, va, oa + (uint32_t)(r.idx * DVC * kChunkBytes), id_s);
                 mma_commit(&c.dp_full);
                 return true;
             };
@@ -290,12 +290,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                 nxt.next(ST);
                 if (!(ok = mbar_wait_1t(&c.p_full, (uint32_t)t & 1u, abort_flag, err))) break;
                 tc_fence_after();
-                mma_tile_ts(t_dv, t_s, 32u, oa + (uint32_t)(cur.idx * DVC * kChunkBytes), id_v, t != 0);
+                mma_tile_ts<32>(t_dv, t_s, oa + (uint32_t)(cur.idx * DVC * kChunkBytes), id_v, t != 0);
                 mma_commit(&c.b_empty[cur.idx]);
                 if (t + 1 < nt && !(ok = scores(nxt))) break;
                 if (!(ok = mbar_wait_1t(&c.ds_full, (uint32_t)t & 1u, abort_flag, err))) break;
                 tc_fence_after();
-                mma_tile_ts(t_dk, t_dp, 32u, qa + (uint32_t)(cur.idx * DKC * kChunkBytes), id_k, t != 0);
+                mma_tile_ts<32>(t_dk, t_dp, qa + (uint32_t)(cur.idx * DKC * kChunkBytes), id_k, t != 0);
                 mma_commit(&c.a_empty[cur.idx]);
                 if (t + 1 < nt && !(ok = dprod(nxt))) break;
                 cur = nxt;
@@ -518,14 +518,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             auto scores = [&](const RingPos& r) {
                 if (!mbar_wait_1t(fix ? &c.a_ready[r.idx] : &c.a_full[r.idx], r.phase, abort_flag, err)) return false;
                 tc_fence_after();
-                mma_tile_ss(t_s, qa, ka + (uint32_t)(r.idx * DKC * kChunkBytes), id_s, p.ksteps);
+                mma_tile_ss<DKC>(t_s, qa, ka + (uint32_t)(r.idx * DKC * kChunkBytes), id_s);
                 mma_commit(&c.s_full);
                 return true;
             };
             auto dprod = [&](const RingPos& r) {
                 if (!mbar_wait_1t(&c.b_full[r.idx], r.phase, abort_flag, err)) return false;
                 tc_fence_after();
-                mma_tile_ss(t_dp, oa, va + (uint32_t)(r.idx * DVC * kChunkBytes), id_s, p.vsteps);
+                mma_tile_ss<DVC>(t_dp, oa, va + (uint32_t)(r.idx * DVC * kChunkBytes), id_s);
                 mma_commit(&c.dp_full);
                 mma_commit(&c.b_empty[r.idx]);
                 return true;
@@ -539,7 +539,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (t + 1 < nt && !(ok = mbar_wait_1t(&c.dp_free, ph, abort_flag, err) && dprod(nxt))) break;
                 if (!(ok = mbar_wait_1t(&c.ds_full, ph, abort_flag, err))) break;
                 tc_fence_after();
-                mma_tile_ts(t_dq, t_ds, 16u, ka + (uint32_t)(cur.idx * DKC * kChunkBytes), id_q, t != 0);
+                mma_tile_ts<16>(t_dq, t_ds, ka + (uint32_t)(cur.idx * DKC * kChunkBytes), id_q, t != 0);
                 mma_commit(&c.ds_free);
                 mma_commit(&c.a_empty[cur.idx]);
                 cur = nxt;
@@ -702,8 +702,6 @@ cudaError_t launch_xattn_bwd_tc(const XattnArgs& a, int device, cudaStream_t s) 
     p.nl = kTile / a.G;
     p.rtiles = (a.Lq + p.nl - 1) / p.nl;
     p.ktiles = (a.Lk + kTile - 1) / kTile;
-    p.ksteps = (a.dk + 15) / 16;
-    p.vsteps = (a.dv + 15) / 16;
     p.vec_q = on_vectors(a.dQ, a.B, a.Lq, a.Hq, a.dk);
     p.vec_k = on_vectors(a.dK, a.B, a.Lk, a.Hkv, a.dk);
     p.vec_v = on_vectors(a.dV, a.B, a.Lk, a.Hkv, a.dv);

@@ -48,7 +48,7 @@ struct Params {
     int qmul, kmul, khmul, vmul, vhmul;  // HeadMap multipliers of q (batch), k and v (batch, head)
     int nl;                              // query positions of a row tile: 128 / G
     long long units;                     // row units (pairs or single tiles) per (b, key head)
-    int ktiles, ksteps;
+    int ktiles;
     int o_vec;
 };
 
@@ -205,13 +205,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             };
             auto stage = [&]() { return ringa + (uint32_t)(rp.idx * C::kStageBytes); };
             auto scores = [&](int t) {
-                mma_tile_ss(tmem + s_col[t], qa + (uint32_t)((PAIR ? t : 0) * DKC * kChunkBytes), stage(), id_s, p.ksteps);
+                mma_tile_ss<DKC>(tmem + s_col[t], qa + (uint32_t)((PAIR ? t : 0) * DKC * kChunkBytes), stage(), id_s);
                 mma_commit(&c.s_full[t]);
             };
             auto values = [&](int t, uint32_t k, uint32_t v) {  // weights of group t's k-th key tile
                 if (!mbar_wait_1t(&c.p_full[t], k & 1u, abort_flag, err)) return false;
                 tc_fence_after();
-                mma_tile_ts(tmem + o_col[t], tmem + s_col[t], 16u, v, id_o, k != 0);
+                mma_tile_ts<16>(tmem + o_col[t], tmem + s_col[t], v, id_o, k != 0);
                 mma_commit(&c.o_done[t]);
                 return true;
             };
@@ -511,7 +511,6 @@ cudaError_t launch_xattn_tc(const XattnArgs& a, int sms, int device, cudaStream_
     const long long tile_rows = (long long)p.nl * a.G;
     p.units = (a.rows + tile_rows * (pair ? 2 : 1) - 1) / (tile_rows * (pair ? 2 : 1));
     p.ktiles = (a.Lk + kTile - 1) / kTile;
-    p.ksteps = (a.dk + 15) / 16;
     p.o_vec = a.dv % 8 == 0 && (uintptr_t)a.o.p % 16 == 0 && (a.B <= 1 || a.o.b % 8 == 0) && (a.Lq <= 1 || a.o.l % 8 == 0) &&
               (a.Hq <= 1 || a.o.h % 8 == 0);
     HeadMap q, k, v;

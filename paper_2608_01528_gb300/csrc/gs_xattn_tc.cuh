@@ -40,20 +40,25 @@ static __device__ __forceinline__ uint64_t sdesc_mn(uint32_t saddr) {
 }
 __host__ __device__ constexpr uint32_t idesc_bf16_bmn(int n) { return idesc_bf16_f32(n) | (1u << 16); }
 
-// D[tmem] (+)= A[smem] B[smem]^T over `ksteps` steps of 16: both K-major, in chunks of 64 columns
-static __device__ __forceinline__ void mma_tile_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, int ksteps) {
-    for (int k = 0; k < ksteps; ++k) {
-        const uint32_t off = (uint32_t)((k >> 2) * kChunkBytes + (k & 3) * 32);
-        mma_f16_ss(d, sdesc_sw128(a + off), sdesc_sw128(b + off), idesc, k != 0 ? 1u : 0u);
+// D[tmem] = A[smem] B[smem]^T over CHUNKS chunks of 64 columns, both K-major.  Unrolled, the descriptors advanced by
+// constants: one thread issues all MMAs, and a loop that built a descriptor per step took longer than the MMAs.
+template <int CHUNKS>
+static __device__ __forceinline__ void mma_tile_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
+    const uint64_t ad = sdesc_sw128(a), bd = sdesc_sw128(b);
+#pragma unroll
+    for (int k = 0; k < CHUNKS * 4; ++k) {
+        const uint64_t off = (uint64_t)((k >> 2) * (kChunkBytes >> 4) + (k & 3) * 2);
+        mma_f16_ss(d, ad + off, bd + off, idesc, k != 0 ? 1u : 0u);
     }
 }
-// D[tmem] (+)= A[tmem: bf16 pairs] B over 128 rows of B: 32 rows of A's K axis (two steps of 8 columns) every `gap`
-// columns
-static __device__ __forceinline__ void mma_tile_ts(uint32_t d, uint32_t a, uint32_t gap, uint32_t b, uint32_t idesc,
-                                                   bool accumulate) {
+// D[tmem] (+)= A[tmem: bf16 pairs] B over 128 rows of B (MN-major): 32 rows of A's K axis (two steps of 8 columns)
+// every GAP columns
+template <int GAP>
+static __device__ __forceinline__ void mma_tile_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate) {
+    const uint64_t bd = sdesc_mn(b);
 #pragma unroll
     for (int k = 0; k < kTile / 16; ++k)
-        mma_bf16_ts(d, a + (uint32_t)(k >> 1) * gap + (uint32_t)(k & 1) * 8, sdesc_mn(b + (uint32_t)k * 2048), idesc,
+        mma_bf16_ts(d, a + (uint32_t)((k >> 1) * GAP + (k & 1) * 8), bd + (uint64_t)(k * 128), idesc,
                     accumulate || k != 0 ? 1u : 0u);
 }
 // Untiled copy of `bytes` (a multiple of 16, both addresses on 16-byte boundaries) to shared memory.
