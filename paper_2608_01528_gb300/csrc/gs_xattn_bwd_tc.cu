@@ -14,6 +14,11 @@
 // core runs dP or the sums, and the other way round.  The rows' statistics (-lse log2 e, -D) are laid out
 // per row tile by k_xattn_stats, so that a tile's come with one copy.
 //
+// Both kernels wait for their loads (about 1 us each under load) unless the ring is deep: the second keeps Q and dO in
+// TMEM (as bf16 pairs, 32 columns a chunk of 64), which leaves four stages of K; the first has no TMEM left at
+// width 128 (S, dP, dK and dV fill it).  Halves of 64 streamed rows, which would leave room, lose more: a
+// 128 x 64 x 16 product takes 46 cycles, a 128 x 128 x 16 one 64.5 (0.87 -> 1.24 ms at 4,096 x 4,096).
+//
 // Keys that are not read: P = dS = 0, and in the second kernel their rows of K are zeroed in shared memory before
 // the MMA reads them (0 * NaN).  Rows past the end have lse = +inf: P = 0.
 
@@ -37,12 +42,12 @@ constexpr int kCols = 32;        // of a softmax warp
 constexpr int kStats = 2 * kTile;  // floats of a row tile: -lse log2 e (-inf: no weight), then -D
 
 struct Ctl {
-    uint64_t own_full;                               // the tiles that stay
+    uint64_t own_full;                               // the tiles that stay are there
     uint64_t a_full[4], a_empty[4], a_ready[4];      // Q (dkv) or K (dq) stages
     uint64_t b_full[4], b_empty[4];                  // dO (dkv) or V (dq) stages
     uint64_t st_full[4], st_empty[4];                // dkv: row statistics
     uint64_t s_full, p_full, dp_full, ds_full;       // MMA <-> softmax
-    uint64_t s_free, dp_free, ds_free;               // dq
+    uint64_t s_free;                                 // dq: S has been read
     uint64_t done;
     alignas(16) float stats[4][kStats];              // dkv; read 16 bytes at a time
     uint32_t tmem_base;
@@ -67,7 +72,27 @@ struct Cfg {
     static constexpr int kStages = kRoom < 4 ? kRoom : 4;
     static constexpr size_t kSmem = 1024 + (size_t)kOwn * (1 + kStages) + sizeof(Ctl);
     static_assert(kStages >= 2, "ring too short");
+    // dq: K and V stages
+    static constexpr int kFree = 227 * 1024 - 1024 - (int)sizeof(Ctl);
+    static constexpr int kKRoom = (kFree - 2 * DVC * kChunkBytes) / (DKC * kChunkBytes);
+    static constexpr int kKStages = kKRoom < 4 ? kKRoom : 4;
+    static constexpr int kVRoom = (kFree - kKStages * DKC * kChunkBytes) / (DVC * kChunkBytes);
+    static constexpr int kVStages = kVRoom < 4 ? kVRoom : 4;
+    static constexpr size_t kDqSmem = 1024 + (size_t)(kKStages * DKC + kVStages * DVC) * kChunkBytes + sizeof(Ctl);
 };
+
+// The row at `row` (w elements, zeros where !has) into columns [taddr, + CHUNKS * 32) of this thread's lane: the part of the
+// warp with number `part` of four that share the lanes.
+template <int CHUNKS>
+__device__ __forceinline__ void keep_row(uint32_t taddr, const __nv_bfloat16* row, int w, bool has, int part) {
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+        const int e = c * kChunk + part * 16;
+        uint32_t x[8];
+        load_words(x, row, e, w, has);
+        tmem_st8(taddr + (uint32_t)(e / 2), x);
+    }
+}
 
 // -lse log2 e of a row: -inf where the row has no weight (P = 0); a NaN or +inf lse gives NaN, as the forward result is
 __device__ __forceinline__ float neg_lse2(float lse) {
@@ -409,18 +434,15 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 template <int DKC, int DVC>
 __global__ void __launch_bounds__(kThreads, 1)
-    k_xattn_dq_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mo,
-                  const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const Params p) {
+    k_xattn_dq_tc(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const Params p) {
     using C = Cfg<DKC, DVC>;
-    constexpr int ST = C::kStages;
+    constexpr int SK = C::kKStages, SV = C::kVStages;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     uint8_t* base = smem_raw + (((raw + 1023u) & ~1023u) - raw);
-    uint8_t* Qs = base;
-    uint8_t* Os = Qs + DKC * kChunkBytes;
-    uint8_t* Kr = Os + DVC * kChunkBytes;               // ring of K tiles
-    uint8_t* Vr = Kr + (size_t)ST * DKC * kChunkBytes;  // ring of V tiles
-    Ctl& c = *reinterpret_cast<Ctl*>(Vr + (size_t)ST * DVC * kChunkBytes);
+    uint8_t* Kr = base;                                 // ring of K tiles
+    uint8_t* Vr = Kr + (size_t)SK * DKC * kChunkBytes;  // ring of V tiles
+    Ctl& c = *reinterpret_cast<Ctl*>(Vr + (size_t)SV * DVC * kChunkBytes);
     volatile int* abort_flag = &c.abort_flag;
     unsigned* err = &g_err_xbwd;
     const XattnArgs& a = p.a;
@@ -440,11 +462,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     const bool fix = a.lens != nullptr || a.mask != nullptr;
 
     if (threadIdx.x == 0) {
-        mbar_init(&c.own_full, 1);
-        for (int s = 0; s < ST; ++s) {
+        mbar_init(&c.own_full, kSoftWarps);
+        for (int s = 0; s < SK; ++s) {
             mbar_init(&c.a_full[s], 1);
             mbar_init(&c.a_empty[s], 1);
             mbar_init(&c.a_ready[s], 1);
+        }
+        for (int s = 0; s < SV; ++s) {
             mbar_init(&c.b_full[s], 1);
             mbar_init(&c.b_empty[s], 1);
         }
@@ -452,8 +476,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_init(&c.dp_full, 1);
         mbar_init(&c.ds_full, kSoftWarps);
         mbar_init(&c.s_free, kSoftWarps);
-        mbar_init(&c.dp_free, kSoftWarps);
-        mbar_init(&c.ds_free, 1);
         mbar_init(&c.done, 1);
         c.abort_flag = 0;
         fence_barrier_init();
@@ -466,40 +488,34 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = c.tmem_base;
-    const uint32_t t_s = tmem, t_dp = tmem + 128, t_dq = tmem + 256, t_ds = tmem + 384;  // dS: 64 columns of bf16 pairs
+    const uint32_t t_q = tmem, t_do = t_q + 32 * DKC, t_dq = t_do + 32 * DVC;
+    const uint32_t t_s = t_dq + 64 * DKC, t_dp = t_s + 128;  // dS over dP
 
     if (warp == kTmaWarp) {
         if (lane == 0 && nt > 0) {
-            mbar_arrive_expect_tx(&c.own_full, (uint32_t)((DKC + DVC) * kChunk * 2 * tile_rows));
-            for (int k = 0; k < DKC; ++k)
-                tma_load_4d(Qs + (size_t)k * kChunkBytes, &mq, &c.own_full, k * kChunk, hk * a.G, (int)rt * p.nl, b * p.qmul);
-            for (int k = 0; k < DVC; ++k)
-                tma_load_4d(Os + (size_t)k * kChunkBytes, &mo, &c.own_full, k * kChunk, hk * a.G, (int)rt * p.nl, b * p.omul);
-            RingPos rp;
+            RingPos rk, rv;
             int sa = 0, sb = 0;
-            for (int t = 0; t < nt; ++t, rp.next(ST)) {
-                const int s = rp.idx;
-                if (!mbar_wait_1t(&c.a_empty[s], rp.phase ^ 1u, abort_flag, err)) break;
-                mbar_arrive_expect_tx(&c.a_full[s], (uint32_t)(DKC * kChunkBytes));
+            for (int t = 0; t < nt; ++t, rk.next(SK), rv.next(SV)) {
+                if (!mbar_wait_1t(&c.a_empty[rk.idx], rk.phase ^ 1u, abort_flag, err)) break;
+                mbar_arrive_expect_tx(&c.a_full[rk.idx], (uint32_t)(DKC * kChunkBytes));
                 for (int k = 0; k < DKC; ++k)
-                    tma_load_4d(Kr + (size_t)(s * DKC + k) * kChunkBytes, &mk, &c.a_full[s], k * kChunk, hk * p.khmul,
+                    tma_load_4d(Kr + (size_t)(rk.idx * DKC + k) * kChunkBytes, &mk, &c.a_full[rk.idx], k * kChunk, hk * p.khmul,
                                 (t0 + t) * kTile, b * p.kmul);
                 ++sa;
-                if (!mbar_wait_1t(&c.b_empty[s], rp.phase ^ 1u, abort_flag, err)) break;
-                mbar_arrive_expect_tx(&c.b_full[s], (uint32_t)(DVC * kChunkBytes));
+                if (!mbar_wait_1t(&c.b_empty[rv.idx], rv.phase ^ 1u, abort_flag, err)) break;
+                mbar_arrive_expect_tx(&c.b_full[rv.idx], (uint32_t)(DVC * kChunkBytes));
                 for (int k = 0; k < DVC; ++k)
-                    tma_load_4d(Vr + (size_t)(s * DVC + k) * kChunkBytes, &mv, &c.b_full[s], k * kChunk, hk * p.vhmul,
+                    tma_load_4d(Vr + (size_t)(rv.idx * DVC + k) * kChunkBytes, &mv, &c.b_full[rv.idx], k * kChunk, hk * p.vhmul,
                                 (t0 + t) * kTile, b * p.vmul);
                 ++sb;
             }
-            mbar_drain(&c.own_full, 0, err);
-            for (int j = std::max(0, sa - ST); j < sa; ++j) mbar_drain(&c.a_full[j % ST], (uint32_t)(j / ST) & 1u, err);
-            for (int j = std::max(0, sb - ST); j < sb; ++j) mbar_drain(&c.b_full[j % ST], (uint32_t)(j / ST) & 1u, err);
+            for (int j = std::max(0, sa - SK); j < sa; ++j) mbar_drain(&c.a_full[j % SK], (uint32_t)(j / SK) & 1u, err);
+            for (int j = std::max(0, sb - SV); j < sb; ++j) mbar_drain(&c.b_full[j % SV], (uint32_t)(j / SV) & 1u, err);
         }
     } else if (warp == kMaskWarp) {
         // ------------------------------------------------------------- rows of K that are not read
         RingPos rp;
-        for (int t = 0; t < nt && fix; ++t, rp.next(ST)) {
+        for (int t = 0; t < nt && fix; ++t, rp.next(SK)) {
             uint32_t w[4];
             valid_words(w, a, b, (t0 + t) * kTile, n);
             if (!mbar_wait_warp(&c.a_full[rp.idx], rp.phase, abort_flag, err)) break;
@@ -513,36 +529,35 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else if (warp == kMmaWarp) {
         if (lane == 0 && nt > 0) {
             const uint32_t id_s = idesc_bf16_f32(kTile), id_q = idesc_bf16_bmn(DKC * kChunk);
-            const uint32_t qa = smem_u32(Qs), oa = smem_u32(Os), ka = smem_u32(Kr), va = smem_u32(Vr);
-            RingPos cur, nxt;
-            auto scores = [&](const RingPos& r) {
-                if (!mbar_wait_1t(fix ? &c.a_ready[r.idx] : &c.a_full[r.idx], r.phase, abort_flag, err)) return false;
+            const uint32_t ka = smem_u32(Kr), va = smem_u32(Vr);
+            RingPos cur, ns, nd;  // stages of dQ's tile, of S's and of dP's
+            auto scores = [&]() {
+                if (!mbar_wait_1t(fix ? &c.a_ready[ns.idx] : &c.a_full[ns.idx], ns.phase, abort_flag, err)) return false;
                 tc_fence_after();
-                mma_tile_ss<DKC>(t_s, qa, ka + (uint32_t)(r.idx * DKC * kChunkBytes), id_s);
+                mma_rows_ts<DKC>(t_s, t_q, ka + (uint32_t)(ns.idx * DKC * kChunkBytes), id_s);
                 mma_commit(&c.s_full);
+                ns.next(SK);
                 return true;
             };
-            auto dprod = [&](const RingPos& r) {
-                if (!mbar_wait_1t(&c.b_full[r.idx], r.phase, abort_flag, err)) return false;
+            auto dprod = [&]() {
+                if (!mbar_wait_1t(&c.b_full[nd.idx], nd.phase, abort_flag, err)) return false;
                 tc_fence_after();
-                mma_tile_ss<DVC>(t_dp, oa, va + (uint32_t)(r.idx * DVC * kChunkBytes), id_s);
+                mma_rows_ts<DVC>(t_dp, t_do, va + (uint32_t)(nd.idx * DVC * kChunkBytes), id_s);
                 mma_commit(&c.dp_full);
-                mma_commit(&c.b_empty[r.idx]);
+                mma_commit(&c.b_empty[nd.idx]);
+                nd.next(SV);
                 return true;
             };
-            bool ok = mbar_wait_1t(&c.own_full, 0, abort_flag, err) && scores(cur) && dprod(cur);
+            bool ok = mbar_wait_1t(&c.own_full, 0, abort_flag, err) && scores() && dprod();
             for (int t = 0; t < nt && ok; ++t) {
                 const uint32_t ph = (uint32_t)t & 1u;
-                nxt = cur;
-                nxt.next(ST);
-                if (t + 1 < nt && !(ok = mbar_wait_1t(&c.s_free, ph, abort_flag, err) && scores(nxt))) break;
-                if (t + 1 < nt && !(ok = mbar_wait_1t(&c.dp_free, ph, abort_flag, err) && dprod(nxt))) break;
+                if (t + 1 < nt && !(ok = mbar_wait_1t(&c.s_free, ph, abort_flag, err) && scores())) break;
                 if (!(ok = mbar_wait_1t(&c.ds_full, ph, abort_flag, err))) break;
                 tc_fence_after();
-                mma_tile_ts<16>(t_dq, t_ds, ka + (uint32_t)(cur.idx * DKC * kChunkBytes), id_q, t != 0);
-                mma_commit(&c.ds_free);
+                mma_tile_ts<32>(t_dq, t_dp, ka + (uint32_t)(cur.idx * DKC * kChunkBytes), id_q, t != 0);
                 mma_commit(&c.a_empty[cur.idx]);
-                cur = nxt;
+                cur.next(SK);
+                if (t + 1 < nt && !(ok = dprod())) break;
             }
             mma_commit(&c.done);
             mbar_drain(&c.done, 0, err);
@@ -551,12 +566,28 @@ __global__ void __launch_bounds__(kThreads, 1)
         // ------------------------------------------------------------- softmax warps: a lane is a row
         const int quarter = warp >> 2, quad = warp & 3;
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
-        const uint32_t ts = t_s + lane_base + (uint32_t)(kCols * quarter), td = t_dp + lane_base + (uint32_t)(kCols * quarter);
+        const uint32_t col = lane_base + (uint32_t)(kCols * quarter);
+        const uint32_t ts = t_s + col, td = t_dp + col;
         const int r = quad * 32 + lane;
+        const long long pr = rt * tile_rows + r;
+        const bool mine = r < tile_rows && pr < a.rows;
+        const int l = r / a.G;
+        const long long ql = mine ? rt * p.nl + l : 0;
+        const int hq = hk * a.G + (mine ? r - l * a.G : 0);
         const float cs = a.scale * kLog2e;
         const float* stats = a.ws + (((long long)b * a.Hkv + hk) * p.rtiles + rt) * kStats;
         const float nl = stats[r], nd = stats[kTile + r];
         const bool none = nl == -INFINITY;  // no row, or one without weight
+        if (nt > 0) {
+            keep_row<DKC>(t_q + lane_base, reinterpret_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.b + ql * a.q.l + hq * a.q.h,
+                          a.dk, mine, quarter);
+            keep_row<DVC>(t_do + lane_base, reinterpret_cast<const __nv_bfloat16*>(a.dO.p) + b * a.dO.b + ql * a.dO.l + hq * a.dO.h,
+                          a.dv, mine, quarter);
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&c.own_full);
+        }
         bool ok = true;
         for (int t = 0; t < nt; ++t) {
             const uint32_t ph = (uint32_t)t & 1u;
@@ -594,9 +625,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             float* d = reinterpret_cast<float*>(dr);
             tmem_ld32_issue(td, dr);
             tmem_wait_ld32(dr);
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&c.dp_free);
 #pragma unroll
             for (int q = 0; q < kCols; q += 2) {
                 add2(d[q], d[q + 1], nd, nd);
@@ -608,12 +636,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
 #pragma unroll
             for (int q = 0; q < kCols / 2; ++q) pk[q] = none ? 0u : pack_bf16(d[2 * q], d[2 * q + 1]);
-            if (t > 0 && !mbar_wait_warp_inline(&c.ds_free, (uint32_t)(t - 1) & 1u, abort_flag, err)) {
-                ok = false;
-                break;
-            }
-            tc_fence_after();
-            tmem_st16(t_ds + lane_base + (uint32_t)(kCols / 2 * quarter), pk);
+            tmem_st16(td, pk);
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
@@ -621,16 +644,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (ok && nt > 0) ok = mbar_wait_warp_inline(&c.done, 0, abort_flag, err);
         tc_fence_after();
-        if (ok) {  // 32 columns of dQ a quarter
-            const long long pr = rt * tile_rows + r;
-            const bool mine = r < tile_rows && pr < a.rows;
-            const int l = r / a.G;
-            const long long ql = mine ? rt * p.nl + l : 0;
-            const int h = hk * a.G + (mine ? r - l * a.G : 0);
-            const long long at = ((long long)b * a.Hq + h) * a.Lq + ql;
+        if (ok) {  // 32 columns of dQ a warp
+            const long long at = ((long long)b * a.Hq + hq) * a.Lq + ql;
             drain_acc(t_dq + lane_base, kCols * quarter, kCols * quarter + kCols, a.dk, nt > 0, !none, mine,
                       a.splits > 1 ? 1.f : a.scale,
-                      reinterpret_cast<__nv_bfloat16*>(a.dQ.p) + b * a.dQ.b + ql * a.dQ.l + h * a.dQ.h, p.vec_q != 0,
+                      reinterpret_cast<__nv_bfloat16*>(a.dQ.p) + b * a.dQ.b + ql * a.dQ.l + hq * a.dQ.h, p.vec_q != 0,
                       a.splits > 1 ? a.ws + xattn_ws_dq(a) + ((long long)part * xattn_rows(a) + at) * a.dk : nullptr);
         }
     }
@@ -654,7 +672,7 @@ cudaError_t launch(const HeadMap& q, const HeadMap& o, const HeadMap& k, const H
     if (!set) {
         e = cudaFuncSetAttribute(k_xattn_dkv_tc<DKC, DVC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
         if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(k_xattn_dq_tc<DKC, DVC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
+            e = cudaFuncSetAttribute(k_xattn_dq_tc<DKC, DVC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kDqSmem);
         if (e != cudaSuccess) return e;
         set = true;
     }
@@ -662,8 +680,7 @@ cudaError_t launch(const HeadMap& q, const HeadMap& o, const HeadMap& k, const H
         q.map, o.map, k.map, v.map, p);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     if (a.rsplits > 1 && (e = launch_xattn_join_dkv(a, s)) != cudaSuccess) return e;
-    k_xattn_dq_tc<DKC, DVC><<<(unsigned)(p.rtiles * a.splits * a.Hkv * a.B), kThreads, C::kSmem, s>>>(q.map, o.map, k.map,
-                                                                                                      v.map, p);
+    k_xattn_dq_tc<DKC, DVC><<<(unsigned)(p.rtiles * a.splits * a.Hkv * a.B), kThreads, C::kDqSmem, s>>>(k.map, v.map, p);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     return a.splits > 1 ? launch_xattn_join_dq(a, s) : cudaSuccess;
 }

@@ -51,16 +51,52 @@ static __device__ __forceinline__ void mma_tile_ss(uint32_t d, uint32_t a, uint3
         mma_f16_ss(d, ad + off, bd + off, idesc, k != 0 ? 1u : 0u);
     }
 }
-// D[tmem] (+)= A[tmem: bf16 pairs] B over 128 rows of B (MN-major): 32 rows of A's K axis (two steps of 8 columns)
+// D[tmem] (+)= A[tmem: bf16 pairs] B over STEPS * 16 rows of B (MN-major): 32 rows of A's K axis (two steps of 8 columns)
 // every GAP columns
-template <int GAP>
+template <int GAP, int STEPS = kTile / 16>
 static __device__ __forceinline__ void mma_tile_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate) {
     const uint64_t bd = sdesc_mn(b);
 #pragma unroll
-    for (int k = 0; k < kTile / 16; ++k)
+    for (int k = 0; k < STEPS; ++k)
         mma_bf16_ts(d, a + (uint32_t)((k >> 1) * GAP + (k & 1) * 8), bd + (uint64_t)(k * 128), idesc,
                     accumulate || k != 0 ? 1u : 0u);
 }
+// D[tmem] = A[tmem: bf16 pairs, CHUNKS * 32 columns] B[smem]^T, B K-major in chunks of 64 columns
+template <int CHUNKS>
+static __device__ __forceinline__ void mma_rows_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
+    const uint64_t bd = sdesc_sw128(b);
+#pragma unroll
+    for (int k = 0; k < CHUNKS * 4; ++k)
+        mma_bf16_ts(d, a + (uint32_t)(8 * k), bd + (uint64_t)((k >> 2) * (kChunkBytes >> 4) + (k & 3) * 2), idesc,
+                    k != 0 ? 1u : 0u);
+}
+// 16 bf16 elements [c, c + 16) of a row of w (zeros past w, and where !has) as 8 words
+static __device__ __forceinline__ void load_words(uint32_t (&x)[8], const __nv_bfloat16* row, int c, int w, bool has) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int e0 = c + 8 * h;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (has && e0 + 8 <= w) {
+            v = __ldg(reinterpret_cast<const uint4*>(row + e0));
+        } else if (has && e0 < w) {
+            uint32_t u[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e0 + e < w) u[e >> 1] |= (uint32_t)__ldg(reinterpret_cast<const unsigned short*>(row) + e0 + e) << (16 * (e & 1));
+            v = make_uint4(u[0], u[1], u[2], u[3]);
+        }
+        x[4 * h] = v.x;
+        x[4 * h + 1] = v.y;
+        x[4 * h + 2] = v.z;
+        x[4 * h + 3] = v.w;
+    }
+}
+static __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(v[0]), "r"(v[1]),
+                 "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
+
 // Untiled copy of `bytes` (a multiple of 16, both addresses on 16-byte boundaries) to shared memory.
 static __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
