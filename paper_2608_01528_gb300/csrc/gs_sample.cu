@@ -9,14 +9,16 @@
 // small probabilities, and a draw whose number ends near a border would go to a neighbour.  (fp64 runs at 1/64
 // of the fp32 rate here: the exponentials of 256 rows of 128,000 alone would take milliseconds.)
 //
-// Rows of up to 4,096 scores (k_sample_row): one block sorts the row in shared memory; prefix sums of the
-// sorted weights give t and cut.  With neither top-k nor top-p nothing is sorted.
+// Rows of up to 512 scores (k_sample_warp): a warp a row, scores and weights in registers; t is built bit by bit
+// from the highest, by the count or weight of the keys at or above it.  Up to 4,096 (k_sample_row): a block sorts the row
+// in shared memory; prefix sums of the sorted weights give t and cut.  Both are bound by instructions (4,096 x 256 with
+// top-p: 41 us sorted, see k_sample_warp for now).
 //
 // Longer rows (k_sample_wide): a cluster of up to 8 CTAs a row, re-reading the row from L2.  Pass 0: largest and
-// smallest score.  Pass 1: a histogram over 2,048 equal steps of log weight -- counts for top-k; for top-p weights
-// cut to 14 bits, which bound the running weight to a factor 1 + 2^-12 -- and the exact total.  Pass 2: the few
-// entries of the steps in which t can lie (top-k: and all above) go to one CTA's list, which sorts them; the exact weight of
-// the rest is summed per warp's stretch of the row.  The draw then only looks through the one stretch in which it
+// smallest score.  Pass 1: a histogram over 2,048 equal steps of log weight -- counts for top-k; for top-p fp32
+// weights cut to some 16 bits, which bound the running weight to 2^-14 of it.  Pass 2: the few entries of the steps in which t
+// can lie (top-k: and all above) go to one CTA's list, which sorts them; the exact weight of what lies above is summed
+// per warp's stretch of the row, and that of the whole row.  The draw then only looks through the one stretch in which it
 // falls.  Where the list overflows (more than 4,096 ties, or top_k beyond that) one block takes
 // the row by radix selects over its bits.
 
@@ -112,6 +114,10 @@ struct Weigher {
         const float ph = d * chi;
         lo = fmaf(d, chi, -ph) + fmaf(d, clo, dl * chi);
         return ph;
+    }
+    __device__ __forceinline__ float log2_only(float x) const {
+        const float d = 0.5f * x - half_max;
+        return d * chi;
     }
     // round(2^41 2^(ph + pl)): 2^(j/1024) from the table, 2^r - 1 of the rest |r| <= 2^-11 from its series in fp32; the
     // roundings of r, of the series and of its last product are 2^-36 each
@@ -261,6 +267,123 @@ __device__ __forceinline__ void answer(const SampleArgs& a, long long n, int i, 
     if (a.prob) a.prob[n] = total ? __ull2float_rn(w) / __ull2float_rn(total) : 0.f;
 }
 
+// ----------------------------------------------------------------- rows of up to 32 E scores: a warp each
+// Sum over the warp of numbers below 2^47.
+__device__ __forceinline__ u64 warp_total(u64 v) {
+    const u64 lo = __reduce_add_sync(0xffffffffu, (unsigned)v & 0xffffffu);
+    const u64 hi = __reduce_add_sync(0xffffffffu, (unsigned)(v >> 24));
+    return lo + (hi << 24);
+}
+
+template <int E>
+__global__ void __launch_bounds__(128) k_sample_warp(const SampleArgs a, long long n0) {
+    const long long n = n0 + (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+    if (n >= a.N) return;
+    const int lane = threadIdx.x & 31, M = a.M;
+    const void* row = static_cast<const char*>(a.S) + n * a.lds * (a.bf16 ? 2 : 4);
+    Settings st;
+    st.load(a, n);
+    uint32_t key[E], top = 0, low = 0xffffffffu;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int i = lane + 32 * e;
+        key[e] = i < M ? key_of(load_score(row, a.bf16, i)) : 0u;
+        top = max(top, key[e]);
+        low = key[e] ? min(low, key[e]) : low;
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    low = __reduce_min_sync(0xffffffffu, low);
+    if (top == 0u || !(st.T > 0.f)) {
+        unsigned first = 0x7fffffffu;
+#pragma unroll
+        for (int e = E - 1; e >= 0; --e) first = key[e] == top ? lane + 32 * e : first;
+        first = __reduce_min_sync(0xffffffffu, first);
+        if (lane == 0) answer(a, n, top ? (int)first : -1, top ? 1 : 0, top ? 1 : 0);
+        return;
+    }
+    Weigher w;
+    w.set(top, st.T);
+    u64 wt[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) wt[e] = w.weight(value_of(key[e]), key[e], g_pow.v);
+    // t: the largest key with enough at or above it; bits above the highest in which keys differ are the same in all
+    uint32_t t = 1;
+    int ties = 0x7fffffff;  // kept ones of the keys equal to t, in index order
+    const int bits = 32 - __clz(top ^ low);
+    const uint32_t common = bits < 32 ? top >> bits << bits : 0u;
+    if (st.top_k >= 1 && st.top_k < M) {
+        auto count = [&](uint32_t from) {
+            int c = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) c += key[e] >= from;
+            return __reduce_add_sync(0xffffffffu, c);
+        };
+        if (count(1) > st.top_k) {
+            t = common;
+            for (int b = bits - 1; b >= 0; --b)
+                if (count(t | 1u << b) >= st.top_k) t |= 1u << b;
+            ties = st.top_k - (t == 0xffffffffu ? 0 : count(t + 1));
+        }
+    }
+    // weight of the keys >= from that top-k keeps
+    auto rank_kept = [&](int e, int& before) {  // whether entry e is kept among the ties; e in ascending order
+        const unsigned m = __ballot_sync(0xffffffffu, key[e] == t);
+        const bool in = key[e] > t || (key[e] == t && before + __popc(m & ((1u << lane) - 1u)) < ties);
+        before += __popc(m);
+        return in;
+    };
+    if (ties != 0x7fffffff) {  // what top-k drops weighs nothing from here on
+        int before = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (!rank_kept(e, before)) {
+                wt[e] = 0;
+                key[e] = 0;
+            }
+        t = 1;
+        ties = 0x7fffffff;
+    }
+    if (st.top_p < 1.f) {
+        auto weigh = [&](uint32_t from) {
+            u64 s = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) s += key[e] >= from ? wt[e] : 0ull;
+            return warp_total(s);
+        };
+        const u64 need = needed(st.top_p, weigh(1));
+        t = common;
+        for (int b = bits - 1; b >= 0; --b)
+            if (weigh(t | 1u << b) >= need) t |= 1u << b;
+        const u64 above = t == 0xffffffffu ? 0 : weigh(t + 1), one = w.weight(value_of(t), t, g_pow.v);
+        ties = (int)min((need - above + one - 1) / max(one, 1ull), 0x7ffffffeull);
+    }
+    u64 total = 0;
+    {
+        int before = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            if (!rank_kept(e, before) || wt[e] < st.least) wt[e] = 0;
+            total += wt[e];
+        }
+    }
+    total = warp_total(total);
+    const u64 target = share_of(st.u, total, false);
+    u64 before = 0;
+    bool found = false;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        if (found) continue;
+        const u64 all = warp_total(wt[e]);
+        if (before + all > target) {
+            const u64 run = before + warp_scan(wt[e]);
+            const unsigned past = __ballot_sync(0xffffffffu, run > target);
+            if (lane == __ffs(past) - 1) answer(a, n, lane + 32 * e, wt[e], total);
+            found = true;
+        }
+        before += all;
+    }
+}
+
 // ----------------------------------------------------------------- rows of up to kList scores: a block each
 __global__ void k_sample_row(const SampleArgs a, long long n0, int n2) {
     extern __shared__ u64 list[];  // n2 sorted entries, then M keys
@@ -329,10 +452,10 @@ struct Wide {
     u64 list[kList];
     u64 seg[kMaxCluster * kWideWarps];  // rank 0: kept weight of every warp's stretch
     u64 above[kMaxCluster];             // rank 0: weight above the list, of each CTA
-    u64 best[kMaxCluster];              // every CTA: each CTA's best entry
-    uint32_t low[kMaxCluster];          // and its smallest key
-    u64 total[kMaxCluster];             // exact weight of each CTA's part
-    uint32_t hist[kBins];
+    u64 total[kMaxCluster];             // and of all its scores
+    u64 range[kMaxCluster];             // every CTA: each CTA's smallest and largest score
+    float2 ends[kWideWarps];
+    alignas(16) uint32_t hist[kBins];
     u64 sh[kWideWarps];
     u64 found[3];
     unsigned count;                     // rank 0: entries sent to the list
@@ -341,10 +464,15 @@ struct Wide {
 __device__ __forceinline__ void st_remote_u64(uint32_t addr, u64 v) {
     asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
 }
-__device__ __forceinline__ uint32_t ld_remote_u32(uint32_t addr) {
-    uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ uint4 ld_remote_v4(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
     return v;
+}
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 __device__ __forceinline__ unsigned add_remote(uint32_t addr, unsigned v) {
     unsigned r;
@@ -524,51 +652,55 @@ __global__ void __launch_bounds__(kWideThreads, 2) k_sample_wide(const SampleArg
     Settings st;
     st.load(a, n);
 
-    // pass 0: the best entry, the smallest key
-    u64 best = 0;
-    uint32_t low = 0xffffffffu;
-    for_scores(row, a.bf16, M, off, v0, v1, [&](int i, float x) {
-        const uint32_t k = key_of(x);
-        best = max(best, entry_of(k, i));
-        low = k ? min(low, k) : low;
+    // pass 0: the largest and the smallest score that can be drawn
+    float hi = -INFINITY, lo = INFINITY;
+    for_scores(row, a.bf16, M, off, v0, v1, [&](int, float x) {
+        hi = fmaxf(hi, x);
+        lo = fminf(lo, x > -INFINITY ? x : INFINITY);
     });
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
-        best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
-        low = min(low, __shfl_xor_sync(0xffffffffu, low, o));
+        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
     }
-    if (lane == 0) {
-        m.sh[warp] = best;
-        m.seg[warp] = low;
-    }
+    if (lane == 0) m.ends[warp] = make_float2(hi, lo);
     __syncthreads();
     ptx::cluster_sync_all();  // every CTA of the cluster runs from here on
     if (warp == 0) {
-        best = lane < kWideWarps ? m.sh[lane] : 0;
-        u64 lo = lane < kWideWarps ? m.seg[lane] : 0xffffffffull;
+        const float2 e = m.ends[lane % kWideWarps];
+        hi = e.x;
+        lo = e.y;
 #pragma unroll
         for (int o = 8; o; o >>= 1) {
-            best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
-            lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+            hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+            lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
         }
-        best = __shfl_sync(0xffffffffu, best, 0);
-        lo = __shfl_sync(0xffffffffu, lo, 0);
-        if (lane < G) {
-            st_remote_u64(remote(&m.best[rank], lane), best);
-            ptx::st_cluster_u32(remote(&m.low[rank], lane), (uint32_t)lo);
-        }
+        if (lane < G) st_remote_u64(remote(&m.range[rank], lane), (u64)__float_as_uint(lo) << 32 | __float_as_uint(hi));
     }
     ptx::cluster_sync_all();
-    best = 0;
-    low = 0xffffffffu;
+    hi = -INFINITY;
+    lo = INFINITY;
     for (int i = 0; i < G; ++i) {
-        best = max(best, m.best[i]);
-        low = min(low, m.low[i]);
+        hi = fmaxf(hi, __uint_as_float((uint32_t)m.range[i]));
+        lo = fminf(lo, __uint_as_float((uint32_t)(m.range[i] >> 32)));
     }
-    const uint32_t top = entry_key(best);
-    if (top == 0u || !(st.T > 0.f)) {
-        if (rank == 0 && tid == 0) answer(a, n, top ? entry_index(best) : -1, top ? 1 : 0, top ? 1 : 0);
-        return;  // (no CTA touches another's memory any more)
+    const uint32_t top = key_of(hi);
+    if (top == 0u) {  // (no CTA touches another's memory any more)
+        if (rank == 0 && tid == 0) answer(a, n, -1, 0, 0);
+        return;
+    }
+    if (!(st.T > 0.f)) {
+        unsigned first = 0x7fffffffu;
+        for_scores(row, a.bf16, M, off, v0, v1, [&](int i, float x) { first = x == hi ? min(first, (unsigned)i) : first; });
+        first = __reduce_min_sync(0xffffffffu, first);
+        if (lane == 0) st_remote_u64(remote(&m.seg[rank * kWideWarps + warp], 0), first);
+        ptx::cluster_sync_all();
+        if (rank == 0 && warp == 0) {
+            for (int i = lane; i < G * kWideWarps; i += 32) first = min(first, (unsigned)m.seg[i]);
+            first = __reduce_min_sync(0xffffffffu, first);
+            if (lane == 0) answer(a, n, (int)first, 1, 1);
+        }
+        return;
     }
     Weigher w;
     w.set(top, st.T);
@@ -586,79 +718,86 @@ __global__ void __launch_bounds__(kWideThreads, 2) k_sample_wide(const SampleArg
         });
     } else {
         // 2,048 equal steps of log2 weight from the largest score down to the smallest, or to where weights vanish
-        float lo;
-        const float range = fminf(-w.log2_hi(value_of(low), lo), 43.f);
-        const float scale = range > 0.f ? (kBins - 1) / range : 0.f;
+        float pl;
+        const float range = fminf(-w.log2_hi(lo, pl), 43.f);
+        const float scale = range > 0.f ? (kBins - 1) / range : 0.f, width = range / (kBins - 1);
         auto step = [&](float ph) { return min((int)(-ph * scale), kBins - 1); };
-        // the shift that leaves 14 bits of a step's weights
-        const float width = range / (kBins - 1);
-        auto shift_of = [&](int b) { return max(0, kOneBits - 14 - (int)((float)b * width)); };
-        u64 total = 0;
+        auto octave = [&](int b) { return (int)((float)b * width); };
+        // bits of a histogram weight: a counter may have to hold all scores of this CTA
+        const int hb = min(20, __clz(per * kWideWarps * V - 1) - 1);
         for_scores(row, a.bf16, M, off, v0, v1, [&](int, float x) {
-            const uint32_t k = key_of(x);
-            if (k == 0u) return;
-            float pl;
-            const float ph = w.log2_hi(x, pl);
+            if (!(x > -INFINITY)) return;
+            const float ph = w.log2_only(x);
             const int b = step(ph);
-            if (by_k) {
-                atomicAdd(&m.hist[b], 1u);
-            } else {
-                const u64 v = w.from_log2(ph, pl, m.pow);
-                total += v;
-                atomicAdd(&m.hist[b], (uint32_t)(v >> shift_of(b)));
-            }
+            // the weight in units of 2^-hb of the step's octave: between 2^(hb - 1.03) and 2^hb
+            atomicAdd(&m.hist[b], by_k ? 1u : (uint32_t)ex2(ph + (float)(octave(b) + hb)));
         });
-        total = block_sum(total, m.sh);
-        if (tid < G) st_remote_u64(remote(&m.total[rank], tid), total);
+        __syncthreads();
         ptx::cluster_sync_all();
-        total = 0;
-        for (int i = 0; i < G; ++i) total += m.total[i];
         // the steps [b0, b1] in which the last kept entry lies
-        const u64 need = by_k ? (u64)st.top_k : needed(st.top_p, total);
         u64 part[kBins / kWideThreads], sum = 0, all;
         constexpr int kPer = kBins / kWideThreads;
+        static_assert(kPer == 4, "16 bytes of each histogram a thread");
+        u64 wide[kPer] = {0, 0, 0, 0};
+        for (int r = 0; r < G; ++r) {
+            const uint4 v = ld_remote_v4(remote(&m.hist[tid * kPer], r));
+            wide[0] += v.x;
+            wide[1] += v.y;
+            wide[2] += v.z;
+            wide[3] += v.w;
+        }
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
-            const int b = tid * kPer + e;
-            u64 v = 0;
-            for (int r = 0; r < G; ++r) v += ld_remote_u32(remote(&m.hist[b], r));
-            part[e] = by_k ? v : v << shift_of(b);
+            const int up = kOneBits - hb - octave(tid * kPer + e);
+            part[e] = by_k ? wide[e] : up >= 0 ? wide[e] << up : wide[e] >> -up;
             sum += part[e];
         }
         if (tid == 0) m.found[0] = m.found[1] = kBins - 1;
         u64 run = block_scan(sum, m.sh, all);
-        // running counts are exact; running weights lie between `run` and run (1 + 2^-12)
-        auto most = [&](u64 r) { return by_k || r == 0 ? r : r + (r >> 12) + 1; };
+        // Counts are exact.  Weights are cut down (by less than 2^(1.03 - hb), and by a unit where a step is shifted down) and off
+        // by the 2^-18 of an fp32 exponent up to 43 and its exponential.
+        auto least = [&](u64 r) { return by_k ? r : r - (r >> 16); };
+        auto most = [&](u64 r) { return by_k || r == 0 ? r : r + (r >> (hb - 2)) + (r >> 15) + kBins; };
+        const u64 need0 = by_k ? (u64)st.top_k : needed(st.top_p, least(all));
+        const u64 need1 = by_k ? (u64)st.top_k : needed(st.top_p, most(all));
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
             const u64 next = run + part[e];
-            if (most(run) < need && most(next) >= need) m.found[0] = tid * kPer + e;
-            if (run < need && next >= need) m.found[1] = tid * kPer + e;
+            if (most(run) < need0 && most(next) >= need0) m.found[0] = tid * kPer + e;
+            if (least(run) < need1 && least(next) >= need1) m.found[1] = tid * kPer + e;
             run = next;
         }
         __syncthreads();
         const int b0 = (int)m.found[0], b1 = (int)m.found[1];
-        // pass 2: the list, and the exact weight of what lies above it
+        // pass 2: the list, the exact weight of what lies above it and of the whole row
         const uint32_t list0 = remote(m.list, 0), count0 = remote(&m.count, 0);
-        u64 above = 0;
+        u64 above = 0, total = 0;
         for_scores(row, a.bf16, M, off, v0, v1, [&](int i, float x) {
-            const uint32_t k = key_of(x);
-            if (k == 0u) return;
+            if (!(x > -INFINITY)) return;
             float pl;
             const float ph = w.log2_hi(x, pl);
             const int b = step(ph);
-            if (b > b1) return;
-            if (by_k || b >= b0) {
-                const unsigned at = add_remote(count0, 1u);
-                if (at < (unsigned)kList) st_remote_u64(list0 + at * 8u, entry_of(k, i));
-            } else {
+            if (!by_k) {
                 const u64 v = w.from_log2(ph, pl, m.pow);
-                above += v;
-                mine += v >= st.least ? v : 0ull;
+                total += v;
+                if (b < b0) {
+                    above += v;
+                    mine += v >= st.least ? v : 0ull;
+                }
+            }
+            if (b <= b1 && (by_k || b >= b0)) {
+                const unsigned at = add_remote(count0, 1u);
+                if (at < (unsigned)kList) st_remote_u64(list0 + at * 8u, entry_of(key_of(x), i));
             }
         });
-        above = block_sum(above, m.sh);
-        if (tid == 0) st_remote_u64(remote(&m.above[rank], 0), above);
+        if (!by_k) {
+            above = block_sum(above, m.sh);
+            total = block_sum(total, m.sh);
+            if (tid == 0) {
+                st_remote_u64(remote(&m.above[rank], 0), above);
+                st_remote_u64(remote(&m.total[rank], 0), total);
+            }
+        }
         mine = warp_sum(mine);
         if (lane == 0) st_remote_u64(remote(&m.seg[rank * kWideWarps + warp], 0), mine);
         ptx::cluster_sync_all();
@@ -702,7 +841,11 @@ __global__ void __launch_bounds__(kWideThreads, 2) k_sample_wide(const SampleArg
             return;
         }
         u64 over = 0;
-        for (int i = 0; i < G; ++i) over += m.above[i];
+        total = 0;
+        for (int i = 0; i < G; ++i) {
+            over += m.above[i];
+            total += m.total[i];
+        }
         last = last_kept(m.list, nl, w, m.pow, st.top_p, over, total, m.sh, &m.found[0]);
         // the list's kept entries join their stretches
         for (int i = tid; i < nl; i += kWideThreads) {
@@ -769,6 +912,22 @@ cudaError_t launch_sample(const SampleArgs& a, int device, cudaStream_t s) {
         if (e != cudaSuccess) return e;
         g_attr[device] = true;
     }
+    if (a.M <= 512) {
+        for (long long n = 0; n < a.N; n += kRows) {
+            const unsigned grid = (unsigned)((std::min(kRows, a.N - n) + 3) / 4);
+            if (a.M <= 64)
+                k_sample_warp<2><<<grid, 128, 0, s>>>(a, n);
+            else if (a.M <= 128)
+                k_sample_warp<4><<<grid, 128, 0, s>>>(a, n);
+            else if (a.M <= 256)
+                k_sample_warp<8><<<grid, 128, 0, s>>>(a, n);
+            else
+                k_sample_warp<16><<<grid, 128, 0, s>>>(a, n);
+            cudaError_t e = cudaGetLastError();
+            if (e != cudaSuccess) return e;
+        }
+        return cudaSuccess;
+    }
     if (a.M <= kList) {
         int n2 = 64;
         while (n2 < a.M) n2 <<= 1;
@@ -781,9 +940,12 @@ cudaError_t launch_sample(const SampleArgs& a, int device, cudaStream_t s) {
         }
         return cudaSuccess;
     }
-    // 16,384 scores a CTA, up to 8 CTAs
+    // CTAs a row: up to 2^18 scores each (the histogram's counters), and where rows are few more, of 4,096 scores or
+    // more: a cluster's waits for one another cost about 10 us a row, hidden only by other rows' work
+    int sms = 0;
+    cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
     int G = 1;
-    while (G < kMaxCluster && (long long)G * 16384 < a.M) G <<= 1;
+    while (G < kMaxCluster && (a.M / G > 1 << 18 || (a.N * G < 4ll * sms && a.M / G >= 8192))) G <<= 1;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;

@@ -187,3 +187,30 @@ def test_layouts_streams_graphs(gs):
     only = gs.sample_scores(S, U, top_k=30, want_prob=False)
     assert set(only) == {"index"} and torch.equal(only["index"], want["index"])
     assert gs.sample_scores(S[:0], U[:0])["index"].shape == (0,)
+
+
+@pytest.mark.parametrize("N", [1, 20, 700])
+def test_long_rows_of_few_and_many(gs, N):
+    """Rows that one CTA, some or eight share."""
+    S, U = scores(N, 9001, "f32", seed=3)
+    for how in (dict(), dict(k=20, p=0.8), dict(p=0.95), dict(p=0.9999), dict(T=0.0), dict(mp=0.2)):
+        out = gs.sample_scores(S, U, temperature=how.get("T", 1.0), top_k=how.get("k", 0), top_p=how.get("p", 1.0),
+                               min_p=how.get("mp", 0.0))
+        pick = torch.arange(0, N, max(1, N // 10)).cuda()
+        part = check(gs, S[pick].contiguous(), U[pick].contiguous(), **how)
+        assert torch.equal(part["index"], out["index"][pick]) and torch.equal(part["prob"], out["prob"][pick])
+
+
+def test_long_rows_that_are_not_finite(gs):
+    S, U = scores(7, 9000, "f32")
+    inf = float("inf")
+    S[0] = -inf
+    S[1] = float("nan")
+    S[2, ::3] = -inf
+    S[3, 100], S[3, 8000], S[3, 8500] = inf, inf, inf
+    S[4] = -inf
+    S[4, 8999] = 1.0
+    S[5] = 2.5
+    S[6, ::2] = torch.finfo(torch.float32).min
+    for how in (dict(), dict(k=2), dict(p=0.7), dict(k=5000, p=0.9), dict(mp=0.5), dict(T=0.0), dict(T=inf), dict(T=1e-40, k=3)):
+        check(gs, S, U, **how)
