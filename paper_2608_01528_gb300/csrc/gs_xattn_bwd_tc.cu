@@ -50,6 +50,7 @@ struct Ctl {
     uint64_t s_free;                                 // dq: S has been read
     uint64_t done;
     alignas(16) float stats[4][kStats];              // dkv; read 16 bytes at a time
+    float dpart[4][kTile];                           // dq: parts of D
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -575,9 +576,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         const long long ql = mine ? rt * p.nl + l : 0;
         const int hq = hk * a.G + (mine ? r - l * a.G : 0);
         const float cs = a.scale * kLog2e;
-        const float* stats = a.ws + (((long long)b * a.Hkv + hk) * p.rtiles + rt) * kStats;
-        const float nl = stats[r], nd = stats[kTile + r];
+        float* stats = a.ws + (((long long)b * a.Hkv + hk) * p.rtiles + rt) * kStats;
+        const float nl = stats[r];
+        float nd = stats[kTile + r];
         const bool none = nl == -INFINITY;  // no row, or one without weight
+        const bool exact = a.splits == 1 && nt == 1;
         if (nt > 0) {
             keep_row<DKC>(t_q + lane_base, reinterpret_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.b + ql * a.q.l + hq * a.q.h,
                           a.dk, mine, quarter);
@@ -599,6 +602,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 w = __ballot_sync(0xffffffffu, j < n && (!a.mask || __ldg(a.mask + (long long)b * a.ldm + j) != 0));
             }
             if (!mbar_wait_warp_inline(&c.s_full, ph, abort_flag, err)) {
+                if (exact) bar_sync_and(1, kSoftWarps * 32, false);
                 ok = false;
                 break;
             }
@@ -617,6 +621,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 s[q + 1] = ex2(s[q + 1]);
             }
             if (!mbar_wait_warp_inline(&c.dp_full, ph, abort_flag, err)) {
+                if (exact) bar_sync_and(1, kSoftWarps * 32, false);
                 ok = false;
                 break;
             }
@@ -625,6 +630,20 @@ __global__ void __launch_bounds__(kThreads, 1)
             float* d = reinterpret_cast<float*>(dr);
             tmem_ld32_issue(td, dr);
             tmem_wait_ld32(dr);
+            if (exact) {
+                // every key of the sequence is here: D = sum_j P dP in fp32, for this kernel and the next.  From a bf16 O
+                // it is off by 2^-9 of <dO, O>, which with a few keys exceeds the rounding of dS (2 keys: dK off by 5e-3, so 2e-3).
+                float sum = 0.f;
+#pragma unroll
+                for (int q = 0; q < kCols; ++q) sum += (w >> q) & 1u ? s[q] * d[q] : 0.f;
+                c.dpart[quarter][r] = sum;
+                if (!bar_sync_and(1, kSoftWarps * 32, true)) {  // a warp gave up
+                    ok = false;
+                    break;
+                }
+                nd = none ? 0.f : -((c.dpart[0][r] + c.dpart[1][r]) + (c.dpart[2][r] + c.dpart[3][r]));
+                if (quarter == 0) stats[kTile + r] = nd;
+            }
 #pragma unroll
             for (int q = 0; q < kCols; q += 2) {
                 add2(d[q], d[q + 1], nd, nd);
@@ -676,13 +695,14 @@ cudaError_t launch(const HeadMap& q, const HeadMap& o, const HeadMap& k, const H
         if (e != cudaSuccess) return e;
         set = true;
     }
+    // first dQ: for short sequences it leaves a more exact D to the other
+    k_xattn_dq_tc<DKC, DVC><<<(unsigned)(p.rtiles * a.splits * a.Hkv * a.B), kThreads, C::kDqSmem, s>>>(k.map, v.map, p);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if (a.splits > 1 && (e = launch_xattn_join_dq(a, s)) != cudaSuccess) return e;
     k_xattn_dkv_tc<DKC, DVC><<<(unsigned)((long long)p.ktiles * a.rsplits * a.Hkv * a.B), kThreads, C::kSmem, s>>>(
         q.map, o.map, k.map, v.map, p);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    if (a.rsplits > 1 && (e = launch_xattn_join_dkv(a, s)) != cudaSuccess) return e;
-    k_xattn_dq_tc<DKC, DVC><<<(unsigned)(p.rtiles * a.splits * a.Hkv * a.B), kThreads, C::kDqSmem, s>>>(k.map, v.map, p);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    return a.splits > 1 ? launch_xattn_join_dq(a, s) : cudaSuccess;
+    return a.rsplits > 1 ? launch_xattn_join_dkv(a, s) : cudaSuccess;
 }
 
 bool on_vectors(const HeadView& v, int B, int L, int H, int w) {

@@ -378,6 +378,25 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long l
         float s[4][4] = {}, dp[4][4] = {};
         dots<DK>(s, Qs, Ks);
         dots<DV>(dp, Ds, Vs);
+        if (a.splits == 1 && n <= kTile) {
+            // every key of the sequence is here: D = sum_j P dP, for this kernel and the next (a bf16 O gives it to 2^-9 of
+            // <dO, O> only, which with a few keys is more than dP - D)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float L = lse2[ty + 16 * i];
+                float sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (ok[tx + 16 * j] && L != INFINITY) sum = fmaf(exp2f(s[i][j] * a.scale * kLog2e - L), dp[i][j], sum);
+                sum = row_sum(sum);
+                const long long r = r0 + ty + 16 * i;
+                if (tx == 0) {
+                    delta[ty + 16 * i] = sum;
+                    if (r < a.rows) a.ws[row_index(a, bl.b, bl.hk, r)] = sum;
+                }
+            }
+            __syncthreads();
+        }
         tile_grad(s, dp, ok, lse2, delta, a.scale * kLog2e);
 #pragma unroll
         for (int i = 0; i < 4; ++i)

@@ -351,3 +351,23 @@ def test_growing_maxima(gs):
         K[..., 0] = up[None, :, None].bfloat16()
         Q[..., 0] = (torch.arange(200) % 7 - 3).cuda()[None, :, None].bfloat16() * 4
         check_forward(gs, Q, K, V, 0.5, None, None, "tensor", True)
+
+
+@pytest.mark.parametrize("path", ["simt", "auto"])
+@pytest.mark.parametrize("Lk", [1, 2, 3, 8, 40, 64, 100, 128])
+def test_gradient_over_few_keys(gs, Lk, path):
+    """With few keys dP - D cancels: dS rounded to bf16 (the tensor cores) or not at all (CUDA cores) and the outputs'
+    rounding are what may be off, not a bf16 O's 2^-9 of <dO, O>.  In the 2-norm over thousands of independent
+    roundings of at most h, whose mean square is h^2 / 3 or less (1.2 of room for their spread)."""
+    Q, K, V, dO = make(6, 50, Lk, 4, 2, 64, 64, "bf16")
+    r = Ref(Q, K, V, 0.125)
+    O, lse = r.o.permute(0, 2, 1, 3).bfloat16().cuda(), r.lse.float().cuda()
+    got = gs.cross_attention_backward(Q, K, V, O, lse, dO, 0.125, path=path)
+    gs.stream_status()
+    n = 2 if path == "auto" else 1
+    for name, (want, _) in r.grad(dO).items():
+        off = (got[name].cpu().double() - want).norm()
+        if Lk == 1 and name != "dV":  # P = 1: dS = 0, whatever fp32 leaves of it
+            assert off <= 1e-5 * dO.float().norm().cpu() * 64
+            continue
+        assert off <= 1.2 * (n / 3) ** 0.5 * 2.0 ** -8 * want.norm(), (name, float(off / want.norm()))
