@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "gs_internal.h"
 #include "gs_xattn.h"
@@ -903,11 +904,18 @@ gs_status attn_args(const gs_attn* p, gs::XattnArgs& a) {
     return GS_OK;
 }
 
+// The current device, if it is an sm_103, and its multiprocessors (asked for once: a small call is mostly its host time).
 gs_status attn_device(int& dev, int& sms) {
+    static std::atomic<int> known[64];  // 0: not asked yet, -1: another architecture, else the multiprocessors
     if (cudaGetDevice(&dev) != cudaSuccess) return GS_ERR_CUDA;
-    if (!device_supported(dev)) return GS_ERR_UNSUPPORTED;
-    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1) return GS_ERR_CUDA;
-    return GS_OK;
+    if (dev < 0 || dev >= 64) return GS_ERR_UNSUPPORTED;
+    sms = known[dev].load(std::memory_order_relaxed);
+    if (sms == 0) {
+        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1) return GS_ERR_CUDA;
+        if (!device_supported(dev) || !gs::tc_available(dev)) sms = -1;
+        known[dev].store(sms, std::memory_order_relaxed);
+    }
+    return sms < 0 ? GS_ERR_UNSUPPORTED : GS_OK;
 }
 
 gs_status attn_workspace(const float* ws, long long bytes, long long floats) {
@@ -958,7 +966,7 @@ gs_status gs_cross_attention(const gs_attn* p, const gs_heads* Q, const gs_heads
     a.lse = lse;
     a.ws = (float*)workspace;
     cudaStream_t s = (cudaStream_t)stream;
-    const bool tc_ok = gs::tc_available(dev) && gs::xattn_tc_supported(a);
+    const bool tc_ok = gs::xattn_tc_supported(a);
     if (p->flags == GS_PATH_TENSOR && !tc_ok)
         return a.dtype != GS_BF16 || a.G > 128 ? GS_ERR_UNSUPPORTED : GS_ERR_ALIGNMENT;
     if (tc_ok && p->flags != GS_PATH_SIMT && a.Lk > 0) {
@@ -994,7 +1002,7 @@ gs_status gs_cross_attention_backward(const gs_attn* p, const gs_heads* Q, const
     a.lse = const_cast<float*>(lse);
     a.ws = (float*)workspace;
     cudaStream_t s = (cudaStream_t)stream;
-    const bool tc_ok = gs::tc_available(dev) && gs::xattn_bwd_tc_supported(a);
+    const bool tc_ok = gs::xattn_bwd_tc_supported(a);
     if (p->flags == GS_PATH_TENSOR && !tc_ok)
         return a.dtype != GS_BF16 || a.G > 128 ? GS_ERR_UNSUPPORTED : GS_ERR_ALIGNMENT;
     if (tc_ok && p->flags != GS_PATH_SIMT && a.Lq > 0 && a.Lk > 0) {
@@ -1021,7 +1029,7 @@ gs_status gs_sample_scores(const void* S, int s_dtype, long long N, int M, long 
     a.S = S; a.bf16 = s_dtype == GS_BF16; a.N = N; a.M = M; a.lds = lds;
     a.how = *how;
     a.U = U; a.index = index; a.prob = prob;
-    return from_cuda(gs::launch_sample(a, dev, (cudaStream_t)stream));
+    return from_cuda(gs::launch_sample(a, sms, dev, (cudaStream_t)stream));
 }
 
 gs_status gs_selftest_wait_timeout(void* stream) {

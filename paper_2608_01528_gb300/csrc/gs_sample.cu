@@ -902,7 +902,7 @@ bool g_attr[64];
 
 }  // namespace
 
-cudaError_t launch_sample(const SampleArgs& a, int device, cudaStream_t s) {
+cudaError_t launch_sample(const SampleArgs& a, int sms, int device, cudaStream_t s) {
     if (device < 0 || device >= 64) return cudaErrorInvalidDevice;
     constexpr long long kRows = 1 << 27;  // rows of a launch
     if (!g_attr[device]) {
@@ -942,8 +942,6 @@ cudaError_t launch_sample(const SampleArgs& a, int device, cudaStream_t s) {
     }
     // CTAs a row: up to 2^18 scores each (the histogram's counters), and where rows are few more, of 4,096 scores or
     // more: a cluster's waits for one another cost about 10 us a row, hidden only by other rows' work
-    int sms = 0;
-    cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
     int G = 1;
     while (G < kMaxCluster && (a.M / G > 1 << 18 || (a.N * G < 4ll * sms && a.M / G >= 8192))) G <<= 1;
     cudaLaunchConfig_t cfg = {};

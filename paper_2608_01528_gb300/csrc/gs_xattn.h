@@ -26,6 +26,7 @@ struct XattnArgs {
     float* ws;     // workspace
     int splits;    // forward, dQ: parts of the key axis
     int rsplits;   // dK / dV: parts of the packed rows
+    int vec;       // CUDA-core kernels: which arrays allow loads of four elements
     long long stats;  // backward: floats of the rows' statistics at the start of the workspace
 };
 
@@ -93,6 +94,6 @@ struct SampleArgs {
     int* index;
     float* prob;
 };
-cudaError_t launch_sample(const SampleArgs& a, int device, cudaStream_t s);
+cudaError_t launch_sample(const SampleArgs& a, int sms, int device, cudaStream_t s);
 
 }  // namespace gs

@@ -28,6 +28,9 @@ constexpr int kThreads = 256;  // 16 x 16, a 4 x 4 piece of the tile each
 constexpr int kPP = kTile + 4; // pitch of a tile of weights
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+// bits of XattnArgs::vec: the array's rows start on boundaries of four elements
+constexpr int kVecQ = 1, kVecK = 2, kVecV = 4, kVecDO = 8;
+
 template <typename T>
 __device__ __forceinline__ float to_f32(T v);
 template <>
@@ -67,24 +70,41 @@ __device__ __forceinline__ long long row_index(const XattnArgs& a, int b, int hk
     return ((long long)b * a.Hq + hk * a.G + g) * a.Lq + l;
 }
 
-// 64 packed rows from r0, D floats each (zero past the width w and past the last row).
+// Four elements from p (zeros from the w-th on), as one load where the array allows it (vec) and all are there.
+__device__ __forceinline__ float4 load4(const float* p, int left, bool vec) {
+    if (vec && left >= 4) return __ldg(reinterpret_cast<const float4*>(p));
+    return make_float4(left > 0 ? p[0] : 0.f, left > 1 ? p[1] : 0.f, left > 2 ? p[2] : 0.f, left > 3 ? p[3] : 0.f);
+}
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p, int left, bool vec) {
+    if (vec && left >= 4) {
+        const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
+        return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16),
+                           __uint_as_float(v.y & 0xffff0000u));
+    }
+    return make_float4(left > 0 ? to_f32(p[0]) : 0.f, left > 1 ? to_f32(p[1]) : 0.f, left > 2 ? to_f32(p[2]) : 0.f,
+                       left > 3 ? to_f32(p[3]) : 0.f);
+}
+// 64 packed rows from r0, D floats each (zero past the width w and past the last row): four threads a row, so that a row's
+// address is worked out once.
 template <typename T, int D>
 __device__ __forceinline__ void load_rows(float* dst, const XattnArgs& a, const HeadView& v, int b, int hk,
-                                          long long r0, int w) {
-    for (int e = threadIdx.x; e < kTile * D; e += kThreads) {
-        const int i = e / D, c = e % D;
-        const long long r = r0 + i;
-        dst[i * (D + 4) + c] = r < a.rows && c < w ? to_f32(row_at<T>(a, v, b, hk, r)[c]) : 0.f;
-    }
+                                          long long r0, int w, bool vec) {
+    const int i = threadIdx.x >> 2, c0 = (threadIdx.x & 3) * 4;
+    const bool has = r0 + i < a.rows;
+    const T* p = row_at<T>(a, v, b, hk, has ? r0 + i : 0);
+#pragma unroll
+    for (int c = 0; c < D; c += 16)
+        *reinterpret_cast<float4*>(dst + i * (D + 4) + c + c0) = load4(p + c + c0, has ? w - c - c0 : 0, vec);
 }
 // 64 keys from j0 (zero where ok[] says that a key is not read).
 template <typename T, int D>
-__device__ __forceinline__ void load_keys(float* dst, const HeadView& v, int b, int hk, int j0, int w, const int* ok) {
-    const T* p = reinterpret_cast<const T*>(v.p) + b * v.b + hk * v.h;
-    for (int e = threadIdx.x; e < kTile * D; e += kThreads) {
-        const int i = e / D, c = e % D;
-        dst[i * (D + 4) + c] = ok[i] && c < w ? to_f32(p[(long long)(j0 + i) * v.l + c]) : 0.f;
-    }
+__device__ __forceinline__ void load_keys(float* dst, const HeadView& v, int b, int hk, int j0, int w, const int* ok, bool vec) {
+    const int i = threadIdx.x >> 2, c0 = (threadIdx.x & 3) * 4;
+    const bool has = ok[i] != 0;
+    const T* p = reinterpret_cast<const T*>(v.p) + b * v.b + hk * v.h + (has ? (long long)(j0 + i) * v.l : 0);
+#pragma unroll
+    for (int c = 0; c < D; c += 16)
+        *reinterpret_cast<float4*>(dst + i * (D + 4) + c + c0) = load4(p + c + c0, has ? w - c - c0 : 0, vec);
 }
 __device__ __forceinline__ void load_valid(int* ok, const XattnArgs& a, int b, int j0, int n) {
     if (threadIdx.x < kTile) {
@@ -95,10 +115,10 @@ __device__ __forceinline__ void load_valid(int* ok, const XattnArgs& a, int b, i
 
 // acc[i][j] += <A row ty + 16 i, B row tx + 16 j>
 template <int D>
-__device__ __forceinline__ void dots(float (&acc)[4][4], const float* A, const float* B) {
+__device__ __forceinline__ void dots(float (&acc)[4][4], const float* A, const float* B, int w) {
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
 #pragma unroll 4
-    for (int d = 0; d < D; d += 4) {
+    for (int d = 0; d < w; d += 4) {
         float4 x[4], y[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const float4*>(A + (ty + 16 * i) * (D + 4) + d);
@@ -183,7 +203,7 @@ __global__ void __launch_bounds__(kThreads) k_xattn(const XattnArgs a, long long
     const int ktiles = (a.Lk + kTile - 1) / kTile;
     const int t0 = (int)((long long)ktiles * bl.part / a.splits), t1 = (int)((long long)ktiles * (bl.part + 1) / a.splits);
     const float c = a.scale * kLog2e;
-    load_rows<T, DK>(Qs, a, a.q, bl.b, bl.hk, r0, a.dk);
+    load_rows<T, DK>(Qs, a, a.q, bl.b, bl.hk, r0, a.dk, a.vec & kVecQ);
     float m[4], l[4], o[4][DV / 16];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -196,11 +216,11 @@ __global__ void __launch_bounds__(kThreads) k_xattn(const XattnArgs a, long long
         __syncthreads();  // the last tile's weights and values have been read
         load_valid(ok, a, bl.b, t * kTile, n);
         __syncthreads();
-        load_keys<T, DK>(Ks, a.k, bl.b, bl.hk, t * kTile, a.dk, ok);
-        load_keys<T, DV>(Vs, a.v, bl.b, bl.hk, t * kTile, a.dv, ok);
+        load_keys<T, DK>(Ks, a.k, bl.b, bl.hk, t * kTile, a.dk, ok, a.vec & kVecK);
+        load_keys<T, DV>(Vs, a.v, bl.b, bl.hk, t * kTile, a.dv, ok, a.vec & kVecV);
         __syncthreads();
         float s[4][4] = {};
-        dots<DK>(s, Qs, Ks);
+        dots<DK>(s, Qs, Ks, a.dk);
         __syncthreads();  // K has been read: the weights go over it
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -364,20 +384,20 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long l
     const int n = keys_of(a, bl.b);
     const int ktiles = (a.Lk + kTile - 1) / kTile;
     const int t0 = (int)((long long)ktiles * bl.part / a.splits), t1 = (int)((long long)ktiles * (bl.part + 1) / a.splits);
-    load_rows<T, DK>(Qs, a, a.q, bl.b, bl.hk, r0, a.dk);
-    load_rows<T, DV>(Ds, a, a.dO, bl.b, bl.hk, r0, a.dv);
+    load_rows<T, DK>(Qs, a, a.q, bl.b, bl.hk, r0, a.dk, a.vec & kVecQ);
+    load_rows<T, DV>(Ds, a, a.dO, bl.b, bl.hk, r0, a.dv, a.vec & kVecDO);
     load_stats(lse2, delta, a, bl.b, bl.hk, r0);
     float o[4][DK / 16] = {};
     for (int t = t0; t < t1 && t * kTile < n; ++t) {
         __syncthreads();
         load_valid(ok, a, bl.b, t * kTile, n);
         __syncthreads();
-        load_keys<T, DK>(Ks, a.k, bl.b, bl.hk, t * kTile, a.dk, ok);
-        load_keys<T, DV>(Vs, a.v, bl.b, bl.hk, t * kTile, a.dv, ok);
+        load_keys<T, DK>(Ks, a.k, bl.b, bl.hk, t * kTile, a.dk, ok, a.vec & kVecK);
+        load_keys<T, DV>(Vs, a.v, bl.b, bl.hk, t * kTile, a.dv, ok, a.vec & kVecV);
         __syncthreads();
         float s[4][4] = {}, dp[4][4] = {};
-        dots<DK>(s, Qs, Ks);
-        dots<DV>(dp, Ds, Vs);
+        dots<DK>(s, Qs, Ks, a.dk);
+        dots<DV>(dp, Ds, Vs, a.dv);
         if (a.splits == 1 && n <= kTile) {
             // every key of the sequence is here: D = sum_j P dP, for this kernel and the next (a bf16 O gives it to 2^-9 of
             // <dO, O> only, which with a few keys is more than dP - D)
@@ -441,18 +461,18 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dkv(const XattnArgs a, int k
     if (j0 >= n) t1 = t0;  // no key of the tile is read
     load_valid(ok, a, bl.b, j0, n);
     __syncthreads();
-    load_keys<T, DK>(Ks, a.k, bl.b, bl.hk, j0, a.dk, ok);
-    load_keys<T, DV>(Vs, a.v, bl.b, bl.hk, j0, a.dv, ok);
+    load_keys<T, DK>(Ks, a.k, bl.b, bl.hk, j0, a.dk, ok, a.vec & kVecK);
+    load_keys<T, DV>(Vs, a.v, bl.b, bl.hk, j0, a.dv, ok, a.vec & kVecV);
     float ok_[4][DK / 16] = {}, ov[4][DV / 16] = {};
     for (long long t = t0; t < t1; ++t) {
         __syncthreads();
-        load_rows<T, DK>(Qs, a, a.q, bl.b, bl.hk, t * kTile, a.dk);
-        load_rows<T, DV>(Ds, a, a.dO, bl.b, bl.hk, t * kTile, a.dv);
+        load_rows<T, DK>(Qs, a, a.q, bl.b, bl.hk, t * kTile, a.dk, a.vec & kVecQ);
+        load_rows<T, DV>(Ds, a, a.dO, bl.b, bl.hk, t * kTile, a.dv, a.vec & kVecDO);
         load_stats(lse2, delta, a, bl.b, bl.hk, t * kTile);
         __syncthreads();
         float s[4][4] = {}, dp[4][4] = {};
-        dots<DK>(s, Qs, Ks);
-        dots<DV>(dp, Ds, Vs);
+        dots<DK>(s, Qs, Ks, a.dk);
+        dots<DV>(dp, Ds, Vs, a.dv);
         tile_grad(s, dp, ok, lse2, delta, a.scale * kLog2e);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -546,13 +566,22 @@ cudaError_t backward(const XattnArgs& a, cudaStream_t s) {
     return e;
 }
 
+bool on_fours(const XattnArgs& a, const HeadView& v, int L, int H) {
+    const int bytes = a.dtype == GS_F32 ? 16 : 8;
+    return (uintptr_t)v.p % bytes == 0 && (a.B <= 1 || v.b % 4 == 0) && (L <= 1 || v.l % 4 == 0) && (H <= 1 || v.h % 4 == 0);
+}
+
 template <typename T>
-cudaError_t forward_t(const XattnArgs& a, cudaStream_t s) {
+cudaError_t forward_t(XattnArgs a, cudaStream_t s) {
+    a.vec = (on_fours(a, a.q, a.Lq, a.Hq) ? kVecQ : 0) | (on_fours(a, a.k, a.Lk, a.Hkv) ? kVecK : 0) |
+            (on_fours(a, a.v, a.Lk, a.Hkv) ? kVecV : 0);
     if (a.dk <= 64) return a.dv <= 64 ? forward<T, 64, 64>(a, s) : forward<T, 64, 128>(a, s);
     return a.dv <= 64 ? forward<T, 128, 64>(a, s) : forward<T, 128, 128>(a, s);
 }
 template <typename T>
-cudaError_t backward_t(const XattnArgs& a, cudaStream_t s) {
+cudaError_t backward_t(XattnArgs a, cudaStream_t s) {
+    a.vec = (on_fours(a, a.q, a.Lq, a.Hq) ? kVecQ : 0) | (on_fours(a, a.k, a.Lk, a.Hkv) ? kVecK : 0) |
+            (on_fours(a, a.v, a.Lk, a.Hkv) ? kVecV : 0) | (on_fours(a, a.dO, a.Lq, a.Hq) ? kVecDO : 0);
     if (a.dk <= 64) return a.dv <= 64 ? backward<T, 64, 64>(a, s) : backward<T, 64, 128>(a, s);
     return a.dv <= 64 ? backward<T, 128, 64>(a, s) : backward<T, 128, 128>(a, s);
 }

@@ -482,43 +482,44 @@ def attention_scores(Yq, Yk, scale, apply_softmax=True, path="auto", out=None, s
     return A
 
 
-def _launch_stream(stream, device):
-    """The context in which a call that runs on `stream` allocates: memory from torch's allocator belongs to the
-    stream that is current when it is taken, so outputs and workspaces are taken under the launch stream."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+def _on_stream(device, stream):
+    """The context of a call that runs on `stream`, or nothing to do.  The call's device is current in it, and so is its
+    stream: memory from torch's allocator belongs to the stream that is current when it is taken, so outputs and
+    workspaces are taken under the stream that writes them."""
+    return _on(device) if stream is None else torch.cuda.stream(stream)
 
 
-def _heads(t, name, L, H, w, like):
+def _heads(t, name, shape, like):
     """gs_heads of a B x L x H x w tensor with a dense last axis."""
-    if t.dim() != 4 or tuple(t.shape) != (like.shape[0], L, H, w):
-        raise ValueError(f"{name} must be {like.shape[0]} x {L} x {H} x {w}, got {tuple(t.shape)}")
-    if t.dtype != like.dtype or t.device != like.device:
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {' x '.join(map(str, shape))}, got {tuple(t.shape)}")
+    if t.dtype is not like.dtype or t.device != like.device:
         raise TypeError(f"{name} must be {like.dtype} on {like.device}, got {t.dtype} on {t.device}")
     s = t.stride()
-    if w > 1 and s[3] != 1:
+    if s[3] != 1 and shape[3] > 1:
         raise ValueError(f"{name} must have unit stride along its last axis")
     return _Heads(t.data_ptr(), s[0], s[1], s[2])
 
 
 def _attn(Q, K, V, scale, key_lens, key_mask, path):
     """gs_attn and the gs_heads of the inputs, after the checks that need no device."""
-    for name, t in (("Q", Q), ("K", K), ("V", V)):
-        if t.dim() != 4:
-            raise ValueError(f"{name} must be 4-D (batch, length, heads, width), got {tuple(t.shape)}")
+    if Q.dim() != 4 or K.dim() != 4 or V.dim() != 4:
+        raise ValueError("Q, K and V must be 4-D (batch, length, heads, width)")
     code = _dtype_code(Q)
     B, Lq, Hq, dk = Q.shape
-    Lk, Hkv, dv = K.shape[1], K.shape[2], V.shape[3]
-    hs = [_heads(Q, "Q", Lq, Hq, dk, Q), _heads(K, "K", Lk, Hkv, dk, Q), _heads(V, "V", Lk, Hkv, dv, Q)]
-    a = _Attn(code, B, Lq, Lk, Hq, Hkv, dk, dv, dk ** -0.5 if scale is None and dk else scale or 0.0, None, None, 0,
-              PATHS[path])
+    _, Lk, Hkv, dv = V.shape
+    hs = (_heads(Q, "Q", Q.shape, Q), _heads(K, "K", (B, Lk, Hkv, dk), Q), _heads(V, "V", (B, Lk, Hkv, dv), Q))
+    if scale is None:
+        scale = dk ** -0.5 if dk else 1.0
+    a = _Attn(code, B, Lq, Lk, Hq, Hkv, dk, dv, scale, None, None, 0, PATHS[path])
     if key_lens is not None:
-        if key_lens.dtype != torch.int32 or tuple(key_lens.shape) != (B,) or not key_lens.is_contiguous():
+        if key_lens.dtype is not torch.int32 or key_lens.shape != (B,) or not key_lens.is_contiguous():
             raise ValueError(f"key_lens must be a contiguous int32 vector of {B} lengths")
         if key_lens.device != Q.device:
             raise TypeError(f"key_lens must be on {Q.device}")
         a.key_lens = key_lens.data_ptr()
     if key_mask is not None:
-        if key_mask.dtype not in (torch.bool, torch.uint8) or tuple(key_mask.shape) != (B, Lk) \
+        if key_mask.dtype not in (torch.bool, torch.uint8) or key_mask.shape != (B, Lk) \
                 or (Lk > 1 and key_mask.stride(1) != 1):
             raise ValueError(f"key_mask must be a {B} x {Lk} bool (or uint8) tensor with unit column stride")
         if key_mask.device != Q.device:
@@ -531,15 +532,19 @@ def _attn(Q, K, V, scale, key_lens, key_mask, path):
 
 
 def _attn_workspace(L, a, backward, device):
+    """(tensor to keep until the call has been made, its address, its bytes)"""
     n = ctypes.c_longlong()
-    _check(L.gs_cross_attention_workspace(ctypes.byref(a), int(backward), ctypes.byref(n)), "gs_cross_attention_workspace")
-    return torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
+    _check(L.gs_cross_attention_workspace(ctypes.byref(a), backward, ctypes.byref(n)), "gs_cross_attention_workspace")
+    if n.value == 0:
+        return None, None, 0
+    ws = torch.empty(n.value, dtype=torch.uint8, device=device)
+    return ws, ws.data_ptr(), n.value
 
 
-def _attn_lse(lse, B, Hq, Lq, device):
-    if lse.dtype != torch.float32 or tuple(lse.shape) != (B, Hq, Lq) or not lse.is_contiguous() or lse.device != device:
-        raise ValueError(f"lse must be a contiguous float32 {B} x {Hq} x {Lq} tensor on {device}")
-    return lse
+def _attn_lse(lse, shape, device):
+    if lse.dtype is not torch.float32 or lse.shape != shape or not lse.is_contiguous() or lse.device != device:
+        raise ValueError(f"lse must be a contiguous float32 {' x '.join(map(str, shape))} tensor on {device}")
+    return lse.data_ptr()
 
 
 def cross_attention(Q, K, V, scale=None, key_lens=None, key_mask=None, want_lse=False, path="auto", out=None,
@@ -552,18 +557,17 @@ def cross_attention(Q, K, V, scale=None, key_lens=None, key_mask=None, want_lse=
     bool B x Lk, False = not read.  Returns {"O": B x Lq x Hq x dv, "lse": B x Hq x Lq float32 with want_lse};
     `out` may supply them."""
     a, hs = _attn(Q, K, V, scale, key_lens, key_mask, path)
-    L = load_library()
-    out = dict(out or {})
-    with _on(Q.device), _launch_stream(stream, Q.device):
+    L, dev, ref = load_library(), Q.device, ctypes.byref
+    out = dict(out) if out else {}
+    with _on_stream(dev, stream):
         if "O" not in out:
-            out["O"] = torch.empty((a.B, a.Lq, a.Hq, a.dv), dtype=Q.dtype, device=Q.device)
+            out["O"] = torch.empty((a.B, a.Lq, a.Hq, a.dv), dtype=Q.dtype, device=dev)
         if want_lse and "lse" not in out:
-            out["lse"] = torch.empty((a.B, a.Hq, a.Lq), dtype=torch.float32, device=Q.device)
-        o = _heads(out["O"], "O", a.Lq, a.Hq, a.dv, Q)
-        lse = _ptr(_attn_lse(out["lse"], a.B, a.Hq, a.Lq, Q.device)) if out.get("lse") is not None else None
-        ws = _attn_workspace(L, a, False, Q.device)
-        st = L.gs_cross_attention(ctypes.byref(a), *map(ctypes.byref, hs), ctypes.byref(o), lse, _ptr(ws),
-                                  ws.numel() if ws is not None else 0, _stream(stream, Q.device))
+            out["lse"] = torch.empty((a.B, a.Hq, a.Lq), dtype=torch.float32, device=dev)
+        o = _heads(out["O"], "O", (a.B, a.Lq, a.Hq, a.dv), Q)
+        lse = _attn_lse(out["lse"], (a.B, a.Hq, a.Lq), dev) if out.get("lse") is not None else None
+        keep, ws, size = _attn_workspace(L, a, 0, dev)
+        st = L.gs_cross_attention(ref(a), ref(hs[0]), ref(hs[1]), ref(hs[2]), ref(o), lse, ws, size, _stream(stream, dev))
     _check(st, "gs_cross_attention")
     return out
 
@@ -574,20 +578,19 @@ def cross_attention_backward(Q, K, V, O, lse, dO, scale=None, key_lens=None, key
     call's (want_lse=True), dO the gradient of O; the other arguments as there.  Returns {"dQ", "dK", "dV"} with
     the shapes and type of Q, K and V; `out` may supply them."""
     a, hs = _attn(Q, K, V, scale, key_lens, key_mask, path)
-    L = load_library()
-    out = dict(out or {})
-    o, do = _heads(O, "O", a.Lq, a.Hq, a.dv, Q), _heads(dO, "dO", a.Lq, a.Hq, a.dv, Q)
-    _attn_lse(lse, a.B, a.Hq, a.Lq, Q.device)
-    with _on(Q.device), _launch_stream(stream, Q.device):
+    L, dev, ref = load_library(), Q.device, ctypes.byref
+    out = dict(out) if out else {}
+    shape = (a.B, a.Lq, a.Hq, a.dv)
+    o, do = _heads(O, "O", shape, Q), _heads(dO, "dO", shape, Q)
+    lse = _attn_lse(lse, (a.B, a.Hq, a.Lq), dev)
+    with _on_stream(dev, stream):
         for name, t in (("dQ", Q), ("dK", K), ("dV", V)):
             if name not in out:
-                out[name] = torch.empty(t.shape, dtype=t.dtype, device=t.device)
-        gh = [_heads(out["dQ"], "dQ", a.Lq, a.Hq, a.dk, Q), _heads(out["dK"], "dK", a.Lk, a.Hkv, a.dk, Q),
-              _heads(out["dV"], "dV", a.Lk, a.Hkv, a.dv, Q)]
-        ws = _attn_workspace(L, a, True, Q.device)
-        st = L.gs_cross_attention_backward(ctypes.byref(a), *map(ctypes.byref, hs), ctypes.byref(o), _ptr(lse),
-                                           ctypes.byref(do), *map(ctypes.byref, gh), _ptr(ws),
-                                           ws.numel() if ws is not None else 0, _stream(stream, Q.device))
+                out[name] = torch.empty(t.shape, dtype=t.dtype, device=dev)
+        gq, gk, gv = _heads(out["dQ"], "dQ", Q.shape, Q), _heads(out["dK"], "dK", K.shape, Q), _heads(out["dV"], "dV", V.shape, Q)
+        keep, ws, size = _attn_workspace(L, a, 1, dev)
+        st = L.gs_cross_attention_backward(ref(a), ref(hs[0]), ref(hs[1]), ref(hs[2]), ref(o), lse, ref(do), ref(gq), ref(gk),
+                                           ref(gv), ws, size, _stream(stream, dev))
     _check(st, "gs_cross_attention_backward")
     return out
 
@@ -599,35 +602,38 @@ def sample_scores(S, U, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, want_pro
     {"index": N int32, "prob": N float32}."""
     ld = _ld(S)
     N, M = S.shape
+    dev = S.device
     code = _dtype_code(S)
+
+    def vector(t, name, dt):
+        if t.dtype is not dt or t.shape != (N,) or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dt} vector of N = {N} entries")
+        if t.device != dev:
+            raise TypeError(f"{name} must be on {dev}")
+        return t.data_ptr()
+
     how = _Sampling()
-    rows = (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
-            ("min_p", min_p, torch.float32))
-    for name, v, dt in rows + (("U", U, torch.float32),):
-        if isinstance(v, torch.Tensor) or name == "U":
-            if v.dtype != dt or tuple(v.shape) != (N,) or not v.is_contiguous():
-                raise ValueError(f"{name} must be a contiguous {dt} vector of N = {N} entries")
-            if v.device != S.device:
-                raise TypeError(f"{name} must be on {S.device}")
-            if name != "U":
-                setattr(how, name + "_rows", v.data_ptr())
+    for name, v, dt in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                        ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+        if isinstance(v, torch.Tensor):
+            setattr(how, name + "_rows", vector(v, name, dt))
         else:
-            setattr(how, name, int(v) if dt == torch.int32 else float(v))
-    out = dict(out or {})
+            setattr(how, name, int(v) if name == "top_k" else float(v))
+    u = vector(U, "U", torch.float32)
+    out = dict(out) if out else {}
     for name, dt in (("index", torch.int32), ("prob", torch.float32)):
-        t = out.get(name)
-        if t is not None and (t.dtype != dt or tuple(t.shape) != (N,) or not t.is_contiguous() or t.device != S.device):
-            raise ValueError(f"out[{name!r}] must be a contiguous {dt} vector of N = {N} entries on {S.device}")
+        if out.get(name) is not None:
+            vector(out[name], f"out[{name!r}]", dt)
     if not S.is_cuda:
         raise TypeError("S must be a CUDA tensor")
     L = load_library()
-    with _on(S.device), _launch_stream(stream, S.device):
+    with _on_stream(dev, stream):
         if "index" not in out:
-            out["index"] = torch.empty(N, dtype=torch.int32, device=S.device)
+            out["index"] = torch.empty(N, dtype=torch.int32, device=dev)
         if want_prob and "prob" not in out:
-            out["prob"] = torch.empty(N, dtype=torch.float32, device=S.device)
-        st = L.gs_sample_scores(_ptr(S), code, N, M, ld if N > 1 else M, ctypes.byref(how), _ptr(U), _ptr(out.get("index")),
-                                _ptr(out.get("prob")), _stream(stream, S.device))
+            out["prob"] = torch.empty(N, dtype=torch.float32, device=dev)
+        st = L.gs_sample_scores(S.data_ptr(), code, N, M, ld if N > 1 else M, ctypes.byref(how), u, _ptr(out.get("index")),
+                                _ptr(out.get("prob")), _stream(stream, dev))
     _check(st, "gs_sample_scores")
     return out
 
