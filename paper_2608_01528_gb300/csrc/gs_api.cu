@@ -918,6 +918,25 @@ gs_status attn_device(int& dev, int& sms) {
     return sms < 0 ? GS_ERR_UNSUPPORTED : GS_OK;
 }
 
+// Which forward kernels take a call (us, 8 x 8,192 keys unless said otherwise).  Tensor cores against a few rows' CUDA cores:
+// one row of 64, 64 x 1,500 keys of 16 heads, 113 / 92; one row of 128 98 / 139; four rows 66 / 111.  Few rows against tiles of
+// 64 on CUDA cores, fp32: 4 rows of 128 133 / 615, 16 rows (16 x 2,048 keys of 4 heads) 129 / 174, 32 rows of 40 78 / 48.
+enum AttnPath { ATTN_ROWS, ATTN_SIMT, ATTN_TC };
+AttnPath attn_path(const gs::XattnArgs& a, unsigned flags, bool tc_ok) {
+    if (tc_ok && flags == GS_PATH_TENSOR) return ATTN_TC;
+    if (tc_ok && flags == GS_PATH_AUTO && (a.rows > 1 || a.dk > 64 || a.dv > 64)) return ATTN_TC;
+    return a.rows <= 16 ? ATTN_ROWS : ATTN_SIMT;
+}
+
+void attn_plan(gs::XattnArgs& a, AttnPath path, int sms) {
+    if (path == ATTN_TC)
+        gs::xattn_tc_plan(a, sms);
+    else if (path == ATTN_ROWS)
+        gs::xattn_rows_plan(a, sms);
+    else
+        gs::xattn_simt_plan(a, false, sms);
+}
+
 gs_status attn_workspace(const float* ws, long long bytes, long long floats) {
     if (floats == 0) return GS_OK;
     if (!ws) return GS_ERR_INVALID_ARG;
@@ -938,11 +957,15 @@ gs_status gs_cross_attention_workspace(const gs_attn* p, int backward, long long
     int dev = 0, sms = 0;
     if ((st = attn_device(dev, sms)) != GS_OK) return st;
     // the arrays' alignment, not known here, decides between the paths: room for either
-    gs::xattn_simt_plan(a, backward != 0, sms);
-    long long floats = backward ? gs::xattn_ws_backward(a) : gs::xattn_ws_forward(a);
-    if (a.dtype == GS_BF16 && a.G <= 128) {
-        backward ? gs::xattn_bwd_tc_plan(a, sms) : gs::xattn_tc_plan(a, sms);
-        floats = std::max(floats, backward ? gs::xattn_ws_backward(a) : gs::xattn_ws_forward(a));
+    long long floats = 0;
+    for (int tc = 0; tc < (a.dtype == GS_BF16 && a.G <= 128 && a.Lk > 0 ? 2 : 1); ++tc) {
+        if (backward) {
+            tc ? gs::xattn_bwd_tc_plan(a, sms) : gs::xattn_simt_plan(a, true, sms);
+            floats = std::max(floats, gs::xattn_ws_backward(a));
+        } else {
+            attn_plan(a, attn_path(a, p->flags, tc != 0), sms);
+            floats = std::max(floats, gs::xattn_ws_forward(a));
+        }
     }
     *bytes = 4 * floats;
     return GS_OK;
@@ -969,14 +992,12 @@ gs_status gs_cross_attention(const gs_attn* p, const gs_heads* Q, const gs_heads
     const bool tc_ok = gs::xattn_tc_supported(a);
     if (p->flags == GS_PATH_TENSOR && !tc_ok)
         return a.dtype != GS_BF16 || a.G > 128 ? GS_ERR_UNSUPPORTED : GS_ERR_ALIGNMENT;
-    if (tc_ok && p->flags != GS_PATH_SIMT && a.Lk > 0) {
-        gs::xattn_tc_plan(a, sms);
-        if ((st = attn_workspace(a.ws, workspace_bytes, gs::xattn_ws_forward(a))) != GS_OK) return st;
-        return from_cuda(gs::launch_xattn_tc(a, sms, dev, s));
-    }
-    gs::xattn_simt_plan(a, false, sms);
+    const AttnPath path = attn_path(a, p->flags, tc_ok && a.Lk > 0);
+    attn_plan(a, path, sms);
     if ((st = attn_workspace(a.ws, workspace_bytes, gs::xattn_ws_forward(a))) != GS_OK) return st;
-    return from_cuda(gs::launch_xattn_simt(a, s));
+    return from_cuda(path == ATTN_TC     ? gs::launch_xattn_tc(a, sms, dev, s)
+                     : path == ATTN_ROWS ? gs::launch_xattn_rows(a, s)
+                                         : gs::launch_xattn_simt(a, s));
 }
 
 gs_status gs_cross_attention_backward(const gs_attn* p, const gs_heads* Q, const gs_heads* K, const gs_heads* V,

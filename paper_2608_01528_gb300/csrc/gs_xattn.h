@@ -61,6 +61,10 @@ GS_XWS xattn_ws_backward(const XattnArgs& a) {
 }
 #undef GS_XWS
 
+// ----------------------------------------------------------------- few rows (gs_xattn_rows.cu)
+void xattn_rows_plan(XattnArgs& a, int sms);
+cudaError_t launch_xattn_rows(const XattnArgs& a, cudaStream_t s);
+
 // ----------------------------------------------------------------- CUDA cores (gs_xattn_simt.cu)
 // the parts (splits, rsplits) that the CUDA-core kernels take on `sms` multiprocessors
 void xattn_simt_plan(XattnArgs& a, bool backward, int sms);

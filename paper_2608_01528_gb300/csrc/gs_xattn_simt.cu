@@ -602,9 +602,9 @@ cudaError_t launch_delta(const XattnArgs& a, cudaStream_t s) {
 
 void xattn_simt_plan(XattnArgs& a, bool backward, int sms) {
     const long long rt = (a.rows + kTile - 1) / kTile, kt = (a.Lk + kTile - 1) / kTile;
-    // two blocks a multiprocessor where they fit, and parts of four tiles or more
-    a.splits = xattn_parts(rt * a.Hkv * a.B, kt, 2 * sms, 4);
-    a.rsplits = backward ? xattn_parts(kt * a.Hkv * a.B, rt, 2 * sms, 4) : 1;
+    // two blocks a multiprocessor where they fit, and parts of two tiles or more
+    a.splits = xattn_parts(rt * a.Hkv * a.B, kt, 2 * sms, 2);
+    a.rsplits = backward ? xattn_parts(kt * a.Hkv * a.B, rt, 2 * sms, 2) : 1;
     a.stats = xattn_round4(xattn_rows(a));  // D_i
 }
 

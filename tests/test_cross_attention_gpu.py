@@ -64,6 +64,10 @@ SHAPES = [
     (3, 33, 64, 2, 2, 10, 5),
     (1, 1, 3000, 8, 2, 128, 64),
     (2, 257, 127, 6, 3, 72, 8),
+    (1, 40, 2500, 2, 1, 64, 128),        # more rows than a few, keys in parts
+    (3, 9, 700, 3, 1, 33, 20),           # a few rows, in chunks of four
+    (2, 1, 9000, 1, 1, 24, 100),         # one row, keys in parts
+    (1, 1, 500, 4, 4, 128, 128),
 ]
 
 
