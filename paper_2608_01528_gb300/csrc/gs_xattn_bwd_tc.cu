@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     volatile int* abort_flag = &c.abort_flag;
     unsigned* err = &g_err_xbwd;
     const XattnArgs& a = p.a;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31;
 
     long long i = blockIdx.x;
     const int kt = (int)(i % p.ktiles);
@@ -219,7 +219,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int tile_rows = p.nl * a.G;
     const int n = keys_of(a, b), j0 = kt * kTile;
     const long long t0 = p.rtiles * part / a.rsplits, t1 = p.rtiles * (part + 1) / a.rsplits;
-    const int nt = j0 < n ? (int)(t1 - t0) : 0;  // row tiles
+    const int nt = uniform(j0 < n ? (int)(t1 - t0) : 0);  // row tiles
 
     if (threadIdx.x == 0) {
         mbar_init(&c.own_full, 1);
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = c.tmem_base;
+    const uint32_t tmem = uniform(c.tmem_base);
     const uint32_t t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 256 + DVC * kChunk;
 
     if (warp == kTmaWarp) {
@@ -292,41 +292,42 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int j = std::max(0, sb - ST); j < sb; ++j) mbar_drain(&c.b_full[j % ST], (uint32_t)(j / ST) & 1u, err);
         }
     } else if (warp == kMmaWarp) {
-        if (lane == 0 && nt > 0) {
+        if (nt > 0) {
+            const uint32_t el = elect_one();
             const uint32_t id_s = idesc_bf16_f32(kTile), id_v = idesc_bf16_bmn(DVC * kChunk), id_k = idesc_bf16_bmn(DKC * kChunk);
             const uint32_t ka = smem_u32(Ks), va = smem_u32(Vs), qa = smem_u32(Qr), oa = smem_u32(Or);
             RingPos cur, nxt;  // stages of this row tile and of the next
             auto scores = [&](const RingPos& r) {
-                if (!mbar_wait_1t(&c.a_full[r.idx], r.phase, abort_flag, err)) return false;
+                if (!mbar_wait_warp_inline(&c.a_full[r.idx], r.phase, abort_flag, err)) return false;
                 tc_fence_after();
-                mma_tile_ss<DKC>(t_s, ka, qa + (uint32_t)(r.idx * DKC * kChunkBytes), id_s);
-                mma_commit(&c.s_full);
+                mma_tile_ss<DKC>(t_s, ka, qa + (uint32_t)(r.idx * DKC * kChunkBytes), id_s, el);
+                commit_to(&c.s_full, el);
                 return true;
             };
             auto dprod = [&](const RingPos& r) {
-                if (!mbar_wait_1t(&c.b_full[r.idx], r.phase, abort_flag, err)) return false;
+                if (!mbar_wait_warp_inline(&c.b_full[r.idx], r.phase, abort_flag, err)) return false;
                 tc_fence_after();
-                mma_tile_ss<DVC>(t_dp, va, oa + (uint32_t)(r.idx * DVC * kChunkBytes), id_s);
-                mma_commit(&c.dp_full);
+                mma_tile_ss<DVC>(t_dp, va, oa + (uint32_t)(r.idx * DVC * kChunkBytes), id_s, el);
+                commit_to(&c.dp_full, el);
                 return true;
             };
-            bool ok = mbar_wait_1t(&c.own_full, 0, abort_flag, err) && scores(cur) && dprod(cur);
+            bool ok = mbar_wait_warp_inline(&c.own_full, 0, abort_flag, err) && scores(cur) && dprod(cur);
             for (int t = 0; t < nt && ok; ++t) {
                 nxt = cur;
                 nxt.next(ST);
-                if (!(ok = mbar_wait_1t(&c.p_full, (uint32_t)t & 1u, abort_flag, err))) break;
+                if (!(ok = mbar_wait_warp_inline(&c.p_full, (uint32_t)t & 1u, abort_flag, err))) break;
                 tc_fence_after();
-                mma_tile_ts<32>(t_dv, t_s, oa + (uint32_t)(cur.idx * DVC * kChunkBytes), id_v, t != 0);
-                mma_commit(&c.b_empty[cur.idx]);
+                mma_tile_ts<32>(t_dv, t_s, oa + (uint32_t)(cur.idx * DVC * kChunkBytes), id_v, t != 0, el);
+                commit_to(&c.b_empty[cur.idx], el);
                 if (t + 1 < nt && !(ok = scores(nxt))) break;
-                if (!(ok = mbar_wait_1t(&c.ds_full, (uint32_t)t & 1u, abort_flag, err))) break;
+                if (!(ok = mbar_wait_warp_inline(&c.ds_full, (uint32_t)t & 1u, abort_flag, err))) break;
                 tc_fence_after();
-                mma_tile_ts<32>(t_dk, t_dp, qa + (uint32_t)(cur.idx * DKC * kChunkBytes), id_k, t != 0);
-                mma_commit(&c.a_empty[cur.idx]);
+                mma_tile_ts<32>(t_dk, t_dp, qa + (uint32_t)(cur.idx * DKC * kChunkBytes), id_k, t != 0, el);
+                commit_to(&c.a_empty[cur.idx], el);
                 if (t + 1 < nt && !(ok = dprod(nxt))) break;
                 cur = nxt;
             }
-            mma_commit(&c.done);
+            commit_to(&c.done, el);
             mbar_drain(&c.done, 0, err);
         }
     } else if (warp < kSoftWarps) {
@@ -447,7 +448,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     volatile int* abort_flag = &c.abort_flag;
     unsigned* err = &g_err_xbwd;
     const XattnArgs& a = p.a;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31;
 
     long long i = blockIdx.x;
     const long long rt = i % p.rtiles;
@@ -459,7 +460,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int n = keys_of(a, b);
     const int t0 = (int)((long long)p.ktiles * part / a.splits);
     const int t1 = min((int)((long long)p.ktiles * (part + 1) / a.splits), (n + kTile - 1) / kTile);
-    const int nt = max(0, t1 - t0);  // key tiles
+    const int nt = uniform(max(0, t1 - t0));  // key tiles
     const bool fix = a.lens != nullptr || a.mask != nullptr;
 
     if (threadIdx.x == 0) {
@@ -488,7 +489,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = c.tmem_base;
+    const uint32_t tmem = uniform(c.tmem_base);
     const uint32_t t_q = tmem, t_do = t_q + 32 * DKC, t_dq = t_do + 32 * DVC;
     const uint32_t t_s = t_dq + 64 * DKC, t_dp = t_s + 128;  // dS over dP
 
@@ -528,39 +529,40 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (lane == 0) mbar_arrive(&c.a_ready[rp.idx]);
         }
     } else if (warp == kMmaWarp) {
-        if (lane == 0 && nt > 0) {
+        if (nt > 0) {
+            const uint32_t el = elect_one();
             const uint32_t id_s = idesc_bf16_f32(kTile), id_q = idesc_bf16_bmn(DKC * kChunk);
             const uint32_t ka = smem_u32(Kr), va = smem_u32(Vr);
             RingPos cur, ns, nd;  // stages of dQ's tile, of S's and of dP's
             auto scores = [&]() {
-                if (!mbar_wait_1t(fix ? &c.a_ready[ns.idx] : &c.a_full[ns.idx], ns.phase, abort_flag, err)) return false;
+                if (!mbar_wait_warp_inline(fix ? &c.a_ready[ns.idx] : &c.a_full[ns.idx], ns.phase, abort_flag, err)) return false;
                 tc_fence_after();
-                mma_rows_ts<DKC>(t_s, t_q, ka + (uint32_t)(ns.idx * DKC * kChunkBytes), id_s);
-                mma_commit(&c.s_full);
+                mma_rows_ts<DKC>(t_s, t_q, ka + (uint32_t)(ns.idx * DKC * kChunkBytes), id_s, el);
+                commit_to(&c.s_full, el);
                 ns.next(SK);
                 return true;
             };
             auto dprod = [&]() {
-                if (!mbar_wait_1t(&c.b_full[nd.idx], nd.phase, abort_flag, err)) return false;
+                if (!mbar_wait_warp_inline(&c.b_full[nd.idx], nd.phase, abort_flag, err)) return false;
                 tc_fence_after();
-                mma_rows_ts<DVC>(t_dp, t_do, va + (uint32_t)(nd.idx * DVC * kChunkBytes), id_s);
-                mma_commit(&c.dp_full);
-                mma_commit(&c.b_empty[nd.idx]);
+                mma_rows_ts<DVC>(t_dp, t_do, va + (uint32_t)(nd.idx * DVC * kChunkBytes), id_s, el);
+                commit_to(&c.dp_full, el);
+                commit_to(&c.b_empty[nd.idx], el);
                 nd.next(SV);
                 return true;
             };
-            bool ok = mbar_wait_1t(&c.own_full, 0, abort_flag, err) && scores() && dprod();
+            bool ok = mbar_wait_warp_inline(&c.own_full, 0, abort_flag, err) && scores() && dprod();
             for (int t = 0; t < nt && ok; ++t) {
                 const uint32_t ph = (uint32_t)t & 1u;
-                if (t + 1 < nt && !(ok = mbar_wait_1t(&c.s_free, ph, abort_flag, err) && scores())) break;
-                if (!(ok = mbar_wait_1t(&c.ds_full, ph, abort_flag, err))) break;
+                if (t + 1 < nt && !(ok = mbar_wait_warp_inline(&c.s_free, ph, abort_flag, err) && scores())) break;
+                if (!(ok = mbar_wait_warp_inline(&c.ds_full, ph, abort_flag, err))) break;
                 tc_fence_after();
-                mma_tile_ts<32>(t_dq, t_dp, ka + (uint32_t)(cur.idx * DKC * kChunkBytes), id_q, t != 0);
-                mma_commit(&c.a_empty[cur.idx]);
+                mma_tile_ts<32>(t_dq, t_dp, ka + (uint32_t)(cur.idx * DKC * kChunkBytes), id_q, t != 0, el);
+                commit_to(&c.a_empty[cur.idx], el);
                 cur.next(SK);
                 if (t + 1 < nt && !(ok = dprod())) break;
             }
-            mma_commit(&c.done);
+            commit_to(&c.done, el);
             mbar_drain(&c.done, 0, err);
         }
     } else {

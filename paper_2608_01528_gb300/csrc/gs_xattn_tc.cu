@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     volatile int* abort_flag = &c.abort_flag;
     unsigned* err = &g_err_xattn;
     const XattnArgs& a = p.a;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31;
     const int tile_rows = p.nl * a.G;
     const bool fix = a.lens != nullptr || a.mask != nullptr;
 
@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = c.tmem_base;
+    const uint32_t tmem = uniform(c.tmem_base);
 
     if (warp == kTmaWarp) {
         // ------------------------------------------------------------- Q, then K and V tiles
@@ -217,40 +217,43 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
     } else if (warp == kMmaWarp) {
         // ------------------------------------------------------------- MMA issue
-        if (lane == 0) {
+        {
+            const uint32_t el = elect_one();
             const uint32_t id_s = idesc_bf16_f32(kTile), id_o = idesc_bf16_bmn(DV);
             const uint32_t ringa = smem_u32(ring);
             RingPos rp, rq;
             uint32_t done0 = 0, done1 = 0;  // weights consumed of each group
             bool ok = true;
             for (long long it = blockIdx.x; it < p.items && ok; it += gridDim.x) {
-                const Item m = item_of<PAIR>(p, it);
+                Item m = item_of<PAIR>(p, it);
+                m.nt = uniform(m.nt);
+                m.nq = uniform(m.nq);
                 if (m.nt == 0) continue;
                 const uint32_t qa = smem_u32(Qs) + (uint32_t)(rq.idx * C::kQBytes);
                 auto arrived = [&]() {
-                    const bool in = mbar_wait_1t(fix ? &c.ready[rp.idx] : &c.full[rp.idx], rp.phase, abort_flag, err);
+                    const bool in = mbar_wait_warp_inline(fix ? &c.ready[rp.idx] : &c.full[rp.idx], rp.phase, abort_flag, err);
                     tc_fence_after();
                     return in;
                 };
                 auto stage = [&]() { return ringa + (uint32_t)(rp.idx * C::kStageBytes); };
                 auto scores = [&](int t) {
-                    mma_tile_ss<DKC>(tmem + (t ? 128u : 0u), qa + (uint32_t)((PAIR ? t : 0) * DKC * kChunkBytes), stage(), id_s);
-                    mma_commit(&c.s_full[t]);
+                    mma_tile_ss<DKC>(tmem + (t ? 128u : 0u), qa + (uint32_t)((PAIR ? t : 0) * DKC * kChunkBytes), stage(), id_s, el);
+                    commit_to(&c.s_full[t], el);
                 };
                 auto values = [&](int t, bool first, uint32_t v) {  // the weights of group t's next key tile
-                    if (!mbar_wait_1t(&c.p_full[t], (t ? done1 : done0) & 1u, abort_flag, err)) return false;
+                    if (!mbar_wait_warp_inline(&c.p_full[t], (t ? done1 : done0) & 1u, abort_flag, err)) return false;
                     (t ? done1 : done0) += 1;
                     tc_fence_after();
-                    mma_tile_ts<16>(tmem + 256u + (t ? (uint32_t)DV : 0u), tmem + (t ? 128u : 0u), v, id_o, !first);
-                    mma_commit(&c.o_done[t]);
+                    mma_tile_ts<16>(tmem + 256u + (t ? (uint32_t)DV : 0u), tmem + (t ? 128u : 0u), v, id_o, !first, el);
+                    commit_to(&c.o_done[t], el);
                     return true;
                 };
-                if (!(ok = mbar_wait_1t(&c.q_full[rq.idx], rq.phase, abort_flag, err))) break;
+                if (!(ok = mbar_wait_warp_inline(&c.q_full[rq.idx], rq.phase, abort_flag, err))) break;
                 if (PAIR) {
                     if (!(ok = arrived())) break;
                     for (int t = 0; t < m.nq; ++t) scores(t);
-                    mma_commit(&c.empty[rp.idx]);
-                    if (m.nt == 1) mma_commit(&c.q_empty[rq.idx]);
+                    commit_to(&c.empty[rp.idx], el);
+                    if (m.nt == 1) commit_to(&c.q_empty[rq.idx], el);
                     rp.next(ST);
                     for (int j = 0; j < m.nt && ok; ++j) {
                         if (!(ok = arrived())) break;
@@ -262,10 +265,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                             if (ok && j + 1 < m.nt && (t != 0 || (ok = arrived()))) scores(t);
                         }
                         if (!ok) break;
-                        mma_commit(&c.empty[vs]);
+                        commit_to(&c.empty[vs], el);
                         if (j + 1 < m.nt) {
-                            mma_commit(&c.empty[rp.idx]);
-                            if (j + 2 == m.nt) mma_commit(&c.q_empty[rq.idx]);
+                            commit_to(&c.empty[rp.idx], el);
+                            if (j + 2 == m.nt) commit_to(&c.q_empty[rq.idx], el);
                             rp.next(ST);
                         }
                     }
@@ -273,26 +276,26 @@ __global__ void __launch_bounds__(kThreads, 1)
                     for (int j = 0; j < 2 && j < m.nt && ok; ++j) {
                         if (!(ok = arrived())) break;
                         scores(j);
-                        mma_commit(&c.empty[rp.idx]);
-                        if (j + 1 == m.nt) mma_commit(&c.q_empty[rq.idx]);
+                        commit_to(&c.empty[rp.idx], el);
+                        if (j + 1 == m.nt) commit_to(&c.q_empty[rq.idx], el);
                         rp.next(ST);
                     }
                     for (int j = 0; j < m.nt && ok; ++j) {
                         if (!(ok = arrived()) || !(ok = values(j & 1, j < 2, stage()))) break;
-                        mma_commit(&c.empty[rp.idx]);
+                        commit_to(&c.empty[rp.idx], el);
                         rp.next(ST);
                         if (j + 2 < m.nt) {
                             if (!(ok = arrived())) break;
                             scores(j & 1);
-                            mma_commit(&c.empty[rp.idx]);
-                            if (j + 3 == m.nt) mma_commit(&c.q_empty[rq.idx]);
+                            commit_to(&c.empty[rp.idx], el);
+                            if (j + 3 == m.nt) commit_to(&c.q_empty[rq.idx], el);
                             rp.next(ST);
                         }
                     }
                 }
                 rq.next(QS);
             }
-            mma_commit(&c.mma_done);
+            commit_to(&c.mma_done, el);
             mbar_drain(&c.mma_done, 0, err);
         }
     } else {

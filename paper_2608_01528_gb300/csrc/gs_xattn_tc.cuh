@@ -40,35 +40,71 @@ static __device__ __forceinline__ uint64_t sdesc_mn(uint32_t saddr) {
 }
 __host__ __device__ constexpr uint32_t idesc_bf16_bmn(int n) { return idesc_bf16_f32(n) | (1u << 16); }
 
-// D[tmem] = A[smem] B[smem]^T over CHUNKS chunks of 64 columns, both K-major.  Unrolled, the descriptors advanced by
-// constants: one thread issues all MMAs, and a loop that built a descriptor per step took longer than the MMAs.
+// The MMA warps run converged: all lanes take the waits and the loops, one elected lane issues.  Descriptors and addresses are
+// then the same in all lanes and stay in uniform registers, where the tensor core takes them from; issued from a branch
+// of one lane, a product took 46 cycles at least (and 80 beside busy softmax warps), so 32 (128 x 64 x 16).
+static __device__ __forceinline__ uint32_t elect_one() {
+    uint32_t e;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+    return e;
+}
+// a value that all lanes share, known to be so
+template <typename T>
+static __device__ __forceinline__ T uniform(T v) {
+    return __shfl_sync(0xffffffffu, v, 0);
+}
+static __device__ __forceinline__ void issue_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t el) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %5, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(el)
+        : "memory");
+}
+static __device__ __forceinline__ void issue_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t el) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %5, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(el)
+        : "memory");
+}
+static __device__ __forceinline__ void commit_to(uint64_t* bar, uint32_t el) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %1, 0;\n\t"
+        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar)),
+        "r"(el)
+        : "memory");
+}
+// D[tmem] = A[smem] B[smem]^T over CHUNKS chunks of 64 columns, both K-major.
 template <int CHUNKS>
-static __device__ __forceinline__ void mma_tile_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
+static __device__ __forceinline__ void mma_tile_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t el) {
     const uint64_t ad = sdesc_sw128(a), bd = sdesc_sw128(b);
 #pragma unroll
     for (int k = 0; k < CHUNKS * 4; ++k) {
         const uint64_t off = (uint64_t)((k >> 2) * (kChunkBytes >> 4) + (k & 3) * 2);
-        mma_f16_ss(d, ad + off, bd + off, idesc, k != 0 ? 1u : 0u);
+        issue_ss(d, ad + off, bd + off, idesc, k != 0 ? 1u : 0u, el);
     }
 }
-// D[tmem] (+)= A[tmem: bf16 pairs] B over STEPS * 16 rows of B (MN-major): 32 rows of A's K axis (two steps of 8 columns)
-// every GAP columns
-template <int GAP, int STEPS = kTile / 16>
-static __device__ __forceinline__ void mma_tile_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate) {
+// D[tmem] (+)= A[tmem: bf16 pairs] B over 128 rows of B (MN-major): 32 rows of A's K axis (two steps of 8 columns) every GAP
+// columns
+template <int GAP>
+static __device__ __forceinline__ void mma_tile_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate,
+                                                   uint32_t el) {
     const uint64_t bd = sdesc_mn(b);
 #pragma unroll
-    for (int k = 0; k < STEPS; ++k)
-        mma_bf16_ts(d, a + (uint32_t)((k >> 1) * GAP + (k & 1) * 8), bd + (uint64_t)(k * 128), idesc,
-                    accumulate || k != 0 ? 1u : 0u);
+    for (int k = 0; k < kTile / 16; ++k)
+        issue_ts(d, a + (uint32_t)((k >> 1) * GAP + (k & 1) * 8), bd + (uint64_t)(k * 128), idesc,
+                 accumulate || k != 0 ? 1u : 0u, el);
 }
 // D[tmem] = A[tmem: bf16 pairs, CHUNKS * 32 columns] B[smem]^T, B K-major in chunks of 64 columns
 template <int CHUNKS>
-static __device__ __forceinline__ void mma_rows_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
+static __device__ __forceinline__ void mma_rows_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t el) {
     const uint64_t bd = sdesc_sw128(b);
 #pragma unroll
     for (int k = 0; k < CHUNKS * 4; ++k)
-        mma_bf16_ts(d, a + (uint32_t)(8 * k), bd + (uint64_t)((k >> 2) * (kChunkBytes >> 4) + (k & 3) * 2), idesc,
-                    k != 0 ? 1u : 0u);
+        issue_ts(d, a + (uint32_t)(8 * k), bd + (uint64_t)((k >> 2) * (kChunkBytes >> 4) + (k & 3) * 2), idesc,
+                 k != 0 ? 1u : 0u, el);
 }
 // 16 bf16 elements [c, c + 16) of a row of w (zeros past w, and where !has) as 8 words
 static __device__ __forceinline__ void load_words(uint32_t (&x)[8], const __nv_bfloat16* row, int c, int w, bool has) {
