@@ -15,7 +15,7 @@
 // top-p: 41 us sorted, see k_sample_warp for now).
 //
 // Longer rows (k_sample_wide): a cluster of up to 8 CTAs a row, re-reading the row from L2.  Pass 0: largest and
-// smallest score.  Pass 1: a histogram over 2,048 equal steps of log weight -- counts for top-k; for top-p fp32
+// smallest score.  Pass 1: a histogram over up to 2,048 equal steps of log weight -- counts for top-k; for top-p fp32
 // weights cut to some 16 bits, which bound the running weight to 2^-14 of it.  Pass 2: the few entries of the steps in which t
 // can lie (top-k: and all above) go to one CTA's list, which sorts them; the exact weight of what lies above is summed
 // per warp's stretch of the row, and that of the whole row.  The draw then only looks through the one stretch in which it
@@ -122,7 +122,7 @@ struct Weigher {
     // round(2^41 2^(ph + pl)): 2^(j/1024) from the table, 2^r - 1 of the rest |r| <= 2^-11 from its series in fp32; the
     // roundings of r, of the series and of its last product are 2^-36 each
     __device__ __forceinline__ u64 from_log2(float ph, float pl, const u64* pow) const {
-        if (!(ph > -43.f)) return 0ull;
+        ph = fmaxf(ph, -43.f);
         const float magic = 12582912.f;  // 1.5 * 2^23: adding it rounds to an integer
         const float t = fmaf(ph, 1024.f, magic);
         const int k = __float_as_int(t) - 0x4B400000;
@@ -480,42 +480,34 @@ __device__ __forceinline__ unsigned add_remote(uint32_t addr, unsigned v) {
     return r;
 }
 
-// The row in a warp's stretch [v0, v1) of vectors of V scores, f(index, score); `off`: scores between the 16-byte
-// boundary at or before the row's start and the start.
+// The row in a warp's stretch [v0, v1) of vectors of 16 bytes, f(index, score); `off`: scores between the 16-byte
+// boundary at or before the row's start and the start.  The next vector is on its way while one is worked on.
 template <typename F>
 __device__ __forceinline__ void for_scores(const void* row, bool bf16, int M, int off, int v0, int v1, F&& f) {
-    const int lane = threadIdx.x & 31;
-    if (bf16) {
-        const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(row) - off;
-        for (int v = v0 + lane; v < v1; v += 32) {
-            const int i = v * 8 - off;
-            if (i >= 0 && i + 8 <= M) {
-                const uint4 x = __ldg(reinterpret_cast<const uint4*>(p) + v);
-                const uint32_t q[4] = {x.x, x.y, x.z, x.w};
+    const int lane = threadIdx.x & 31, V = bf16 ? 8 : 4;
+    const char* p = static_cast<const char*>(row) - off * (16 / V);
+    auto inside = [&](int v) { return v * V - off >= 0 && v * V - off + V <= M; };
+    uint4 next = make_uint4(0, 0, 0, 0);
+    if (v0 + lane < v1 && inside(v0 + lane)) next = __ldg(reinterpret_cast<const uint4*>(p) + v0 + lane);
+    for (int v = v0 + lane; v < v1; v += 32) {
+        const uint4 x = next;
+        if (v + 32 < v1 && inside(v + 32)) next = __ldg(reinterpret_cast<const uint4*>(p) + v + 32);
+        const int i = v * V - off;
+        if (inside(v)) {
+            const uint32_t q[4] = {x.x, x.y, x.z, x.w};
+            if (bf16) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     f(i + 2 * e, __uint_as_float(q[e] << 16));
                     f(i + 2 * e + 1, __uint_as_float(q[e] & 0xffff0000u));
                 }
             } else {
-                for (int e = 0; e < 8; ++e)
-                    if (i + e >= 0 && i + e < M) f(i + e, __bfloat162float(p[v * 8 + e]));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f(i + e, __uint_as_float(q[e]));
             }
-        }
-    } else {
-        const float* p = static_cast<const float*>(row) - off;
-        for (int v = v0 + lane; v < v1; v += 32) {
-            const int i = v * 4 - off;
-            if (i >= 0 && i + 4 <= M) {
-                const float4 x = __ldg(reinterpret_cast<const float4*>(p) + v);
-                f(i, x.x);
-                f(i + 1, x.y);
-                f(i + 2, x.z);
-                f(i + 3, x.w);
-            } else {
-                for (int e = 0; e < 4; ++e)
-                    if (i + e >= 0 && i + e < M) f(i + e, p[v * 4 + e]);
-            }
+        } else {
+            for (int e = 0; e < V; ++e)
+                if (i + e >= 0 && i + e < M) f(i + e, load_score(row, bf16, i + e));
         }
     }
 }
@@ -705,7 +697,7 @@ __global__ void __launch_bounds__(kWideThreads, 2) k_sample_wide(const SampleArg
     Weigher w;
     w.set(top, st.T);
     const bool by_k = st.top_k >= 1 && st.top_k < M, by_p = st.top_p < 1.f;
-    if (w.only_top && (by_k || by_p)) {
+    if (w.only_top) {
         if (rank == 0) radix_row(a, n, row, st, w, m);
         return;
     }
@@ -713,24 +705,28 @@ __global__ void __launch_bounds__(kWideThreads, 2) k_sample_wide(const SampleArg
     u64 mine = 0;           // kept weight of this thread's scores
     if (!by_k && !by_p) {
         for_scores(row, a.bf16, M, off, v0, v1, [&](int, float x) {
-            const u64 v = w.weight(x, key_of(x), m.pow);
+            float pl;
+            const float ph = w.log2_hi(x, pl);
+            const u64 v = w.from_log2(ph, pl, m.pow);
             mine += v >= st.least ? v : 0ull;
         });
     } else {
-        // 2,048 equal steps of log2 weight from the largest score down to the smallest, or to where weights vanish
+        // steps of 2^-ks of log2 weight, from the largest score down to the smallest or to where weights vanish
         float pl;
         const float range = fminf(-w.log2_hi(lo, pl), 43.f);
-        const float scale = range > 0.f ? (kBins - 1) / range : 0.f, width = range / (kBins - 1);
-        auto step = [&](float ph) { return min((int)(-ph * scale), kBins - 1); };
-        auto octave = [&](int b) { return (int)((float)b * width); };
+        int ks = 5;
+        while (ks < 20 && range * (float)(2 << ks) < (float)(kBins - 8)) ++ks;
+        const float steps = (float)(1 << ks);
+        // rounded to the nearest step by adding 1.5 * 2^23 (what cannot be drawn falls into the last one)
+        auto step = [&](float ph) { return __float_as_int(fmaf(-fmaxf(ph, -range), steps, 12582912.f)) - 0x4B400000; };
         // bits of a histogram weight: a counter may have to hold all scores of this CTA
         const int hb = min(20, __clz(per * kWideWarps * V - 1) - 1);
         for_scores(row, a.bf16, M, off, v0, v1, [&](int, float x) {
-            if (!(x > -INFINITY)) return;
-            const float ph = w.log2_only(x);
+            const float ph = fmaxf(w.log2_only(x), -range);
             const int b = step(ph);
-            // the weight in units of 2^-hb of the step's octave: between 2^(hb - 1.03) and 2^hb
-            atomicAdd(&m.hist[b], by_k ? 1u : (uint32_t)ex2(ph + (float)(octave(b) + hb)));
+            // the weight in units of 2^-hb of the step's octave b >> ks: between 2^(hb - 1.03) and 2^(hb + 0.03)
+            const uint32_t v = by_k ? 1u : (uint32_t)__int_as_float(__float_as_int(ex2(ph)) + (((b >> ks) + hb) << 23));
+            atomicAdd(&m.hist[b], x > -INFINITY ? v : 0u);
         });
         __syncthreads();
         ptx::cluster_sync_all();
@@ -748,7 +744,7 @@ __global__ void __launch_bounds__(kWideThreads, 2) k_sample_wide(const SampleArg
         }
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
-            const int up = kOneBits - hb - octave(tid * kPer + e);
+            const int up = kOneBits - hb - ((tid * kPer + e) >> ks);
             part[e] = by_k ? wide[e] : up >= 0 ? wide[e] << up : wide[e] >> -up;
             sum += part[e];
         }
@@ -772,24 +768,27 @@ __global__ void __launch_bounds__(kWideThreads, 2) k_sample_wide(const SampleArg
         // pass 2: the list, the exact weight of what lies above it and of the whole row
         const uint32_t list0 = remote(m.list, 0), count0 = remote(&m.count, 0);
         u64 above = 0, total = 0;
-        for_scores(row, a.bf16, M, off, v0, v1, [&](int i, float x) {
+        auto send = [&](int i, float x) {
             if (!(x > -INFINITY)) return;
-            float pl;
-            const float ph = w.log2_hi(x, pl);
-            const int b = step(ph);
-            if (!by_k) {
+            const unsigned at = add_remote(count0, 1u);
+            if (at < (unsigned)kList) st_remote_u64(list0 + at * 8u, entry_of(key_of(x), i));
+        };
+        if (by_k) {
+            for_scores(row, a.bf16, M, off, v0, v1, [&](int i, float x) {
+                if (step(w.log2_only(x)) <= b1) send(i, x);
+            });
+        } else {
+            for_scores(row, a.bf16, M, off, v0, v1, [&](int i, float x) {
+                float pl;
+                const float ph = w.log2_hi(x, pl);
                 const u64 v = w.from_log2(ph, pl, m.pow);
+                const int b = step(ph);
                 total += v;
-                if (b < b0) {
-                    above += v;
-                    mine += v >= st.least ? v : 0ull;
-                }
-            }
-            if (b <= b1 && (by_k || b >= b0)) {
-                const unsigned at = add_remote(count0, 1u);
-                if (at < (unsigned)kList) st_remote_u64(list0 + at * 8u, entry_of(key_of(x), i));
-            }
-        });
+                above += b < b0 ? v : 0ull;
+                mine += b < b0 && v >= st.least ? v : 0ull;
+                if (b >= b0 && b <= b1) send(i, x);
+            });
+        }
         if (!by_k) {
             above = block_sum(above, m.sh);
             total = block_sum(total, m.sh);
@@ -940,10 +939,11 @@ cudaError_t launch_sample(const SampleArgs& a, int sms, int device, cudaStream_t
         }
         return cudaSuccess;
     }
-    // CTAs a row: up to 2^18 scores each (the histogram's counters), and where rows are few more, of 4,096 scores or
-    // more: a cluster's waits for one another cost about 10 us a row, hidden only by other rows' work
+    // CTAs a row: as many as all rows' CTAs run at once (two a multiprocessor), with 8,192 scores each or more; up to 2^18
+    // (the histogram's counters).  A cluster's waits for one another cost more than they give where rows alone fill the GPU:
+    // rows of 131,072, top-p: 64 in 1 / 2 / 4 / 8 CTAs 122 / 73 / 66 / 82 us, 256 in 1 / 2 / 4 207 / 213 / 221 us.
     int G = 1;
-    while (G < kMaxCluster && (a.M / G > 1 << 18 || (a.N * G < 4ll * sms && a.M / G >= 8192))) G <<= 1;
+    while (G < kMaxCluster && (a.M / G > 1 << 18 || (a.N * G * 2 <= 2ll * sms && a.M / G >= 16384))) G <<= 1;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;

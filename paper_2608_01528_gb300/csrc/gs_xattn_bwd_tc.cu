@@ -143,18 +143,18 @@ __device__ __forceinline__ void drain_acc(uint32_t taddr, int c0, int c1, int co
     }
 }
 
-// Statistics of every row tile of a key head: slots without a row get (-inf, 0).  16 threads a row, 8 columns each.
-// Bound by reading O and dO once.
+// Statistics of every row tile of a key head: slots without a row get (-inf, 0).  16 threads a row, 8 columns each, 32 slots
+// a block.  Bound by reading O and dO once.
 __global__ void __launch_bounds__(256) k_xattn_stats(const XattnArgs a, int nl, long long rtiles, int vec) {
-    long long i = blockIdx.x;
+    long long i = blockIdx.x >> 2;
+    float* dst = a.ws + i * kStats;
     const long long rt = i % rtiles;
     i /= rtiles;
     const int hk = (int)(i % a.Hkv), b = (int)(i / a.Hkv);
-    const int grp = threadIdx.x >> 4, ln = threadIdx.x & 15, c0 = ln * 8;
-    float* dst = a.ws + (long long)blockIdx.x * kStats;
-    float acc[8];
+    const int grp = (blockIdx.x & 3) * 32 + (threadIdx.x >> 4), ln = threadIdx.x & 15, c0 = ln * 8;
+    float acc[2];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < 2; ++k) {
         const int r = grp + 16 * k, l = r / a.G, h = hk * a.G + r - l * a.G;
         const long long ql = rt * nl + l;
         acc[k] = 0.f;
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(256) k_xattn_stats(const XattnArgs a, int nl, 
         }
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < 2; ++k) {
 #pragma unroll
         for (int o = 8; o; o >>= 1) acc[k] += __shfl_xor_sync(0xffffffffu, acc[k], o);
         const int r = grp + 16 * k, l = r / a.G, h = hk * a.G + r - l * a.G;
@@ -755,7 +755,7 @@ cudaError_t launch_xattn_bwd_tc(const XattnArgs& a, int device, cudaStream_t s) 
     p.vmul = v.bmul;
     p.vhmul = v.hmul;
     const int vec = on_vectors(a.o, a.B, a.Lq, a.Hq, a.dv) && on_vectors(a.dO, a.B, a.Lq, a.Hq, a.dv);
-    k_xattn_stats<<<(unsigned)(p.rtiles * a.Hkv * a.B), 256, 0, s>>>(a, p.nl, p.rtiles, vec);
+    k_xattn_stats<<<(unsigned)(4 * p.rtiles * a.Hkv * a.B), 256, 0, s>>>(a, p.nl, p.rtiles, vec);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     const bool k2 = a.dk > kChunk, v2 = a.dv > kChunk;
