@@ -9,15 +9,19 @@
 // kernel, needs fp32 atomics on 4 bytes per product of 128 x 128 x dk, and their order changes results.
 //
 // P and dS go from TMEM to registers and back as bf16, where they are the A operand (lanes are keys in the first kernel,
-// rows in the second, so neither needs a transpose); the B operands Q, dO, K are read as they lie (MN-major).
-// Sixteen softmax warps: warp w reads lanes 32 (w % 4)..+31 and columns 32 (w / 4)..+31.  While they work on S the tensor
-// core runs dP or the sums, and the other way round.  The rows' statistics (-lse log2 e, -D) are laid out
-// per row tile by k_xattn_stats, so that a tile's come with one copy.
+// rows in the second, so neither needs a transpose); the B operands Q, dO, K are read as they lie (MN-major).  The tile
+// that stays lies in TMEM as well (bf16 pairs, 32 columns a chunk of 64), which leaves shared memory to the ring of streamed
+// tiles: with two stages the kernels waited for loads of about 1 us each.
 //
-// Both kernels wait for their loads (about 1 us each under load) unless the ring is deep: the second keeps Q and dO in
-// TMEM (as bf16 pairs, 32 columns a chunk of 64), which leaves four stages of K; the first has no TMEM left at
-// width 128 (S, dP, dK and dV fill it).  Halves of 64 streamed rows, which would leave room, lose more: a
-// 128 x 64 x 16 product takes 46 cycles, a 128 x 128 x 16 one 64.5 (0.87 -> 1.24 ms at 4,096 x 4,096).
+// The streamed tile is taken in halves of 64: TMEM then holds everything (width 128: 64 + 64 columns of
+// operands, 256 of sums, 64 of S, 64 of dP), and two groups of eight softmax warps work in turn, group h on half h.
+// Where TMEM has room (in k_xattn_dq_tc; in the first at widths up to 64) each half has an S and a dP of its own.  Warp
+// w of a group reads lanes 32 (w % 4)..+31 and columns 32 (w / 4)..+31 of its half.  The rows'
+// statistics (-lse log2 e, -D) are laid out per row tile by k_xattn_stats, so that a tile's come with one copy.
+//
+// Measured at 2 sequences of 4,096 x 4,096, 32 / 8 heads of 128: dK and dV 0.71 ms, dQ 0.57 ms.  Each CTA reads 64 KB a tile,
+// 7 to 8 TB/s from L2 over all: that bounds both.  At width 64 (8 x 1,024 x 1,500, 16 heads: 114 and 106 us) the way of a
+// tile from S to dQ and a CTA's start and end do.
 //
 // Keys that are not read: P = dS = 0, and in the second kernel their rows of K are zeroed in shared memory before
 // the MMA reads them (0 * NaN).  Rows past the end have lse = +inf: P = 0.
@@ -35,19 +39,21 @@ using namespace xtc;
 
 __device__ unsigned g_err_xbwd = 0;
 
-constexpr int kSoftWarps = 16;
+constexpr int kSoftWarps = 16, kGroupWarps = 8;
 constexpr int kMmaWarp = 16, kTmaWarp = 17, kMaskWarp = 18;
 constexpr int kThreads = 19 * 32;
-constexpr int kCols = 32;        // of a softmax warp
+constexpr int kCols = 32;          // of a softmax warp
+constexpr int kHalf = kTile / 2;
+constexpr uint32_t kHalfBytes = kHalf * kChunk * 2;  // 64 rows of a chunk
 constexpr int kStats = 2 * kTile;  // floats of a row tile: -lse log2 e (-inf: no weight), then -D
 
 struct Ctl {
-    uint64_t own_full;                               // the tiles that stay are there
+    uint64_t own_full;                               // the tiles that stay are in TMEM
     uint64_t a_full[4], a_empty[4], a_ready[4];      // Q (dkv) or K (dq) stages
     uint64_t b_full[4], b_empty[4];                  // dO (dkv) or V (dq) stages
     uint64_t st_full[4], st_empty[4];                // dkv: row statistics
-    uint64_t s_full, p_full, dp_full, ds_full;       // MMA <-> softmax
-    uint64_t s_free;                                 // dq: S has been read
+    uint64_t s_full[2], p_full[2], dp_full[2], ds_full[2];  // MMA <-> softmax group
+    uint64_t s_free[2];                              // dq: S has been read
     uint64_t done;
     alignas(16) float stats[4][kStats];              // dkv; read 16 bytes at a time
     float dpart[4][kTile];                           // dq: parts of D
@@ -65,21 +71,15 @@ struct Params {
     int vec_q, vec_k, vec_v;  // outputs on 16-byte boundaries
 };
 
-// stages of the streamed operands
 template <int DKC, int DVC>
 struct Cfg {
-    static constexpr int kOwn = (DKC + DVC) * kChunkBytes;
-    static constexpr int kRoom = (227 * 1024 - 1024 - (int)sizeof(Ctl) - kOwn) / kOwn;
+    static constexpr int kStageBytes = (DKC + DVC) * kChunkBytes;
+    static constexpr int kRoom = (227 * 1024 - 1024 - (int)sizeof(Ctl)) / kStageBytes;
     static constexpr int kStages = kRoom < 4 ? kRoom : 4;
-    static constexpr size_t kSmem = 1024 + (size_t)kOwn * (1 + kStages) + sizeof(Ctl);
+    static constexpr size_t kSmem = 1024 + (size_t)kStageBytes * kStages + sizeof(Ctl);
+    static constexpr int kBuffers = 96 * (DKC + DVC) + 256 <= 512 ? 2 : 1;  // dkv: S and dP of each half, or one for both
     static_assert(kStages >= 2, "ring too short");
-    // dq: K and V stages
-    static constexpr int kFree = 227 * 1024 - 1024 - (int)sizeof(Ctl);
-    static constexpr int kKRoom = (kFree - 2 * DVC * kChunkBytes) / (DKC * kChunkBytes);
-    static constexpr int kKStages = kKRoom < 4 ? kKRoom : 4;
-    static constexpr int kVRoom = (kFree - kKStages * DKC * kChunkBytes) / (DVC * kChunkBytes);
-    static constexpr int kVStages = kVRoom < 4 ? kVRoom : 4;
-    static constexpr size_t kDqSmem = 1024 + (size_t)(kKStages * DKC + kVStages * DVC) * kChunkBytes + sizeof(Ctl);
+    static_assert(96 * (DKC + DVC) + 128 * kBuffers <= 512 && 96 * DKC + 32 * DVC + 256 <= 512, "TMEM");
 };
 
 // The row at `row` (w elements, zeros where !has) into columns [taddr, + CHUNKS * 32) of this thread's lane: the part of the
@@ -193,16 +193,13 @@ __global__ void __launch_bounds__(256) k_xattn_stats(const XattnArgs a, int nl, 
 
 template <int DKC, int DVC>
 __global__ void __launch_bounds__(kThreads, 1)
-    k_xattn_dkv_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mo,
-                   const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const Params p) {
+    k_xattn_dkv_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mo, const Params p) {
     using C = Cfg<DKC, DVC>;
-    constexpr int ST = C::kStages;
+    constexpr int ST = C::kStages, NB = C::kBuffers;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     uint8_t* base = smem_raw + (((raw + 1023u) & ~1023u) - raw);
-    uint8_t* Ks = base;
-    uint8_t* Vs = Ks + DKC * kChunkBytes;
-    uint8_t* Qr = Vs + DVC * kChunkBytes;                 // ring of Q tiles
+    uint8_t* Qr = base;                                   // ring of Q tiles
     uint8_t* Or = Qr + (size_t)ST * DKC * kChunkBytes;    // ring of dO tiles
     Ctl& c = *reinterpret_cast<Ctl*>(Or + (size_t)ST * DVC * kChunkBytes);
     volatile int* abort_flag = &c.abort_flag;
@@ -222,7 +219,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int nt = uniform(j0 < n ? (int)(t1 - t0) : 0);  // row tiles
 
     if (threadIdx.x == 0) {
-        mbar_init(&c.own_full, 1);
+        mbar_init(&c.own_full, kSoftWarps);
         for (int s = 0; s < ST; ++s) {
             mbar_init(&c.a_full[s], 1);
             mbar_init(&c.a_empty[s], 1);
@@ -231,10 +228,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(&c.st_full[s], 1);
             mbar_init(&c.st_empty[s], kSoftWarps);
         }
-        mbar_init(&c.s_full, 1);
-        mbar_init(&c.dp_full, 1);
-        mbar_init(&c.p_full, kSoftWarps);
-        mbar_init(&c.ds_full, kSoftWarps);
+        for (int h = 0; h < 2; ++h) {
+            mbar_init(&c.s_full[h], 1);
+            mbar_init(&c.dp_full[h], 1);
+            mbar_init(&c.p_full[h], kGroupWarps);
+            mbar_init(&c.ds_full[h], kGroupWarps);
+        }
         mbar_init(&c.done, 1);
         c.abort_flag = 0;
         fence_barrier_init();
@@ -255,15 +254,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = uniform(c.tmem_base);
-    const uint32_t t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 256 + DVC * kChunk;
+    const uint32_t t_k = tmem, t_v = t_k + 32 * DKC, t_dk = t_v + 32 * DVC, t_dv = t_dk + 64 * DKC;
+    const uint32_t t_s = t_dv + 64 * DVC, t_dp = t_s + 64 * NB;  // half h: + 64 h where each has its own
 
     if (warp == kTmaWarp) {
         if (lane == 0 && nt > 0) {
-            mbar_arrive_expect_tx(&c.own_full, (uint32_t)C::kOwn);
-            for (int k = 0; k < DKC; ++k)
-                tma_load_4d(Ks + (size_t)k * kChunkBytes, &mk, &c.own_full, k * kChunk, hk * p.khmul, j0, b * p.kmul);
-            for (int k = 0; k < DVC; ++k)
-                tma_load_4d(Vs + (size_t)k * kChunkBytes, &mv, &c.own_full, k * kChunk, hk * p.vhmul, j0, b * p.vmul);
             RingPos rp;
             int sa = 0, sb = 0, ss = 0;
             for (int t = 0; t < nt; ++t, rp.next(ST)) {
@@ -286,7 +281,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 b * p.omul);
                 ++sb;
             }
-            mbar_drain(&c.own_full, 0, err);
             for (int j = std::max(0, sa - ST); j < sa; ++j) mbar_drain(&c.a_full[j % ST], (uint32_t)(j / ST) & 1u, err);
             for (int j = std::max(0, ss - ST); j < ss; ++j) mbar_drain(&c.st_full[j % ST], (uint32_t)(j / ST) & 1u, err);
             for (int j = std::max(0, sb - ST); j < sb; ++j) mbar_drain(&c.b_full[j % ST], (uint32_t)(j / ST) & 1u, err);
@@ -294,57 +288,79 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else if (warp == kMmaWarp) {
         if (nt > 0) {
             const uint32_t el = elect_one();
-            const uint32_t id_s = idesc_bf16_f32(kTile), id_v = idesc_bf16_bmn(DVC * kChunk), id_k = idesc_bf16_bmn(DKC * kChunk);
-            const uint32_t ka = smem_u32(Ks), va = smem_u32(Vs), qa = smem_u32(Qr), oa = smem_u32(Or);
-            RingPos cur, nxt;  // stages of this row tile and of the next
-            auto scores = [&](const RingPos& r) {
-                if (!mbar_wait_warp_inline(&c.a_full[r.idx], r.phase, abort_flag, err)) return false;
+            const uint32_t id_s = idesc_bf16_f32(kHalf), id_v = idesc_bf16_bmn(DVC * kChunk), id_k = idesc_bf16_bmn(DKC * kChunk);
+            const uint32_t qa = smem_u32(Qr), oa = smem_u32(Or);
+            // step u: half u % 2 of row tile u / 2; S and dP run NB steps ahead of the sums
+            RingPos cur, nxt;  // stages of the sums' tile and of S and dP's
+            const int steps = 2 * nt;
+            auto scores = [&](int u) {
+                const int h = u & 1;
+                if (h == 0 && !mbar_wait_warp_inline(&c.a_full[nxt.idx], nxt.phase, abort_flag, err)) return false;
                 tc_fence_after();
-                mma_tile_ss<DKC>(t_s, ka, qa + (uint32_t)(r.idx * DKC * kChunkBytes), id_s, el);
-                commit_to(&c.s_full, el);
+                mma_rows_ts<DKC>(t_s + (NB == 2 ? 64u * h : 0u), t_k, qa + (uint32_t)(nxt.idx * DKC * kChunkBytes) + h * kHalfBytes,
+                                 id_s, el);
+                commit_to(&c.s_full[h], el);
                 return true;
             };
-            auto dprod = [&](const RingPos& r) {
-                if (!mbar_wait_warp_inline(&c.b_full[r.idx], r.phase, abort_flag, err)) return false;
+            auto dprod = [&](int u) {
+                const int h = u & 1;
+                if (h == 0 && !mbar_wait_warp_inline(&c.b_full[nxt.idx], nxt.phase, abort_flag, err)) return false;
                 tc_fence_after();
-                mma_tile_ss<DVC>(t_dp, va, oa + (uint32_t)(r.idx * DVC * kChunkBytes), id_s, el);
-                commit_to(&c.dp_full, el);
+                mma_rows_ts<DVC>(t_dp + (NB == 2 ? 64u * h : 0u), t_v, oa + (uint32_t)(nxt.idx * DVC * kChunkBytes) + h * kHalfBytes,
+                                 id_s, el);
+                commit_to(&c.dp_full[h], el);
+                if (h == 1) nxt.next(ST);
                 return true;
             };
-            bool ok = mbar_wait_warp_inline(&c.own_full, 0, abort_flag, err) && scores(cur) && dprod(cur);
-            for (int t = 0; t < nt && ok; ++t) {
-                nxt = cur;
-                nxt.next(ST);
-                if (!(ok = mbar_wait_warp_inline(&c.p_full, (uint32_t)t & 1u, abort_flag, err))) break;
+            bool ok = mbar_wait_warp_inline(&c.own_full, 0, abort_flag, err);
+            for (int u = 0; u < NB && ok; ++u) ok = scores(u) && dprod(u);
+            for (int u = 0; u < steps && ok; ++u) {
+                const int h = u & 1;
+                const uint32_t ph = (uint32_t)(u >> 1) & 1u, buf = NB == 2 ? 64u * h : 0u;
+                if (!(ok = mbar_wait_warp_inline(&c.p_full[h], ph, abort_flag, err))) break;
                 tc_fence_after();
-                mma_tile_ts<32>(t_dv, t_s, oa + (uint32_t)(cur.idx * DVC * kChunkBytes), id_v, t != 0, el);
-                commit_to(&c.b_empty[cur.idx], el);
-                if (t + 1 < nt && !(ok = scores(nxt))) break;
-                if (!(ok = mbar_wait_warp_inline(&c.ds_full, (uint32_t)t & 1u, abort_flag, err))) break;
+                mma_tile_ts<32, 4>(t_dv, t_s + buf, oa + (uint32_t)(cur.idx * DVC * kChunkBytes) + h * kHalfBytes, id_v, u != 0, el);
+                if (u + NB < steps && !(ok = scores(u + NB))) break;
+                if (!(ok = mbar_wait_warp_inline(&c.ds_full[h], ph, abort_flag, err))) break;
                 tc_fence_after();
-                mma_tile_ts<32>(t_dk, t_dp, qa + (uint32_t)(cur.idx * DKC * kChunkBytes), id_k, t != 0, el);
-                commit_to(&c.a_empty[cur.idx], el);
-                if (t + 1 < nt && !(ok = dprod(nxt))) break;
-                cur = nxt;
+                mma_tile_ts<32, 4>(t_dk, t_dp + buf, qa + (uint32_t)(cur.idx * DKC * kChunkBytes) + h * kHalfBytes, id_k, u != 0, el);
+                if (u + NB < steps && !(ok = dprod(u + NB))) break;
+                if (h == 1) {
+                    commit_to(&c.b_empty[cur.idx], el);
+                    commit_to(&c.a_empty[cur.idx], el);
+                    cur.next(ST);
+                }
             }
             commit_to(&c.done, el);
             mbar_drain(&c.done, 0, err);
         }
     } else if (warp < kSoftWarps) {
         // ------------------------------------------------------------- softmax warps: a lane is a key
-        const int quarter = warp >> 2, quad = warp & 3;
+        const int h = warp >> 3, cw = (warp >> 2) & 1, quad = warp & 3;
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
-        const uint32_t ts = t_s + lane_base + (uint32_t)(kCols * quarter), td = t_dp + lane_base + (uint32_t)(kCols * quarter);
+        const uint32_t col = lane_base + (NB == 2 ? 64u * h : 0u) + (uint32_t)(kCols * cw);
+        const uint32_t ts = t_s + col, td = t_dp + col;
         const int j = j0 + quad * 32 + lane;
         const bool valid = j < n && (!a.mask || __ldg(a.mask + (long long)b * a.ldm + j) != 0);
         const bool whole = __all_sync(0xffffffffu, valid);
         const float cs = a.scale * kLog2e;
+        if (nt > 0) {
+            const long long jj = j < a.Lk ? j : 0;
+            keep_row<DKC>(t_k + lane_base, reinterpret_cast<const __nv_bfloat16*>(a.k.p) + b * a.k.b + jj * a.k.l + hk * a.k.h,
+                          a.dk, j < a.Lk, warp >> 2);
+            keep_row<DVC>(t_v + lane_base, reinterpret_cast<const __nv_bfloat16*>(a.v.p) + b * a.v.b + jj * a.v.l + hk * a.v.h,
+                          a.dv, j < a.Lk, warp >> 2);
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&c.own_full);
+        }
         RingPos rp;
         bool ok = true;
         for (int t = 0; t < nt; ++t, rp.next(ST)) {
             const uint32_t ph = (uint32_t)t & 1u;
             if (!mbar_wait_warp_inline(&c.st_full[rp.idx], rp.phase, abort_flag, err) ||
-                !mbar_wait_warp_inline(&c.s_full, ph, abort_flag, err)) {
+                !mbar_wait_warp_inline(&c.s_full[h], ph, abort_flag, err)) {
                 ok = false;
                 break;
             }
@@ -353,8 +369,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             float* s = reinterpret_cast<float*>(sr);
             tmem_ld32_issue(ts, sr);
             tmem_wait_ld32(sr);
-            const float4* nl = reinterpret_cast<const float4*>(&c.stats[rp.idx][kCols * quarter]);
-            const float4* nd = reinterpret_cast<const float4*>(&c.stats[rp.idx][kTile + kCols * quarter]);
+            const float4* nl = reinterpret_cast<const float4*>(&c.stats[rp.idx][kHalf * h + kCols * cw]);
+            const float4* nd = reinterpret_cast<const float4*>(&c.stats[rp.idx][kTile + kHalf * h + kCols * cw]);
 #pragma unroll
             for (int q = 0; q < kCols / 4; ++q) {
                 const float4 L = nl[q];
@@ -374,8 +390,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&c.p_full);
-            if (!mbar_wait_warp_inline(&c.dp_full, ph, abort_flag, err)) {
+            if (lane == 0) mbar_arrive(&c.p_full[h]);
+            if (!mbar_wait_warp_inline(&c.dp_full[h], ph, abort_flag, err)) {
                 ok = false;
                 break;
             }
@@ -404,19 +420,19 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc_fence_before();
             __syncwarp();
             if (lane == 0) {
-                mbar_arrive(&c.ds_full);
+                mbar_arrive(&c.ds_full[h]);
                 mbar_arrive(&c.st_empty[rp.idx]);
             }
         }
         if (ok && nt > 0) ok = mbar_wait_warp_inline(&c.done, 0, abort_flag, err);
         tc_fence_after();
-        if (ok) {  // quarters 0 and 1 write dV, 2 and 3 dK
+        if (ok) {  // group 0 writes dV, group 1 dK, 64 columns a warp
             const bool mine = j < a.Lk;
             const long long jj = mine ? j : 0;
             const long long at = (long long)part * xattn_keys(a) + ((long long)b * a.Hkv + hk) * a.Lk + jj;
             const bool parts = a.rsplits > 1;
-            const int c0 = (quarter & 1) * 64;
-            if (quarter < 2)
+            const int c0 = cw * 64;
+            if (h == 0)
                 drain_acc(t_dv + lane_base, c0, c0 + 64, a.dv, nt > 0, valid, mine, 1.f,
                           reinterpret_cast<__nv_bfloat16*>(a.dV.p) + b * a.dV.b + jj * a.dV.l + hk * a.dV.h, p.vec_v != 0,
                           parts ? a.ws + xattn_ws_dv(a) + at * a.dv : nullptr);
@@ -438,13 +454,13 @@ template <int DKC, int DVC>
 __global__ void __launch_bounds__(kThreads, 1)
     k_xattn_dq_tc(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const Params p) {
     using C = Cfg<DKC, DVC>;
-    constexpr int SK = C::kKStages, SV = C::kVStages;
+    constexpr int ST = C::kStages;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     uint8_t* base = smem_raw + (((raw + 1023u) & ~1023u) - raw);
     uint8_t* Kr = base;                                 // ring of K tiles
-    uint8_t* Vr = Kr + (size_t)SK * DKC * kChunkBytes;  // ring of V tiles
-    Ctl& c = *reinterpret_cast<Ctl*>(Vr + (size_t)SV * DVC * kChunkBytes);
+    uint8_t* Vr = Kr + (size_t)ST * DKC * kChunkBytes;  // ring of V tiles
+    Ctl& c = *reinterpret_cast<Ctl*>(Vr + (size_t)ST * DVC * kChunkBytes);
     volatile int* abort_flag = &c.abort_flag;
     unsigned* err = &g_err_xbwd;
     const XattnArgs& a = p.a;
@@ -465,19 +481,19 @@ __global__ void __launch_bounds__(kThreads, 1)
 
     if (threadIdx.x == 0) {
         mbar_init(&c.own_full, kSoftWarps);
-        for (int s = 0; s < SK; ++s) {
+        for (int s = 0; s < ST; ++s) {
             mbar_init(&c.a_full[s], 1);
             mbar_init(&c.a_empty[s], 1);
             mbar_init(&c.a_ready[s], 1);
-        }
-        for (int s = 0; s < SV; ++s) {
             mbar_init(&c.b_full[s], 1);
             mbar_init(&c.b_empty[s], 1);
         }
-        mbar_init(&c.s_full, 1);
-        mbar_init(&c.dp_full, 1);
-        mbar_init(&c.ds_full, kSoftWarps);
-        mbar_init(&c.s_free, kSoftWarps);
+        for (int h = 0; h < 2; ++h) {
+            mbar_init(&c.s_full[h], 1);
+            mbar_init(&c.dp_full[h], 1);
+            mbar_init(&c.ds_full[h], kGroupWarps);
+            mbar_init(&c.s_free[h], kGroupWarps);
+        }
         mbar_init(&c.done, 1);
         c.abort_flag = 0;
         fence_barrier_init();
@@ -491,33 +507,34 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_fence_after();
     const uint32_t tmem = uniform(c.tmem_base);
     const uint32_t t_q = tmem, t_do = t_q + 32 * DKC, t_dq = t_do + 32 * DVC;
-    const uint32_t t_s = t_dq + 64 * DKC, t_dp = t_s + 128;  // dS over dP
+    const uint32_t t_s = t_dq + 64 * DKC, t_dp = t_s + 128;  // half h: + 64 h
 
     if (warp == kTmaWarp) {
         if (lane == 0 && nt > 0) {
-            RingPos rk, rv;
+            RingPos rp;
             int sa = 0, sb = 0;
-            for (int t = 0; t < nt; ++t, rk.next(SK), rv.next(SV)) {
-                if (!mbar_wait_1t(&c.a_empty[rk.idx], rk.phase ^ 1u, abort_flag, err)) break;
-                mbar_arrive_expect_tx(&c.a_full[rk.idx], (uint32_t)(DKC * kChunkBytes));
+            for (int t = 0; t < nt; ++t, rp.next(ST)) {
+                const int s = rp.idx;
+                if (!mbar_wait_1t(&c.a_empty[s], rp.phase ^ 1u, abort_flag, err)) break;
+                mbar_arrive_expect_tx(&c.a_full[s], (uint32_t)(DKC * kChunkBytes));
                 for (int k = 0; k < DKC; ++k)
-                    tma_load_4d(Kr + (size_t)(rk.idx * DKC + k) * kChunkBytes, &mk, &c.a_full[rk.idx], k * kChunk, hk * p.khmul,
+                    tma_load_4d(Kr + (size_t)(s * DKC + k) * kChunkBytes, &mk, &c.a_full[s], k * kChunk, hk * p.khmul,
                                 (t0 + t) * kTile, b * p.kmul);
                 ++sa;
-                if (!mbar_wait_1t(&c.b_empty[rv.idx], rv.phase ^ 1u, abort_flag, err)) break;
-                mbar_arrive_expect_tx(&c.b_full[rv.idx], (uint32_t)(DVC * kChunkBytes));
+                if (!mbar_wait_1t(&c.b_empty[s], rp.phase ^ 1u, abort_flag, err)) break;
+                mbar_arrive_expect_tx(&c.b_full[s], (uint32_t)(DVC * kChunkBytes));
                 for (int k = 0; k < DVC; ++k)
-                    tma_load_4d(Vr + (size_t)(rv.idx * DVC + k) * kChunkBytes, &mv, &c.b_full[rv.idx], k * kChunk, hk * p.vhmul,
+                    tma_load_4d(Vr + (size_t)(s * DVC + k) * kChunkBytes, &mv, &c.b_full[s], k * kChunk, hk * p.vhmul,
                                 (t0 + t) * kTile, b * p.vmul);
                 ++sb;
             }
-            for (int j = std::max(0, sa - SK); j < sa; ++j) mbar_drain(&c.a_full[j % SK], (uint32_t)(j / SK) & 1u, err);
-            for (int j = std::max(0, sb - SV); j < sb; ++j) mbar_drain(&c.b_full[j % SV], (uint32_t)(j / SV) & 1u, err);
+            for (int j = std::max(0, sa - ST); j < sa; ++j) mbar_drain(&c.a_full[j % ST], (uint32_t)(j / ST) & 1u, err);
+            for (int j = std::max(0, sb - ST); j < sb; ++j) mbar_drain(&c.b_full[j % ST], (uint32_t)(j / ST) & 1u, err);
         }
     } else if (warp == kMaskWarp) {
         // ------------------------------------------------------------- rows of K that are not read
         RingPos rp;
-        for (int t = 0; t < nt && fix; ++t, rp.next(SK)) {
+        for (int t = 0; t < nt && fix; ++t, rp.next(ST)) {
             uint32_t w[4];
             valid_words(w, a, b, (t0 + t) * kTile, n);
             if (!mbar_wait_warp(&c.a_full[rp.idx], rp.phase, abort_flag, err)) break;
@@ -531,45 +548,55 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else if (warp == kMmaWarp) {
         if (nt > 0) {
             const uint32_t el = elect_one();
-            const uint32_t id_s = idesc_bf16_f32(kTile), id_q = idesc_bf16_bmn(DKC * kChunk);
+            const uint32_t id_s = idesc_bf16_f32(kHalf), id_q = idesc_bf16_bmn(DKC * kChunk);
             const uint32_t ka = smem_u32(Kr), va = smem_u32(Vr);
+            // step u: half u % 2 of key tile u / 2; S and dP run two steps ahead of dQ
             RingPos cur, ns, nd;  // stages of dQ's tile, of S's and of dP's
-            auto scores = [&]() {
-                if (!mbar_wait_warp_inline(fix ? &c.a_ready[ns.idx] : &c.a_full[ns.idx], ns.phase, abort_flag, err)) return false;
+            const int steps = 2 * nt;
+            auto scores = [&](int u) {
+                const int h = u & 1;
+                if (h == 0 && !mbar_wait_warp_inline(fix ? &c.a_ready[ns.idx] : &c.a_full[ns.idx], ns.phase, abort_flag, err)) return false;
                 tc_fence_after();
-                mma_rows_ts<DKC>(t_s, t_q, ka + (uint32_t)(ns.idx * DKC * kChunkBytes), id_s, el);
-                commit_to(&c.s_full, el);
-                ns.next(SK);
+                mma_rows_ts<DKC>(t_s + 64u * h, t_q, ka + (uint32_t)(ns.idx * DKC * kChunkBytes) + h * kHalfBytes, id_s, el);
+                commit_to(&c.s_full[h], el);
+                if (h == 1) ns.next(ST);
                 return true;
             };
-            auto dprod = [&]() {
-                if (!mbar_wait_warp_inline(&c.b_full[nd.idx], nd.phase, abort_flag, err)) return false;
+            auto dprod = [&](int u) {
+                const int h = u & 1;
+                if (h == 0 && !mbar_wait_warp_inline(&c.b_full[nd.idx], nd.phase, abort_flag, err)) return false;
                 tc_fence_after();
-                mma_rows_ts<DVC>(t_dp, t_do, va + (uint32_t)(nd.idx * DVC * kChunkBytes), id_s, el);
-                commit_to(&c.dp_full, el);
-                commit_to(&c.b_empty[nd.idx], el);
-                nd.next(SV);
+                mma_rows_ts<DVC>(t_dp + 64u * h, t_do, va + (uint32_t)(nd.idx * DVC * kChunkBytes) + h * kHalfBytes, id_s, el);
+                commit_to(&c.dp_full[h], el);
+                if (h == 1) {
+                    commit_to(&c.b_empty[nd.idx], el);
+                    nd.next(ST);
+                }
                 return true;
             };
-            bool ok = mbar_wait_warp_inline(&c.own_full, 0, abort_flag, err) && scores() && dprod();
-            for (int t = 0; t < nt && ok; ++t) {
-                const uint32_t ph = (uint32_t)t & 1u;
-                if (t + 1 < nt && !(ok = mbar_wait_warp_inline(&c.s_free, ph, abort_flag, err) && scores())) break;
-                if (!(ok = mbar_wait_warp_inline(&c.ds_full, ph, abort_flag, err))) break;
+            bool ok = mbar_wait_warp_inline(&c.own_full, 0, abort_flag, err);
+            for (int u = 0; u < 2 && ok; ++u) ok = scores(u) && dprod(u);
+            for (int u = 0; u < steps && ok; ++u) {
+                const int h = u & 1;
+                const uint32_t ph = (uint32_t)(u >> 1) & 1u;
+                if (u + 2 < steps && !(ok = mbar_wait_warp_inline(&c.s_free[h], ph, abort_flag, err) && scores(u + 2))) break;
+                if (!(ok = mbar_wait_warp_inline(&c.ds_full[h], ph, abort_flag, err))) break;
                 tc_fence_after();
-                mma_tile_ts<32>(t_dq, t_dp, ka + (uint32_t)(cur.idx * DKC * kChunkBytes), id_q, t != 0, el);
-                commit_to(&c.a_empty[cur.idx], el);
-                cur.next(SK);
-                if (t + 1 < nt && !(ok = dprod())) break;
+                mma_tile_ts<32, 4>(t_dq, t_dp + 64u * h, ka + (uint32_t)(cur.idx * DKC * kChunkBytes) + h * kHalfBytes, id_q, u != 0, el);
+                if (h == 1) {
+                    commit_to(&c.a_empty[cur.idx], el);
+                    cur.next(ST);
+                }
+                if (u + 2 < steps && !(ok = dprod(u + 2))) break;
             }
             commit_to(&c.done, el);
             mbar_drain(&c.done, 0, err);
         }
     } else {
         // ------------------------------------------------------------- softmax warps: a lane is a row
-        const int quarter = warp >> 2, quad = warp & 3;
+        const int h = warp >> 3, cw = (warp >> 2) & 1, quad = warp & 3;
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
-        const uint32_t col = lane_base + (uint32_t)(kCols * quarter);
+        const uint32_t col = lane_base + 64u * h + (uint32_t)(kCols * cw);
         const uint32_t ts = t_s + col, td = t_dp + col;
         const int r = quad * 32 + lane;
         const long long pr = rt * tile_rows + r;
@@ -585,9 +612,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool exact = a.splits == 1 && nt == 1;
         if (nt > 0) {
             keep_row<DKC>(t_q + lane_base, reinterpret_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.b + ql * a.q.l + hq * a.q.h,
-                          a.dk, mine, quarter);
+                          a.dk, mine, warp >> 2);
             keep_row<DVC>(t_do + lane_base, reinterpret_cast<const __nv_bfloat16*>(a.dO.p) + b * a.dO.b + ql * a.dO.l + hq * a.dO.h,
-                          a.dv, mine, quarter);
+                          a.dv, mine, warp >> 2);
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
@@ -600,10 +627,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             const bool whole = j0 + kTile <= n && !a.mask;
             uint32_t w = 0xffffffffu;
             if (!whole) {
-                const int j = j0 + kCols * quarter + lane;
+                const int j = j0 + kHalf * h + kCols * cw + lane;
                 w = __ballot_sync(0xffffffffu, j < n && (!a.mask || __ldg(a.mask + (long long)b * a.ldm + j) != 0));
             }
-            if (!mbar_wait_warp_inline(&c.s_full, ph, abort_flag, err)) {
+            if (!mbar_wait_warp_inline(&c.s_full[h], ph, abort_flag, err)) {
                 if (exact) bar_sync_and(1, kSoftWarps * 32, false);
                 ok = false;
                 break;
@@ -615,14 +642,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_wait_ld32(sr);
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&c.s_free);
+            if (lane == 0) mbar_arrive(&c.s_free[h]);
 #pragma unroll
             for (int q = 0; q < kCols; q += 2) {
                 fma2(s[q], s[q + 1], cs, nl);
                 s[q] = ex2(s[q]);
                 s[q + 1] = ex2(s[q + 1]);
             }
-            if (!mbar_wait_warp_inline(&c.dp_full, ph, abort_flag, err)) {
+            if (!mbar_wait_warp_inline(&c.dp_full[h], ph, abort_flag, err)) {
                 if (exact) bar_sync_and(1, kSoftWarps * 32, false);
                 ok = false;
                 break;
@@ -638,13 +665,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                 float sum = 0.f;
 #pragma unroll
                 for (int q = 0; q < kCols; ++q) sum += (w >> q) & 1u ? s[q] * d[q] : 0.f;
-                c.dpart[quarter][r] = sum;
+                c.dpart[2 * h + cw][r] = sum;
                 if (!bar_sync_and(1, kSoftWarps * 32, true)) {  // a warp gave up
                     ok = false;
                     break;
                 }
                 nd = none ? 0.f : -((c.dpart[0][r] + c.dpart[1][r]) + (c.dpart[2][r] + c.dpart[3][r]));
-                if (quarter == 0) stats[kTile + r] = nd;
+                if (warp < 4) stats[kTile + r] = nd;
             }
 #pragma unroll
             for (int q = 0; q < kCols; q += 2) {
@@ -661,13 +688,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&c.ds_full);
+            if (lane == 0) mbar_arrive(&c.ds_full[h]);
         }
         if (ok && nt > 0) ok = mbar_wait_warp_inline(&c.done, 0, abort_flag, err);
         tc_fence_after();
         if (ok) {  // 32 columns of dQ a warp
             const long long at = ((long long)b * a.Hq + hq) * a.Lq + ql;
-            drain_acc(t_dq + lane_base, kCols * quarter, kCols * quarter + kCols, a.dk, nt > 0, !none, mine,
+            drain_acc(t_dq + lane_base, kCols * (warp >> 2), kCols * (warp >> 2) + kCols, a.dk, nt > 0, !none, mine,
                       a.splits > 1 ? 1.f : a.scale,
                       reinterpret_cast<__nv_bfloat16*>(a.dQ.p) + b * a.dQ.b + ql * a.dQ.l + hq * a.dQ.h, p.vec_q != 0,
                       a.splits > 1 ? a.ws + xattn_ws_dq(a) + ((long long)part * xattn_rows(a) + at) * a.dk : nullptr);
@@ -693,16 +720,16 @@ cudaError_t launch(const HeadMap& q, const HeadMap& o, const HeadMap& k, const H
     if (!set) {
         e = cudaFuncSetAttribute(k_xattn_dkv_tc<DKC, DVC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
         if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(k_xattn_dq_tc<DKC, DVC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kDqSmem);
+            e = cudaFuncSetAttribute(k_xattn_dq_tc<DKC, DVC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
         if (e != cudaSuccess) return e;
         set = true;
     }
     // first dQ: for short sequences it leaves a more exact D to the other
-    k_xattn_dq_tc<DKC, DVC><<<(unsigned)(p.rtiles * a.splits * a.Hkv * a.B), kThreads, C::kDqSmem, s>>>(k.map, v.map, p);
+    k_xattn_dq_tc<DKC, DVC><<<(unsigned)(p.rtiles * a.splits * a.Hkv * a.B), kThreads, C::kSmem, s>>>(k.map, v.map, p);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     if (a.splits > 1 && (e = launch_xattn_join_dq(a, s)) != cudaSuccess) return e;
     k_xattn_dkv_tc<DKC, DVC><<<(unsigned)((long long)p.ktiles * a.rsplits * a.Hkv * a.B), kThreads, C::kSmem, s>>>(
-        q.map, o.map, k.map, v.map, p);
+        q.map, o.map, p);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     return a.rsplits > 1 ? launch_xattn_join_dkv(a, s) : cudaSuccess;
 }

@@ -86,14 +86,14 @@ static __device__ __forceinline__ void mma_tile_ss(uint32_t d, uint32_t a, uint3
         issue_ss(d, ad + off, bd + off, idesc, k != 0 ? 1u : 0u, el);
     }
 }
-// D[tmem] (+)= A[tmem: bf16 pairs] B over 128 rows of B (MN-major): 32 rows of A's K axis (two steps of 8 columns) every GAP
-// columns
-template <int GAP>
+// D[tmem] (+)= A[tmem: bf16 pairs] B over 16 * STEPS rows of B (MN-major): 32 rows of A's K axis (two steps of 8 columns)
+// every GAP columns
+template <int GAP, int STEPS = kTile / 16>
 static __device__ __forceinline__ void mma_tile_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate,
                                                    uint32_t el) {
     const uint64_t bd = sdesc_mn(b);
 #pragma unroll
-    for (int k = 0; k < kTile / 16; ++k)
+    for (int k = 0; k < STEPS; ++k)
         issue_ts(d, a + (uint32_t)((k >> 1) * GAP + (k & 1) * 8), bd + (uint64_t)(k * 128), idesc,
                  accumulate || k != 0 ? 1u : 0u, el);
 }
