@@ -135,7 +135,13 @@ __device__ __forceinline__ void dots(float (&acc)[4][4], const float* A, const f
             }
     }
 }
-// out[i][4 c + q] += sum_k W[ty + 16 i][k] X[k][64 c + 4 tx + q] over a tile of 64
+// Column of a row of D that a thread's q-th sum belongs to: four (D = 32: two) neighbouring ones every 64.
+template <int D>
+__device__ __forceinline__ int column(int q) {
+    const int tx = threadIdx.x & 15;
+    return D == 32 ? 2 * tx + q : 64 * (q / 4) + 4 * tx + q % 4;
+}
+// out[i][q] += sum_k W[ty + 16 i][k] X[k][column(q)] over a tile of 64
 template <int D>
 __device__ __forceinline__ void weigh(float (&out)[4][D / 16], const float* W, const float* X) {
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
@@ -144,6 +150,18 @@ __device__ __forceinline__ void weigh(float (&out)[4][D / 16], const float* W, c
         float4 w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const float4*>(W + (ty + 16 * i) * kPP + k);
+        if constexpr (D == 32) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float2 x = *reinterpret_cast<const float2*>(X + (k + q) * (D + 4) + 2 * tx);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float p = q == 0 ? w[i].x : q == 1 ? w[i].y : q == 2 ? w[i].z : w[i].w;
+                    out[i][0] = fmaf(p, x.x, out[i][0]);
+                    out[i][1] = fmaf(p, x.y, out[i][1]);
+                }
+            }
+        }
 #pragma unroll
         for (int q = 0; q < 4; ++q)
 #pragma unroll
@@ -258,7 +276,7 @@ __global__ void __launch_bounds__(kThreads) k_xattn(const XattnArgs a, long long
             float* po = a.ws + ((long long)bl.part * nrows + at) * a.dv;
 #pragma unroll
             for (int q = 0; q < DV / 16; ++q) {
-                const int col = 64 * (q / 4) + 4 * tx + q % 4;
+                const int col = column<DV>(q);
                 if (col < a.dv) po[col] = o[i][q];
             }
             if (tx == 0) {
@@ -271,7 +289,7 @@ __global__ void __launch_bounds__(kThreads) k_xattn(const XattnArgs a, long long
             const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
 #pragma unroll
             for (int q = 0; q < DV / 16; ++q) {
-                const int col = 64 * (q / 4) + 4 * tx + q % 4;
+                const int col = column<DV>(q);
                 if (col < a.dv) po[col] = from_f32<T>(o[i][q] * inv);
             }
             if (tx == 0 && a.lse) a.lse[at] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * kLn2;
@@ -432,7 +450,7 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long l
         if (r >= a.rows) continue;
 #pragma unroll
         for (int q = 0; q < DK / 16; ++q) {
-            const int col = 64 * (q / 4) + 4 * tx + q % 4;
+            const int col = column<DK>(q);
             if (col >= a.dk) continue;
             if (a.splits > 1)
                 a.ws[xattn_ws_dq(a) + ((long long)bl.part * nrows + row_index(a, bl.b, bl.hk, r)) * a.dk + col] = o[i][q];
@@ -496,7 +514,7 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dkv(const XattnArgs a, int k
         const long long at = ((long long)bl.b * a.Hkv + bl.hk) * a.Lk + j;
 #pragma unroll
         for (int q = 0; q < DK / 16; ++q) {
-            const int col = 64 * (q / 4) + 4 * tx + q % 4;
+            const int col = column<DK>(q);
             if (col >= a.dk) continue;
             if (a.rsplits > 1)
                 a.ws[xattn_ws_dk(a) + ((long long)bl.part * nk + at) * a.dk + col] = ok_[i][q];
@@ -506,7 +524,7 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dkv(const XattnArgs a, int k
         }
 #pragma unroll
         for (int q = 0; q < DV / 16; ++q) {
-            const int col = 64 * (q / 4) + 4 * tx + q % 4;
+            const int col = column<DV>(q);
             if (col >= a.dv) continue;
             if (a.rsplits > 1)
                 a.ws[xattn_ws_dv(a) + ((long long)bl.part * nk + at) * a.dv + col] = ov[i][q];
@@ -575,14 +593,17 @@ template <typename T>
 cudaError_t forward_t(XattnArgs a, cudaStream_t s) {
     a.vec = (on_fours(a, a.q, a.Lq, a.Hq) ? kVecQ : 0) | (on_fours(a, a.k, a.Lk, a.Hkv) ? kVecK : 0) |
             (on_fours(a, a.v, a.Lk, a.Hkv) ? kVecV : 0);
-    if (a.dk <= 64) return a.dv <= 64 ? forward<T, 64, 64>(a, s) : forward<T, 64, 128>(a, s);
+    if (a.dk <= 64)
+        return a.dv <= 32 ? forward<T, 64, 32>(a, s) : a.dv <= 64 ? forward<T, 64, 64>(a, s) : forward<T, 64, 128>(a, s);
     return a.dv <= 64 ? forward<T, 128, 64>(a, s) : forward<T, 128, 128>(a, s);
 }
 template <typename T>
 cudaError_t backward_t(XattnArgs a, cudaStream_t s) {
     a.vec = (on_fours(a, a.q, a.Lq, a.Hq) ? kVecQ : 0) | (on_fours(a, a.k, a.Lk, a.Hkv) ? kVecK : 0) |
             (on_fours(a, a.v, a.Lk, a.Hkv) ? kVecV : 0) | (on_fours(a, a.dO, a.Lq, a.Hq) ? kVecDO : 0);
-    if (a.dk <= 64) return a.dv <= 64 ? backward<T, 64, 64>(a, s) : backward<T, 64, 128>(a, s);
+    if (a.dk <= 32 && a.dv <= 32) return backward<T, 32, 32>(a, s);
+    if (a.dk <= 64)
+        return a.dv <= 32 ? backward<T, 64, 32>(a, s) : a.dv <= 64 ? backward<T, 64, 64>(a, s) : backward<T, 64, 128>(a, s);
     return a.dv <= 64 ? backward<T, 128, 64>(a, s) : backward<T, 128, 128>(a, s);
 }
 
@@ -602,9 +623,9 @@ cudaError_t launch_delta(const XattnArgs& a, cudaStream_t s) {
 
 void xattn_simt_plan(XattnArgs& a, bool backward, int sms) {
     const long long rt = (a.rows + kTile - 1) / kTile, kt = (a.Lk + kTile - 1) / kTile;
-    // two blocks a multiprocessor where they fit, and parts of two tiles or more
-    a.splits = xattn_parts(rt * a.Hkv * a.B, kt, 2 * sms, 2);
-    a.rsplits = backward ? xattn_parts(kt * a.Hkv * a.B, rt, 2 * sms, 2) : 1;
+    // up to four blocks a multiprocessor, and parts of two tiles or more
+    a.splits = xattn_parts(rt * a.Hkv * a.B, kt, 4 * sms, 2);
+    a.rsplits = backward ? xattn_parts(kt * a.Hkv * a.B, rt, 4 * sms, 2) : 1;
     a.stats = xattn_round4(xattn_rows(a));  // D_i
 }
 

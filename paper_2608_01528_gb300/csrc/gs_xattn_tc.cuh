@@ -179,10 +179,11 @@ static __device__ __forceinline__ int keys_of(const XattnArgs& a, int b) {
     return a.lens ? min(max(__ldg(a.lens + b), 0), a.Lk) : a.Lk;
 }
 // bit l of word i: key j0 + 32 i + l may be read (taken by a whole warp)
-static __device__ __forceinline__ void valid_words(uint32_t (&w)[4], const XattnArgs& a, int b, int j0, int n) {
+template <int W>
+static __device__ __forceinline__ void valid_words(uint32_t (&w)[W], const XattnArgs& a, int b, int j0, int n) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < W; ++i) {
         const int j = j0 + 32 * i + lane;
         const bool ok = j < n && (!a.mask || __ldg(a.mask + (long long)b * a.ldm + j) != 0);
         w[i] = __ballot_sync(0xffffffffu, ok);
