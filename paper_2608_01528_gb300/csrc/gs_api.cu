@@ -918,9 +918,10 @@ gs_status attn_device(int& dev, int& sms) {
     return sms < 0 ? GS_ERR_UNSUPPORTED : GS_OK;
 }
 
-// Which forward kernels take a call (us, 8 x 8,192 keys unless said otherwise).  Tensor cores against a few rows' CUDA cores:
-// one row of 64, 64 x 1,500 keys of 16 heads, 113 / 92; one row of 128 98 / 139; four rows 66 / 111.  Few rows against tiles of
-// 64 on CUDA cores, fp32: 4 rows of 128 133 / 615, 16 rows (16 x 2,048 keys of 4 heads) 129 / 174, 32 rows of 40 78 / 48.
+// Which forward kernels take a call (us, 8 x 8,192 keys unless said otherwise).  Tensor cores against a few rows' CUDA cores,
+// bf16: one row of 64, 64 x 1,500 keys of 16 heads, 90 / 92, and with half of the padding masked 58 / 61, but 4 x 197 keys cost 3 us
+// less host time without tensor maps; one row of 128 98 / 147; two 98 / 117; four 64 / 90.  Few rows against tiles of 64 on CUDA
+// cores, fp32: 4 rows of 128 123 / 615, 16 rows (16 x 2,048 keys of 4 heads) 111 / 174, 32 rows of 40 53 / 48.
 enum AttnPath { ATTN_ROWS, ATTN_SIMT, ATTN_TC };
 AttnPath attn_path(const gs::XattnArgs& a, unsigned flags, bool tc_ok) {
     if (tc_ok && flags == GS_PATH_TENSOR) return ATTN_TC;

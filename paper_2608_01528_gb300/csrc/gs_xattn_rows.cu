@@ -2,13 +2,15 @@
 // cores: any type, width, alignment and stride.
 //
 // A block takes up to R packed rows of a key head; the keys go to its eight warps in batches.  LK lanes share a key, each
-// holding 16 bytes of it: a key's dot products with the R rows (in registers) are summed across the LK lanes by
-// shuffles, and the same lanes then add the weighted value -- K and V are read once, 16 bytes a lane, straight from memory, four keys of
-// each in flight per lane.  Every LK lanes keep a running maximum, sum and output of their own; they meet in
-// registers, then shared memory, and parts of long memories in k_xattn_join.
+// holding 16 bytes of it: a key's dot products with the R rows (in registers) are summed across the LK lanes, and the same
+// lanes then add the weighted value -- K and V are read once, 16 bytes a lane, straight from memory, four keys of
+// each in flight per lane.  The sums of four keys and R rows go by halving: at each step a lane passes on half of its values
+// and keeps the others', so that each lane ends with a logit of its own (15 shuffles for 16 of them instead of 64), takes its
+// exponential, and the weights come back by shuffles.  Every LK lanes keep running maxima, sums and an output of their own;
+// they meet in registers, then shared memory, and parts of long memories in k_xattn_join.
 //
-// Bound by memory with one row (64 sequences of 1,500 keys, 16 heads of 64), by instructions (about 12 per key, row and
-// 16 bytes) with more.
+// One row is bound by the loads in flight (64 x 1,500 keys, 16 heads of 64, bf16: 5.0 TB/s with half of the
+// padding read; fp32 8 x 8,192 keys, 16 heads of 128: 4.5 TB/s), more rows by instructions.
 
 #include <algorithm>
 
@@ -23,7 +25,7 @@ using xtc::kLog2e;
 using xtc::keys_of;
 
 constexpr int kWarps = 8, kThreads = kWarps * 32;
-constexpr int kBatch = 4;  // keys in flight per LK lanes
+constexpr int kBatch = 4;  // keys that LK lanes work on at a time
 constexpr int kVecQ = 1, kVecK = 2, kVecV = 4;
 
 template <typename T>
@@ -66,6 +68,9 @@ template <typename T, int LK, int R>
 __global__ void __launch_bounds__(kThreads, R == 1 ? 3 : 2) k_xattn_rows(const XattnArgs a, long long chunks) {
     using V = Vec<T>;
     constexpr int N = V::N, W = LK * N, KS = 32 / LK;
+    // Two rows leave registers for the next four keys on their way as well (8 x 8,192 keys, 16 heads of 128, fp32: 209 -> 195 us);
+    // one row does better with a third block a multiprocessor (242 against 297 us).
+    constexpr bool kAhead = R == 2;
     __shared__ float acc_s[kWarps][R][W];
     __shared__ float2 ml_s[kWarps][R];
     long long i = blockIdx.x;
@@ -79,35 +84,54 @@ __global__ void __launch_bounds__(kThreads, R == 1 ? 3 : 2) k_xattn_rows(const X
     const int k0 = (int)((long long)a.Lk * part / a.splits), k1 = min(n, (int)((long long)a.Lk * (part + 1) / a.splits));
     const float cs = a.scale * kLog2e;
 
-    float q[R][N], acc[R][N], m[R], l[R];
+    // After the halving, lane x of a key's LK holds values x * kOwn .. + kOwn - 1 of row-major [R][kBatch] (kOwn values, or one
+    // that kSame lanes share); m and l are those of that value's row.
+    constexpr int kValues = R * kBatch, kOwn = kValues > LK ? kValues / LK : 1, kSame = kValues > LK ? 1 : LK / kValues;
+    static_assert(kOwn <= kBatch, "a lane's values belong to one row");
+    const int x = lane % LK, own = x * kOwn / kSame;
+    float q[R][N], acc[R][N], m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const long long pr = chunk * R + r;
         const bool has = pr < a.rows;
         const long long ql = has ? pr / a.G : 0;
         const int h = hk * a.G + (has ? (int)(pr - ql * a.G) : 0);
-        V x;
-        x.load(reinterpret_cast<const T*>(a.q.p) + b * a.q.b + ql * a.q.l + h * a.q.h + e0, has ? a.dk - e0 : 0, a.vec & kVecQ);
-        x.get(q[r]);
-        m[r] = -INFINITY;
-        l[r] = 0.f;
+        V y;
+        y.load(reinterpret_cast<const T*>(a.q.p) + b * a.q.b + ql * a.q.l + h * a.q.h + e0, has ? a.dk - e0 : 0, a.vec & kVecQ);
+        y.get(q[r]);
 #pragma unroll
         for (int e = 0; e < N; ++e) acc[r][e] = 0.f;
     }
     const T* kp = reinterpret_cast<const T*>(a.k.p) + b * a.k.b + hk * a.k.h + e0;
     const T* vp = reinterpret_cast<const T*>(a.v.p) + b * a.v.b + hk * a.v.h + e0;
     const unsigned char* mask = a.mask ? a.mask + (long long)b * a.ldm : nullptr;
-    for (int j0 = k0 + warp * (KS * kBatch); j0 < k1; j0 += kWarps * KS * kBatch) {
-        V kx[kBatch], vx[kBatch];
-        bool ok[kBatch];
+    V kx[kBatch], vx[kBatch], kn[kBatch], vn[kBatch];
+    bool ok[kBatch], okn[kBatch];
+    auto fetch = [&](int j0, V(&kk)[kBatch], V(&vv)[kBatch], bool(&o)[kBatch]) {
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
             const int j = j0 + u * KS + slot;
-            ok[u] = j < k1 && (!mask || __ldg(mask + j) != 0);
-            kx[u].load(kp + (ok[u] ? (long long)j * a.k.l : 0), ok[u] ? a.dk - e0 : 0, a.vec & kVecK);
-            vx[u].load(vp + (ok[u] ? (long long)j * a.v.l : 0), ok[u] ? a.dv - e0 : 0, a.vec & kVecV);
+            o[u] = j < k1 && (!mask || __ldg(mask + j) != 0);
+            kk[u].load(kp + (o[u] ? (long long)j * a.k.l : 0), o[u] ? a.dk - e0 : 0, a.vec & kVecK);
+            vv[u].load(vp + (o[u] ? (long long)j * a.v.l : 0), o[u] ? a.dv - e0 : 0, a.vec & kVecV);
         }
-        float s[R][kBatch];
+    };
+    constexpr int kStep = kWarps * KS * kBatch;
+    int j0 = k0 + warp * (KS * kBatch);
+    if (kAhead && j0 < k1) fetch(j0, kn, vn, okn);
+    for (; j0 < k1; j0 += kStep) {
+        if constexpr (kAhead) {
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                kx[u] = kn[u];
+                vx[u] = vn[u];
+                ok[u] = okn[u];
+            }
+            if (j0 + kStep < k1) fetch(j0 + kStep, kn, vn, okn);
+        } else {
+            fetch(j0, kx, vx, ok);
+        }
+        float s[kValues];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
             float f[N];
@@ -117,55 +141,87 @@ __global__ void __launch_bounds__(kThreads, R == 1 ? 3 : 2) k_xattn_rows(const X
                 float d = 0.f;
 #pragma unroll
                 for (int e = 0; e < N; ++e) d = fmaf(q[r][e], f[e], d);
-                s[r][u] = d;
+                s[r * kBatch + u] = d;
             }
         }
+        // lanes with bit o keep the upper half of the values that are left, the others the lower
 #pragma unroll
-        for (int o = LK / 2; o; o >>= 1)
+        for (int o = LK / 2, left = kValues; o; o >>= 1) {
+            if (left > 1) {
+                left /= 2;
+                const bool up = (x & o) != 0;
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int u = 0; u < kBatch; ++u) s[r][u] += __shfl_xor_sync(0xffffffffu, s[r][u], o);
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            float mn = m[r];
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                s[r][u] = ok[u] ? s[r][u] * cs : -INFINITY;
-                mn = fmaxf(mn, s[r][u]);
-            }
-            const float ms = mn == -INFINITY ? 0.f : mn;
-            const float f = ex2(m[r] - ms);
-            m[r] = mn;
-            l[r] *= f;
-#pragma unroll
-            for (int e = 0; e < N; ++e) acc[r][e] *= f;
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                s[r][u] = ex2(s[r][u] - ms);
-                l[r] += s[r][u];
+                for (int i = 0; i < kValues / 2; ++i)
+                    if (i < left) {
+                        const float mine = up ? s[i + left] : s[i], other = up ? s[i] : s[i + left];
+                        s[i] = mine + __shfl_xor_sync(0xffffffffu, other, o);
+                    }
+            } else {
+                s[0] += __shfl_xor_sync(0xffffffffu, s[0], o);
             }
         }
+        float mn = m;
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            const int u = (own + i) % kBatch;
+            bool in = ok[0];
+#pragma unroll
+            for (int k = 1; k < kBatch; ++k) in = u == k ? ok[k] : in;
+            s[i] = in ? s[i] * cs : -INFINITY;
+            mn = fmaxf(mn, s[i]);
+        }
+        // the row's maximum over the lanes that hold its other keys
+#pragma unroll
+        for (int o = kSame; o < kSame * kBatch / kOwn; o <<= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, o));
+        const float ms = mn == -INFINITY ? 0.f : mn;
+        const float f = ex2(m - ms);
+        if (__any_sync(0xffffffffu, f != 1.f)) {  // (NaN too)
+            l *= f;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float fr = __shfl_sync(0xffffffffu, f, r * (LK / R), LK);
+#pragma unroll
+                for (int e = 0; e < N; ++e) acc[r][e] *= fr;
+            }
+        }
+        m = mn;
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            s[i] = ex2(s[i] - ms);
+            l += s[i];
+        }
+        float w[kValues];
+#pragma unroll
+        for (int i = 0; i < kValues; ++i) w[i] = __shfl_sync(0xffffffffu, s[i % kOwn], i / kOwn * kSame, LK);
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            float f[N];
-            vx[u].get(f);
+            float f2[N];
+            vx[u].get(f2);
 #pragma unroll
             for (int r = 0; r < R; ++r)
 #pragma unroll
-                for (int e = 0; e < N; ++e) acc[r][e] = fmaf(s[r][u], f[e], acc[r][e]);
+                for (int e = 0; e < N; ++e) acc[r][e] = fmaf(w[r * kBatch + u], f2[e], acc[r][e]);
         }
+    }
+    // a row's sum over the lanes that hold its keys; then every lane has every row's maximum and sum
+#pragma unroll
+    for (int o = kSame; o < kSame * kBatch / kOwn; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    float mr[R], lr[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        mr[r] = __shfl_sync(0xffffffffu, m, r * (LK / R), LK);
+        lr[r] = __shfl_sync(0xffffffffu, l, r * (LK / R), LK);
     }
     // the keys of a warp's lanes, then the warps
 #pragma unroll
     for (int o = LK; o < 32; o <<= 1)
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const float mo = __shfl_xor_sync(0xffffffffu, m[r], o), lo = __shfl_xor_sync(0xffffffffu, l[r], o);
-            const float mn = fmaxf(m[r], mo), ms = mn == -INFINITY ? 0.f : mn;
-            const float f = ex2(m[r] - ms), g = ex2(mo - ms);
-            m[r] = mn;
-            l[r] = l[r] * f + lo * g;
+            const float mo = __shfl_xor_sync(0xffffffffu, mr[r], o), lo = __shfl_xor_sync(0xffffffffu, lr[r], o);
+            const float mn = fmaxf(mr[r], mo), ms = mn == -INFINITY ? 0.f : mn;
+            const float f = ex2(mr[r] - ms), g = ex2(mo - ms);
+            mr[r] = mn;
+            lr[r] = lr[r] * f + lo * g;
 #pragma unroll
             for (int e = 0; e < N; ++e) acc[r][e] = acc[r][e] * f + __shfl_xor_sync(0xffffffffu, acc[r][e], o) * g;
         }
@@ -174,13 +230,13 @@ __global__ void __launch_bounds__(kThreads, R == 1 ? 3 : 2) k_xattn_rows(const X
         for (int r = 0; r < R; ++r) {
 #pragma unroll
             for (int e = 0; e < N; ++e) acc_s[warp][r][e0 + e] = acc[r][e];
-            if (lane == 0) ml_s[warp][r] = make_float2(m[r], l[r]);
+            if (lane == 0) ml_s[warp][r] = make_float2(mr[r], lr[r]);
         }
     }
     __syncthreads();
     const long long all = xattn_rows(a);
-    for (int x = threadIdx.x; x < R * W; x += kThreads) {
-        const int r = x / W, c = x % W;
+    for (int e = threadIdx.x; e < R * W; e += kThreads) {
+        const int r = e / W, c = e % W;
         const long long pr = chunk * R + r;
         if (pr >= a.rows || (c >= a.dv && c != 0)) continue;
         float mm = -INFINITY, ll = 0.f, o = 0.f;
