@@ -486,7 +486,17 @@ def _on_stream(device, stream):
     """The context of a call that runs on `stream`, or nothing to do.  The call's device is current in it, and so is its
     stream: memory from torch's allocator belongs to the stream that is current when it is taken, so outputs and
     workspaces are taken under the stream that writes them."""
-    return _on(device) if stream is None else torch.cuda.stream(stream)
+    if stream is None:
+        return _on(device)
+    if stream.device != device:
+        raise ValueError(f"the tensors are on {device}, the stream on {stream.device}")
+    return torch.cuda.stream(stream)
+
+
+def _c_int(*sizes):
+    """Refuses sizes that a C int does not hold (ctypes would cut them)."""
+    if max(sizes) > 0x7fffffff:
+        raise ValueError(f"sizes above 2^31 - 1: {sizes}")
 
 
 def _heads(t, name, shape, like):
@@ -508,6 +518,7 @@ def _attn(Q, K, V, scale, key_lens, key_mask, path):
     code = _dtype_code(Q)
     B, Lq, Hq, dk = Q.shape
     _, Lk, Hkv, dv = V.shape
+    _c_int(B, Lq, Lk, Hq, Hkv, dk, dv)
     hs = (_heads(Q, "Q", Q.shape, Q), _heads(K, "K", (B, Lk, Hkv, dk), Q), _heads(V, "V", (B, Lk, Hkv, dv), Q))
     if scale is None:
         scale = dk ** -0.5 if dk else 1.0
@@ -562,7 +573,7 @@ def cross_attention(Q, K, V, scale=None, key_lens=None, key_mask=None, want_lse=
     with _on_stream(dev, stream):
         if "O" not in out:
             out["O"] = torch.empty((a.B, a.Lq, a.Hq, a.dv), dtype=Q.dtype, device=dev)
-        if want_lse and "lse" not in out:
+        if want_lse and out.get("lse") is None:
             out["lse"] = torch.empty((a.B, a.Hq, a.Lq), dtype=torch.float32, device=dev)
         o = _heads(out["O"], "O", (a.B, a.Lq, a.Hq, a.dv), Q)
         lse = _attn_lse(out["lse"], (a.B, a.Hq, a.Lq), dev) if out.get("lse") is not None else None
@@ -602,6 +613,7 @@ def sample_scores(S, U, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, want_pro
     {"index": N int32, "prob": N float32}."""
     ld = _ld(S)
     N, M = S.shape
+    _c_int(M)
     dev = S.device
     code = _dtype_code(S)
 
@@ -618,7 +630,7 @@ def sample_scores(S, U, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, want_pro
         if isinstance(v, torch.Tensor):
             setattr(how, name + "_rows", vector(v, name, dt))
         else:
-            setattr(how, name, int(v) if name == "top_k" else float(v))
+            setattr(how, name, max(0, min(int(v), M)) if name == "top_k" else float(v))
     u = vector(U, "U", torch.float32)
     out = dict(out) if out else {}
     for name, dt in (("index", torch.int32), ("prob", torch.float32)):

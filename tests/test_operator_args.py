@@ -99,3 +99,46 @@ def test_sampling_arguments(g):
         g.sample_scores(S, U)
     with pytest.raises(ValueError):
         g.sample_scores(S.t(), torch.zeros(5))
+
+
+def test_sizes_past_a_c_int(g):
+    """Broadcast tensors reach sizes that a C int would cut to small ones."""
+    big = 2 ** 32 + 1
+    one = torch.zeros(1, 1, 1, 8)
+    for q, k in ((one.expand(big, 1, 1, 8), one.expand(big, 1, 1, 8)), (one, one.expand(1, big, 1, 8)),
+                 (one.expand(1, big, 1, 8), one)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            g.cross_attention(q, k, k)
+    with pytest.raises(ValueError):
+        g.sample_scores(torch.zeros(big, dtype=torch.bfloat16, device="meta")[None], torch.zeros(1, device="meta"))
+
+
+def test_top_k_past_a_c_int(g):
+    """2^32 + 1 means all scores, not one."""
+    seen = []
+
+    class Library:
+        def gs_sample_scores(self, S, code, N, M, ld, how, *rest):
+            seen.append(how._obj.top_k)
+            return g.GS_OK
+
+    class Fake(torch.Tensor):  # a host tensor that says it is a CUDA one: the call goes as far as the library
+        is_cuda = True
+
+    S = torch.zeros(2, 6).as_subclass(Fake)
+    load, on, stream = g.load_library, g._on_stream, g._stream
+    g.load_library, g._on_stream, g._stream = Library, lambda *a: g._STAY, lambda *a: 0
+    try:
+        for k in (2 ** 32 + 1, 7, 6, 3, 0, -5, -2 ** 32 + 2):
+            g.sample_scores(S, torch.zeros(2), top_k=k)
+    finally:
+        g.load_library, g._on_stream, g._stream = load, on, stream
+    assert seen == [6, 6, 6, 3, 0, 0, 0]
+
+
+def test_stream_of_another_device(g):
+    class Stream:
+        device = torch.device("cuda", 1)
+
+    with pytest.raises(ValueError, match="cuda:0"):
+        g._on_stream(torch.device("cuda", 0), Stream())
