@@ -420,7 +420,7 @@ typedef struct gs_attn {
     int B, Lq, Lk;        /* sequences, query rows and keys of each (0 allowed)           */
     int Hq, Hkv;          /* query heads and key heads, Hkv divides Hq                   */
     int dk, dv;           /* widths of a head's queries / keys and values, 1 to 128       */
-    float scale;          /* finite and > 0                                              */
+    float scale;          /* > 0, at most 2e38                                           */
     const int* key_lens;  /* B keys to read of each sequence (NULL: Lk); values outside
                              [0, Lk] count as the nearer end                             */
     const unsigned char* key_mask; /* B x Lk, 0 = not read (NULL: all)                   */
@@ -441,13 +441,13 @@ GS_API gs_status gs_cross_attention_workspace(const gs_attn* a, int backward, lo
  * workspace: a 16-byte aligned device buffer of gs_cross_attention_workspace's
  * size, overwritten; calls that may run at the same time (on two streams, or in two graphs that
  * may be launched together) need one each.
- * Tensor-core path: GS_BF16 with data on 16-byte boundaries and strides that are
- * multiples of 8 elements; logits, statistics and sums in fp32, weights rounded to
+ * Tensor-core path: GS_BF16 with inputs on 16-byte boundaries, strides that are
+ * multiples of 8 elements, and no stride of 0 along rows or (queries) heads; logits, statistics and sums in fp32, weights rounded to
  * bf16 for the product with the values.  Otherwise fp32 CUDA cores.  Results do not depend on
  * what else runs, and a call repeated gives the same bits.
  * Errors: GS_ERR_INVALID_ARG (null pointer, unknown type or path, scale), GS_ERR_SHAPE
  * (sizes, strides, workspace too small), GS_ERR_ALIGNMENT (a forced
- * tensor-core path with unaligned data; a workspace off a 16-byte boundary),
+ * tensor-core path with unaligned data; a workspace off a 16-byte boundary; an array off its elements' boundary),
  * GS_ERR_UNSUPPORTED (a width above 128; a forced tensor-core path with GS_F32 or more than 128 query
  * heads to a key head), GS_ERR_CUDA.
  */
@@ -463,7 +463,7 @@ GS_API gs_status gs_cross_attention(const gs_attn* a, const gs_heads* Q, const g
  * lse are the forward call's.  dQ, dK, dV have the shapes of Q, K, V and type dtype; keys
  * that are not valid get zeros, rows without a valid key zeros in dQ.  Where inputs repeat
  * memory (stride 0), the gradients still come one per index: the caller sums them.
- * Deterministic: no atomics.  Workspace, paths and errors as gs_cross_attention.
+ * No gradient may overlap an input or another gradient.  Deterministic: no atomics.  Workspace, paths and errors as gs_cross_attention.
  */
 GS_API gs_status gs_cross_attention_backward(const gs_attn* a, const gs_heads* Q, const gs_heads* K,
                                              const gs_heads* V, const gs_heads* O, const float* lse,
@@ -496,7 +496,7 @@ GS_API gs_status gs_cross_attention_backward(const gs_attn* a, const gs_heads* Q
  * NULL, one per row (device arrays of N).  index (N int32) and prob (N fp32) are
  * optional, not both NULL.  N = 0 is a no-op.  No workspace.
  * Errors: GS_ERR_INVALID_ARG, GS_ERR_SHAPE (N < 0, M < 1 or above 2^19, 0 < lds < M),
- * GS_ERR_CUDA.
+ * GS_ERR_ALIGNMENT (an array off its elements' boundary), GS_ERR_CUDA.
  */
 typedef struct gs_sampling {
     float temperature, top_p, min_p;

@@ -876,17 +876,24 @@ bool valid_heads(const gs_heads* v, int B, int L, int H, bool output) {
     if (!v || v->batch < 0 || v->row < 0 || v->head < 0) return false;
     return !output || ((v->batch > 0 || B <= 1) && (v->row > 0 || L <= 1) && (v->head > 0 || H <= 1));
 }
+// Whether the pointers lie on the boundaries of their elements (of `bytes`); null pointers do.
+template <typename... P>
+bool on_elements(int bytes, const P*... p) {
+    return ((... | (uintptr_t)p) & (uintptr_t)(bytes - 1)) == 0;
+}
+constexpr float kMaxScale = 2e38f;  // scale * log2(e) is an fp32 number
 gs::HeadView view_of(const gs_heads* v) { return {(char*)v->data, v->batch, v->row, v->head}; }
 
 // The checks that both calls and the workspace query share; fills what the kernels take.
 gs_status attn_args(const gs_attn* p, gs::XattnArgs& a) {
     if (!p || !valid_path(p->flags)) return GS_ERR_INVALID_ARG;
     if (p->dtype != GS_F32 && p->dtype != GS_BF16) return GS_ERR_INVALID_ARG;
-    if (!isfinite(p->scale) || !(p->scale > 0.f)) return GS_ERR_INVALID_ARG;
+    if (!(p->scale > 0.f) || !(p->scale <= kMaxScale)) return GS_ERR_INVALID_ARG;
     if (p->B < 0 || p->Lq < 0 || p->Lk < 0 || p->Hq < 1 || p->Hkv < 1 || p->Hq % p->Hkv || p->dk < 1 || p->dv < 1)
         return GS_ERR_SHAPE;
     if (p->dk > 128 || p->dv > 128) return GS_ERR_UNSUPPORTED;
     if (p->key_mask && p->ld_mask != 0 && p->ld_mask < p->Lk) return GS_ERR_SHAPE;
+    if (!on_elements(4, p->key_lens)) return GS_ERR_ALIGNMENT;
     // block and row numbers are 32-bit, positions stay clear of that limit when a tile is added
     const long long limit = 0x7fffffffLL, far = limit - 1024;
     if (p->Lk > far || (long long)p->Lq * (p->Hq / p->Hkv) > far || (long long)p->B * p->Hq > limit) return GS_ERR_SHAPE;
@@ -984,6 +991,7 @@ gs_status gs_cross_attention(const gs_attn* p, const gs_heads* Q, const gs_heads
         return GS_ERR_SHAPE;
     if (a.B == 0 || a.Lq == 0) return GS_OK;
     if (!Q->data || !O->data || (a.Lk > 0 && (!K->data || !V->data))) return GS_ERR_INVALID_ARG;
+    if (!on_elements(a.dtype == GS_F32 ? 4 : 2, Q->data, K->data, V->data, O->data) || !on_elements(4, lse)) return GS_ERR_ALIGNMENT;
     int dev = 0, sms = 0;
     if ((st = attn_device(dev, sms)) != GS_OK) return st;
     a.q = view_of(Q); a.k = view_of(K); a.v = view_of(V); a.o = view_of(O);
@@ -1017,6 +1025,9 @@ gs_status gs_cross_attention_backward(const gs_attn* p, const gs_heads* Q, const
     if (a.B == 0 || (a.Lq == 0 && a.Lk == 0)) return GS_OK;
     if (a.Lq > 0 && (!Q->data || !O->data || !dO->data || !dQ->data || !lse)) return GS_ERR_INVALID_ARG;
     if (a.Lk > 0 && (!K->data || !V->data || !dK->data || !dV->data)) return GS_ERR_INVALID_ARG;
+    if (!on_elements(a.dtype == GS_F32 ? 4 : 2, Q->data, K->data, V->data, O->data, dO->data, dQ->data, dK->data, dV->data) ||
+        !on_elements(4, lse))
+        return GS_ERR_ALIGNMENT;
     int dev = 0, sms = 0;
     if ((st = attn_device(dev, sms)) != GS_OK) return st;
     a.q = view_of(Q); a.k = view_of(K); a.v = view_of(V); a.o = view_of(O);
@@ -1044,6 +1055,9 @@ gs_status gs_sample_scores(const void* S, int s_dtype, long long N, int M, long 
     if (N < 0 || N > 0x7fffffffLL || M < 1 || M > (1 << 19) || lds < 0 || (lds > 0 && lds < M)) return GS_ERR_SHAPE;
     if (N == 0) return GS_OK;
     if (!S || !U || (!index && !prob)) return GS_ERR_INVALID_ARG;
+    if (!on_elements(s_dtype == GS_F32 ? 4 : 2, S) ||
+        !on_elements(4, U, index, prob, how->temperature_rows, how->top_p_rows, how->min_p_rows, how->top_k_rows))
+        return GS_ERR_ALIGNMENT;
     int dev = 0, sms = 0;
     gs_status st = attn_device(dev, sms);
     if (st != GS_OK) return st;

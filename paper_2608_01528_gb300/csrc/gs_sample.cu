@@ -25,6 +25,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "gs_tc_ptx.cuh"
 #include "gs_xattn.h"
@@ -897,7 +898,7 @@ __global__ void __launch_bounds__(kWideThreads, 2) k_sample_wide(const SampleArg
         }
 }
 
-bool g_attr[64];
+std::atomic<bool> g_attr[64];
 
 }  // namespace
 

@@ -29,6 +29,7 @@
 #include <stddef.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "gs_xattn_tc.cuh"
 
@@ -708,14 +709,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
 }
 
-bool g_attr[64][4];
+std::atomic<bool> g_attr[64][4];
 
 template <int DKC, int DVC>
 cudaError_t launch(const HeadMap& q, const HeadMap& o, const HeadMap& k, const HeadMap& v, const Params& p, int device,
                    cudaStream_t s) {
     using C = Cfg<DKC, DVC>;
     const XattnArgs& a = p.a;
-    bool& set = g_attr[device][(DKC - 1) * 2 + DVC - 1];
+    std::atomic<bool>& set = g_attr[device][(DKC - 1) * 2 + DVC - 1];
     cudaError_t e = cudaSuccess;
     if (!set) {
         e = cudaFuncSetAttribute(k_xattn_dkv_tc<DKC, DVC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);

@@ -22,6 +22,7 @@
 // MMA issuer, 9 TMA, 10 masks.  Every wait is bounded.
 
 #include <algorithm>
+#include <atomic>
 
 #include "gs_xattn_tc.cuh"
 
@@ -497,12 +498,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
 }
 
-bool g_attr[64][8];
+std::atomic<bool> g_attr[64][8];
 
 template <int DKC, int DVC, bool PAIR>
 cudaError_t launch(const HeadMap& q, const HeadMap& k, const HeadMap& v, const Params& p, int sms, int device, cudaStream_t s) {
     using C = Cfg<DKC, DVC, PAIR>;
-    bool& set = g_attr[device][(DKC - 1) * 4 + (DVC - 1) * 2 + PAIR];
+    std::atomic<bool>& set = g_attr[device][(DKC - 1) * 4 + (DVC - 1) * 2 + PAIR];
     if (!set) {
         cudaError_t e = cudaFuncSetAttribute(k_xattn_tc<DKC, DVC, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                              (int)C::kSmem);

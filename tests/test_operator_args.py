@@ -142,3 +142,41 @@ def test_stream_of_another_device(g):
 
     with pytest.raises(ValueError, match="cuda:0"):
         g._on_stream(torch.device("cuda", 0), Stream())
+
+
+def test_arrays_off_their_elements(g):
+    """A pointer between two elements would fault the kernels: refused before any device is asked for."""
+    L = g.load_library()
+    n = ctypes.c_longlong()
+    for dt, off in ((0, 2), (0, 1), (1, 1)):
+        good = [heads(g, 4096) for _ in range(8)]
+        for i in range(4):
+            hs = list(good[:4])
+            hs[i] = heads(g, 4096 + off)
+            assert forward(g, attn(g, dtype=dt), *hs) == g.GS_ERR_ALIGNMENT
+        for i in range(8):
+            hs = list(good)
+            hs[i] = heads(g, 4096 + off)
+            assert L.gs_cross_attention_backward(ctypes.byref(attn(g, dtype=dt)), *map(ctypes.byref, hs[:4]), 4096,
+                                                 *map(ctypes.byref, hs[4:]), None, 0, None) == g.GS_ERR_ALIGNMENT
+    for lse in (4097, 4098):
+        assert L.gs_cross_attention(ctypes.byref(attn(g)), *map(ctypes.byref, good[:4]), lse, None, 0, None) == g.GS_ERR_ALIGNMENT
+    assert L.gs_cross_attention_workspace(ctypes.byref(attn(g, key_lens=4098)), 0, ctypes.byref(n)) == g.GS_ERR_ALIGNMENT
+    how = g._Sampling(1.0, 1.0, 0.0, 0)
+    for i in range(4):
+        p = [4096] * 4
+        p[i] += 2
+        assert L.gs_sample_scores(p[0], 0, 4, 10, 10, ctypes.byref(how), *p[1:], None) == g.GS_ERR_ALIGNMENT
+    assert L.gs_sample_scores(4097, 1, 4, 10, 10, ctypes.byref(how), 4096, 4096, 4096, None) == g.GS_ERR_ALIGNMENT
+    for name in ("temperature_rows", "top_p_rows", "min_p_rows", "top_k_rows"):
+        how = g._Sampling(1.0, 1.0, 0.0, 0)
+        setattr(how, name, 4098)
+        assert L.gs_sample_scores(4096, 0, 4, 10, 10, ctypes.byref(how), 4096, 4096, 4096, None) == g.GS_ERR_ALIGNMENT
+
+
+def test_scale_past_fp32(g):
+    """scale * log2(e) has to be an fp32 number, else every logit of 0 would become NaN."""
+    assert forward(g, attn(g, scale=3e38)) == g.GS_ERR_INVALID_ARG
+    n = ctypes.c_longlong()
+    assert g.load_library().gs_cross_attention_workspace(ctypes.byref(attn(g, scale=2.5e38)), 1, ctypes.byref(n)) == g.GS_ERR_INVALID_ARG
+    assert forward(g, attn(g, scale=2e38, B=0)) == g.GS_OK
