@@ -189,20 +189,20 @@ static __device__ __forceinline__ void valid_words(uint32_t (&w)[W], const Xattn
         w[i] = __ballot_sync(0xffffffffu, ok);
     }
 }
-// zeroes the rows of a tile of `chunks` chunks whose bit is clear (a whole warp; generic-proxy writes)
+// zeroes the rows of a tile of `chunks` chunks whose bit is clear (a whole warp, four rows at a time; generic-proxy writes)
 static __device__ __forceinline__ void zero_rows(uint8_t* tile, int chunks, const uint32_t (&w)[4]) {
     const int lane = threadIdx.x & 31;
+    for (int c = 0; c < chunks; ++c)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint32_t bad = ~w[i];
-        while (bad) {
-            const int r = 32 * i + __ffs(bad) - 1;
-            bad &= bad - 1;
-            if (lane < 8 * chunks)
-                *reinterpret_cast<uint4*>(tile + (size_t)(lane >> 3) * kChunkBytes + r * 128 + (lane & 7) * 16) =
-                    make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < 4; ++i) {
+            if (w[i] == 0xffffffffu) continue;
+            const uint32_t bits = w[i] >> (lane >> 3);
+#pragma unroll
+            for (int r = 0; r < 32; r += 4)
+                if (!(bits >> r & 1u))
+                    *reinterpret_cast<uint4*>(tile + (size_t)c * kChunkBytes + (32 * i + r + (lane >> 3)) * 128 + (lane & 7) * 16) =
+                        make_uint4(0, 0, 0, 0);
         }
-    }
 }
 
 // A tensor map over a (B, L, H, width) bf16 array, axes (width, H, L, B), box {64, bh, bl, 1}.  A batch (or head) stride of 0
