@@ -83,17 +83,17 @@ struct Cfg {
     static_assert(96 * (DKC + DVC) + 128 * kBuffers <= 512 && 96 * DKC + 32 * DVC + 256 <= 512, "TMEM");
 };
 
-// The row at `row` (w elements, zeros where !has) into columns [taddr, + CHUNKS * 32) of this thread's lane: the part of the
-// warp with number `part` of four that share the lanes.
+// The part with number `part` of four of the row at `row` (w elements, zeros where !has): bf16 pairs, CHUNKS * 8 words.
 template <int CHUNKS>
-__device__ __forceinline__ void keep_row(uint32_t taddr, const __nv_bfloat16* row, int w, bool has, int part) {
+__device__ __forceinline__ void load_row(uint32_t (&x)[CHUNKS][8], const __nv_bfloat16* row, int w, bool has, int part) {
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) {
-        const int e = c * kChunk + part * 16;
-        uint32_t x[8];
-        load_words(x, row, e, w, has);
-        tmem_st8(taddr + (uint32_t)(e / 2), x);
-    }
+    for (int c = 0; c < CHUNKS; ++c) load_words(x[c], row, c * kChunk + part * 16, w, has);
+}
+// into columns [taddr, + CHUNKS * 32) of this thread's lane, which four warps share
+template <int CHUNKS>
+__device__ __forceinline__ void keep_row(uint32_t taddr, const uint32_t (&x)[CHUNKS][8], int part) {
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) tmem_st8(taddr + (uint32_t)((c * kChunk + part * 16) / 2), x[c]);
 }
 
 // -lse log2 e of a row: -inf where the row has no weight (P = 0); a NaN or +inf lse gives NaN, as the forward result is
@@ -101,20 +101,7 @@ __device__ __forceinline__ float neg_lse2(float lse) {
     return lse == -INFINITY ? -INFINITY : lse == INFINITY ? NAN : -lse * kLog2e;
 }
 
-// 32 fp32 columns of this thread's lane as bf16 to global (or zeros)
-__device__ __forceinline__ void store32(__nv_bfloat16* dst, const float* v, int left, bool vec) {
-    if (vec) {
-#pragma unroll
-        for (int e = 0; e < 32; e += 8)
-            if (e < left)
-                *reinterpret_cast<uint4*>(dst + e) = make_uint4(pack_bf16(v[e], v[e + 1]), pack_bf16(v[e + 2], v[e + 3]),
-                                                                pack_bf16(v[e + 4], v[e + 5]), pack_bf16(v[e + 6], v[e + 7]));
-    } else {
-#pragma unroll
-        for (int e = 0; e < 32; ++e)
-            if (e < left) dst[e] = __float2bfloat16_rn(v[e]);
-    }
-}
+// 32 fp32 columns of this thread's lane to global
 __device__ __forceinline__ void store32(float* dst, const float* v, int left, bool vec) {
     if (vec) {
 #pragma unroll
@@ -135,11 +122,17 @@ __device__ __forceinline__ void drain_acc(uint32_t taddr, int c0, int c1, int co
         if (any) tmem_ld32(taddr + (uint32_t)q, v);
 #pragma unroll
         for (int e = 0; e < 32; ++e) v[e] = any && keep ? v[e] * mul : 0.f;
-        if (mine) {
-            if (part)
-                store32(part + q, v, cols - q, cols % 4 == 0);
-            else
-                store32(out + q, v, cols - q, vec);
+        if (part) {
+            if (mine) store32(part + q, v, cols - q, cols % 4 == 0);
+        } else if (vec) {
+            uint32_t w[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+            store_rows(out + q, w, cols - q, mine);
+        } else if (mine) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+                if (q + e < cols) out[q + e] = __float2bfloat16_rn(v[e]);
         }
     }
 }
@@ -219,6 +212,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     const long long t0 = p.rtiles * part / a.rsplits, t1 = p.rtiles * (part + 1) / a.rsplits;
     const int nt = uniform(j0 < n ? (int)(t1 - t0) : 0);  // row tiles
 
+    // the softmax warps' parts of K and V, on their way while the CTA is set up
+    uint32_t kx[DKC][8], vx[DVC][8];
+    if (warp < kSoftWarps && nt > 0) {
+        const int j = j0 + (warp & 3) * 32 + lane;
+        const long long jj = j < a.Lk ? j : 0;
+        load_row(kx, reinterpret_cast<const __nv_bfloat16*>(a.k.p) + b * a.k.b + jj * a.k.l + hk * a.k.h, a.dk, j < a.Lk, warp >> 2);
+        load_row(vx, reinterpret_cast<const __nv_bfloat16*>(a.v.p) + b * a.v.b + jj * a.v.l + hk * a.v.h, a.dv, j < a.Lk, warp >> 2);
+    }
     if (threadIdx.x == 0) {
         mbar_init(&c.own_full, kSoftWarps);
         for (int s = 0; s < ST; ++s) {
@@ -346,11 +347,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool whole = __all_sync(0xffffffffu, valid);
         const float cs = a.scale * kLog2e;
         if (nt > 0) {
-            const long long jj = j < a.Lk ? j : 0;
-            keep_row<DKC>(t_k + lane_base, reinterpret_cast<const __nv_bfloat16*>(a.k.p) + b * a.k.b + jj * a.k.l + hk * a.k.h,
-                          a.dk, j < a.Lk, warp >> 2);
-            keep_row<DVC>(t_v + lane_base, reinterpret_cast<const __nv_bfloat16*>(a.v.p) + b * a.v.b + jj * a.v.l + hk * a.v.h,
-                          a.dv, j < a.Lk, warp >> 2);
+            keep_row(t_k + lane_base, kx, warp >> 2);
+            keep_row(t_v + lane_base, vx, warp >> 2);
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
@@ -480,6 +478,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int nt = uniform(max(0, t1 - t0));  // key tiles
     const bool fix = a.lens != nullptr || a.mask != nullptr;
 
+    // the softmax warps' parts of Q and dO, on their way while the CTA is set up
+    uint32_t qx[DKC][8], ox[DVC][8];
+    if (warp < kSoftWarps && nt > 0) {
+        const int r = (warp & 3) * 32 + lane, l = r / a.G;
+        const bool mine = r < tile_rows && rt * tile_rows + r < a.rows;
+        const long long ql = mine ? rt * p.nl + l : 0;
+        const int hq = hk * a.G + (mine ? r - l * a.G : 0);
+        load_row(qx, reinterpret_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.b + ql * a.q.l + hq * a.q.h, a.dk, mine, warp >> 2);
+        load_row(ox, reinterpret_cast<const __nv_bfloat16*>(a.dO.p) + b * a.dO.b + ql * a.dO.l + hq * a.dO.h, a.dv, mine, warp >> 2);
+    }
     if (threadIdx.x == 0) {
         mbar_init(&c.own_full, kSoftWarps);
         for (int s = 0; s < ST; ++s) {
@@ -612,10 +620,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool none = nl == -INFINITY;  // no row, or one without weight
         const bool exact = a.splits == 1 && nt == 1;
         if (nt > 0) {
-            keep_row<DKC>(t_q + lane_base, reinterpret_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.b + ql * a.q.l + hq * a.q.h,
-                          a.dk, mine, warp >> 2);
-            keep_row<DVC>(t_do + lane_base, reinterpret_cast<const __nv_bfloat16*>(a.dO.p) + b * a.dO.b + ql * a.dO.l + hq * a.dO.h,
-                          a.dv, mine, warp >> 2);
+            keep_row(t_q + lane_base, qx, warp >> 2);
+            keep_row(t_do + lane_base, ox, warp >> 2);
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();

@@ -446,8 +446,15 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] = v[e] * fo + u[e] * f1;
                     }
-                    if (!mine) continue;
                     const int w = a.dv - 32 * q;  // columns left
+                    if (a.splits == 1 && p.o_vec) {
+                        uint32_t u[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) u[e] = pack_bf16(v[2 * e] * inv, v[2 * e + 1] * inv);
+                        store_rows(out + 32 * q, u, w, mine);
+                        continue;
+                    }
+                    if (!mine) continue;
                     if (a.splits > 1) {
                         if (a.dv % 4 == 0) {
 #pragma unroll
@@ -459,13 +466,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                             for (int e = 0; e < 32; ++e)
                                 if (e < w) po[32 * q + e] = v[e];
                         }
-                    } else if (p.o_vec) {
-#pragma unroll
-                        for (int e = 0; e < 32; e += 8)
-                            if (e < w)
-                                *reinterpret_cast<uint4*>(out + 32 * q + e) =
-                                    make_uint4(pack_bf16(v[e] * inv, v[e + 1] * inv), pack_bf16(v[e + 2] * inv, v[e + 3] * inv),
-                                               pack_bf16(v[e + 4] * inv, v[e + 5] * inv), pack_bf16(v[e + 6] * inv, v[e + 7] * inv));
                     } else {
 #pragma unroll
                         for (int e = 0; e < 32; ++e)

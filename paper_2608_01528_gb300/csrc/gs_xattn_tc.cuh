@@ -175,6 +175,40 @@ static __device__ __forceinline__ void mul2(float& a0, float& a1, float b0, floa
         : "f"(b0), "f"(b1));
 }
 
+// 32 bf16 columns (16 words) of each lane's row to global memory, a warp at once; `left` columns are there (a multiple of 8), rows
+// start on 16-byte boundaries, lanes without `mine` have none.  Lane after lane would store 16 bytes to 32 rows, 32 wavefronts an
+// instruction (3,100 clocks for 128 keys' dK and dV of 64); four lanes exchange their pieces, so that they store 64 bytes of a row.
+static __device__ __forceinline__ void store_rows(__nv_bfloat16* row, const uint32_t (&p)[16], int left, bool mine) {
+    const int lane = threadIdx.x & 31;
+    const bool odd = lane & 1, high = lane & 2;
+    uint32_t x[2][4], y[2][4], z[4][4];  // piece lane % 2 (x) and 2 + lane % 2 (y) of the even and the odd row; lane % 4 of four rows
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t a = __shfl_xor_sync(0xffffffffu, odd ? p[e] : p[4 + e], 1);
+        const uint32_t b = __shfl_xor_sync(0xffffffffu, odd ? p[8 + e] : p[12 + e], 1);
+        x[0][e] = odd ? a : p[e];
+        x[1][e] = odd ? p[4 + e] : a;
+        y[0][e] = odd ? b : p[8 + e];
+        y[1][e] = odd ? p[12 + e] : b;
+    }
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t a = __shfl_xor_sync(0xffffffffu, high ? x[r][e] : y[r][e], 2);
+            z[r][e] = high ? a : x[r][e];
+            z[2 + r][e] = high ? y[r][e] : a;
+        }
+    const unsigned rows = __ballot_sync(0xffffffffu, mine);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int from = (lane & ~3) + r;
+        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row), from));
+        if ((rows >> from & 1u) && (lane & 3) * 8 < left)
+            *reinterpret_cast<uint4*>(dst + (lane & 3) * 8) = make_uint4(z[r][0], z[r][1], z[r][2], z[r][3]);
+    }
+}
+
 static __device__ __forceinline__ int keys_of(const XattnArgs& a, int b) {
     return a.lens ? min(max(__ldg(a.lens + b), 0), a.Lk) : a.Lk;
 }
