@@ -319,8 +319,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int k = 0; k < steps; ++k, ++taken) {
                 const int j0 = (im.t0 + (PAIR ? k : 2 * k + t)) * kTile;
                 uint32_t w[4];
-                const bool whole = j0 + kTile <= im.n && !a.mask;
-                if (busy && !whole) valid_words(w, a, im.b, j0, im.n);
+                bool whole = j0 + kTile <= im.n && !a.mask;
+                if (busy && !whole) {
+                    valid_words(w, a, im.b, j0, im.n);
+                    whole = (w[0] & w[1] & w[2] & w[3]) == 0xffffffffu;
+                }
                 if (!mbar_wait_warp_inline(&c.s_full[t], taken & 1u, abort_flag, err)) {
                     ok = false;
                     break;
