@@ -137,50 +137,54 @@ __device__ __forceinline__ void drain_acc(uint32_t taddr, int c0, int c1, int co
     }
 }
 
-// Statistics of every row tile of a key head: slots without a row get (-inf, 0).  16 threads a row, 8 columns each, 32 slots
-// a block.  Bound by reading O and dO once.
+// Statistics of every row tile of a key head: slots without a row get (-inf, 0).  16 threads a row, 8 columns each, four rows
+// in flight a thread, 64 slots a block.  Bound by the latency of its loads (8 x 1,024 rows of 16 heads of 64, 34 MB: 15 us; two rows in flight and lse read last 17).
+constexpr int kStatRows = 4, kStatBlocks = kTile / (16 * kStatRows);
 __global__ void __launch_bounds__(256) k_xattn_stats(const XattnArgs a, int nl, long long rtiles, int vec) {
-    long long i = blockIdx.x >> 2;
+    long long i = blockIdx.x / kStatBlocks;
     float* dst = a.ws + i * kStats;
     const long long rt = i % rtiles;
     i /= rtiles;
     const int hk = (int)(i % a.Hkv), b = (int)(i / a.Hkv);
-    const int grp = (blockIdx.x & 3) * 32 + (threadIdx.x >> 4), ln = threadIdx.x & 15, c0 = ln * 8;
-    float acc[2];
+    const int grp = (blockIdx.x % kStatBlocks) * (16 * kStatRows) + (threadIdx.x >> 4), ln = threadIdx.x & 15, c0 = ln * 8;
+    float L[kStatRows], acc[kStatRows];
+    uint4 x[kStatRows], y[kStatRows];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < kStatRows; ++k) {
         const int r = grp + 16 * k, l = r / a.G, h = hk * a.G + r - l * a.G;
         const long long ql = rt * nl + l;
+        const bool row = l < nl && ql < a.Lq;
+        L[k] = -INFINITY;
         acc[k] = 0.f;
-        if (l >= nl || ql >= a.Lq || c0 >= a.dv) continue;
+        x[k] = y[k] = make_uint4(0, 0, 0, 0);
+        if (row && ln == 0) L[k] = a.lse[((long long)b * a.Hq + h) * a.Lq + ql];
+        if (!row || c0 >= a.dv) continue;
         const __nv_bfloat16* o = reinterpret_cast<const __nv_bfloat16*>(a.o.p) + b * a.o.b + ql * a.o.l + h * a.o.h + c0;
         const __nv_bfloat16* d = reinterpret_cast<const __nv_bfloat16*>(a.dO.p) + b * a.dO.b + ql * a.dO.l + h * a.dO.h + c0;
         if (vec) {
-            const uint4 x = __ldg(reinterpret_cast<const uint4*>(o)), y = __ldg(reinterpret_cast<const uint4*>(d));
-            const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                acc[k] = fmaf(__uint_as_float(xs[e] << 16), __uint_as_float(ys[e] << 16), acc[k]);
-                acc[k] = fmaf(__uint_as_float(xs[e] & 0xffff0000u), __uint_as_float(ys[e] & 0xffff0000u), acc[k]);
-            }
+            x[k] = __ldg(reinterpret_cast<const uint4*>(o));
+            y[k] = __ldg(reinterpret_cast<const uint4*>(d));
         } else {
             for (int e = 0; e < 8 && c0 + e < a.dv; ++e) acc[k] = fmaf(__bfloat162float(o[e]), __bfloat162float(d[e]), acc[k]);
         }
     }
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < kStatRows; ++k) {
+        if (vec) {
+            const uint32_t xs[4] = {x[k].x, x[k].y, x[k].z, x[k].w}, ys[4] = {y[k].x, y[k].y, y[k].z, y[k].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                acc[k] = fmaf(__uint_as_float(xs[e] << 16), __uint_as_float(ys[e] << 16), acc[k]);
+                acc[k] = fmaf(__uint_as_float(xs[e] & 0xffff0000u), __uint_as_float(ys[e] & 0xffff0000u), acc[k]);
+            }
+        }
 #pragma unroll
         for (int o = 8; o; o >>= 1) acc[k] += __shfl_xor_sync(0xffffffffu, acc[k], o);
-        const int r = grp + 16 * k, l = r / a.G, h = hk * a.G + r - l * a.G;
-        const long long ql = rt * nl + l;
         if (ln == 0) {
-            float L = -INFINITY, D = 0.f;
-            if (l < nl && ql < a.Lq) {
-                L = neg_lse2(a.lse[((long long)b * a.Hq + h) * a.Lq + ql]);
-                if (L != -INFINITY) D = -acc[k];
-            }
-            dst[r] = L;
-            dst[kTile + r] = D;
+            const int r = grp + 16 * k;
+            const float nl2 = neg_lse2(L[k]);
+            dst[r] = nl2;
+            dst[kTile + r] = nl2 == -INFINITY ? 0.f : -acc[k];
         }
     }
 }
@@ -789,7 +793,7 @@ cudaError_t launch_xattn_bwd_tc(const XattnArgs& a, int device, cudaStream_t s) 
     p.vmul = v.bmul;
     p.vhmul = v.hmul;
     const int vec = on_vectors(a.o, a.B, a.Lq, a.Hq, a.dv) && on_vectors(a.dO, a.B, a.Lq, a.Hq, a.dv);
-    k_xattn_stats<<<(unsigned)(4 * p.rtiles * a.Hkv * a.B), 256, 0, s>>>(a, p.nl, p.rtiles, vec);
+    k_xattn_stats<<<(unsigned)(kStatBlocks * p.rtiles * a.Hkv * a.B), 256, 0, s>>>(a, p.nl, p.rtiles, vec);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     const bool k2 = a.dk > kChunk, v2 = a.dv > kChunk;
