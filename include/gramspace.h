@@ -442,8 +442,11 @@ GS_API gs_status gs_cross_attention_workspace(const gs_attn* a, int backward, lo
  * size, overwritten; calls that may run at the same time (on two streams, or in two graphs that
  * may be launched together) need one each.
  * Tensor-core path: GS_BF16 with inputs on 16-byte boundaries, strides that are
- * multiples of 8 elements, and no stride of 0 along rows or (queries) heads; logits, statistics and sums in fp32, weights rounded to
- * bf16 for the product with the values.  Otherwise fp32 CUDA cores.  Results do not depend on
+ * multiples of 8 elements, and no stride of 0 along rows or (queries) heads; inputs whose width is not a
+ * multiple of 8 are copied to the workspace first (GS_PATH_AUTO: where four query rows or more share a key
+ * head).  Logits, statistics and sums in fp32, weights rounded to
+ * bf16 for the product with the values.  Otherwise fp32 CUDA cores; GS_PATH_AUTO takes them for a single row of
+ * width up to 64 as well.  Results do not depend on
  * what else runs, and a call repeated gives the same bits.
  * Errors: GS_ERR_INVALID_ARG (null pointer, unknown type or path, scale), GS_ERR_SHAPE
  * (sizes, strides, workspace too small), GS_ERR_ALIGNMENT (a forced

@@ -945,6 +945,23 @@ void attn_plan(gs::XattnArgs& a, AttnPath path, int sms) {
         gs::xattn_simt_plan(a, false, sms);
 }
 
+// Floats of workspace for inputs that may have to be laid out again for the tensor cores.
+long long attn_pack_room(const gs::XattnArgs& a, bool backward, unsigned flags) {
+    if (flags == GS_PATH_SIMT || !gs::xattn_packs(a, backward, flags == GS_PATH_TENSOR)) return 0;
+    return gs::xattn_ws_pack(a, gs::xattn_pack_room(a, backward));
+}
+
+// Whether the tensor-core kernels take the call; pack: the inputs that are laid out again first.
+bool attn_on_tensor(const gs::XattnArgs& a, bool backward, unsigned flags, int& pack) {
+    pack = 0;
+    if (a.dtype != GS_BF16 || a.G > 128) return false;
+    const int need = gs::xattn_pack_need(a, backward);
+    if (need == 0) return true;
+    if ((need & ~gs::xattn_pack_room(a, backward)) || !gs::xattn_packs(a, backward, flags == GS_PATH_TENSOR)) return false;
+    pack = need;
+    return true;
+}
+
 gs_status attn_workspace(const float* ws, long long bytes, long long floats) {
     if (floats == 0) return GS_OK;
     if (!ws) return GS_ERR_INVALID_ARG;
@@ -969,10 +986,10 @@ gs_status gs_cross_attention_workspace(const gs_attn* p, int backward, long long
     for (int tc = 0; tc < (a.dtype == GS_BF16 && a.G <= 128 && a.Lk > 0 ? 2 : 1); ++tc) {
         if (backward) {
             tc ? gs::xattn_bwd_tc_plan(a, sms) : gs::xattn_simt_plan(a, true, sms);
-            floats = std::max(floats, gs::xattn_ws_backward(a));
+            floats = std::max(floats, gs::xattn_round4(gs::xattn_ws_backward(a)) + (tc ? attn_pack_room(a, true, p->flags) : 0));
         } else {
             attn_plan(a, attn_path(a, p->flags, tc != 0), sms);
-            floats = std::max(floats, gs::xattn_ws_forward(a));
+            floats = std::max(floats, gs::xattn_round4(gs::xattn_ws_forward(a)) + (tc ? attn_pack_room(a, false, p->flags) : 0));
         }
     }
     *bytes = 4 * floats;
@@ -998,12 +1015,16 @@ gs_status gs_cross_attention(const gs_attn* p, const gs_heads* Q, const gs_heads
     a.lse = lse;
     a.ws = (float*)workspace;
     cudaStream_t s = (cudaStream_t)stream;
-    const bool tc_ok = gs::xattn_tc_supported(a);
+    int pack = 0;
+    const bool tc_ok = attn_on_tensor(a, false, p->flags, pack);
     if (p->flags == GS_PATH_TENSOR && !tc_ok)
         return a.dtype != GS_BF16 || a.G > 128 ? GS_ERR_UNSUPPORTED : GS_ERR_ALIGNMENT;
     const AttnPath path = attn_path(a, p->flags, tc_ok && a.Lk > 0);
     attn_plan(a, path, sms);
-    if ((st = attn_workspace(a.ws, workspace_bytes, gs::xattn_ws_forward(a))) != GS_OK) return st;
+    const long long own = gs::xattn_round4(gs::xattn_ws_forward(a));
+    if (path != ATTN_TC) pack = 0;
+    if ((st = attn_workspace(a.ws, workspace_bytes, own + gs::xattn_ws_pack(a, pack))) != GS_OK) return st;
+    if (pack && (st = from_cuda(gs::launch_xattn_pack(a, pack, a.ws + own, s))) != GS_OK) return st;
     return from_cuda(path == ATTN_TC     ? gs::launch_xattn_tc(a, sms, dev, s)
                      : path == ATTN_ROWS ? gs::launch_xattn_rows(a, s)
                                          : gs::launch_xattn_simt(a, s));
@@ -1035,16 +1056,19 @@ gs_status gs_cross_attention_backward(const gs_attn* p, const gs_heads* Q, const
     a.lse = const_cast<float*>(lse);
     a.ws = (float*)workspace;
     cudaStream_t s = (cudaStream_t)stream;
-    const bool tc_ok = gs::xattn_bwd_tc_supported(a);
+    int pack = 0;
+    const bool tc_ok = attn_on_tensor(a, true, p->flags, pack);
     if (p->flags == GS_PATH_TENSOR && !tc_ok)
         return a.dtype != GS_BF16 || a.G > 128 ? GS_ERR_UNSUPPORTED : GS_ERR_ALIGNMENT;
     if (tc_ok && p->flags != GS_PATH_SIMT && a.Lq > 0 && a.Lk > 0) {
         gs::xattn_bwd_tc_plan(a, sms);
-        if ((st = attn_workspace(a.ws, workspace_bytes, gs::xattn_ws_backward(a))) != GS_OK) return st;
+        const long long own = gs::xattn_round4(gs::xattn_ws_backward(a));
+        if ((st = attn_workspace(a.ws, workspace_bytes, own + gs::xattn_ws_pack(a, pack))) != GS_OK) return st;
+        if (pack && (st = from_cuda(gs::launch_xattn_pack(a, pack, a.ws + own, s))) != GS_OK) return st;
         return from_cuda(gs::launch_xattn_bwd_tc(a, dev, s));
     }
     gs::xattn_simt_plan(a, true, sms);
-    if ((st = attn_workspace(a.ws, workspace_bytes, gs::xattn_ws_backward(a))) != GS_OK) return st;
+    if ((st = attn_workspace(a.ws, workspace_bytes, gs::xattn_round4(gs::xattn_ws_backward(a)))) != GS_OK) return st;
     return from_cuda(gs::launch_xattn_simt_backward(a, s));
 }
 

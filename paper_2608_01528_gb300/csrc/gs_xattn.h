@@ -76,16 +76,25 @@ cudaError_t launch_xattn_join_dq(const XattnArgs& a, cudaStream_t s);
 cudaError_t launch_xattn_join_dkv(const XattnArgs& a, cudaStream_t s);
 
 // ----------------------------------------------------------------- tcgen05 (gs_xattn_tc.cu)
-// bf16, at most 128 query heads to a key head, Q, K, V on 16-byte boundaries with strides in multiples of 8
-bool xattn_tc_supported(const XattnArgs& a);
+// bf16, at most 128 query heads to a key head, inputs on 16-byte boundaries with strides in multiples of 8
 void xattn_tc_plan(XattnArgs& a, int sms);
 cudaError_t launch_xattn_tc(const XattnArgs& a, int sms, int device, cudaStream_t s);
 unsigned take_device_error_xattn();
-// the gradient (gs_xattn_bwd_tc.cu); dO as Q
-bool xattn_bwd_tc_supported(const XattnArgs& a);
+// the gradient (gs_xattn_bwd_tc.cu)
 void xattn_bwd_tc_plan(XattnArgs& a, int sms);
 cudaError_t launch_xattn_bwd_tc(const XattnArgs& a, int device, cudaStream_t s);
 unsigned take_device_error_xbwd();
+
+// ----------------------------------------------------------------- odd widths for the tensor cores (gs_xattn_pack.cu)
+enum { kPackQ = 1, kPackK = 2, kPackV = 4, kPackDO = 8 };
+// whether inputs may be laid out again for this call; which arrays the workspace has room for (by their widths); which a
+// tensor map cannot describe as they lie
+bool xattn_packs(const XattnArgs& a, bool backward, bool forced);
+int xattn_pack_room(const XattnArgs& a, bool backward);
+int xattn_pack_need(const XattnArgs& a, bool backward);
+long long xattn_ws_pack(const XattnArgs& a, int which);  // floats
+// copies the arrays `which` to `room` and turns a's views to them
+cudaError_t launch_xattn_pack(XattnArgs& a, int which, float* room, cudaStream_t s);
 
 // ----------------------------------------------------------------- sampling (gs_sample.cu)
 struct SampleArgs {

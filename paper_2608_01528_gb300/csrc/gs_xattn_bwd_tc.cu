@@ -759,10 +759,6 @@ unsigned take_device_error_xbwd() {
     return v;
 }
 
-bool xattn_bwd_tc_supported(const XattnArgs& a) {
-    return xattn_tc_supported(a) && map_supported(a.dO, a.B, a.Lq, a.Hq) && (a.Hq <= 1 || a.dO.h > 0);
-}
-
 void xattn_bwd_tc_plan(XattnArgs& a, int sms) {
     const long long nl = kTile / a.G;
     const long long kt = (a.Lk + kTile - 1) / kTile, rt = (a.Lq + nl - 1) / nl;

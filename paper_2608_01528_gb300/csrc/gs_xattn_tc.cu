@@ -535,11 +535,6 @@ unsigned take_device_error_xattn() {
     return v;
 }
 
-bool xattn_tc_supported(const XattnArgs& a) {
-    return a.dtype == GS_BF16 && a.G <= kTile && map_supported(a.q, a.B, a.Lq, a.Hq) && (a.Hq <= 1 || a.q.h > 0) &&
-           map_supported(a.k, a.B, a.Lk, a.Hkv) && map_supported(a.v, a.B, a.Lk, a.Hkv);
-}
-
 void xattn_tc_plan(XattnArgs& a, int sms) {
     const long long tile_rows = (long long)(kTile / a.G) * a.G;
     const long long kt = (a.Lk + kTile - 1) / kTile;

@@ -260,3 +260,66 @@ def test_first_call_of_a_process_is_captured(gs):
     root = str(pathlib.Path(__file__).resolve().parent.parent)
     r = subprocess.run([sys.executable, "-c", FIRST.format(root=root)], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("kind", ["none", "lens", "holes"])
+@pytest.mark.parametrize("width", [(68, 64), (64, 87), (47, 128), (33, 33), (1, 127), (7, 1)], ids=str)
+@pytest.mark.parametrize("shape", [(2, 40, 300, 4, 2), (3, 300, 70, 7, 1), (1, 17, 3000, 2, 2), (20, 129, 129, 8, 8)], ids=str)
+def test_odd_widths_on_tensor_cores(gs, shape, width, kind):
+    """bf16 widths that are no multiple of 8 are laid out again: dense, padded and broadcast inputs."""
+    (B, Lq, Lk, Hq, Hkv), (dk, dv) = shape, width
+    g = torch.Generator().manual_seed(dk + dv + Lk)
+    Q, K, V, dO = (rand(g, *s, dtype="bf16") for s in ((B, Lq, Hq, dk), (B, Lk, Hkv, dk), (B, Lk, Hkv, dv), (B, Lq, Hq, dv)))
+    lens = torch.randint(0, Lk + 1, (B,), generator=g, dtype=torch.int32).cuda() if kind == "lens" else None
+    mask = (torch.rand(B, Lk, generator=g) < 0.6).cuda() if kind == "holes" else None
+    ok = torch.ones(B, Lk, dtype=torch.bool)
+    if lens is not None:
+        ok &= torch.arange(Lk)[None] < lens.cpu()[:, None]
+    if mask is not None:
+        ok &= mask.cpu()
+    K[~ok.cuda()], V[~ok.cuda()] = math.nan, math.inf
+    scale = dk ** -0.5
+    r = Ref(Q, K, V, scale, lens, mask, True)
+    want = r.grad(dO)
+    forms = [(Q, K, V, dO)]
+    if kind == "none":  # rows padded to other lengths, heads first, one sequence's states for all
+        pad = [torch.full((*t.shape[:3], t.shape[3] + 5), math.nan, dtype=t.dtype, device="cuda") for t in (Q, K, V, dO)]
+        for p, t in zip(pad, (Q, K, V, dO)):
+            p[..., 3:3 + t.shape[3]] = t
+        forms.append(tuple(p[..., 3:3 + t.shape[3]] for p, t in zip(pad, (Q, K, V, dO))))
+        forms.append(tuple(t.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3) for t in (Q, K, V, dO)))
+    for q, k, v, d in forms:
+        # only widths that are no multiple of 8 are laid out again: a forced path with others off their 16 bytes is refused
+        off = any(t.shape[3] % 8 == 0 and t.data_ptr() % 16 for t in (q, k, v))
+        if off:
+            with pytest.raises(gs.GramSpaceError, match="ALIGNMENT"):
+                gs.cross_attention(q, k, v, path="tensor")
+        for path in ("auto",) if off else ("auto", "tensor"):
+            out = attend(gs, q, k, v, lens, mask, path, True)
+            O, lse = r.o.permute(0, 2, 1, 3).bfloat16().cuda(), r.lse.float().cuda()
+            got = gs.cross_attention_backward(q, k, v, O, lse, d, scale, key_lens=lens, key_mask=mask, path=path)
+            gs.stream_status()
+            for name, (w, tol) in want.items():
+                close(got[name], w, tol, name)
+            assert out["O"].shape == O.shape
+
+
+def test_odd_widths_broadcast_and_captured(gs):
+    g = torch.Generator().manual_seed(12)
+    Q, K, V, dO = rand(g, 3, 50, 4, 36, dtype="bf16"), rand(g, 1, 90, 1, 36, dtype="bf16"), rand(g, 1, 90, 1, 20, dtype="bf16"), \
+        rand(g, 20, dtype="bf16")
+    K, V, dO = K.expand(3, 90, 2, 36), V.expand(3, 90, 2, 20), dO.expand(3, 50, 4, 20)
+    out = attend(gs, Q, K, V)
+    got = gs.cross_attention_backward(Q, K, V, out["O"], out["lse"], dO)
+    r = Ref(Q, K, V, 1 / 6, None, None, True)
+    exact = gs.cross_attention_backward(Q, K, V, r.o.permute(0, 2, 1, 3).bfloat16().cuda(), r.lse.float().cuda(), dO)
+    for name, (w, tol) in r.grad(dO).items():
+        close(exact[name], w, tol, name)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o = gs.cross_attention(Q, K, V, want_lse=True)
+        b = gs.cross_attention_backward(Q, K, V, o["O"], o["lse"], dO)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(o[k], out[k]) for k in out) and all(torch.equal(b[k], got[k]) for k in got)
+    gs.stream_status()
