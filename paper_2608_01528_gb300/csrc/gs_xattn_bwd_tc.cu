@@ -19,9 +19,10 @@
 // w of a group reads lanes 32 (w % 4)..+31 and columns 32 (w / 4)..+31 of its half.  The rows'
 // statistics (-lse log2 e, -D) are laid out per row tile by k_xattn_stats, so that a tile's come with one copy.
 //
-// Measured at 2 sequences of 4,096 x 4,096, 32 / 8 heads of 128: dK and dV 0.71 ms, dQ 0.57 ms.  Each CTA reads 64 KB a tile,
-// 7 to 8 TB/s from L2 over all: that bounds both.  At width 64 (8 x 1,024 x 1,500, 16 heads: 114 and 106 us) the way of a
-// tile from S to dQ and a CTA's start and end do.
+// Measured at 2 sequences of 4,096 x 4,096, 32 / 8 heads of 128: dK and dV 0.71 ms, dQ 0.56 ms.  Each CTA reads 64 KB a tile,
+// 7 to 8 TB/s from L2 over all: that bounds both.  At width 64 (8 x 1,024 x 750..1,500, 16 heads: 109 and 88 us) a tile takes 1,580
+// and 1,470 clocks, its products 1,024, and a CTA's start and end 9,000 of 22,000 clocks.  (CTAs that go on with another
+// item spill in the loop over tiles, which has no register left: 230 us for the whole gradient instead of 207.)
 //
 // Keys that are not read: P = dS = 0, and in the second kernel their rows of K are zeroed in shared memory before
 // the MMA reads them (0 * NaN).  Rows past the end have lse = +inf: P = 0.
