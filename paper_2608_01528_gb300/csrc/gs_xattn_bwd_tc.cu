@@ -125,15 +125,14 @@ __device__ __forceinline__ void drain_acc(uint32_t taddr, int c0, int c1, int co
         for (int e = 0; e < 32; ++e) v[e] = any && keep ? v[e] * mul : 0.f;
         if (part) {
             if (mine) store32(part + q, v, cols - q, cols % 4 == 0);
-        } else if (vec) {
+        } else {
             uint32_t w[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
-            store_rows(out + q, w, cols - q, mine);
-        } else if (mine) {
-#pragma unroll
-            for (int e = 0; e < 32; ++e)
-                if (q + e < cols) out[q + e] = __float2bfloat16_rn(v[e]);
+            if (vec)
+                store_rows(out + q, w, cols - q, mine);
+            else
+                store_rows_any(out + q, w, cols - q, mine);
         }
     }
 }

@@ -2,8 +2,8 @@
 // attention: rows of round8(width) elements, zeros behind the width, so that every row starts on a 16-byte boundary.
 //
 // A copy costs one more read and a write of the inputs; the products that it makes room for run many times as fast as on CUDA
-// cores: 35 x 1,472 x 384, 28 / 4 heads of 32 and 87: 1.36 ms against 4.53; gradient of 26 x 704 x 1,536, 2 / 1 heads of
-// 68 and 64: 0.13 against 1.89; 32 x 20 x 4,000, 8 heads of 100: 0.27 against 0.97, 4 rows 0.27 against 0.36.  Below that the CUDA cores
+// cores: 35 x 1,472 x 384, 28 / 4 heads of 32 and 87: 0.46 ms against 4.53; gradient of 26 x 704 x 1,536, 2 / 1 heads of
+// 68 and 64: 0.10 against 1.89; 32 x 20 x 4,000, 8 heads of 100: 0.27 against 0.97, 4 rows 0.27 against 0.36.  Below that the CUDA cores
 // read the memory once, in less than the copies take.  One launch for all arrays; a thread writes 16 bytes.
 
 #include <algorithm>

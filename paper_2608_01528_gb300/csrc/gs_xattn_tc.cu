@@ -455,29 +455,26 @@ __global__ void __launch_bounds__(kThreads, 1)
                         for (int e = 0; e < 32; ++e) v[e] = v[e] * fo + u[e] * f1;
                     }
                     const int w = a.dv - 32 * q;  // columns left
-                    if (a.splits == 1 && p.o_vec) {
+                    if (a.splits == 1) {
                         uint32_t u[16];
 #pragma unroll
                         for (int e = 0; e < 16; ++e) u[e] = pack_bf16(v[2 * e] * inv, v[2 * e + 1] * inv);
-                        store_rows(out + 32 * q, u, w, mine);
+                        if (p.o_vec)
+                            store_rows(out + 32 * q, u, w, mine);
+                        else
+                            store_rows_any(out + 32 * q, u, w, mine);
                         continue;
                     }
                     if (!mine) continue;
-                    if (a.splits > 1) {
-                        if (a.dv % 4 == 0) {
+                    if (a.dv % 4 == 0) {
 #pragma unroll
-                            for (int e = 0; e < 32; e += 4)
-                                if (e < w)
-                                    *reinterpret_cast<float4*>(po + 32 * q + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 32; ++e)
-                                if (e < w) po[32 * q + e] = v[e];
-                        }
+                        for (int e = 0; e < 32; e += 4)
+                            if (e < w)
+                                *reinterpret_cast<float4*>(po + 32 * q + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
                     } else {
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
-                            if (e < w) out[32 * q + e] = __float2bfloat16_rn(v[e] * inv);
+                            if (e < w) po[32 * q + e] = v[e];
                     }
                 }
                 if (mine) {

@@ -209,6 +209,39 @@ static __device__ __forceinline__ void store_rows(__nv_bfloat16* row, const uint
     }
 }
 
+// The same for rows on any boundary and any number of columns: the 16 lanes of a half warp exchange their words until each has
+// one word of 16 rows, so that they store 64 bytes of a row together (32 columns element by element: 1,024 wavefronts, so 64).
+static __device__ __forceinline__ void store_rows_any(__nv_bfloat16* row, uint32_t (&p)[16], int left, bool mine) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int bit = 1; bit < 16; bit <<= 1)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            if (i & bit) continue;
+            const bool up = lane & bit;
+            const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? p[i] : p[i | bit], bit);
+            if (up)
+                p[i] = got;
+            else
+                p[i | bit] = got;
+        }
+    const unsigned rows = __ballot_sync(0xffffffffu, mine);
+    const int c = 2 * (lane & 15);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const int from = (lane & 16) + r;
+        unsigned short* dst = reinterpret_cast<unsigned short*>(
+            __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row), from));
+        if (!(rows >> from & 1u)) continue;
+        if (c + 1 < left && (reinterpret_cast<uintptr_t>(dst) & 3) == 0) {
+            *reinterpret_cast<uint32_t*>(dst + c) = p[r];
+        } else {
+            if (c < left) dst[c] = (unsigned short)p[r];
+            if (c + 1 < left) dst[c + 1] = (unsigned short)(p[r] >> 16);
+        }
+    }
+}
+
 static __device__ __forceinline__ int keys_of(const XattnArgs& a, int b) {
     return a.lens ? min(max(__ldg(a.lens + b), 0), a.Lk) : a.Lk;
 }
