@@ -86,12 +86,13 @@ __device__ __forceinline__ float4 load4(const __nv_bfloat16* p, int left, bool v
     return make_float4(left > 0 ? to_f32(p[0]) : 0.f, left > 1 ? to_f32(p[1]) : 0.f, left > 2 ? to_f32(p[2]) : 0.f,
                        left > 3 ? to_f32(p[3]) : 0.f);
 }
-// 64 packed rows from r0, D floats each (zero past the width w and past the last row): four threads a row, so that a row's
+// R packed rows from r0, D floats each (zero past the width w and past the last row): four threads a row, so that a row's
 // address is worked out once.
-template <typename T, int D>
+template <typename T, int D, int R = kTile>
 __device__ __forceinline__ void load_rows(float* dst, const XattnArgs& a, const HeadView& v, int b, int hk,
                                           long long r0, int w, bool vec) {
     const int i = threadIdx.x >> 2, c0 = (threadIdx.x & 3) * 4;
+    if (i >= R) return;
     const bool has = r0 + i < a.rows;
     const T* p = row_at<T>(a, v, b, hk, has ? r0 + i : 0);
 #pragma unroll
@@ -116,18 +117,18 @@ __device__ __forceinline__ void load_valid(int* ok, const XattnArgs& a, int b, i
 }
 
 // acc[i][j] += <A row ty + 16 i, B row tx + 16 j>
-template <int D>
-__device__ __forceinline__ void dots(float (&acc)[4][4], const float* A, const float* B, int w) {
+template <int D, int RI>
+__device__ __forceinline__ void dots(float (&acc)[RI][4], const float* A, const float* B, int w) {
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
 #pragma unroll 4
     for (int d = 0; d < w; d += 4) {
-        float4 x[4], y[4];
+        float4 x[RI], y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const float4*>(A + (ty + 16 * i) * (D + 4) + d);
+        for (int i = 0; i < RI; ++i) x[i] = *reinterpret_cast<const float4*>(A + (ty + 16 * i) * (D + 4) + d);
 #pragma unroll
         for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4*>(B + (tx + 16 * j) * (D + 4) + d);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < RI; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 acc[i][j] = fmaf(x[i].x, y[j].x, acc[i][j]);
@@ -143,21 +144,21 @@ __device__ __forceinline__ int column(int q) {
     const int tx = threadIdx.x & 15;
     return D == 32 ? 2 * tx + q : 64 * (q / 4) + 4 * tx + q % 4;
 }
-// out[i][q] += sum_k W[ty + 16 i][k] X[k][column(q)] over a tile of 64
-template <int D>
-__device__ __forceinline__ void weigh(float (&out)[4][D / 16], const float* W, const float* X) {
+// out[i][q] += sum_k W[ty + 16 i][k] X[k][column(q)] over a tile of K
+template <int D, int K = kTile, int RI>
+__device__ __forceinline__ void weigh(float (&out)[RI][D / 16], const float* W, const float* X) {
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
 #pragma unroll 2
-    for (int k = 0; k < kTile; k += 4) {
-        float4 w[4];
+    for (int k = 0; k < K; k += 4) {
+        float4 w[RI];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const float4*>(W + (ty + 16 * i) * kPP + k);
+        for (int i = 0; i < RI; ++i) w[i] = *reinterpret_cast<const float4*>(W + (ty + 16 * i) * (K + 4) + k);
         if constexpr (D == 32) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const float2 x = *reinterpret_cast<const float2*>(X + (k + q) * (D + 4) + 2 * tx);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < RI; ++i) {
                     const float p = q == 0 ? w[i].x : q == 1 ? w[i].y : q == 2 ? w[i].z : w[i].w;
                     out[i][0] = fmaf(p, x.x, out[i][0]);
                     out[i][1] = fmaf(p, x.y, out[i][1]);
@@ -170,7 +171,7 @@ __device__ __forceinline__ void weigh(float (&out)[4][D / 16], const float* W, c
             for (int c = 0; c < D / 64; ++c) {
                 const float4 x = *reinterpret_cast<const float4*>(X + (k + q) * (D + 4) + 64 * c + 4 * tx);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < RI; ++i) {
                     const float p = q == 0 ? w[i].x : q == 1 ? w[i].y : q == 2 ? w[i].z : w[i].w;
                     out[i][4 * c + 0] = fmaf(p, x.x, out[i][4 * c + 0]);
                     out[i][4 * c + 1] = fmaf(p, x.y, out[i][4 * c + 1]);
@@ -350,11 +351,12 @@ __global__ void __launch_bounds__(256) k_xattn_delta(const XattnArgs a) {
 }
 
 // P and dS of a tile from S, dO V^T and the rows' statistics; a row without weight (lse = -inf) has P = 0
-__device__ __forceinline__ void tile_grad(float (&s)[4][4], float (&dp)[4][4], const int* ok, const float* lse2,
+template <int RI>
+__device__ __forceinline__ void tile_grad(float (&s)[RI][4], float (&dp)[RI][4], const int* ok, const float* lse2,
                                           const float* delta, float c) {
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < RI; ++i) {
         const float L = lse2[ty + 16 * i], D = delta[ty + 16 * i];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -364,9 +366,10 @@ __device__ __forceinline__ void tile_grad(float (&s)[4][4], float (&dp)[4][4], c
         }
     }
 }
-// lse (base 2; +inf: the row has no weight) and D of 64 packed rows
+// lse (base 2; +inf: the row has no weight) and D of R packed rows
+template <int R>
 __device__ __forceinline__ void load_stats(float* lse2, float* delta, const XattnArgs& a, int b, int hk, long long r0) {
-    if (threadIdx.x < kTile) {
+    if (threadIdx.x < R) {
         const long long r = r0 + threadIdx.x;
         float L = INFINITY, D = 0.f;
         if (r < a.rows) {
@@ -383,31 +386,36 @@ __device__ __forceinline__ void load_stats(float* lse2, float* delta, const Xatt
     }
 }
 
-template <int DK, int DV>
-constexpr size_t bwd_smem() {
-    return sizeof(float) * kTile * (2 * (DK + 4) + 2 * (DV + 4) + kPP);
+// Tiles of R rows: 64, or 16 where a key head has few (a tile's products are taken whole).  fp32, 17 x 832 keys, 16 / 64: 14 rows,
+// 16 key heads of 128 and 81, 499 / 948 us; 32 rows of 128 988 / 1,212; 20 rows of 64 438 / 425.
+int bwd_rows(const XattnArgs& a) { return a.rows <= 32 ? 16 : kTile; }
+
+template <int DK, int DV, int R>
+constexpr size_t bwd_smem() {  // weights: R x 64, or 64 keys x R
+    return sizeof(float) * ((kTile + R) * ((DK + 4) + (DV + 4)) + (R * kPP > kTile * (R + 4) ? R * kPP : kTile * (R + 4)));
 }
 
-template <typename T, int DK, int DV>
+template <typename T, int DK, int DV, int R>
 __global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long long tiles) {
     extern __shared__ float4 sm4[];
     float* Qs = reinterpret_cast<float*>(sm4);
-    float* Ks = Qs + kTile * (DK + 4);
+    float* Ks = Qs + R * (DK + 4);
     float* Vs = Ks + kTile * (DK + 4);
     float* Ds = Vs + kTile * (DV + 4);  // dO
-    float* Ws = Ds + kTile * (DV + 4);
+    float* Ws = Ds + R * (DV + 4);
     __shared__ int ok[kTile];
-    __shared__ float lse2[kTile], delta[kTile];
+    __shared__ float lse2[R], delta[R];
+    constexpr int RI = R / 16;
     const Block bl = block_of(tiles, a.splits, a.Hkv);
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-    const long long r0 = bl.tile * kTile;
+    const long long r0 = bl.tile * R;
     const int n = keys_of(a, bl.b);
     const int ktiles = (a.Lk + kTile - 1) / kTile;
     const int t0 = (int)((long long)ktiles * bl.part / a.splits), t1 = (int)((long long)ktiles * (bl.part + 1) / a.splits);
-    load_rows<T, DK>(Qs, a, a.q, bl.b, bl.hk, r0, a.dk, a.vec & kVecQ);
-    load_rows<T, DV>(Ds, a, a.dO, bl.b, bl.hk, r0, a.dv, a.vec & kVecDO);
-    load_stats(lse2, delta, a, bl.b, bl.hk, r0);
-    float o[4][DK / 16] = {};
+    load_rows<T, DK, R>(Qs, a, a.q, bl.b, bl.hk, r0, a.dk, a.vec & kVecQ);
+    load_rows<T, DV, R>(Ds, a, a.dO, bl.b, bl.hk, r0, a.dv, a.vec & kVecDO);
+    load_stats<R>(lse2, delta, a, bl.b, bl.hk, r0);
+    float o[RI][DK / 16] = {};
     for (int t = t0; t < t1 && t * kTile < n; ++t) {
         __syncthreads();
         load_valid(ok, a, bl.b, t * kTile, n);
@@ -415,14 +423,14 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long l
         load_keys<T, DK>(Ks, a.k, bl.b, bl.hk, t * kTile, a.dk, ok, a.vec & kVecK);
         load_keys<T, DV>(Vs, a.v, bl.b, bl.hk, t * kTile, a.dv, ok, a.vec & kVecV);
         __syncthreads();
-        float s[4][4] = {}, dp[4][4] = {};
+        float s[RI][4] = {}, dp[RI][4] = {};
         dots<DK>(s, Qs, Ks, a.dk);
         dots<DV>(dp, Ds, Vs, a.dv);
         if (a.splits == 1 && n <= kTile) {
             // every key of the sequence is here: D = sum_j P dP, for this kernel and the next (a bf16 O gives it to 2^-9 of
             // <dO, O> only, which with a few keys is more than dP - D)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < RI; ++i) {
                 const float L = lse2[ty + 16 * i];
                 float sum = 0.f;
 #pragma unroll
@@ -439,7 +447,7 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long l
         }
         tile_grad(s, dp, ok, lse2, delta, a.scale * kLog2e);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < RI; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) Ws[(ty + 16 * i) * kPP + tx + 16 * j] = dp[i][j];
         __syncthreads();
@@ -447,7 +455,7 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long l
     }
     const long long nrows = (long long)a.B * a.Hq * a.Lq;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < RI; ++i) {
         const long long r = r0 + ty + 16 * i;
         if (r >= a.rows) continue;
 #pragma unroll
@@ -462,21 +470,22 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long l
     }
 }
 
-template <typename T, int DK, int DV>
+template <typename T, int DK, int DV, int R>
 __global__ void __launch_bounds__(kThreads) k_xattn_dkv(const XattnArgs a, int ktiles) {
     extern __shared__ float4 sm4[];
     float* Qs = reinterpret_cast<float*>(sm4);
-    float* Ks = Qs + kTile * (DK + 4);
+    float* Ks = Qs + R * (DK + 4);
     float* Vs = Ks + kTile * (DK + 4);
     float* Ds = Vs + kTile * (DV + 4);
-    float* Ws = Ds + kTile * (DV + 4);  // P^T, then dS^T: [key][row]
+    float* Ws = Ds + R * (DV + 4);  // P^T, then dS^T: [key][row]
     __shared__ int ok[kTile];
-    __shared__ float lse2[kTile], delta[kTile];
+    __shared__ float lse2[R], delta[R];
+    constexpr int RI = R / 16, kPR = R + 4;
     const Block bl = block_of(ktiles, a.rsplits, a.Hkv);
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
     const int j0 = (int)bl.tile * kTile;
     const int n = keys_of(a, bl.b);
-    const long long rtiles = (a.rows + kTile - 1) / kTile;
+    const long long rtiles = (a.rows + R - 1) / R;
     long long t0 = rtiles * bl.part / a.rsplits, t1 = rtiles * (bl.part + 1) / a.rsplits;
     if (j0 >= n) t1 = t0;  // no key of the tile is read
     load_valid(ok, a, bl.b, j0, n);
@@ -486,27 +495,27 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dkv(const XattnArgs a, int k
     float ok_[4][DK / 16] = {}, ov[4][DV / 16] = {};
     for (long long t = t0; t < t1; ++t) {
         __syncthreads();
-        load_rows<T, DK>(Qs, a, a.q, bl.b, bl.hk, t * kTile, a.dk, a.vec & kVecQ);
-        load_rows<T, DV>(Ds, a, a.dO, bl.b, bl.hk, t * kTile, a.dv, a.vec & kVecDO);
-        load_stats(lse2, delta, a, bl.b, bl.hk, t * kTile);
+        load_rows<T, DK, R>(Qs, a, a.q, bl.b, bl.hk, t * R, a.dk, a.vec & kVecQ);
+        load_rows<T, DV, R>(Ds, a, a.dO, bl.b, bl.hk, t * R, a.dv, a.vec & kVecDO);
+        load_stats<R>(lse2, delta, a, bl.b, bl.hk, t * R);
         __syncthreads();
-        float s[4][4] = {}, dp[4][4] = {};
+        float s[RI][4] = {}, dp[RI][4] = {};
         dots<DK>(s, Qs, Ks, a.dk);
         dots<DV>(dp, Ds, Vs, a.dv);
         tile_grad(s, dp, ok, lse2, delta, a.scale * kLog2e);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < RI; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) Ws[(tx + 16 * j) * kPP + ty + 16 * i] = s[i][j];
+            for (int j = 0; j < 4; ++j) Ws[(tx + 16 * j) * kPR + ty + 16 * i] = s[i][j];
         __syncthreads();
-        weigh<DV>(ov, Ws, Ds);
+        weigh<DV, R>(ov, Ws, Ds);
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < RI; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) Ws[(tx + 16 * j) * kPP + ty + 16 * i] = dp[i][j];
+            for (int j = 0; j < 4; ++j) Ws[(tx + 16 * j) * kPR + ty + 16 * i] = dp[i][j];
         __syncthreads();
-        weigh<DK>(ok_, Ws, Qs);
+        weigh<DK, R>(ok_, Ws, Qs);
     }
     const long long nk = (long long)a.B * a.Hkv * a.Lk;
 #pragma unroll
@@ -565,25 +574,30 @@ cudaError_t forward(const XattnArgs& a, cudaStream_t s) {
     k_xattn<T, DK, DV><<<(unsigned)grid, kThreads, smem, s>>>(a, tiles);
     return cudaGetLastError();
 }
-template <typename T, int DK, int DV>
-cudaError_t backward(const XattnArgs& a, cudaStream_t s) {
-    const size_t smem = bwd_smem<DK, DV>();
+template <typename T, int DK, int DV, int R>
+cudaError_t backward_r(const XattnArgs& a, cudaStream_t s) {
+    const size_t smem = bwd_smem<DK, DV, R>();
     cudaError_t e = cudaSuccess;
     if (a.rows > 0) {
-        const long long tiles = (a.rows + kTile - 1) / kTile;
-        if ((e = allow_smem(k_xattn_dq<T, DK, DV>, smem)) != cudaSuccess) return e;
-        k_xattn_dq<T, DK, DV><<<(unsigned)(tiles * a.splits * a.Hkv * a.B), kThreads, smem, s>>>(a, tiles);
+        const long long tiles = (a.rows + R - 1) / R;
+        if ((e = allow_smem(k_xattn_dq<T, DK, DV, R>, smem)) != cudaSuccess) return e;
+        k_xattn_dq<T, DK, DV, R><<<(unsigned)(tiles * a.splits * a.Hkv * a.B), kThreads, smem, s>>>(a, tiles);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
         if (a.splits > 1 && (e = launch_xattn_join_dq(a, s)) != cudaSuccess) return e;
     }
     if (a.Lk > 0) {
         const int ktiles = (a.Lk + kTile - 1) / kTile;
-        if ((e = allow_smem(k_xattn_dkv<T, DK, DV>, smem)) != cudaSuccess) return e;
-        k_xattn_dkv<T, DK, DV><<<(unsigned)((long long)ktiles * a.rsplits * a.Hkv * a.B), kThreads, smem, s>>>(a, ktiles);
+        if ((e = allow_smem(k_xattn_dkv<T, DK, DV, R>, smem)) != cudaSuccess) return e;
+        k_xattn_dkv<T, DK, DV, R><<<(unsigned)((long long)ktiles * a.rsplits * a.Hkv * a.B), kThreads, smem, s>>>(a, ktiles);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
         if (a.rsplits > 1) e = launch_xattn_join_dkv(a, s);
     }
     return e;
+}
+
+template <typename T, int DK, int DV>
+cudaError_t backward(const XattnArgs& a, cudaStream_t s) {
+    return bwd_rows(a) == 16 ? backward_r<T, DK, DV, 16>(a, s) : backward_r<T, DK, DV, kTile>(a, s);
 }
 
 bool on_fours(const XattnArgs& a, const HeadView& v, int L, int H) {
@@ -624,7 +638,8 @@ cudaError_t launch_delta(const XattnArgs& a, cudaStream_t s) {
 }  // namespace
 
 void xattn_simt_plan(XattnArgs& a, bool backward, int sms) {
-    const long long rt = (a.rows + kTile - 1) / kTile, kt = (a.Lk + kTile - 1) / kTile;
+    const int R = backward ? bwd_rows(a) : kTile;
+    const long long rt = (a.rows + R - 1) / R, kt = (a.Lk + kTile - 1) / kTile;
     // up to four blocks a multiprocessor, and parts of two tiles or more
     a.splits = xattn_parts(rt * a.Hkv * a.B, kt, 4 * sms, 2);
     a.rsplits = backward ? xattn_parts(kt * a.Hkv * a.B, rt, 4 * sms, 2) : 1;
