@@ -138,7 +138,8 @@ __device__ __forceinline__ void drain_acc(uint32_t taddr, int c0, int c1, int co
 }
 
 // Statistics of every row tile of a key head: slots without a row get (-inf, 0).  16 threads a row, 8 columns each, four rows
-// in flight a thread, 64 slots a block.  Bound by the latency of its loads (8 x 1,024 rows of 16 heads of 64, 34 MB: 15 us; two rows in flight and lse read last 17).
+// in flight a thread, 64 slots a block.  Bound by instructions, mostly addresses (issue 69 %; 8 x 1,024 rows of 16 heads of 64, 34 MB: 15 us; two rows in flight and lse read
+// last 17).
 constexpr int kStatRows = 4, kStatBlocks = kTile / (16 * kStatRows);
 __global__ void __launch_bounds__(256) k_xattn_stats(const XattnArgs a, int nl, long long rtiles, int vec) {
     long long i = blockIdx.x / kStatBlocks;
