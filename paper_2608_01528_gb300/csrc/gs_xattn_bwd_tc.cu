@@ -21,7 +21,8 @@
 //
 // Measured at 2 sequences of 4,096 x 4,096, 32 / 8 heads of 128: dK and dV 0.71 ms, dQ 0.56 ms.  Each CTA reads 64 KB a tile,
 // 7 to 8 TB/s from L2 over all: that bounds both.  At width 64 (8 x 1,024 x 750..1,500, 16 heads: 109 and 88 us) a tile takes 1,580
-// and 1,470 clocks, its products 1,024, and a CTA's start and end 9,000 of 22,000 clocks.  (CTAs that go on with another
+// and 1,470 clocks, its products 1,024, and a CTA's start and end took 9,000 of 22,000 clocks before its own tiles came while it is
+// set up and results went out 64 bytes of a row at a time (221 -> 207 us for the whole gradient).  (CTAs that go on with another
 // item spill in the loop over tiles, which has no register left: 230 us for the whole gradient instead of 207.)
 //
 // Keys that are not read: P = dS = 0, and in the second kernel their rows of K are zeroed in shared memory before
@@ -138,8 +139,8 @@ __device__ __forceinline__ void drain_acc(uint32_t taddr, int c0, int c1, int co
 }
 
 // Statistics of every row tile of a key head: slots without a row get (-inf, 0).  16 threads a row, 8 columns each, four rows
-// in flight a thread, 64 slots a block.  Bound by instructions, mostly addresses (issue 69 %; 8 x 1,024 rows of 16 heads of 64, 34 MB: 15 us; two rows in flight and lse read
-// last 17).
+// in flight a thread, 64 slots a block.  Bound by instructions, mostly addresses (issue 69 %; 8 x 1,024 rows of 16 heads of 64,
+// 34 MB: 15 us; two rows in flight and lse read last 17).
 constexpr int kStatRows = 4, kStatBlocks = kTile / (16 * kStatRows);
 __global__ void __launch_bounds__(256) k_xattn_stats(const XattnArgs a, int nl, long long rtiles, int vec) {
     long long i = blockIdx.x / kStatBlocks;
