@@ -463,7 +463,8 @@ GS_API gs_status gs_cross_attention(const gs_attn* a, const gs_heads* Q, const g
  * D_i = <dO_i, O_i>, dS_ij = P_ij (<dO_i, V_j> - D_i),
  *     dV_j = sum_i P_ij dO_i,  dK_j = scale sum_i dS_ij Q_i,  dQ_i = scale sum_j dS_ij K_j,
  * the sums over i running over the query heads that share the key head.  O and
- * lse are the forward call's.  dQ, dK, dV have the shapes of Q, K, V and type dtype; keys
+ * lse are the forward call's (for bf16 sequences that end within a tile of keys, 128 or 64 by path, or
+ * whose mask leaves 16 keys or fewer, D_i is summed from P_ij <dO_i, V_j>, the same without O's rounding).  dQ, dK, dV have the shapes of Q, K, V and type dtype; keys
  * that are not valid get zeros, rows without a valid key zeros in dQ.  Where inputs repeat
  * memory (stride 0), the gradients still come one per index: the caller sums them.
  * No gradient may overlap an input or another gradient.  Deterministic: no atomics.  Workspace, paths and errors as gs_cross_attention.

@@ -61,6 +61,38 @@ GS_XWS xattn_ws_backward(const XattnArgs& a) {
 }
 #undef GS_XWS
 
+// The keys of [j0, j1) that sequence b may read under its mask, where they are kFewKeys or fewer: lane i of the warp gets the
+// i-th in `mine`, the result is their number; -1 where there are more (found within the first keys, unless the mask is nearly empty).
+// D of the gradient is then summed from P and dP: a bf16 O gives <dO, O> to 2^-8 of the sum of |dO O|, which with weights on
+// one of a few keys passes what dP - D is rounded to (error of dQ and dK, logits of standard deviation 1.5 / 4, from a bf16 O:
+// 2 keys 3.4e-3 / 6.4e-3 of their norm, 16 keys 1.3e-3 / 3.5e-3, 1,024 keys 4e-4 / 2.3e-3; dS in bf16: 1.7e-3).
+constexpr int kFewKeys = 16;
+static __device__ __forceinline__ int few_keys(const XattnArgs& a, int b, int j0, int j1, int& mine) {
+    constexpr int kAhead = 16;  // masks of 32 keys on their way
+    const int lane = threadIdx.x & 31;
+    const unsigned char* mask = a.mask + (long long)b * a.ldm;
+    int found = 0;
+    for (; j0 < j1; j0 += 32 * kAhead) {
+        unsigned char m[kAhead];
+        unsigned any = 0;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int j = j0 + 32 * u + lane;
+            m[u] = j < j1 ? __ldg(mask + j) : 0;
+            any |= m[u];
+        }
+        if (!__any_sync(0xffffffffu, any)) continue;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            unsigned w = __ballot_sync(0xffffffffu, m[u] != 0);
+            if (found + __popc(w) > kFewKeys) return -1;
+            for (; w; w &= w - 1, ++found)
+                if (lane == found) mine = j0 + 32 * u + __ffs(w) - 1;
+        }
+    }
+    return found;
+}
+
 // ----------------------------------------------------------------- few rows (gs_xattn_rows.cu)
 void xattn_rows_plan(XattnArgs& a, int sms);
 cudaError_t launch_xattn_rows(const XattnArgs& a, cudaStream_t s);

@@ -138,6 +138,17 @@ __device__ __forceinline__ void drain_acc(uint32_t taddr, int c0, int c1, int co
     }
 }
 
+// sum of the products of two rows' 8 bf16 elements
+__device__ __forceinline__ float dot_eight(const uint4& x, const uint4& y, float acc) {
+    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        acc = fmaf(__uint_as_float(xs[e] << 16), __uint_as_float(ys[e] << 16), acc);
+        acc = fmaf(__uint_as_float(xs[e] & 0xffff0000u), __uint_as_float(ys[e] & 0xffff0000u), acc);
+    }
+    return acc;
+}
+
 // Statistics of every row tile of a key head: slots without a row get (-inf, 0).  16 threads a row, 8 columns each, four rows
 // in flight a thread, 64 slots a block.  Bound by instructions, mostly addresses (issue 69 %; 8 x 1,024 rows of 16 heads of 64,
 // 34 MB: 15 us; two rows in flight and lse read last 17).
@@ -172,14 +183,7 @@ __global__ void __launch_bounds__(256) k_xattn_stats(const XattnArgs a, int nl, 
     }
 #pragma unroll
     for (int k = 0; k < kStatRows; ++k) {
-        if (vec) {
-            const uint32_t xs[4] = {x[k].x, x[k].y, x[k].z, x[k].w}, ys[4] = {y[k].x, y[k].y, y[k].z, y[k].w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                acc[k] = fmaf(__uint_as_float(xs[e] << 16), __uint_as_float(ys[e] << 16), acc[k]);
-                acc[k] = fmaf(__uint_as_float(xs[e] & 0xffff0000u), __uint_as_float(ys[e] & 0xffff0000u), acc[k]);
-            }
-        }
+        if (vec) acc[k] = dot_eight(x[k], y[k], acc[k]);
 #pragma unroll
         for (int o = 8; o; o >>= 1) acc[k] += __shfl_xor_sync(0xffffffffu, acc[k], o);
         if (ln == 0) {
@@ -188,6 +192,47 @@ __global__ void __launch_bounds__(256) k_xattn_stats(const XattnArgs a, int nl, 
             dst[r] = nl2;
             dst[kTile + r] = nl2 == -INFINITY ? 0.f : -acc[k];
         }
+    }
+    const int n = keys_of(a, b);
+    if (!a.mask || n <= kTile) return;  // (up to a tile's keys: k_xattn_dq_tc sums D)
+    // each warp looks through an eighth of the mask (65,536 keys, nine of them read: the whole call 305 us where each took all of it)
+    __shared__ int counts[8], found[8][kFewKeys];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, piece = (n + 7) / 8, from = min(n, warp * piece);
+    int key = 0, few = few_keys(a, b, from, min(n, from + piece), key);
+    if (lane < few) found[warp][lane] = key;
+    if (lane == 0) counts[warp] = few;
+    __syncthreads();
+    few = 0;
+    for (int w = 0; w < 8; ++w) {
+        const int m = counts[w];
+        if (m < 0 || few + m > kFewKeys) return;  // too many: D stays <dO, O>
+        if (lane >= few && lane < few + m) key = found[w][lane - few];
+        few += m;
+    }
+    const __nv_bfloat16* keys = reinterpret_cast<const __nv_bfloat16*>(a.k.p) + b * a.k.b + hk * a.k.h;
+    const __nv_bfloat16* values = reinterpret_cast<const __nv_bfloat16*>(a.v.p) + b * a.v.b + hk * a.v.h;
+    const float cs = a.scale * kLog2e;
+#pragma unroll 1
+    for (int r = grp; r < grp + 16 * kStatRows; r += 16) {  // D = sum_j P dP instead
+        const int l = r / a.G, h = hk * a.G + r - l * a.G;
+        const bool row = l < nl && rt * nl + l < a.Lq;
+        const long long ql = row ? rt * nl + l : 0;
+        const uint4 q = load_eight(reinterpret_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.b + ql * a.q.l + (row ? h : 0) * a.q.h, c0, a.dk, row);
+        const uint4 d = load_eight(reinterpret_cast<const __nv_bfloat16*>(a.dO.p) + b * a.dO.b + ql * a.dO.l + (row ? h : 0) * a.dO.h, c0, a.dv, row);
+        const float nl2 = row ? neg_lse2(a.lse[((long long)b * a.Hq + h) * a.Lq + ql]) : -INFINITY;
+        float sum = 0.f;
+        for (int f = 0; f < few; ++f) {
+            const long long j = __shfl_sync(0xffffffffu, key, f);
+            float s = dot_eight(q, load_eight(keys + j * a.k.l, c0, a.dk, true), 0.f);
+            float dp = dot_eight(d, load_eight(values + j * a.v.l, c0, a.dv, true), 0.f);
+#pragma unroll
+            for (int o = 8; o; o >>= 1) {
+                s += __shfl_xor_sync(0xffffffffu, s, o);
+                dp += __shfl_xor_sync(0xffffffffu, dp, o);
+            }
+            sum = fmaf(ex2(fmaf(s, cs, nl2)), dp, sum);
+        }
+        if (ln == 0) dst[kTile + r] = nl2 == -INFINITY ? 0.f : -sum;
     }
 }
 
@@ -622,9 +667,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         const float cs = a.scale * kLog2e;
         float* stats = a.ws + (((long long)b * a.Hkv + hk) * p.rtiles + rt) * kStats;
         const float nl = stats[r];
-        float nd = stats[kTile + r];
+        float nd = nt > 0 ? stats[kTile + r] : 0.f;  // (the part that has all keys may write it)
         const bool none = nl == -INFINITY;  // no row, or one without weight
-        const bool exact = a.splits == 1 && nt == 1;
+        const bool exact = n <= kTile && nt == 1;  // by the sequence, not by its padding: other parts have no tile then
         if (nt > 0) {
             keep_row(t_q + lane_base, qx, warp >> 2);
             keep_row(t_do + lane_base, ox, warp >> 2);
@@ -674,7 +719,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_wait_ld32(dr);
             if (exact) {
                 // every key of the sequence is here: D = sum_j P dP in fp32, for this kernel and the next.  From a bf16 O
-                // it is off by 2^-9 of <dO, O>, which with a few keys exceeds the rounding of dS (2 keys: dK off by 5e-3, so 2e-3).
+                // it is off by up to 2^-8 of the sum of |dO O|, which with a few keys exceeds the rounding of dS (2 keys: dK off by
+                // 5e-3, so 2e-3).
                 float sum = 0.f;
 #pragma unroll
                 for (int q = 0; q < kCols; ++q) sum += (w >> q) & 1u ? s[q] * d[q] : 0.f;

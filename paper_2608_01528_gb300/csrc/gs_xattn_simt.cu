@@ -333,7 +333,7 @@ __global__ void __launch_bounds__(256) k_xattn_join(const XattnArgs a) {
     if (lane == 0 && a.lse) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-// D_i = <dO_i, O_i>: one warp per row.
+// D_i = <dO_i, O_i>: one warp per row.  Under a mask that leaves few keys, from bf16: sum_j P dP (few_keys).
 template <typename T>
 __global__ void __launch_bounds__(256) k_xattn_delta(const XattnArgs a) {
     const long long nrows = (long long)a.B * a.Hq * a.Lq;
@@ -347,6 +347,30 @@ __global__ void __launch_bounds__(256) k_xattn_delta(const XattnArgs a) {
     for (int q = lane; q < a.dv; q += 32) acc = fmaf(to_f32(o[q]), to_f32(d[q]), acc);
 #pragma unroll
     for (int k = 16; k; k >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, k);
+    if constexpr (sizeof(T) == 2) {
+        const int b = (int)(bh / a.Hq), h = (int)(bh % a.Hq), hk = h / a.G, n = keys_of(a, b);
+        int key = 0;
+        const int few = a.mask && n > kTile ? few_keys(a, b, 0, n, key) : 0;  // (up to a tile's: k_xattn_dq sums D)
+        if (few > 0) {
+            const T* q = reinterpret_cast<const T*>(a.q.p) + b * a.q.b + i * a.q.l + h * a.q.h;
+            const float cs = a.scale * kLog2e, L = a.lse[at] * kLog2e;
+            acc = 0.f;
+            for (int f = 0; f < few; ++f) {
+                const long long j = __shfl_sync(0xffffffffu, key, f);
+                const T* kr = reinterpret_cast<const T*>(a.k.p) + b * a.k.b + j * a.k.l + hk * a.k.h;
+                const T* vr = reinterpret_cast<const T*>(a.v.p) + b * a.v.b + j * a.v.l + hk * a.v.h;
+                float s = 0.f, dp = 0.f;
+                for (int c = lane; c < a.dk; c += 32) s = fmaf(to_f32(q[c]), to_f32(kr[c]), s);
+                for (int c = lane; c < a.dv; c += 32) dp = fmaf(to_f32(d[c]), to_f32(vr[c]), dp);
+#pragma unroll
+                for (int k = 16; k; k >>= 1) {
+                    s += __shfl_xor_sync(0xffffffffu, s, k);
+                    dp += __shfl_xor_sync(0xffffffffu, dp, k);
+                }
+                acc = fmaf(exp2f(s * cs - L), dp, acc);
+            }
+        }
+    }
     if (lane == 0) a.ws[at] = acc;
 }
 
@@ -414,7 +438,7 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long l
     const int t0 = (int)((long long)ktiles * bl.part / a.splits), t1 = (int)((long long)ktiles * (bl.part + 1) / a.splits);
     load_rows<T, DK, R>(Qs, a, a.q, bl.b, bl.hk, r0, a.dk, a.vec & kVecQ);
     load_rows<T, DV, R>(Ds, a, a.dO, bl.b, bl.hk, r0, a.dv, a.vec & kVecDO);
-    load_stats<R>(lse2, delta, a, bl.b, bl.hk, r0);
+    if (t0 < t1 && t0 * kTile < n) load_stats<R>(lse2, delta, a, bl.b, bl.hk, r0);  // (the part that has the keys may write D)
     float o[RI][DK / 16] = {};
     for (int t = t0; t < t1 && t * kTile < n; ++t) {
         __syncthreads();
@@ -426,9 +450,9 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long l
         float s[RI][4] = {}, dp[RI][4] = {};
         dots<DK>(s, Qs, Ks, a.dk);
         dots<DV>(dp, Ds, Vs, a.dv);
-        if (a.splits == 1 && n <= kTile) {
-            // every key of the sequence is here: D = sum_j P dP, for this kernel and the next (a bf16 O gives it to 2^-9 of
-            // <dO, O> only, which with a few keys is more than dP - D)
+        if (n <= kTile) {
+            // every key of the sequence is here, whatever its padding (other parts have no tile): D = sum_j P dP, for this kernel
+            // and the next (a bf16 O gives it to 2^-8 of the sum of |dO O|, which with a few keys is more than dP - D)
 #pragma unroll
             for (int i = 0; i < RI; ++i) {
                 const float L = lse2[ty + 16 * i];

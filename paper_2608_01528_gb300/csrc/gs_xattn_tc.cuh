@@ -106,21 +106,22 @@ static __device__ __forceinline__ void mma_rows_ts(uint32_t d, uint32_t a, uint3
         issue_ts(d, a + (uint32_t)(8 * k), bd + (uint64_t)((k >> 2) * (kChunkBytes >> 4) + (k & 3) * 2), idesc,
                  k != 0 ? 1u : 0u, el);
 }
-// 16 bf16 elements [c, c + 16) of a row of w (zeros past w, and where !has) as 8 words
+// 8 bf16 elements [e0, e0 + 8) of a row of w on a 16-byte boundary (zeros past w, and where !has)
+static __device__ __forceinline__ uint4 load_eight(const __nv_bfloat16* row, int e0, int w, bool has) {
+    if (has && e0 + 8 <= w) return __ldg(reinterpret_cast<const uint4*>(row + e0));
+    uint32_t u[4] = {0, 0, 0, 0};
+    if (has && e0 < w) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e0 + e < w) u[e >> 1] |= (uint32_t)__ldg(reinterpret_cast<const unsigned short*>(row) + e0 + e) << (16 * (e & 1));
+    }
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
+// 16 elements [c, c + 16) as 8 words
 static __device__ __forceinline__ void load_words(uint32_t (&x)[8], const __nv_bfloat16* row, int c, int w, bool has) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int e0 = c + 8 * h;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (has && e0 + 8 <= w) {
-            v = __ldg(reinterpret_cast<const uint4*>(row + e0));
-        } else if (has && e0 < w) {
-            uint32_t u[4] = {0, 0, 0, 0};
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (e0 + e < w) u[e >> 1] |= (uint32_t)__ldg(reinterpret_cast<const unsigned short*>(row) + e0 + e) << (16 * (e & 1));
-            v = make_uint4(u[0], u[1], u[2], u[3]);
-        }
+        const uint4 v = load_eight(row, c + 8 * h, w, has);
         x[4 * h] = v.x;
         x[4 * h + 1] = v.y;
         x[4 * h + 2] = v.z;
