@@ -26,6 +26,8 @@
 // Warp roles (352 threads): 0-3 and 4-7 softmax groups (warp w reads TMEM lanes 32 (w % 4)..+31), 8 TMEM allocator and
 // MMA issuer, 9 TMA, 10 masks.  Every wait is bounded.
 
+#include <float.h>
+
 #include <algorithm>
 #include <atomic>
 
@@ -311,6 +313,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t ts = tmem + lane_base + (t ? 128u : 0u), to0 = tmem + lane_base + 256u, to = to0 + (t ? (uint32_t)DV : 0u);
         const int r = quad * 32 + lane;  // row of the tile
         const float cs = a.scale * kLog2e;
+        // The lowest maximum, instead of -inf: its product with cs is finite, so that what lies below (a dot product of -inf, a key
+        // that is not read, a dot product that only the scale takes to -inf) weighs 0 without a test a tile.
+        const float lowest = fmaxf(-3.3e38f / cs, -FLT_MAX);
         uint32_t taken = 0, joins = 0;  // key tiles and joined items of this group so far
         bool ok = true;
         for (long long it = blockIdx.x; it < p.items && ok; it += gridDim.x) {
@@ -320,7 +325,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int nrows = (int)(left < tile_rows ? left : tile_rows);
             const bool busy = quad * 32 < nrows;  // a warp without a row only keeps the barriers' count
             const int steps = PAIR ? im.nt : (im.nt - t + 1) / 2;  // key tiles of this group
-            float m = -INFINITY, l = 0.f;  // m in units of the logits s
+            float m = lowest, l = 0.f;  // m in units of the logits s
             for (int k = 0; k < steps; ++k, ++taken) {
                 const int j0 = (im.t0 + (PAIR ? k : 2 * k + t)) * kTile;
                 uint32_t w[4];
@@ -356,8 +361,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const float mn = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                     if (k == 0) {
                         m = mn;
-                    } else if (__any_sync(0xffffffffu, (mn - m) * cs > kGrow)) {  // (-inf - -inf: NaN, no)
-                        const float f = mn == -INFINITY ? 1.f : ex2((m - mn) * cs);
+                    } else if (__any_sync(0xffffffffu, (mn - m) * cs > kGrow)) {
+                        const float f = ex2((m - mn) * cs);
                         m = mn;
                         l *= f;
                         if (!mbar_wait_warp_inline(&c.o_done[t], (taken - 1) & 1u, abort_flag, err)) {
@@ -374,7 +379,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             tmem_st16(to + 16u * q, orr);
                         }
                     }
-                    const float ms = m == -INFINITY ? 0.f : -m * cs;
+                    const float ms = -m * cs;
                     float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
@@ -406,6 +411,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (steps > 0 && !(ok = mbar_wait_warp_inline(&c.o_done[t], (taken - 1) & 1u, abort_flag, err))) break;
             tc_fence_after();
             float m2 = m * cs;          // base-2 units from here on
+            if (m2 == INFINITY) l = NAN;  // a logit past fp32, where the dot product may have been finite
             float fo = 1.f, f1 = 0.f;  // what group 0's and group 1's O are multiplied by
             const bool two = !PAIR && im.nt > 1;
             if (two) {
@@ -420,9 +426,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (!(ok = mbar_wait_warp_inline(&c.posted, ph, abort_flag, err))) break;
                     tc_fence_after();
                     const float2 o = c.ml[r];
-                    const float mm = fmaxf(m2, o.x), ms = mm == -INFINITY ? 0.f : mm;
-                    f1 = ex2(o.x - ms);
-                    fo = ex2(m2 - ms);
+                    const float mm = fmaxf(m2, o.x);
+                    f1 = ex2(o.x - mm);
+                    fo = ex2(m2 - mm);
                     l = l * fo + o.y * f1;
                     m2 = mm;
                 }

@@ -1,4 +1,4 @@
-"""Cross attention where its documented limits meet: few keys in a long memory."""
+"""Cross attention where its documented limits meet: few keys in a long memory, logits past fp32."""
 import math
 
 import pytest
@@ -45,3 +45,59 @@ def test_gradient_over_few_keys_of_a_long_memory(gs, n, how, path):
             assert off <= 1e-5 * dO.float().norm().cpu() * 64
             continue
         assert off <= 1.2 * (m / 3) ** 0.5 * 2.0 ** -8 * want.norm(), (name, float(off / want.norm()))
+
+
+@pytest.mark.parametrize("path", ["simt", "auto"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(3, 1, 700, 2, 64), (3, 1, 5000, 2, 128), (3, 40, 300, 2, 64), (3, 3, 5000, 2, 128),
+                                   (3, 200, 400, 2, 64), (39, 200, 400, 4, 64)], ids=lambda s: "x".join(map(str, s)))
+def test_logits_past_fp32(gs, shape, dtype, path):
+    """Dot products of 4 and -4 under a scale of 2e38: +inf makes a row NaN, -inf weighs nothing, and a row of
+    nothing else is empty; rows beside them are as they were."""
+    B, Lq, Lk, H, w = shape
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    g = torch.Generator().manual_seed(Lk + w)
+    Q, K = torch.zeros(B, Lq, H, w), torch.zeros(B, Lk, H, w)
+    V, dO = torch.randn(B, Lk, H, w, generator=g).to(dt).cuda(), torch.randn(B, Lq, H, w, generator=g).to(dt).cuda()
+    sign = (torch.arange(B)[:, None, None] + torch.arange(Lq)[:, None] + torch.arange(H) + 2) % 3 - 1  # -1, 0, 1 by row
+    Q[..., 0] = sign
+    K[..., 0] = -4.0
+    zero = torch.rand(B, Lk, generator=g) < 0.3   # logits of 0 in every row
+    zero[0] = False                               # none in the first sequence
+    zero[1, :Lk - 60] = False                     # and only at the second one's end
+    K[..., 0][zero] = 0.0
+    Q, K, zero = Q.to(dt).cuda(), K.to(dt).cuda(), zero.cuda()
+
+    def weights(sign):  # B x H x Lq x Lk
+        s = sign.cuda().permute(0, 2, 1)[..., None]
+        p = ((s == 0) | zero[:, None, None, :]).double()
+        return p / p.sum(-1, keepdim=True).clamp(min=1), p.sum(-1)
+
+    out = gs.cross_attention(Q, K, V, 2e38, want_lse=True, path=path)
+    gs.stream_status()
+    p, n = weights(sign)
+    o, lse = out["O"].double().permute(0, 2, 1, 3), out["lse"].double()
+    bad = (sign.cuda() < 0).permute(0, 2, 1)      # 4 * 2e38 among the logits
+    assert torch.isnan(o[bad]).all() and torch.isnan(lse[bad]).all()
+    want = p @ V.double().permute(0, 2, 1, 3)
+    # weights of 1 are exact: sums of Lk terms in fp32 (and their rescalings), the division, a bf16 output
+    tol = (Lk + 40) * 2.0 ** -24 * (p @ V.double().abs().permute(0, 2, 1, 3)) + (2.0 ** -8 if dt == torch.bfloat16 else 2.0 ** -24) * want.abs() + 1e-37
+    assert ((o - want).abs() <= tol)[~bad].all()
+    none = ~bad & (n == 0)
+    assert none.any() and (o[none] == 0).all() and (lse[none] == -math.inf).all()
+    some = ~bad & (n > 0)
+    assert ((lse - n.log()).abs() <= 8 * 2.0 ** -24 * (n.log() + 1))[some].all()
+    # the gradient, over rows without a NaN among them
+    sign = sign.abs()
+    Q[..., 0] = sign.to(dt).cuda()
+    out = gs.cross_attention(Q, K, V, 2e38, want_lse=True, path=path)
+    got = gs.cross_attention_backward(Q, K, V, out["O"], out["lse"], dO, 2e38, path=path)
+    gs.stream_status()
+    p, n = weights(sign)
+    d = dO.double().permute(0, 2, 1, 3)
+    want = (p.transpose(2, 3) @ d).permute(0, 2, 1, 3)
+    half = 2.0 ** -8 if dt == torch.bfloat16 else 2.0 ** -24
+    # a weight 1 / n: lse to 8 u (log n + 1) and its way through the exponential, rounded to bf16 on the tensor cores
+    tol = (half + (Lq + 200) * 2.0 ** -24) * (p.transpose(2, 3) @ d.abs()).permute(0, 2, 1, 3) * 1.01 + half * want.abs() + 1e-37
+    assert ((got["dV"].double() - want).abs() <= tol).all()
+    assert (got["dQ"].permute(0, 2, 1, 3)[n == 0] == 0).all()
