@@ -955,6 +955,7 @@ long long attn_pack_room(const gs::XattnArgs& a, bool backward, unsigned flags) 
 bool attn_on_tensor(const gs::XattnArgs& a, bool backward, unsigned flags, int& pack) {
     pack = 0;
     if (a.dtype != GS_BF16 || a.G > 128) return false;
+    if (a.Lq == 0 || a.Lk == 0) return true;  // nothing to lay out: the other kernels write the zeros
     const int need = gs::xattn_pack_need(a, backward);
     if (need == 0) return true;
     if ((need & ~gs::xattn_pack_room(a, backward)) || !gs::xattn_packs(a, backward, flags == GS_PATH_TENSOR)) return false;

@@ -1,4 +1,4 @@
-"""Cross attention where its documented limits meet: few keys in a long memory, logits past fp32."""
+"""Cross attention where its documented limits meet: few keys in a long memory, logits past fp32, empty axes."""
 import math
 
 import pytest
@@ -101,3 +101,20 @@ def test_logits_past_fp32(gs, shape, dtype, path):
     tol = (half + (Lq + 200) * 2.0 ** -24) * (p.transpose(2, 3) @ d.abs()).permute(0, 2, 1, 3) * 1.01 + half * want.abs() + 1e-37
     assert ((got["dV"].double() - want).abs() <= tol).all()
     assert (got["dQ"].permute(0, 2, 1, 3)[n == 0] == 0).all()
+
+
+@pytest.mark.parametrize("width", [(64, 64), (47, 64), (64, 47), (33, 7)], ids=str)
+def test_forced_tensor_path_without_rows_or_keys(gs, width):
+    """An empty axis is no matter of layout: zeros come out whatever the width and alignment."""
+    dk, dv = width
+    Q, K, V, dO = (torch.randn(2, n, 4, w + 1).bfloat16().cuda()[..., 1:] for n, w in ((9, dk), (70, dk), (70, dv), (9, dv)))
+    out = gs.cross_attention(Q, K[:, :0], V[:, :0], 0.2, want_lse=True, path="tensor")
+    assert (out["O"] == 0).all() and (out["lse"] == -math.inf).all()
+    g = gs.cross_attention_backward(Q, K[:, :0], V[:, :0], out["O"], out["lse"], dO, 0.2, path="tensor")
+    assert (g["dQ"] == 0).all() and g["dK"].shape[1] == 0
+    g = gs.cross_attention_backward(Q[:, :0], K, V, out["O"][:, :0], out["lse"][:, :, :0].contiguous(), dO[:, :0], 0.2, path="tensor")
+    assert (g["dK"] == 0).all() and (g["dV"] == 0).all()
+    gs.stream_status()
+    f = [t.float() for t in (Q, K[:, :0], V[:, :0])]
+    with pytest.raises(gs.GramSpaceError, match="UNSUPPORTED"):  # the type is one
+        gs.cross_attention(*f, 0.2, path="tensor")
