@@ -92,6 +92,15 @@ __device__ __forceinline__ u64 entry_of(uint32_t key, int i) { return (u64)key <
 __device__ __forceinline__ uint32_t entry_key(u64 e) { return (uint32_t)(e >> 32); }
 __device__ __forceinline__ int entry_index(u64 e) { return (int)~(uint32_t)e; }
 
+// Halves of scores below 2^-125, and quotients by a T below 2^-126, lose bits.  Where the largest score and T are both below
+// 2^-60, the row is drawn with all scores and T kUp times as large: the weights are the same, and scores so far below the
+// largest that they overflow to -inf weigh 0 either way.  (Where only one of them is small, what is lost moves no weight.)
+constexpr float kUp = 36893488147419103232.f;  // 2^65
+__device__ __forceinline__ bool tiny_row(float most, float T) {
+    constexpr float kSmall = 8.673617379884035e-19f;  // 2^-60
+    return T < kSmall && fabsf(most) < kSmall;
+}
+
 // A row's settings and its weights.
 struct Weigher {
     float half_max;  // max / 2 (halves: the difference of two finite scores does not overflow)
@@ -304,6 +313,17 @@ __global__ void __launch_bounds__(128) k_sample_warp(const SampleArgs a, long lo
         if (lane == 0) answer(a, n, top ? (int)first : -1, top ? 1 : 0, top ? 1 : 0);
         return;
     }
+    if (tiny_row(value_of(top), st.T)) {
+        st.T *= kUp;
+        low = 0xffffffffu;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            key[e] = key[e] ? key_of(value_of(key[e]) * kUp) : 0u;
+            low = key[e] ? min(low, key[e]) : low;
+        }
+        top = key_of(value_of(top) * kUp);
+        low = __reduce_min_sync(0xffffffffu, low);
+    }
     Weigher w;
     w.set(top, st.T);
     u64 wt[E];
@@ -387,6 +407,12 @@ __global__ void __launch_bounds__(128) k_sample_warp(const SampleArgs a, long lo
 }
 
 // ----------------------------------------------------------------- rows of up to kList scores: a block each
+// (a function of its own: unrolled into the kernel it cost every row 2 to 5 %)
+__device__ __noinline__ void scale_up(uint32_t* keys, int M) {
+    for (int i = threadIdx.x; i < M; i += blockDim.x) keys[i] = keys[i] ? key_of(value_of(keys[i]) * kUp) : 0u;
+    __syncthreads();
+}
+
 __global__ void k_sample_row(const SampleArgs a, long long n0, int n2) {
     extern __shared__ u64 list[];  // n2 sorted entries, then M keys
     uint32_t* keys = reinterpret_cast<uint32_t*>(list + n2);
@@ -409,10 +435,15 @@ __global__ void k_sample_row(const SampleArgs a, long long n0, int n2) {
     if ((tid & 31) == 0) sh[tid >> 5] = best;
     __syncthreads();
     for (int i = 0; i < (int)(blockDim.x + 31) / 32; ++i) best = max(best, sh[i]);
-    const uint32_t top = entry_key(best);
+    uint32_t top = entry_key(best);
     if (top == 0u || !(st.T > 0.f)) {
         if (tid == 0) answer(a, n, top ? entry_index(best) : -1, top ? 1 : 0, top ? 1 : 0);
         return;
+    }
+    if (tiny_row(value_of(top), st.T)) {
+        st.T *= kUp;
+        top = key_of(value_of(top) * kUp);
+        scale_up(keys, M);
     }
     Weigher w;
     w.set(top, st.T);
@@ -515,11 +546,12 @@ __device__ __forceinline__ void for_scores(const void* row, bool bf16, int M, in
 }
 
 // One block, any row: t and cut by radix selects over the keys, 8 bits a pass, by counts or weights.
-__device__ void radix_row(const SampleArgs& a, long long n, const void* row, const Settings& st, const Weigher& w, Wide& m) {
+// Scores are taken `up` times as large.
+__device__ void radix_row(const SampleArgs& a, long long n, const void* row, const Settings& st, const Weigher& w, float up, Wide& m) {
     u64* hist = m.list;  // 256
     const u64* pow = m.pow;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, M = a.M;
-    auto key_at = [&](int i) { return key_of(load_score(row, a.bf16, i)); };
+    auto key_at = [&](int i) { return key_of(load_score(row, a.bf16, i) * up); };
     auto weight = [&](uint32_t k) { return w.weight(value_of(k), k, pow); };
     auto select = [&](bool by_weight, u64 need, u64& above) {
         uint32_t prefix = 0;
@@ -696,11 +728,13 @@ __global__ void __launch_bounds__(kWideThreads, 2) k_sample_wide(const SampleArg
         }
         return;
     }
+    const float up = tiny_row(hi, st.T) ? kUp : 1.f;
+    st.T *= up;
     Weigher w;
-    w.set(top, st.T);
+    w.set(key_of(hi * up), st.T);
     const bool by_k = st.top_k >= 1 && st.top_k < M, by_p = st.top_p < 1.f;
-    if (w.only_top) {
-        if (rank == 0) radix_row(a, n, row, st, w, m);
+    if (w.only_top || up != 1.f) {  // (the passes below take scores as they are)
+        if (rank == 0) radix_row(a, n, row, st, w, up, m);
         return;
     }
     u64 last = 1ull << 32;  // entries from this one on are kept
@@ -804,7 +838,7 @@ __global__ void __launch_bounds__(kWideThreads, 2) k_sample_wide(const SampleArg
         ptx::cluster_sync_all();
         if (rank != 0) return;
         if (m.count > (unsigned)kList) {
-            radix_row(a, n, row, st, w, m);
+            radix_row(a, n, row, st, w, 1.f, m);
             return;
         }
         const int nl = (int)m.count;
