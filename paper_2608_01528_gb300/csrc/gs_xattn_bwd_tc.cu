@@ -768,6 +768,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 std::atomic<bool> g_attr[64][4];
+std::atomic<bool> g_launched;  // the error word is read (a blocking copy of some 10 us) only once a kernel may have set it
 
 template <int DKC, int DVC>
 cudaError_t launch(const HeadMap& q, const HeadMap& o, const HeadMap& k, const HeadMap& v, const Params& p, int device,
@@ -802,6 +803,7 @@ bool on_vectors(const HeadView& v, int B, int L, int H, int w) {
 
 unsigned take_device_error_xbwd() {
     unsigned v = 0, z = 0;
+    if (!g_launched) return 0;
     cudaMemcpyFromSymbol(&v, g_err_xbwd, sizeof(v));
     if (v) cudaMemcpyToSymbol(g_err_xbwd, &z, sizeof(z));
     return v;
@@ -818,6 +820,7 @@ void xattn_bwd_tc_plan(XattnArgs& a, int sms) {
 
 cudaError_t launch_xattn_bwd_tc(const XattnArgs& a, int device, cudaStream_t s) {
     if (device < 0 || device >= 64) return cudaErrorInvalidDevice;
+    g_launched = true;
     Params p{};
     p.a = a;
     p.nl = kTile / a.G;

@@ -510,6 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 std::atomic<bool> g_attr[64][8];
+std::atomic<bool> g_launched;  // the error word is read (a blocking copy of some 10 us) only once a kernel may have set it
 
 template <int DKC, int DVC, bool PAIR>
 cudaError_t launch(const HeadMap& q, const HeadMap& k, const HeadMap& v, const Params& p, int sms, int device, cudaStream_t s) {
@@ -538,6 +539,7 @@ bool take_pairs(const XattnArgs& a, int sms) {
 
 unsigned take_device_error_xattn() {
     unsigned v = 0, z = 0;
+    if (!g_launched) return 0;
     cudaMemcpyFromSymbol(&v, g_err_xattn, sizeof(v));
     if (v) cudaMemcpyToSymbol(g_err_xattn, &z, sizeof(z));
     return v;
@@ -552,6 +554,7 @@ void xattn_tc_plan(XattnArgs& a, int sms) {
 
 cudaError_t launch_xattn_tc(const XattnArgs& a, int sms, int device, cudaStream_t s) {
     if (device < 0 || device >= 64) return cudaErrorInvalidDevice;
+    g_launched = true;
     const bool pair = take_pairs(a, sms);
     Params p{};
     p.a = a;
