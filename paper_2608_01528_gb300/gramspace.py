@@ -18,6 +18,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
+import warnings
 
 import torch
 
@@ -566,7 +567,11 @@ def cross_attention(Q, K, V, scale=None, key_lens=None, key_mask=None, want_lse=
     strides with a dense last axis; Hkv divides Hq, head h reads key head h // (Hq // Hkv)).
     scale: dk ** -0.5 by default.  key_lens: int32 [B], keys to read of each sequence.  key_mask:
     bool B x Lk, False = not read.  Returns {"O": B x Lq x Hq x dv, "lse": B x Hq x Lq float32 with want_lse};
-    `out` may supply them."""
+    `out` may supply them.  Like every call of this module it is not recorded by autograd: a graph's backward step calls
+    cross_attention_backward (there is a warning where an input asks for its gradient)."""
+    if (Q.requires_grad or K.requires_grad or V.requires_grad) and torch.is_grad_enabled():
+        warnings.warn("cross_attention is not recorded by autograd, gradients do not pass through it: take them from "
+                      "cross_attention_backward, and call it under torch.no_grad() or on detached tensors", stacklevel=2)
     a, hs = _attn(Q, K, V, scale, key_lens, key_mask, path)
     L, dev, ref = load_library(), Q.device, ctypes.byref
     out = dict(out) if out else {}
@@ -610,7 +615,7 @@ def sample_scores(S, U, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, want_pro
     """One random entry of each row of the scores S (N x M, float32 or bfloat16, CUDA) from the numbers
     U (N float32 of [0, 1)); see gs_sample_scores for the rules.  temperature, top_k, top_p and min_p are
     numbers or, for one setting per row, contiguous CUDA vectors of N (float32; top_k int32).  Returns
-    {"index": N int32, "prob": N float32}."""
+    {"index": N int32, "prob": N float32}, neither recorded by autograd."""
     ld = _ld(S)
     N, M = S.shape
     _c_int(M)
