@@ -499,7 +499,8 @@ GS_API gs_status gs_cross_attention_backward(const gs_attn* a, const gs_heads* Q
  * arithmetic's only where U lies that close to a border.
  * The four settings come as one number for all rows or, where the pointer is not
  * NULL, one per row (device arrays of N).  index (N int32) and prob (N fp32) are
- * optional, not both NULL.  N = 0 is a no-op.  No workspace.
+ * optional, not both NULL.  N = 0 is a no-op.  No workspace.  In rows of more than 4,096 scores, a
+ * top_k above 4,096 or as many equal scores at a cut take a slower way (milliseconds).
  * Errors: GS_ERR_INVALID_ARG, GS_ERR_SHAPE (N < 0, M < 1 or above 2^19, 0 < lds < M),
  * GS_ERR_ALIGNMENT (an array off its elements' boundary), GS_ERR_CUDA.
  */

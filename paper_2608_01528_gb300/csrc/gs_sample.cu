@@ -11,18 +11,21 @@
 //
 // Rows of up to 512 scores (k_sample_warp): a warp a row, scores and weights in registers; t is built bit by bit
 // from the highest, by the count or weight of the keys at or above it.  Up to 4,096 (k_sample_row): a block sorts the row
-// in shared memory; prefix sums of the sorted weights give t and cut.  Both are bound by instructions (4,096 x 256 with
-// top-p: 9 us of kernel by warps, 41 sorted).
+// in shared memory; prefix sums of the sorted weights give t and cut.  Warps are bound by integer instructions (4,096 x 256 with
+// top-p: 19 us, ALU pipe 70 % busy, 41 us if sorted; 7.6 us without top-k and top-p), the sort by shared memory (1,024 x 2,048
+// with top-p: 112 us, L1 86 % busy; 18 us without).
 //
 // Longer rows (k_sample_wide): a cluster of up to 8 CTAs a row, re-reading the row from L2.  Pass 0: largest and
 // smallest score.  Pass 1: a histogram over up to 2,048 equal steps of log weight -- counts for top-k; for top-p fp32
-// weights cut to some 16 bits, which bound the running weight to 2^-14 of it.  Pass 2: the few entries of the steps in which t
+// weights cut to hb bits, so many that a 32-bit counter holds all scores of a CTA (20 at most, 14 for 128,000 of them), which
+// bounds the running weight to 2^(2 - hb) of it.  Pass 2: the few entries of the steps in which t
 // can lie (top-k: and all above) go to one CTA's list, which sorts them; the exact weight of what lies above is summed
 // per warp's stretch of the row, and that of the whole row.  The draw then only looks through the one stretch in which it
-// falls.  Where the list overflows (more than 4,096 ties, or top_k beyond that) one block takes
-// the row by radix selects over its bits.  Bound by instructions: some 40 a score for an exact weight, as many for the histogram
-// (256 rows of 128,000 fp32 scores, top-p: 200 us; 64 rows of 131,071 bf16 scores, top-k 50: 63 us, of which clusters' waits and
-// the first pass's loads take most).
+// falls.  Where the list overflows (more than 4,096 ties, or top_k beyond that), and for tiny rows, one block takes
+// the row by radix selects over its bits: 2 ms for a row of 131,072 to 200,000 scores, where top_k = 4,000 takes 0.1 ms.
+// No unit is full: 256 rows of 128,000 fp32 scores, top-p, 196 us, issue slots 61 %, ALU 50 %, the longest waits for loads (one
+// vector ahead) and fixed latencies; 64 rows of 131,071 bf16 scores, top-k 50 for all, 32 us, issue slots 45 %, block barriers,
+// instruction fetches and loads.
 
 #include <math.h>
 

@@ -19,11 +19,16 @@
 // w of a group reads lanes 32 (w % 4)..+31 and columns 32 (w / 4)..+31 of its half.  The rows'
 // statistics (-lse log2 e, -D) are laid out per row tile by k_xattn_stats, so that a tile's come with one copy.
 //
-// Measured at 2 sequences of 4,096 x 4,096, 32 / 8 heads of 128: dK and dV 0.71 ms, dQ 0.56 ms.  Each CTA reads 64 KB a tile,
-// 7 to 8 TB/s from L2 over all: that bounds both.  At width 64 (8 x 1,024 x 750..1,500, 16 heads: 109 and 88 us) a tile takes 1,580
-// and 1,470 clocks, its products 1,024, and a CTA's start and end took 9,000 of 22,000 clocks before its own tiles came while it is
-// set up and results went out 64 bytes of a row at a time (221 -> 207 us for the whole gradient).  (CTAs that go on with another
-// item spill in the loop over tiles, which has no register left: 230 us for the whole gradient instead of 207.)
+// P and dS go to bf16 for their products (half a step, 2^-8 relative): the other operands, dO, Q and K, are bf16, and the tensor
+// core takes both in one type.  Error of dQ, dK and dV against 64 bits: 2.4e-3 of their norm, 1.7e-3 with fp32 P and dS.
+//
+// Measured at 2 sequences of 4,096 x 4,096, 32 / 8 heads of 128: dK and dV 0.71 ms, dQ 0.55 ms, statistics 0.03.  dK and dV keep the
+// tensor pipe busy in 77 % of the multiprocessors' active clocks, which are 84 % of the kernel's (512 CTAs on 152 of them), dQ in
+// 65 %, where the softmax warps wait for TMEM and for one another; L2, 64 KB a tile and CTA, is 18 and 26 % busy.  At width 64 (8 x
+// 1,024 x 750..1,500, 16 heads: 108 and 87 us) a tile takes 1,580 and 1,470 clocks, its four and three products 1,024 and 768, and a CTA's
+// start and end took 9,000 of 22,000 clocks before its own tiles came while it is set up and results went out 64 bytes of a row
+// at a time (221 -> 207 us for the whole gradient).  (CTAs that go on with another item spill in the loop over tiles, which has no
+// register left: 230 us for the whole gradient instead of 207.)
 //
 // Keys that are not read: P = dS = 0, and in the second kernel their rows of K are zeroed in shared memory before
 // the MMA reads them (0 * NaN).  Rows past the end have lse = +inf: P = 0.
@@ -151,7 +156,8 @@ __device__ __forceinline__ float dot_eight(const uint4& x, const uint4& y, float
 
 // Statistics of every row tile of a key head: slots without a row get (-inf, 0).  16 threads a row, 8 columns each, four rows
 // in flight a thread, 64 slots a block.  Bound by instructions, mostly addresses (issue 69 %; 8 x 1,024 rows of 16 heads of 64,
-// 34 MB: 15 us; two rows in flight and lse read last 17).
+// 34 MB: 15 us; two rows in flight and lse read last 17).  Where a mask leaves few keys, D is summed from them instead (9 of
+// 1,500 keys, 4 x 64 rows of 16 heads of 64: the whole gradient 59 -> 73 us).
 constexpr int kStatRows = 4, kStatBlocks = kTile / (16 * kStatRows);
 __global__ void __launch_bounds__(256) k_xattn_stats(const XattnArgs a, int nl, long long rtiles, int vec) {
     long long i = blockIdx.x / kStatBlocks;

@@ -9,8 +9,8 @@
 // exponential, and the weights come back by shuffles.  Every LK lanes keep running maxima, sums and an output of their own;
 // they meet in registers, then shared memory, and parts of long memories in k_xattn_join.
 //
-// One row is bound by the loads in flight (64 x 1,500 keys, 16 heads of 64, bf16: 5.0 TB/s with half of the
-// padding read; fp32 8 x 8,192 keys, 16 heads of 128: 4.5 TB/s), more rows by instructions.
+// One row is bound by the loads in flight (64 x 750 to 1,500 keys, 16 heads of 64, bf16: 4.7 TB/s; fp32 8 x 8,192 keys, 16
+// heads of 128: 5.1 TB/s), more rows by instructions.
 
 #include <algorithm>
 
@@ -293,7 +293,7 @@ bool on_16(const XattnArgs& a, const HeadView& v, int L, int H) {
 
 void xattn_rows_plan(XattnArgs& a, int sms) {
     const int R = rows_per_block(a.rows);
-    // four blocks a multiprocessor, and parts of 256 keys or more
+    // parts of 256 keys or more, up to four blocks a multiprocessor (three of one row or two of more are resident at a time)
     a.splits = xattn_parts((a.rows + R - 1) / R * a.Hkv * a.B, a.Lk / 256, 4 * sms, 1);
     a.rsplits = 1;
 }

@@ -7,14 +7,14 @@
 // A block of 256 threads holds 64 packed rows; per tile of 64 keys each thread has a 4 x 4 piece of S and
 // 4 rows x dv / 16 columns of O in registers, Q, K, V and the weights (over K) in shared memory, rows
 // padded by 4 floats so that 16-byte reads of 8 consecutive rows take 8 different bank groups.  Bound by
-// the shared-memory reads that feed the FMAs (8 16-byte reads per 64 FMAs; fp32, 16 x 64 x 2,048, 4 heads of 64: 109 us,
-// 10 TFLOP/s).  With few blocks the keys are
-// cut into parts whose (O, m, l) a second kernel joins.
+// the shared-memory reads that feed the FMAs (8 16-byte reads per 64 FMAs; fp32, 16 x 64 x 2,048, 4 heads of 64: 89 us,
+// 24 TFLOP/s; 8 x 1,024 x 1,500, 16 heads of 64: 1.62 ms, 31 TFLOP/s).  With few blocks the keys are cut into parts whose (O, m, l) a second kernel joins.
 //
 // Backward, with the forward's lse: P = 2^(c s - lse log2 e), dS = P (dO V^T - D).  One kernel per row
 // tile runs over the keys for dQ, one per key tile over the packed rows for dK and dV (S is
-// computed twice; no sums meet in atomics, so results repeat bit for bit): 16 x 100 x 257, 4 / 2 heads of 40 and 30,
-// fp32: 32 and 33 us of kernels, 81 us with the sums, D and the launches between them.
+// computed twice; no sums meet in atomics, so results repeat bit for bit): 16 x 100 x 129 to 257, 4 / 2 heads of 40 and 30,
+// fp32: 70 us in a graph, 82 us as calls (up to six launches: D, dQ and its sum, dK and dV and theirs); 8 x 1,024 x 1,500, 16 heads
+// of 64: 6.3 ms, 20 TFLOP/s.
 
 #include <math.h>
 
@@ -411,7 +411,7 @@ __device__ __forceinline__ void load_stats(float* lse2, float* delta, const Xatt
 }
 
 // Tiles of R rows: 64, or 16 where a key head has few (a tile's products are taken whole).  fp32, 17 x 832 keys, 16 / 64: 14 rows,
-// 16 key heads of 128 and 81, 499 / 948 us; 32 rows of 128 988 / 1,212; 20 rows of 64 438 / 425.
+// 16 key heads of 128 and 81, 499 / 948 us; 32 rows of 128 988 / 1,212; 20 rows of 64 438 / 425 (the rule loses 3 % there).
 int bwd_rows(const XattnArgs& a) { return a.rows <= 32 ? 16 : kTile; }
 
 template <int DK, int DV, int R>

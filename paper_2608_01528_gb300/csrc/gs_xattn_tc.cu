@@ -18,10 +18,16 @@
 // first scores run while the softmax groups finish the last one (64 sequences of 1,500 keys, one row each: 113 us with a
 // CTA per item).
 //
-// Measured: 4 x 4,096 x 4,096, 32 / 8 heads of 128: 0.70 ms of kernel, 1.57 PFLOP/s, bound by the products and the softmax chain
-// of a group between them; 8 x 1,024 x 750..1,500, 16 heads of 64: 70 us, of which a third is the uneven share of 512 items over
-// 152 CTAs and the rest the softmax warps (a step of 128 keys takes a group 2,500 clocks, XU 40 % and tensor pipe 40 % busy); single
-// rows over 8 x 65,537 keys, 32 / 8 heads of 128: 0.30 ms, 7.1 TB/s.
+// Weights go to bf16 for the product with V (half a step, 2^-8 relative): both operands of the tensor core have one type, and V
+// is bf16; two bf16 terms a weight would double that product.  Their sum l takes them unrounded in fp32.  Error of O against 64
+// bits: 2.3e-3 of its norm, where fp32 weights and the output's own rounding give 1.7e-3.
+//
+// Measured: 4 x 4,096 x 4,096, 32 / 8 heads of 128: 0.69 ms of kernel, 1.59 PFLOP/s (0.74 to 0.75 ms in a stream of calls on
+// changing inputs), tensor pipe 70 %: the products and the softmax chain of a group between them; 8 x 1,024 x 750..1,500, 16
+// heads of 64: 70 us, of which a third is the uneven share of 512 items over 152 CTAs and the rest the softmax warps (a step of
+// 128 keys takes a group 2,500 clocks, XU 39 % and tensor pipe 39 % busy); single rows over 8 x 65,537 keys, 32 / 8 heads of
+// 128: 0.30 ms, 7.1 TB/s.  A softmax thread holds 128 scores: all 168 registers that 11 warps leave it, and 128 to 172 bytes
+// are spilled.
 //
 // Warp roles (352 threads): 0-3 and 4-7 softmax groups (warp w reads TMEM lanes 32 (w % 4)..+31), 8 TMEM allocator and
 // MMA issuer, 9 TMA, 10 masks.  Every wait is bounded.
