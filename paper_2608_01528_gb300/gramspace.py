@@ -598,14 +598,14 @@ def cross_attention_backward(Q, K, V, O, lse, dO, scale=None, key_lens=None, key
     out = dict(out) if out else {}
     shape = (a.B, a.Lq, a.Hq, a.dv)
     o, do = _heads(O, "O", shape, Q), _heads(dO, "dO", shape, Q)
-    lse = _attn_lse(lse, (a.B, a.Hq, a.Lq), dev)
+    logs = _attn_lse(lse, (a.B, a.Hq, a.Lq), dev)  # (the tensor stays in its name: its last reference may be this call's)
     with _on_stream(dev, stream):
         for name, t in (("dQ", Q), ("dK", K), ("dV", V)):
             if name not in out:
                 out[name] = torch.empty(t.shape, dtype=t.dtype, device=dev)
         gq, gk, gv = _heads(out["dQ"], "dQ", Q.shape, Q), _heads(out["dK"], "dK", K.shape, Q), _heads(out["dV"], "dV", V.shape, Q)
         keep, ws, size = _attn_workspace(L, a, 1, dev)
-        st = L.gs_cross_attention_backward(ref(a), ref(hs[0]), ref(hs[1]), ref(hs[2]), ref(o), lse, ref(do), ref(gq), ref(gk),
+        st = L.gs_cross_attention_backward(ref(a), ref(hs[0]), ref(hs[1]), ref(hs[2]), ref(o), logs, ref(do), ref(gq), ref(gk),
                                            ref(gv), ws, size, _stream(stream, dev))
     _check(st, "gs_cross_attention_backward")
     return out
