@@ -450,9 +450,10 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long l
         float s[RI][4] = {}, dp[RI][4] = {};
         dots<DK>(s, Qs, Ks, a.dk);
         dots<DV>(dp, Ds, Vs, a.dv);
-        if (n <= kTile) {
+        if (sizeof(T) == 2 && n <= kTile) {
             // every key of the sequence is here, whatever its padding (other parts have no tile): D = sum_j P dP, for this kernel
-            // and the next (a bf16 O gives it to 2^-8 of the sum of |dO O|, which with a few keys is more than dP - D)
+            // and the next (a bf16 O gives it to 2^-8 of the sum of |dO O|, which with a few keys is more than dP - D; an fp32 O gives
+            // it more exactly than this sum, in which P is off by lse's rounding, |lse| 2^-24)
 #pragma unroll
             for (int i = 0; i < RI; ++i) {
                 const float L = lse2[ty + 16 * i];

@@ -1,10 +1,10 @@
-"""Cross attention where its documented limits meet: few keys in a long memory, logits past fp32, empty axes."""
+"""Cross attention where its documented limits meet: few keys in a long memory, logits past fp32, logits far from 0, empty axes."""
 import math
 
 import pytest
 import torch
 
-from attn_bounds import Ref
+from attn_bounds import Ref, close
 
 pytestmark = pytest.mark.gpu
 
@@ -118,3 +118,22 @@ def test_forced_tensor_path_without_rows_or_keys(gs, width):
     f = [t.float() for t in (Q, K[:, :0], V[:, :0])]
     with pytest.raises(gs.GramSpaceError, match="UNSUPPORTED"):  # the type is one
         gs.cross_attention(*f, 0.2, path="tensor")
+
+
+@pytest.mark.parametrize("Lk", [1, 2, 7, 33, 64, 700])
+@pytest.mark.parametrize("far", [0.0, 30.0, 300.0])
+def test_fp32_gradient_beside_large_logits(gs, far, Lk):
+    """Logits that all lie `far` from 0 leave P off by |lse| 2^-24 or so; dP - D is not to be off by as much of dP."""
+    g = torch.Generator().manual_seed(Lk + int(far))
+    B, Lq, H, w = 5, 20, 3, 16
+    Q, K, V, dO = (torch.randn(B, n, H, m, generator=g) for n, m in ((Lq, w), (Lk, w), (Lk, 4), (Lq, 4)))
+    Q[..., 0], K[..., 0] = 1.0, far
+    Q[..., 1:] *= 3.0
+    Q, K, V, dO = (t.cuda() for t in (Q, K, V, dO))
+    lens = torch.tensor([Lk, 1, (Lk + 1) // 2, 0, min(Lk, 3)], dtype=torch.int32).cuda()
+    r = Ref(Q, K, V, 1.0, lens)
+    O, lse = r.o.permute(0, 2, 1, 3).float().cuda(), r.lse.float().cuda()
+    got = gs.cross_attention_backward(Q, K, V, O, lse, dO, 1.0, key_lens=lens)
+    gs.stream_status()
+    for name, (want, tol) in r.grad(dO).items():
+        close(got[name], want, tol, name)
