@@ -496,7 +496,8 @@ GS_API gs_status gs_cross_attention_backward(const gs_attn* a, const gs_heads* Q
  * below 1 from 1 on.
  * Weights are 64-bit fixed point numbers (2^41 for the largest), exact to a relative 2^-34 and
  * to half a unit, their sums exact in any order, so that a draw differs from exact
- * arithmetic's only where U lies that close to a border.
+ * arithmetic's only where U, top_p or min_p lies that close to a border (two scores alike and a third that
+ * weighs 2^-43 of them: top_p = 0.5 keeps one, not two).
  * The four settings come as one number for all rows or, where the pointer is not
  * NULL, one per row (device arrays of N).  index (N int32) and prob (N fp32) are
  * optional, not both NULL.  N = 0 is a no-op.  No workspace.  In rows of more than 4,096 scores, a

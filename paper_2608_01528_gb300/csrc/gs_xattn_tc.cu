@@ -161,6 +161,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         prefetch_map(&mk);
         prefetch_map(&mv);
     }
+    // Rows of a tile that its box does not write (128 % G != 0) have no result, but a warp moves the maxima of its 32 rows together:
+    // with what an earlier kernel left there, the other rows' roundings would change from call to call.
+    if (tile_rows < kTile) {
+        const int words = (kTile - tile_rows) * 8;  // 16-byte words per chunk
+        for (int e = threadIdx.x; e < QS * C::kQTiles * DKC * words; e += kThreads)
+            *reinterpret_cast<uint4*>(Qs + (size_t)(e / words) * kChunkBytes + tile_rows * 128 + (e % words) * 16) =
+                make_uint4(0, 0, 0, 0);
+        fence_proxy_async();
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
