@@ -406,7 +406,7 @@ GS_API gs_status gs_attention_scores(const void* Yq, const void* Yk, int in_dtyp
  *     lse_i = log sum_{j valid} exp(s_ij),   O[b,i,h] = sum_{j valid} exp(s_ij - lse_i) V[b,j,g]
  * A row without a valid key (or whose valid logits are all -inf) is O = 0, lse = -inf; a
  * row with a valid logit that is NaN or +inf is NaN.  Logits that the scale takes past fp32
- * are infinite (from 2.3e38 on they may be: base-2 logits, log2(e) times as large, are
+ * are infinite (from 2.2e38 on they may be: base-2 logits, log2(e) times as large, are
  * what is computed with).  Keys and values that are not valid are never used, whatever they hold.
  */
 typedef struct gs_heads { /* element (b, l, h, c) of a B x L x H x width array           */
