@@ -477,6 +477,93 @@ GS_API gs_status gs_cross_attention_backward(const gs_attn* a, const gs_heads* Q
                                              void* stream);
 
 /*
+ * Attention over a sliding window of positions, as a decoder's own states are read (causal): query row i of sequence b stands at
+ * position p = start + i and sees the keys j that gs_cross_attention's row would (j < key_lens[b], key_mask[b,j] != 0) and that
+ *     j <= p   and   (j > p - window   or   j < sinks),
+ * the last `window` keys up to its own (INT_MAX: all, causal attention) and the first `sinks`, which stay visible.
+ * Everything else is as in the calls without a window: arguments, layouts, results of rows that see nothing (O = 0,
+ * lse = -inf, no gradient), workspace, paths, errors; besides, GS_ERR_INVALID_ARG for window < 1 or sinks < 0, or w = NULL.
+ * What a row does not see is never used for its result, whatever it holds.  In the gradient this holds for keys and values
+ * that no row sees; what is not finite elsewhere may spread to gradients of its sequence.
+ * Work and traffic grow with the keys that are seen, not with Lk.
+ */
+typedef struct gs_window {
+    int window, sinks;
+    int start;         /* position of every sequence's first query row (may be negative: rows before 0 see nothing) */
+    const int* starts; /* or one per sequence (device array of B), or NULL */
+} gs_window;
+
+GS_API gs_status gs_window_attention_workspace(const gs_attn* a, const gs_window* w, int backward, long long* bytes);
+GS_API gs_status gs_window_attention(const gs_attn* a, const gs_window* w, const gs_heads* Q, const gs_heads* K,
+                                     const gs_heads* V, const gs_heads* O, float* lse, void* workspace,
+                                     long long workspace_bytes, void* stream);
+GS_API gs_status gs_window_attention_backward(const gs_attn* a, const gs_window* w, const gs_heads* Q, const gs_heads* K,
+                                              const gs_heads* V, const gs_heads* O, const float* lse, const gs_heads* dO,
+                                              const gs_heads* dQ, const gs_heads* dK, const gs_heads* dV, void* workspace,
+                                              long long workspace_bytes, void* stream);
+
+/*
+ * A paged cache of keys and values: `pages` pages of page_size rows, gs_heads arrays whose batch axis is the page.  Position
+ * t of request b lies in row t % page_size of page table[b][t / page_size]; slot = page * page_size + row.
+ *
+ * gs_page_slots gives new tokens their slots.  Request b holds lens[b] tokens (in ceil(lens[b] / page_size) pages) and
+ * gets added[b] more.  The pages that they need beyond those come from the free list, from entry *free_from (NULL: 0) on, request
+ * b's behind those of requests 0..b-1; they are written to the table's next columns (the others stay as they are).
+ *     slots[b][i] = the slot of token lens[b] + i, i < Lnew (B x Lnew, dense); -1 for i >= added[b] and where there is none
+ *     new_lens[b] = lens[b] + added[b], or less: up to the first token without a page  (optional)
+ *     taken       = the pages that all requests asked for, also where the list ended before  (optional)
+ * The list is not changed: the caller takes `taken` entries off it (in a captured graph by an addition to free_from).  A page that
+ * the list has not (too short) is -1 in the table; its tokens have slot -1 and do not count in new_lens; entries of
+ * the table or the list outside [0, pages) give slot -1.  lens and added count as the nearer end of [0, columns * page_size] and
+ * [0, Lnew]; tokens behind the table's last column have no slot.  No output may overlap an input or another output.
+ * Requires pages * page_size < 2^31, and columns * page_size, B * columns and B * Lnew near it at most.  No workspace.
+ * Errors: GS_ERR_INVALID_ARG (a null pointer, overlap), GS_ERR_SHAPE, GS_ERR_ALIGNMENT, GS_ERR_CUDA, GS_ERR_UNSUPPORTED.
+ */
+GS_API gs_status gs_page_slots(const int* lens, const int* added, int B, int Lnew, int page_size, int pages,
+                               const int* free_list, int n_free, const int* free_from, int* table, long long ld_table,
+                               int columns, int* slots, int* new_lens, int* taken, void* stream);
+
+/*
+ * Stores new keys and values: row (b, l) of K (B x L x H x dk) and V (B x L x H x dv) to slot slots[b * ld_slots + l] of Kc
+ * and Vc (pages x page_size x H x width), all of type dtype.  Rows whose slot lies outside [0, pages * page_size) are
+ * skipped, slots that no row names keep what they hold.  Slots must differ: of two rows with one slot, which stays is not defined
+ * (each 16 bytes are one's or the other's).  K and V must not overlap the cache.  No workspace.
+ */
+GS_API gs_status gs_page_store(int dtype, int B, int L, int H, int dk, int dv, const gs_heads* K, const gs_heads* V,
+                               const int* slots, long long ld_slots, int pages, int page_size, const gs_heads* Kc,
+                               const gs_heads* Vc, void* stream);
+
+/*
+ * Attention of the newest tokens over a paged cache (a decoding step; several rows: drafted tokens, a piece of a prompt).
+ * Request b holds lens[b] keys, its own newest ones among them, and q_lens[b] query rows (NULL: Lq): row i < q_lens[b]
+ * stands at position p = lens[b] - q_lens[b] + i and sees the keys j <= p with j > p - window or j < sinks (as
+ * gs_window_attention), as far as their pages are in the table: entries outside [0, pages) are keys that are not read.  O (B x Lq
+ * x Hq x dv) and lse (B x Hq x Lq fp32, dense, or NULL) as gs_cross_attention; rows i >= q_lens[b], and rows that see nothing,
+ * are O = 0, lse = -inf.  lens and q_lens count as the nearer end of [0, columns * page_size] and [0, Lq].  What a row does not see
+ * is never used for its result, whatever it holds.
+ * A call repeated gives the same bits; how many other requests there are, and how long, may change a result's rounding.
+ * Sums and statistics in fp32.  Errors as gs_cross_attention.
+ */
+typedef struct gs_paged {
+    int dtype;              /* GS_F32 or GS_BF16: every array but lse                    */
+    int B, Lq;              /* requests, query rows of each                              */
+    int Hq, Hkv, dk, dv;    /* as gs_attn                                                */
+    float scale;
+    int pages, page_size;   /* pages * page_size < 2^31                                  */
+    int columns;            /* of the table                                              */
+    const int* table;       /* B x columns (device)                                      */
+    long long ld_table;     /* row stride >= columns                                     */
+    const int* lens;        /* B (device)                                                */
+    const int* q_lens;      /* B (device) or NULL                                        */
+    int window, sinks;      /* window >= 1 (INT_MAX: no limit), sinks >= 0               */
+    unsigned flags;         /* GS_PATH_*                                                 */
+} gs_paged;
+
+GS_API gs_status gs_paged_attention_workspace(const gs_paged* a, long long* bytes);
+GS_API gs_status gs_paged_attention(const gs_paged* a, const gs_heads* Q, const gs_heads* K, const gs_heads* V,
+                                    const gs_heads* O, float* lse, void* workspace, long long workspace_bytes, void* stream);
+
+/*
  * Draws one entry of each score row (Sec. 2.2: the hard decision on scores, taken at
  * random in proportion to their softmax; argmax when temperature = 0).  S is N x M
  * (s_dtype GS_F32 or GS_BF16, row stride lds >= M, or 0: N draws from one row), U holds N numbers of
@@ -514,6 +601,26 @@ typedef struct gs_sampling {
 
 GS_API gs_status gs_sample_scores(const void* S, int s_dtype, long long N, int M, long long lds,
                                   const gs_sampling* how, const float* U, int* index, float* prob, void* stream);
+
+/*
+ * Verifies drafted tokens against the target's probabilities (what follows gs_sample_scores when a smaller model drafts): the
+ * tokens that come out are distributed as if the target had drawn them.  For request b with n = draft_lens[b] drafts (NULL: K;
+ * counted as the nearer end of [0, K]), P (B x (K+1) x M; row i: the target's probabilities behind i drafts) and D (B x K x M: those that
+ * draft i was drawn from; NULL: drafts were chosen without chance, D_i = 1 at the draft):
+ *     draft x_i is kept while   U[b][i] * D_i(x_i) < P_i(x_i),   i = 0, 1, .. n-1;      a = accepted[b], the drafts kept
+ *     w = max(P_a - D_a, 0) if a < n (P_a where that is zero everywhere), w = P_a if a = n
+ *     tokens[b] = the kept drafts, then the first index whose running weight in w exceeds U[b][K] times its sum, then -1
+ * (B x (K+1), dense; the drawn token is -1 where P_a holds nothing above 0).  U is B x (K+1) numbers of [0, 1), taken as 0 where
+ * negative or NaN and as the largest fp32 below 1 from 1 on.  A draft outside [0, M) is not kept, nor one whose comparison has a NaN.
+ * Weights are integers in units of 2^-44 (entries that are negative or NaN count as 0, above 1 as 1), their sums exact
+ * in any order, so that a draw differs from exact arithmetic's only where U lies that close to a border; the comparison is exact.
+ * P and D: GS_F32 or GS_BF16, strides p_batch, p_row, d_batch, d_row in elements (>= 0), unit stride along M <= 2^19.
+ * accepted (B) and tokens are optional, not both NULL.  No workspace.
+ * Errors: GS_ERR_INVALID_ARG, GS_ERR_SHAPE, GS_ERR_ALIGNMENT, GS_ERR_CUDA, GS_ERR_UNSUPPORTED.
+ */
+GS_API gs_status gs_verify_drafts(const void* P, const void* D, int dtype, int B, int K, int M, long long p_batch,
+                                  long long p_row, long long d_batch, long long d_row, const int* drafts,
+                                  const int* draft_lens, const float* U, int* accepted, int* tokens, void* stream);
 
 /*
  * Project + similarity that allocates nothing (the paper has no counterpart;

@@ -10,6 +10,7 @@
 #include <atomic>
 
 #include "gs_internal.h"
+#include "gs_paged.h"
 #include "gs_xattn.h"
 
 namespace {
@@ -930,19 +931,31 @@ gs_status attn_device(int& dev, int& sms) {
 // less host time without tensor maps; one row of 128 98 / 147; two 98 / 117; four 64 / 90.  Few rows against tiles of 64 on CUDA
 // cores, fp32: 4 rows of 128 123 / 615, 16 rows (16 x 2,048 keys of 4 heads) 111 / 174, 32 rows of 40 53 / 48.
 enum AttnPath { ATTN_ROWS, ATTN_SIMT, ATTN_TC };
+using gs::KeyMode;
 AttnPath attn_path(const gs::XattnArgs& a, unsigned flags, bool tc_ok) {
     if (tc_ok && flags == GS_PATH_TENSOR) return ATTN_TC;
     if (tc_ok && flags == GS_PATH_AUTO && (a.rows > 1 || a.dk > 64 || a.dv > 64)) return ATTN_TC;
     return a.rows <= 16 ? ATTN_ROWS : ATTN_SIMT;
 }
 
-void attn_plan(gs::XattnArgs& a, AttnPath path, int sms) {
+void attn_plan(gs::XattnArgs& a, AttnPath path, KeyMode mode, int sms) {
     if (path == ATTN_TC)
-        gs::xattn_tc_plan(a, sms);
+        gs::xattn_tc_plan(a, mode, sms);
     else if (path == ATTN_ROWS)
-        gs::xattn_rows_plan(a, sms);
+        gs::xattn_rows_plan(a, sms, mode);
     else
-        gs::xattn_simt_plan(a, false, sms);
+        gs::xattn_simt_plan(a, false, sms, mode);
+}
+
+// A window's settings, for the calls that have one (w != NULL).
+gs_status attn_window(const gs_window* w, gs::XattnArgs& a, KeyMode& mode) {
+    mode = gs::kAllKeys;
+    if (!w) return GS_OK;
+    if (w->window < 1 || w->sinks < 0) return GS_ERR_INVALID_ARG;
+    if (!on_elements(4, w->starts)) return GS_ERR_ALIGNMENT;
+    a.win = {w->window, w->sinks, w->start, w->starts};
+    mode = gs::kWindowKeys;
+    return GS_OK;
 }
 
 // Floats of workspace for inputs that may have to be laid out again for the tensor cores.
@@ -970,26 +983,24 @@ gs_status attn_workspace(const float* ws, long long bytes, long long floats) {
     return bytes < 4 * floats ? GS_ERR_SHAPE : GS_OK;
 }
 
-}  // namespace
-
-extern "C" {
-
-gs_status gs_cross_attention_workspace(const gs_attn* p, int backward, long long* bytes) {
+// The three calls of attention over dense arrays, through a window where w is given.
+gs_status attn_workspace_size(const gs_attn* p, const gs_window* w, int backward, long long* bytes) {
     if (!bytes) return GS_ERR_INVALID_ARG;
     *bytes = 0;
     gs::XattnArgs a;
+    KeyMode mode;
     gs_status st = attn_args(p, a);
-    if (st != GS_OK) return st;
+    if (st != GS_OK || (st = attn_window(w, a, mode)) != GS_OK) return st;
     int dev = 0, sms = 0;
     if ((st = attn_device(dev, sms)) != GS_OK) return st;
     // the arrays' alignment, not known here, decides between the paths: room for either
     long long floats = 0;
     for (int tc = 0; tc < (a.dtype == GS_BF16 && a.G <= 128 && a.Lk > 0 ? 2 : 1); ++tc) {
         if (backward) {
-            tc ? gs::xattn_bwd_tc_plan(a, sms) : gs::xattn_simt_plan(a, true, sms);
+            tc ? gs::xattn_bwd_tc_plan(a, mode, sms) : gs::xattn_simt_plan(a, true, sms, mode);
             floats = std::max(floats, gs::xattn_round4(gs::xattn_ws_backward(a)) + (tc ? attn_pack_room(a, true, p->flags) : 0));
         } else {
-            attn_plan(a, attn_path(a, p->flags, tc != 0), sms);
+            attn_plan(a, attn_path(a, p->flags, tc != 0), mode, sms);
             floats = std::max(floats, gs::xattn_round4(gs::xattn_ws_forward(a)) + (tc ? attn_pack_room(a, false, p->flags) : 0));
         }
     }
@@ -997,12 +1008,12 @@ gs_status gs_cross_attention_workspace(const gs_attn* p, int backward, long long
     return GS_OK;
 }
 
-gs_status gs_cross_attention(const gs_attn* p, const gs_heads* Q, const gs_heads* K, const gs_heads* V,
-                             const gs_heads* O, float* lse, void* workspace, long long workspace_bytes,
-                             void* stream) {
+gs_status attn_forward(const gs_attn* p, const gs_window* w, const gs_heads* Q, const gs_heads* K, const gs_heads* V,
+                       const gs_heads* O, float* lse, void* workspace, long long workspace_bytes, void* stream) {
     gs::XattnArgs a;
+    KeyMode mode;
     gs_status st = attn_args(p, a);
-    if (st != GS_OK) return st;
+    if (st != GS_OK || (st = attn_window(w, a, mode)) != GS_OK) return st;
     if (!Q || !K || !V || !O) return GS_ERR_INVALID_ARG;
     if (!valid_heads(Q, a.B, a.Lq, a.Hq, false) || !valid_heads(K, a.B, a.Lk, a.Hkv, false) ||
         !valid_heads(V, a.B, a.Lk, a.Hkv, false) || !valid_heads(O, a.B, a.Lq, a.Hq, true))
@@ -1017,27 +1028,27 @@ gs_status gs_cross_attention(const gs_attn* p, const gs_heads* Q, const gs_heads
     a.ws = (float*)workspace;
     cudaStream_t s = (cudaStream_t)stream;
     int pack = 0;
-    const bool tc_ok = attn_on_tensor(a, false, p->flags, pack);
+    const bool tc_ok = mode == gs::kAllKeys && attn_on_tensor(a, false, p->flags, pack);
     if (p->flags == GS_PATH_TENSOR && !tc_ok)
         return a.dtype != GS_BF16 || a.G > 128 ? GS_ERR_UNSUPPORTED : GS_ERR_ALIGNMENT;
     const AttnPath path = attn_path(a, p->flags, tc_ok && a.Lk > 0);
-    attn_plan(a, path, sms);
+    attn_plan(a, path, mode, sms);
     const long long own = gs::xattn_round4(gs::xattn_ws_forward(a));
     if (path != ATTN_TC) pack = 0;
     if ((st = attn_workspace(a.ws, workspace_bytes, own + gs::xattn_ws_pack(a, pack))) != GS_OK) return st;
     if (pack && (st = from_cuda(gs::launch_xattn_pack(a, pack, a.ws + own, s))) != GS_OK) return st;
-    return from_cuda(path == ATTN_TC     ? gs::launch_xattn_tc(a, sms, dev, s)
-                     : path == ATTN_ROWS ? gs::launch_xattn_rows(a, s)
-                                         : gs::launch_xattn_simt(a, s));
+    return from_cuda(path == ATTN_TC     ? gs::launch_xattn_tc(a, mode, sms, dev, s)
+                     : path == ATTN_ROWS ? gs::launch_xattn_rows(a, mode, s)
+                                         : gs::launch_xattn_simt(a, mode, s));
 }
 
-gs_status gs_cross_attention_backward(const gs_attn* p, const gs_heads* Q, const gs_heads* K, const gs_heads* V,
-                                      const gs_heads* O, const float* lse, const gs_heads* dO, const gs_heads* dQ,
-                                      const gs_heads* dK, const gs_heads* dV, void* workspace,
-                                      long long workspace_bytes, void* stream) {
+gs_status attn_backward(const gs_attn* p, const gs_window* w, const gs_heads* Q, const gs_heads* K, const gs_heads* V,
+                        const gs_heads* O, const float* lse, const gs_heads* dO, const gs_heads* dQ, const gs_heads* dK,
+                        const gs_heads* dV, void* workspace, long long workspace_bytes, void* stream) {
     gs::XattnArgs a;
+    KeyMode mode;
     gs_status st = attn_args(p, a);
-    if (st != GS_OK) return st;
+    if (st != GS_OK || (st = attn_window(w, a, mode)) != GS_OK) return st;
     if (!Q || !K || !V || !O || !dO || !dQ || !dK || !dV) return GS_ERR_INVALID_ARG;
     if (!valid_heads(Q, a.B, a.Lq, a.Hq, false) || !valid_heads(K, a.B, a.Lk, a.Hkv, false) ||
         !valid_heads(V, a.B, a.Lk, a.Hkv, false) || !valid_heads(O, a.B, a.Lq, a.Hq, false) ||
@@ -1058,19 +1069,217 @@ gs_status gs_cross_attention_backward(const gs_attn* p, const gs_heads* Q, const
     a.ws = (float*)workspace;
     cudaStream_t s = (cudaStream_t)stream;
     int pack = 0;
-    const bool tc_ok = attn_on_tensor(a, true, p->flags, pack);
+    const bool tc_ok = mode == gs::kAllKeys && attn_on_tensor(a, true, p->flags, pack);
     if (p->flags == GS_PATH_TENSOR && !tc_ok)
         return a.dtype != GS_BF16 || a.G > 128 ? GS_ERR_UNSUPPORTED : GS_ERR_ALIGNMENT;
     if (tc_ok && p->flags != GS_PATH_SIMT && a.Lq > 0 && a.Lk > 0) {
-        gs::xattn_bwd_tc_plan(a, sms);
+        gs::xattn_bwd_tc_plan(a, mode, sms);
         const long long own = gs::xattn_round4(gs::xattn_ws_backward(a));
         if ((st = attn_workspace(a.ws, workspace_bytes, own + gs::xattn_ws_pack(a, pack))) != GS_OK) return st;
         if (pack && (st = from_cuda(gs::launch_xattn_pack(a, pack, a.ws + own, s))) != GS_OK) return st;
-        return from_cuda(gs::launch_xattn_bwd_tc(a, dev, s));
+        return from_cuda(gs::launch_xattn_bwd_tc(a, mode, dev, s));
     }
-    gs::xattn_simt_plan(a, true, sms);
+    gs::xattn_simt_plan(a, true, sms, mode);
     if ((st = attn_workspace(a.ws, workspace_bytes, gs::xattn_round4(gs::xattn_ws_backward(a)))) != GS_OK) return st;
-    return from_cuda(gs::launch_xattn_simt_backward(a, s));
+    return from_cuda(gs::launch_xattn_simt_backward(a, mode, s));
+}
+
+// Attention over a paged cache: its checks, and what the kernels take.
+gs_status paged_args(const gs_paged* p, gs::XattnArgs& a) {
+    if (!p || !valid_path(p->flags)) return GS_ERR_INVALID_ARG;
+    if (p->dtype != GS_F32 && p->dtype != GS_BF16) return GS_ERR_INVALID_ARG;
+    if (!(p->scale > 0.f) || !(p->scale <= kMaxScale)) return GS_ERR_INVALID_ARG;
+    if (p->window < 1 || p->sinks < 0) return GS_ERR_INVALID_ARG;
+    if (p->B < 0 || p->Lq < 0 || p->Hq < 1 || p->Hkv < 1 || p->Hq % p->Hkv || p->dk < 1 || p->dv < 1 || p->pages < 0 ||
+        p->page_size < 1 || p->columns < 0 || p->ld_table < p->columns)
+        return GS_ERR_SHAPE;
+    if (p->dk > 128 || p->dv > 128) return GS_ERR_UNSUPPORTED;
+    if (!on_elements(4, p->table, p->lens, p->q_lens)) return GS_ERR_ALIGNMENT;
+    const long long limit = 0x7fffffffLL, far = limit - 1024;
+    if ((long long)p->pages * p->page_size > limit || (long long)p->columns * p->page_size > far ||
+        (long long)p->Lq * (p->Hq / p->Hkv) > far || (long long)p->B * p->Hq > limit || (long long)p->B * p->Hq * p->Lq > limit)
+        return GS_ERR_SHAPE;
+    a = gs::XattnArgs{};
+    a.dtype = p->dtype;
+    a.B = p->B; a.Lq = p->Lq; a.Lk = p->columns * p->page_size; a.Hq = p->Hq; a.Hkv = p->Hkv; a.G = p->Hq / p->Hkv;
+    a.dk = p->dk; a.dv = p->dv;
+    a.rows = (long long)a.Lq * a.G;
+    a.scale = p->scale;
+    a.lens = p->lens;
+    a.splits = a.rsplits = 1;
+    a.win = {p->window, p->sinks, 0, nullptr};
+    int shift = 0;
+    while (1 << shift < p->page_size && shift < 30) ++shift;
+    a.pg = {p->pages, p->page_size, p->columns, 1 << shift == p->page_size ? shift : -1, p->table, p->ld_table, p->q_lens};
+    return GS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+gs_status gs_cross_attention_workspace(const gs_attn* p, int backward, long long* bytes) {
+    return attn_workspace_size(p, nullptr, backward, bytes);
+}
+
+gs_status gs_cross_attention(const gs_attn* p, const gs_heads* Q, const gs_heads* K, const gs_heads* V,
+                             const gs_heads* O, float* lse, void* workspace, long long workspace_bytes,
+                             void* stream) {
+    return attn_forward(p, nullptr, Q, K, V, O, lse, workspace, workspace_bytes, stream);
+}
+
+gs_status gs_cross_attention_backward(const gs_attn* p, const gs_heads* Q, const gs_heads* K, const gs_heads* V,
+                                      const gs_heads* O, const float* lse, const gs_heads* dO, const gs_heads* dQ,
+                                      const gs_heads* dK, const gs_heads* dV, void* workspace,
+                                      long long workspace_bytes, void* stream) {
+    return attn_backward(p, nullptr, Q, K, V, O, lse, dO, dQ, dK, dV, workspace, workspace_bytes, stream);
+}
+
+gs_status gs_window_attention_workspace(const gs_attn* p, const gs_window* w, int backward, long long* bytes) {
+    if (!w) return GS_ERR_INVALID_ARG;
+    return attn_workspace_size(p, w, backward, bytes);
+}
+
+gs_status gs_window_attention(const gs_attn* p, const gs_window* w, const gs_heads* Q, const gs_heads* K, const gs_heads* V,
+                              const gs_heads* O, float* lse, void* workspace, long long workspace_bytes, void* stream) {
+    if (!w) return GS_ERR_INVALID_ARG;
+    return attn_forward(p, w, Q, K, V, O, lse, workspace, workspace_bytes, stream);
+}
+
+gs_status gs_window_attention_backward(const gs_attn* p, const gs_window* w, const gs_heads* Q, const gs_heads* K,
+                                       const gs_heads* V, const gs_heads* O, const float* lse, const gs_heads* dO,
+                                       const gs_heads* dQ, const gs_heads* dK, const gs_heads* dV, void* workspace,
+                                       long long workspace_bytes, void* stream) {
+    if (!w) return GS_ERR_INVALID_ARG;
+    return attn_backward(p, w, Q, K, V, O, lse, dO, dQ, dK, dV, workspace, workspace_bytes, stream);
+}
+
+gs_status gs_paged_attention_workspace(const gs_paged* p, long long* bytes) {
+    if (!bytes) return GS_ERR_INVALID_ARG;
+    *bytes = 0;
+    gs::XattnArgs a;
+    gs_status st = paged_args(p, a);
+    if (st != GS_OK) return st;
+    int dev = 0, sms = 0;
+    if ((st = attn_device(dev, sms)) != GS_OK) return st;
+    // the arrays' alignment, not known here, decides between the paths: room for either
+    gs::xattn_rows_plan(a, sms, gs::kPagedKeys);
+    *bytes = 4 * gs::xattn_round4(gs::xattn_ws_forward(a));
+    if (a.dtype == GS_BF16 && p->flags != GS_PATH_SIMT) *bytes = std::max(*bytes, gs::paged_mma_bytes(a, sms));
+    return GS_OK;
+}
+
+gs_status gs_paged_attention(const gs_paged* p, const gs_heads* Q, const gs_heads* K, const gs_heads* V, const gs_heads* O,
+                             float* lse, void* workspace, long long workspace_bytes, void* stream) {
+    gs::XattnArgs a;
+    gs_status st = paged_args(p, a);
+    if (st != GS_OK) return st;
+    if (!Q || !K || !V || !O) return GS_ERR_INVALID_ARG;
+    if (!valid_heads(Q, a.B, a.Lq, a.Hq, false) || !valid_heads(K, p->pages, p->page_size, a.Hkv, false) ||
+        !valid_heads(V, p->pages, p->page_size, a.Hkv, false) || !valid_heads(O, a.B, a.Lq, a.Hq, true))
+        return GS_ERR_SHAPE;
+    if (a.B == 0 || a.Lq == 0) return GS_OK;
+    if (!Q->data || !O->data || !p->lens || (a.Lk > 0 && !p->table) || (p->pages > 0 && (!K->data || !V->data)))
+        return GS_ERR_INVALID_ARG;
+    if (!on_elements(a.dtype == GS_F32 ? 4 : 2, Q->data, K->data, V->data, O->data) || !on_elements(4, lse)) return GS_ERR_ALIGNMENT;
+    int dev = 0, sms = 0;
+    if ((st = attn_device(dev, sms)) != GS_OK) return st;
+    a.q = view_of(Q); a.k = view_of(K); a.v = view_of(V); a.o = view_of(O);
+    a.lse = lse;
+    a.ws = (float*)workspace;
+    const bool tc_ok = gs::paged_mma_supported(a);
+    if (p->flags == GS_PATH_TENSOR && !tc_ok)
+        return a.dtype != GS_BF16 || a.dk % 8 || a.dv % 8 ? GS_ERR_UNSUPPORTED : GS_ERR_ALIGNMENT;
+    if (tc_ok && p->flags != GS_PATH_SIMT) {
+        if ((st = attn_workspace(a.ws, workspace_bytes, (gs::paged_mma_bytes(a, sms) + 3) / 4)) != GS_OK) return st;
+        return from_cuda(gs::launch_paged_mma(a, sms, dev, (cudaStream_t)stream));
+    }
+    gs::xattn_rows_plan(a, sms, gs::kPagedKeys);
+    if ((st = attn_workspace(a.ws, workspace_bytes, gs::xattn_round4(gs::xattn_ws_forward(a)))) != GS_OK) return st;
+    return from_cuda(gs::launch_xattn_rows(a, gs::kPagedKeys, (cudaStream_t)stream));
+}
+
+gs_status gs_page_slots(const int* lens, const int* added, int B, int Lnew, int page_size, int pages, const int* free_list,
+                        int n_free, const int* free_from, int* table, long long ld_table, int columns, int* slots,
+                        int* new_lens, int* taken, void* stream) {
+    if (B < 0 || Lnew < 0 || page_size < 1 || pages < 0 || n_free < 0 || columns < 0 || ld_table < columns) return GS_ERR_SHAPE;
+    const long long limit = 0x7fffffffLL, far = limit - 1024;
+    if ((long long)pages * page_size > limit || (long long)columns * page_size > far || (long long)B * columns > limit ||
+        (long long)B * Lnew > limit)
+        return GS_ERR_SHAPE;
+    if (!on_elements(4, lens, added, free_list, free_from, table, slots, new_lens, taken)) return GS_ERR_ALIGNMENT;
+    if (B > 0 && (!lens || !added || (columns > 0 && !table) || (n_free > 0 && !free_list) || (Lnew > 0 && !slots)))
+        return GS_ERR_INVALID_ARG;
+    // blocks read the lengths of the requests before theirs while others write: no output lies on an input
+    auto apart = [](const int* x, long long nx, const int* y, long long ny) {
+        return !x || !y || nx <= 0 || ny <= 0 || x + nx <= y || y + ny <= x;
+    };
+    const long long cells = B > 0 ? (B - 1) * ld_table + columns : 0, tokens = (long long)B * Lnew;
+    const struct { const int* p; long long n; } in[] = {{lens, B}, {added, B}, {free_list, n_free}, {free_from, 1}},
+                                                out[] = {{table, cells}, {slots, tokens}, {new_lens, B}, {taken, 1}};
+    for (int i = 0; i < 4; ++i) {
+        for (const auto& x : in)
+            if (!apart(x.p, x.n, out[i].p, out[i].n)) return GS_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (!apart(out[j].p, out[j].n, out[i].p, out[i].n)) return GS_ERR_INVALID_ARG;
+    }
+    if (B == 0 && !taken) return GS_OK;
+    int dev = 0, sms = 0;
+    gs_status st = attn_device(dev, sms);
+    if (st != GS_OK) return st;
+    gs::SlotArgs a{};
+    a.lens = lens; a.added = added; a.B = B; a.L = Lnew; a.page = page_size; a.pages = pages;
+    a.free_list = free_list; a.n_free = n_free; a.from = free_from;
+    a.table = table; a.ldt = ld_table; a.cols = columns;
+    a.slots = slots; a.new_lens = new_lens; a.taken = taken;
+    return from_cuda(gs::launch_page_slots(a, sms, (cudaStream_t)stream));
+}
+
+gs_status gs_page_store(int dtype, int B, int L, int H, int dk, int dv, const gs_heads* K, const gs_heads* V, const int* slots,
+                        long long ld_slots, int pages, int page_size, const gs_heads* Kc, const gs_heads* Vc, void* stream) {
+    if (dtype != GS_F32 && dtype != GS_BF16) return GS_ERR_INVALID_ARG;
+    if (!K || !V || !Kc || !Vc) return GS_ERR_INVALID_ARG;
+    const long long limit = 0x7fffffffLL;
+    if (B < 0 || L < 0 || H < 1 || dk < 1 || dv < 1 || pages < 0 || page_size < 1 || ld_slots < L ||
+        (long long)pages * page_size > limit || (long long)B * L > limit || (long long)H * std::max(dk, dv) > limit)
+        return GS_ERR_SHAPE;
+    if (!valid_heads(K, B, L, H, false) || !valid_heads(V, B, L, H, false) || !valid_heads(Kc, pages, page_size, H, true) ||
+        !valid_heads(Vc, pages, page_size, H, true))
+        return GS_ERR_SHAPE;
+    if (B == 0 || L == 0 || pages == 0) return GS_OK;
+    if (!K->data || !V->data || !Kc->data || !Vc->data || !slots) return GS_ERR_INVALID_ARG;
+    if (!on_elements(dtype == GS_F32 ? 4 : 2, K->data, V->data, Kc->data, Vc->data) || !on_elements(4, slots))
+        return GS_ERR_ALIGNMENT;
+    int dev = 0, sms = 0;
+    gs_status st = attn_device(dev, sms);
+    if (st != GS_OK) return st;
+    gs::StoreArgs a{};
+    a.bytes = dtype == GS_F32 ? 4 : 2;
+    a.B = B; a.L = L; a.H = H; a.w[0] = dk; a.w[1] = dv;
+    a.src[0] = view_of(K); a.src[1] = view_of(V); a.dst[0] = view_of(Kc); a.dst[1] = view_of(Vc);
+    a.slots = slots; a.lds = ld_slots; a.pages = pages; a.page = page_size;
+    return from_cuda(gs::launch_page_store(a, sms, (cudaStream_t)stream));
+}
+
+gs_status gs_verify_drafts(const void* P, const void* D, int dtype, int B, int K, int M, long long p_batch, long long p_row,
+                           long long d_batch, long long d_row, const int* drafts, const int* draft_lens, const float* U,
+                           int* accepted, int* tokens, void* stream) {
+    if (dtype != GS_F32 && dtype != GS_BF16) return GS_ERR_INVALID_ARG;
+    if (B < 0 || K < 0 || M < 1 || M > (1 << 19) || p_batch < 0 || p_row < 0 || d_batch < 0 || d_row < 0 ||
+        (long long)B * (K + 1LL) > 0x7fffffffLL)
+        return GS_ERR_SHAPE;
+    if (B == 0) return GS_OK;
+    if (!P || !U || (!accepted && !tokens) || (K > 0 && !drafts)) return GS_ERR_INVALID_ARG;
+    if (!on_elements(dtype == GS_F32 ? 4 : 2, P, D) || !on_elements(4, drafts, draft_lens, U, accepted, tokens))
+        return GS_ERR_ALIGNMENT;
+    int dev = 0, sms = 0;
+    gs_status st = attn_device(dev, sms);
+    if (st != GS_OK) return st;
+    gs::VerifyArgs a{};
+    a.P = P; a.D = D; a.bf16 = dtype == GS_BF16; a.B = B; a.K = K; a.M = M;
+    a.pb = p_batch; a.pr = p_row; a.db = d_batch; a.dr = d_row;
+    a.drafts = drafts; a.dlens = draft_lens; a.U = U; a.accepted = accepted; a.tokens = tokens;
+    return from_cuda(gs::launch_verify(a, sms, (cudaStream_t)stream));
 }
 
 gs_status gs_sample_scores(const void* S, int s_dtype, long long N, int M, long long lds, const gs_sampling* how,

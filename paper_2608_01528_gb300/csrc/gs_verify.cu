@@ -1,0 +1,254 @@
+// gs_verify.cu -- drafted tokens checked against the target's probabilities.
+//
+// Draft x_i is kept while U_i D_i(x_i) < P_i(x_i).  The token behind the kept ones is drawn from max(P_i - D_i, 0) of the first
+// draft that is not kept, or from the target's row behind the last one.  Only that one row of P (and of D) is read: by a cluster of
+// up to 8 CTAs, a contiguous piece a warp.  The pieces' sums meet in shared memory across the cluster, and the warp whose piece holds the
+// drawn point looks through it again (by then in L1 or L2).
+//
+// Weights are integers in units of 2^-44, rint(p 2^44) - rint(d 2^44), so that every sum is exact in any order.  A conversion in two steps of
+// fp32, p 2^21 = hi + lo 2^-23 with hi and lo read off the mantissas of sums with 1.5 2^23, costs four FMAs or adds; conversions to 64-bit
+// integers run at an eighth of that rate.
+
+#include <algorithm>
+
+#include "gs_paged.h"
+#include "gs_tc_ptx.cuh"
+
+namespace gs {
+namespace {
+
+using u64 = unsigned long long;
+
+constexpr int kWarps = 16, kThreads = kWarps * 32;
+constexpr int kMaxCtas = 8;
+constexpr float kHigh = 2097152.f, kLow = 8388608.f, kMagic = 12582912.f;  // 2^21, 2^23, 1.5 * 2^23
+constexpr int kMagicBits = 0x4B400000;
+
+struct Parts {
+    int hi, lo;  // (hi 2^23 + lo) units
+};
+__device__ __forceinline__ Parts parts_of(float p) {  // p in [0, 1]
+    const float a = fmaf(p, kHigh, kMagic), t = a - kMagic;
+    const float b = fmaf(fmaf(p, kHigh, -t), kLow, kMagic);  // (the inner one is exact)
+    return {__float_as_int(a) - kMagicBits, __float_as_int(b) - kMagicBits};
+}
+
+// What the rows weigh: P alone, P without one entry, or P less D.
+enum Rest { kTarget, kWithout, kLess };
+struct Row {
+    const void *p, *d;
+    int rest, x;
+};
+template <typename T>
+__device__ __forceinline__ float read(const void* row, int j) {
+    if constexpr (sizeof(T) == 4)
+        return __ldg(static_cast<const float*>(row) + j);
+    else
+        return __uint_as_float((uint32_t)__ldg(static_cast<const unsigned short*>(row) + j) << 16);
+}
+__device__ __forceinline__ void add(float p, float d, int& hi, int& lo) {  // NaN counts as 0, what is above 1 as 1
+    p = __saturatef(p);
+    d = __saturatef(d);
+    const Parts x = parts_of(p), y = parts_of(d);
+    if (p > d) {
+        hi += x.hi - y.hi;
+        lo += x.lo - y.lo;
+    }
+}
+__device__ __forceinline__ long long units(int hi, int lo) { return (long long)hi * 8388608ll + lo; }
+template <typename T>
+__device__ __forceinline__ u64 weight(const Row& r, int j) {
+    const float p = read<T>(r.p, j), d = r.rest == kLess ? read<T>(r.d, j) : r.rest == kWithout && j == r.x ? 1.f : 0.f;
+    int hi = 0, lo = 0;
+    add(p, d, hi, lo);
+    return (u64)units(hi, lo);
+}
+
+// Sum of the weights [j0, j1) (a warp).
+template <typename T>
+__device__ __forceinline__ u64 sum_piece(const Row& r, int j0, int j1, bool vec) {
+    constexpr int N = 16 / sizeof(T), kAhead = 2;
+    const int lane = threadIdx.x & 31;
+    long long sum = 0;
+    int j = j0;
+    if (vec) {
+        for (; j + 32 * N <= j1; j += 32 * N * kAhead) {
+            uint4 a[kAhead], b[kAhead];
+            bool in[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int at = j + 32 * N * u + lane * N;
+                in[u] = j + 32 * N * (u + 1) <= j1;
+                a[u] = in[u] ? __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(r.p) + at)) : make_uint4(0, 0, 0, 0);
+                b[u] = in[u] && r.rest == kLess ? __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(r.d) + at))
+                                                : make_uint4(0, 0, 0, 0);
+            }
+            int hi = 0, lo = 0;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const uint32_t x[4] = {a[u].x, a[u].y, a[u].z, a[u].w}, y[4] = {b[u].x, b[u].y, b[u].z, b[u].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (sizeof(T) == 4) {
+                        add(__uint_as_float(x[e]), __uint_as_float(y[e]), hi, lo);
+                    } else {
+                        add(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), hi, lo);
+                        add(__uint_as_float(x[e] & 0xffff0000u), __uint_as_float(y[e] & 0xffff0000u), hi, lo);
+                    }
+                }
+            }
+            sum += units(hi, lo);
+            if (!in[kAhead - 1]) {
+                j += 32 * N;
+                break;
+            }
+        }
+        if (r.rest == kWithout && lane == 0 && r.x >= j0 && r.x < j) {  // the entry that is left out, taken off again
+            int hi = 0, lo = 0;
+            add(read<T>(r.p, r.x), 0.f, hi, lo);
+            sum -= units(hi, lo);
+        }
+    }
+    for (j += lane; j < j1; j += 32) sum += (long long)weight<T>(r, j);
+    u64 v = (u64)sum;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// The first index of [j0, j1) whose running weight is above t (there is one); a warp.
+template <typename T>
+__device__ int locate(const Row& r, int j0, int j1, u64 t) {
+    const int lane = threadIdx.x & 31;
+    for (;;) {
+        const int n = j1 - j0, per = (n + 31) / 32, a = min(j1, j0 + lane * per), b = min(j1, a + per);
+        u64 v = 0;
+        for (int j = a; j < b; ++j) v += weight<T>(r, j);
+        u64 run = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const u64 x = __shfl_up_sync(0xffffffffu, run, o);
+            if (lane >= o) run += x;
+        }
+        const unsigned above = __ballot_sync(0xffffffffu, run > t);
+        if (!above) return -1;
+        const int who = __ffs(above) - 1;
+        t -= __shfl_sync(0xffffffffu, run - v, who);
+        j0 = __shfl_sync(0xffffffffu, a, who);
+        j1 = __shfl_sync(0xffffffffu, b, who);
+        if (j1 - j0 <= 1) return j0;
+    }
+}
+
+__device__ __forceinline__ float unit_of(float u) {  // negative and NaN: 0; from 1 on: the last number before it
+    return u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
+}
+__device__ __forceinline__ void put_remote(uint64_t* at, unsigned rank, u64 v) {
+    uint32_t addr;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(ptx::smem_u32(at)), "r"(rank));
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) k_verify(const VerifyArgs a, int ctas) {
+    __shared__ uint64_t totals[2][kMaxCtas];
+    __shared__ u64 sums[kWarps];
+    __shared__ int s_kept;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int b = blockIdx.x / ctas, rank = blockIdx.x % ctas;
+    const int n = a.dlens ? min(max(__ldg(a.dlens + b), 0), a.K) : a.K;
+    const int* drafts = a.drafts + (long long)b * a.K;
+    const float* U = a.U + (long long)b * (a.K + 1);
+    const T* P = static_cast<const T*>(a.P) + b * a.pb;
+    const T* D = a.D ? static_cast<const T*>(a.D) + b * a.db : nullptr;
+    if (warp == 0) {
+        int kept = 0;
+        for (int i0 = 0; i0 < n; i0 += 32) {
+            const int i = i0 + lane;
+            bool ok = false;
+            if (i < n) {
+                const int x = __ldg(drafts + i);
+                if (x >= 0 && x < a.M) {
+                    const double d = D ? (double)read<T>(D + i * a.dr, x) : 1.0;
+                    ok = (double)unit_of(__ldg(U + i)) * d < (double)read<T>(P + i * a.pr, x);
+                }
+            }
+            const unsigned good = __ballot_sync(0xffffffffu, ok);
+            kept = i0 + (good == 0xffffffffu ? 32 : __ffs(~good) - 1);
+            if (good != 0xffffffffu) break;
+        }
+        if (lane == 0) s_kept = min(kept, n);
+    }
+    ptx::cluster_sync_all();  // every CTA of the cluster runs from here on
+    __syncthreads();
+    const int kept = s_kept;
+    Row row;
+    row.p = P + kept * a.pr;
+    row.d = D ? D + kept * a.dr : nullptr;
+    row.rest = kept == n ? kTarget : D ? kLess : kWithout;
+    row.x = kept < n ? __ldg(drafts + kept) : -1;
+    constexpr int kStep = 32 * 16 / sizeof(T);  // entries of a warp's load
+    const int steps = (a.M + kStep - 1) / kStep, me = rank * kWarps + warp, all = ctas * kWarps;
+    const int j0 = min(a.M, (int)((long long)steps * me / all) * kStep), j1 = min(a.M, (int)((long long)steps * (me + 1) / all) * kStep);
+    u64 mine = 0, before = 0, total = 0;
+    for (int turn = 0; turn < 2; ++turn) {  // (again with P alone where nothing is left of it)
+        const bool vec = ((uintptr_t)row.p | (row.rest == kLess ? (uintptr_t)row.d : 0)) % 16 == 0;
+        mine = sum_piece<T>(row, j0, j1, vec);
+        if (lane == 0) sums[warp] = mine;
+        __syncthreads();
+        if (warp == 0) {
+            u64 v = lane < kWarps ? sums[lane] : 0;
+#pragma unroll
+            for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+            if (lane < ctas) put_remote(&totals[turn][rank], lane, v);
+        }
+        ptx::cluster_sync_all();
+        __syncthreads();
+        before = total = 0;
+        for (int c = 0; c < ctas; ++c) {
+            if (c < rank) before += totals[turn][c];
+            total += totals[turn][c];
+        }
+        for (int w = 0; w < warp; ++w) before += sums[w];
+        if (total != 0 || row.rest == kTarget) break;
+        row.rest = kTarget;
+        __syncthreads();
+    }
+    // run > U total, with U 2^64 an integer (from 2^-40 on) and run one: run > floor
+    const float u = unit_of(__ldg(U + a.K));
+    const u64 t = __umul64hi((u64)__float2ull_rz(u * 18446744073709551616.f), total);
+    int drawn = -1;
+    if (total == 0) {
+        if (me != 0) return;
+    } else {
+        if (t < before || t >= before + mine) return;  // another warp's
+        drawn = locate<T>(row, j0, j1, t - before);
+    }
+    if (lane == 0 && a.accepted) a.accepted[b] = kept;
+    if (a.tokens)
+        for (int i = lane; i <= a.K; i += 32)
+            a.tokens[(long long)b * (a.K + 1) + i] = i < kept ? __ldg(drafts + i) : i == kept ? drawn : -1;
+}
+
+}  // namespace
+
+cudaError_t launch_verify(const VerifyArgs& a, int sms, cudaStream_t s) {
+    // a warp's piece of four loads or more, and no more CTAs than run at once while one a row fills the GPU
+    const long long steps = ((long long)a.M * (a.bf16 ? 2 : 4) + 511) / 512;
+    int ctas = 1;
+    while (ctas < kMaxCtas && steps >= 4ll * kWarps * ctas && (long long)a.B * ctas < 4ll * sms) ctas *= 2;
+    if ((long long)a.B * ctas > 0x7fffffffLL) ctas = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(a.B * (long long)ctas));
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)ctas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return a.bf16 ? cudaLaunchKernelEx(&cfg, k_verify<__nv_bfloat16>, a, ctas) : cudaLaunchKernelEx(&cfg, k_verify<float>, a, ctas);
+}
+
+}  // namespace gs

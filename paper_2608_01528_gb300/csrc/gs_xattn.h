@@ -14,6 +14,21 @@ struct HeadView {  // element strides of b, l, h; the last axis is dense
     long long b, l, h;
 };
 
+// A sliding window: row l of sequence b stands at position start + l and reads the keys up to itself, the last `window` of them
+// (kNoWindow: all) and the first `sinks`.
+constexpr int kNoWindow = 0x7fffffff;
+struct KeyWindow {
+    int window, sinks, start;
+    const int* starts;  // one per sequence, or NULL: start
+};
+// Keys and values in pages (the views' b is then the page, l the row in it); the last of a sequence's query rows is its last key.
+struct KeyPages {
+    int pages, page, cols, shift;  // page = 1 << shift, or shift < 0
+    const int* table;              // B x cols
+    long long ldt;
+    const int* qlens;  // query rows of each sequence, or NULL: Lq
+};
+
 struct XattnArgs {
     int dtype, B, Lq, Lk, Hq, Hkv, G, dk, dv;
     long long rows;  // Lq * G packed rows per (b, key head)
@@ -28,7 +43,48 @@ struct XattnArgs {
     int rsplits;   // dK / dV: parts of the packed rows
     int vec;       // CUDA-core kernels: which arrays allow loads of four elements
     long long stats;  // backward: floats of the rows' statistics at the start of the workspace
+    KeyWindow win;
+    KeyPages pg;
 };
+
+// What a kernel reads the keys through.
+enum KeyMode { kAllKeys = 0, kWindowKeys = 1, kPagedKeys = 2 };
+
+// Keys [0, sink) and [lo, hi), sink <= lo: all that a row, or some row of several, sees (before lengths and masks of keys).
+struct KeySpan {
+    int sink, lo, hi;
+    __device__ __forceinline__ int count() const { return sink + hi - lo; }
+    __device__ __forceinline__ int key(int i) const { return i < sink ? i : i - sink + lo; }  // the i-th
+};
+// of the rows l0..l1 of sequence b with n keys (l0 <= l1)
+template <int MODE>
+static __device__ __forceinline__ KeySpan key_span(const XattnArgs& a, int b, long long l0, long long l1, int n) {
+    KeySpan s;
+    if constexpr (MODE == kAllKeys) {
+        s.sink = s.lo = 0;
+        s.hi = n;
+    } else {
+        long long p0 = l0, p1 = l1;
+        if constexpr (MODE == kPagedKeys) {
+            const int m = a.pg.qlens ? min(max(__ldg(a.pg.qlens + b), 0), a.Lq) : a.Lq;
+            p1 = l0 < m ? (l1 < m ? l1 : m - 1) : m - 1 - (long long)n;  // (no row: a position before the first key)
+            p0 += (long long)n - m;
+            p1 += (long long)n - m;
+        } else {
+            const long long first = a.win.starts ? __ldg(a.win.starts + b) : a.win.start;
+            p0 += first;
+            p1 += first;
+        }
+        s.hi = (int)(p1 + 1 < 0 ? 0 : p1 + 1 < n ? p1 + 1 : n);
+        const long long lo = a.win.window == kNoWindow ? 0 : p0 - a.win.window + 1;
+        s.lo = (int)(lo < 0 ? 0 : lo < s.hi ? lo : s.hi);
+        s.sink = a.win.sinks < s.lo ? a.win.sinks : s.lo;
+    }
+    return s;
+}
+// Bits [c0, c1) of the 32 from `at` on.
+static __device__ __forceinline__ uint32_t bits_below(int x) { return x >= 32 ? 0xffffffffu : x <= 0 ? 0u : (1u << x) - 1u; }
+static __device__ __forceinline__ uint32_t bits_between(int c0, int c1) { return bits_below(c1) & ~bits_below(c0); }
 
 // How many parts a kernel cuts its long axis into, so that about `want` blocks run: `base` blocks
 // exist without a split, `tiles` is the axis' length in tiles, and a part has `least` tiles or more.
@@ -93,15 +149,58 @@ static __device__ __forceinline__ int few_keys(const XattnArgs& a, int b, int j0
     return found;
 }
 
+// The same of what one row sees through a window (span), whether a mask thins it out or not: LANES neighbouring lanes work on a
+// row of their own, in step with the warp's others; the i-th key is lane i % LANES's `mine` where i < LANES.
+template <int LANES>
+static __device__ __forceinline__ int few_seen(const XattnArgs& a, int b, const KeySpan& span, int& mine) {
+    static_assert(LANES >= kFewKeys, "a key a lane");
+    const int lane = threadIdx.x & (LANES - 1), shift = (threadIdx.x & 31) & ~(LANES - 1);
+    const unsigned all = LANES == 32 ? 0xffffffffu : (1u << (LANES & 31)) - 1u;
+    const unsigned char* mask = a.mask ? a.mask + (long long)b * a.ldm : nullptr;
+    const int count = span.count();
+    int found = 0;
+    bool done = count == 0 || (!mask && count > kFewKeys);
+    if (done && count) found = -1;
+    for (int i0 = 0; __any_sync(0xffffffffu, !done); i0 += LANES) {
+        const int i = i0 + lane, j = span.key(i);
+        const bool in = !done && i < count && (!mask || __ldg(mask + j) != 0);
+        unsigned w = __ballot_sync(0xffffffffu, in) >> shift & all;
+        if (!done) {
+            if (found + __popc(w) > kFewKeys) {
+                found = -1;
+                done = true;
+            } else {
+                for (; w; w &= w - 1, ++found)
+                    if (lane == found) mine = span.key(i0 + __ffs(w) - 1);
+                done = i0 + LANES >= count;
+            }
+        }
+    }
+    return found;
+}
+
+// Query rows [first, end) of sequence b that see some of the keys [j0, j1).
+struct RowSpan {
+    long long first, end;
+};
+static __device__ __forceinline__ RowSpan row_span(const XattnArgs& a, int b, int j0, int j1) {
+    const long long start = a.win.starts ? __ldg(a.win.starts + b) : a.win.start;
+    RowSpan r;
+    r.first = min(max(j0 - start, 0ll), (long long)a.Lq);
+    r.end = j0 < a.win.sinks || a.win.window == kNoWindow ? a.Lq : min(max(j1 - 1 + (long long)a.win.window - start, r.first), (long long)a.Lq);
+    if (j1 <= j0) r.end = r.first;
+    return r;
+}
+
 // ----------------------------------------------------------------- few rows (gs_xattn_rows.cu)
-void xattn_rows_plan(XattnArgs& a, int sms);
-cudaError_t launch_xattn_rows(const XattnArgs& a, cudaStream_t s);
+void xattn_rows_plan(XattnArgs& a, int sms, KeyMode mode);
+cudaError_t launch_xattn_rows(const XattnArgs& a, KeyMode mode, cudaStream_t s);
 
 // ----------------------------------------------------------------- CUDA cores (gs_xattn_simt.cu)
 // the parts (splits, rsplits) that the CUDA-core kernels take on `sms` multiprocessors
-void xattn_simt_plan(XattnArgs& a, bool backward, int sms);
-cudaError_t launch_xattn_simt(const XattnArgs& a, cudaStream_t s);
-cudaError_t launch_xattn_simt_backward(const XattnArgs& a, cudaStream_t s);
+void xattn_simt_plan(XattnArgs& a, bool backward, int sms, KeyMode mode);
+cudaError_t launch_xattn_simt(const XattnArgs& a, KeyMode mode, cudaStream_t s);
+cudaError_t launch_xattn_simt_backward(const XattnArgs& a, KeyMode mode, cudaStream_t s);
 // O and lse from a.splits parts; dQ, dK, dV from theirs
 cudaError_t launch_xattn_join(const XattnArgs& a, cudaStream_t s);
 cudaError_t launch_xattn_join_dq(const XattnArgs& a, cudaStream_t s);
@@ -109,12 +208,12 @@ cudaError_t launch_xattn_join_dkv(const XattnArgs& a, cudaStream_t s);
 
 // ----------------------------------------------------------------- tcgen05 (gs_xattn_tc.cu)
 // bf16, at most 128 query heads to a key head, inputs on 16-byte boundaries with strides in multiples of 8
-void xattn_tc_plan(XattnArgs& a, int sms);
-cudaError_t launch_xattn_tc(const XattnArgs& a, int sms, int device, cudaStream_t s);
+void xattn_tc_plan(XattnArgs& a, KeyMode mode, int sms);
+cudaError_t launch_xattn_tc(const XattnArgs& a, KeyMode mode, int sms, int device, cudaStream_t s);
 unsigned take_device_error_xattn();
 // the gradient (gs_xattn_bwd_tc.cu)
-void xattn_bwd_tc_plan(XattnArgs& a, int sms);
-cudaError_t launch_xattn_bwd_tc(const XattnArgs& a, int device, cudaStream_t s);
+void xattn_bwd_tc_plan(XattnArgs& a, KeyMode mode, int sms);
+cudaError_t launch_xattn_bwd_tc(const XattnArgs& a, KeyMode mode, int device, cudaStream_t s);
 unsigned take_device_error_xbwd();
 
 // ----------------------------------------------------------------- odd widths for the tensor cores (gs_xattn_pack.cu)

@@ -815,7 +815,7 @@ unsigned take_device_error_xbwd() {
     return v;
 }
 
-void xattn_bwd_tc_plan(XattnArgs& a, int sms) {
+void xattn_bwd_tc_plan(XattnArgs& a, KeyMode mode, int sms) {
     const long long nl = kTile / a.G;
     const long long kt = (a.Lk + kTile - 1) / kTile, rt = (a.Lq + nl - 1) / nl;
     // the keys (rows) are cut into parts of two tiles or more where one CTA per row (key) tile leaves multiprocessors idle
@@ -824,7 +824,7 @@ void xattn_bwd_tc_plan(XattnArgs& a, int sms) {
     a.stats = rt * a.Hkv * a.B * kStats;
 }
 
-cudaError_t launch_xattn_bwd_tc(const XattnArgs& a, int device, cudaStream_t s) {
+cudaError_t launch_xattn_bwd_tc(const XattnArgs& a, KeyMode mode, int device, cudaStream_t s) {
     if (device < 0 || device >= 64) return cudaErrorInvalidDevice;
     g_launched = true;
     Params p{};

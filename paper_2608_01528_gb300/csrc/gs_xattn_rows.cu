@@ -64,7 +64,7 @@ struct Vec {
     }
 };
 
-template <typename T, int LK, int R>
+template <typename T, int LK, int R, int MODE>
 __global__ void __launch_bounds__(kThreads, R == 1 ? 3 : 2) k_xattn_rows(const XattnArgs a, long long chunks) {
     using V = Vec<T>;
     constexpr int N = V::N, W = LK * N, KS = 32 / LK;
@@ -81,7 +81,18 @@ __global__ void __launch_bounds__(kThreads, R == 1 ? 3 : 2) k_xattn_rows(const X
     const int hk = (int)(i % a.Hkv), b = (int)(i / a.Hkv);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, slot = lane / LK, e0 = (lane % LK) * N;
     const int n = keys_of(a, b);
-    const int k0 = (int)((long long)a.Lk * part / a.splits), k1 = min(n, (int)((long long)a.Lk * (part + 1) / a.splits));
+    // Keys k0..k1 - 1 of all, or, through a window, of those that some row of the block sees.
+    KeySpan span;
+    int k0, k1;
+    if constexpr (MODE == kAllKeys) {
+        k0 = (int)((long long)a.Lk * part / a.splits);
+        k1 = min(n, (int)((long long)a.Lk * (part + 1) / a.splits));
+    } else {
+        const long long last = min(a.rows, chunk * R + R) - 1;
+        span = key_span<MODE>(a, b, chunk * R / a.G, last / a.G, n);
+        k0 = (int)((long long)span.count() * part / a.splits);
+        k1 = (int)((long long)span.count() * (part + 1) / a.splits);
+    }
     const float cs = a.scale * kLog2e;
 
     // After the halving, lane x of a key's LK holds values x * kOwn .. + kOwn - 1 of row-major [R][kBatch] (kOwn values, or one
@@ -102,16 +113,42 @@ __global__ void __launch_bounds__(kThreads, R == 1 ? 3 : 2) k_xattn_rows(const X
 #pragma unroll
         for (int e = 0; e < N; ++e) acc[r][e] = 0.f;
     }
-    const T* kp = reinterpret_cast<const T*>(a.k.p) + b * a.k.b + hk * a.k.h + e0;
-    const T* vp = reinterpret_cast<const T*>(a.v.p) + b * a.v.b + hk * a.v.h + e0;
+    const T* kp = reinterpret_cast<const T*>(a.k.p) + (MODE == kPagedKeys ? 0 : b * a.k.b) + hk * a.k.h + e0;
+    const T* vp = reinterpret_cast<const T*>(a.v.p) + (MODE == kPagedKeys ? 0 : b * a.v.b) + hk * a.v.h + e0;
+    [[maybe_unused]] KeySpan mine;  // of the row that this lane's values belong to
+    if constexpr (MODE != kAllKeys) {
+        const long long l = min(a.rows - 1, chunk * R + own / kBatch) / a.G;
+        mine = key_span<MODE>(a, b, l, l, n);
+    }
     const unsigned char* mask = a.mask ? a.mask + (long long)b * a.ldm : nullptr;
     V kx[kBatch], vx[kBatch], kn[kBatch], vn[kBatch];
     bool ok[kBatch], okn[kBatch];
     auto fetch = [&](int j0, V(&kk)[kBatch], V(&vv)[kBatch], bool(&o)[kBatch]) {
+        if constexpr (MODE == kPagedKeys) {
+            int entry[kBatch], row[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const int i = j0 + u * KS + slot, j = i < k1 ? span.key(i) : 0;
+                const int col = a.pg.shift >= 0 ? j >> a.pg.shift : j / a.pg.page;
+                row[u] = j - col * a.pg.page;
+                entry[u] = i < k1 ? __ldg(a.pg.table + (long long)b * a.pg.ldt + col) : -1;
+            }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                o[u] = entry[u] >= 0 && entry[u] < a.pg.pages;
+                kk[u].load(kp + (o[u] ? (long long)entry[u] * a.k.b + (long long)row[u] * a.k.l : 0), o[u] ? a.dk - e0 : 0,
+                           a.vec & kVecK);
+                vv[u].load(vp + (o[u] ? (long long)entry[u] * a.v.b + (long long)row[u] * a.v.l : 0), o[u] ? a.dv - e0 : 0,
+                           a.vec & kVecV);
+            }
+            return;
+        }
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            const int j = j0 + u * KS + slot;
-            o[u] = j < k1 && (!mask || __ldg(mask + j) != 0);
+            int j = j0 + u * KS + slot;
+            const bool in = j < k1;
+            if constexpr (MODE == kWindowKeys) j = span.key(j);
+            o[u] = in && (!mask || __ldg(mask + j) != 0);
             kk[u].load(kp + (o[u] ? (long long)j * a.k.l : 0), o[u] ? a.dk - e0 : 0, a.vec & kVecK);
             vv[u].load(vp + (o[u] ? (long long)j * a.v.l : 0), o[u] ? a.dv - e0 : 0, a.vec & kVecV);
         }
@@ -167,6 +204,10 @@ __global__ void __launch_bounds__(kThreads, R == 1 ? 3 : 2) k_xattn_rows(const X
             bool in = ok[0];
 #pragma unroll
             for (int k = 1; k < kBatch; ++k) in = u == k ? ok[k] : in;
+            if constexpr (MODE != kAllKeys) {
+                const int j = span.key(j0 + u * KS + slot);
+                in = in && j < mine.hi && (j >= mine.lo || j < mine.sink);
+            }
             s[i] = in ? s[i] * cs : -INFINITY;
             mn = fmaxf(mn, s[i]);
         }
@@ -198,9 +239,12 @@ __global__ void __launch_bounds__(kThreads, R == 1 ? 3 : 2) k_xattn_rows(const X
             float f2[N];
             vx[u].get(f2);
 #pragma unroll
-            for (int r = 0; r < R; ++r)
+            for (int r = 0; r < R; ++r) {
+                // (rows of a block may see different keys: what one does not see, whatever it holds, stays out of its sum)
+                if (MODE != kAllKeys && R > 1 && w[r * kBatch + u] == 0.f) continue;
 #pragma unroll
                 for (int e = 0; e < N; ++e) acc[r][e] = fmaf(w[r * kBatch + u], f2[e], acc[r][e]);
+            }
         }
     }
     // a row's sum over the lanes that hold its keys; then every lane has every row's maximum and sum
@@ -270,44 +314,51 @@ __global__ void __launch_bounds__(kThreads, R == 1 ? 3 : 2) k_xattn_rows(const X
 
 int rows_per_block(long long rows) { return rows >= 4 ? 4 : rows >= 2 ? 2 : 1; }
 
-template <typename T, int LK>
+template <typename T, int LK, int MODE>
 cudaError_t launch(const XattnArgs& a, cudaStream_t s) {
     const int R = rows_per_block(a.rows);
     const long long chunks = (a.rows + R - 1) / R;
     const unsigned grid = (unsigned)(chunks * a.splits * a.Hkv * a.B);
     if (R == 4)
-        k_xattn_rows<T, LK, 4><<<grid, kThreads, 0, s>>>(a, chunks);
+        k_xattn_rows<T, LK, 4, MODE><<<grid, kThreads, 0, s>>>(a, chunks);
     else if (R == 2)
-        k_xattn_rows<T, LK, 2><<<grid, kThreads, 0, s>>>(a, chunks);
+        k_xattn_rows<T, LK, 2, MODE><<<grid, kThreads, 0, s>>>(a, chunks);
     else
-        k_xattn_rows<T, LK, 1><<<grid, kThreads, 0, s>>>(a, chunks);
+        k_xattn_rows<T, LK, 1, MODE><<<grid, kThreads, 0, s>>>(a, chunks);
     return cudaGetLastError();
 }
+template <int MODE>
+cudaError_t launch_mode(const XattnArgs& a, cudaStream_t s) {
+    const int w = std::max(a.dk, a.dv);
+    if (a.dtype == GS_BF16) return w <= 64 ? launch<__nv_bfloat16, 8, MODE>(a, s) : launch<__nv_bfloat16, 16, MODE>(a, s);
+    return w <= 32 ? launch<float, 8, MODE>(a, s) : w <= 64 ? launch<float, 16, MODE>(a, s) : launch<float, 32, MODE>(a, s);
+}
 
-bool on_16(const XattnArgs& a, const HeadView& v, int L, int H) {
+bool on_16(const XattnArgs& a, const HeadView& v, int B, int L, int H) {
     const int n = a.dtype == GS_F32 ? 4 : 8;
-    return (uintptr_t)v.p % 16 == 0 && (a.B <= 1 || v.b % n == 0) && (L <= 1 || v.l % n == 0) && (H <= 1 || v.h % n == 0);
+    return (uintptr_t)v.p % 16 == 0 && (B <= 1 || v.b % n == 0) && (L <= 1 || v.l % n == 0) && (H <= 1 || v.h % n == 0);
 }
 
 }  // namespace
 
-void xattn_rows_plan(XattnArgs& a, int sms) {
+void xattn_rows_plan(XattnArgs& a, int sms, KeyMode mode) {
     const int R = rows_per_block(a.rows);
+    // through a window, a block's rows see no more than this
+    const long long keys = mode == kAllKeys ? a.Lk : std::min<long long>(a.Lk, (long long)a.win.window + a.win.sinks + R);
     // parts of 256 keys or more, up to four blocks a multiprocessor (three of one row or two of more are resident at a time)
-    a.splits = xattn_parts((a.rows + R - 1) / R * a.Hkv * a.B, a.Lk / 256, 4 * sms, 1);
+    a.splits = xattn_parts((a.rows + R - 1) / R * a.Hkv * a.B, keys / 256, 4 * sms, 1);
     a.rsplits = 1;
 }
 
-cudaError_t launch_xattn_rows(const XattnArgs& args, cudaStream_t s) {
+cudaError_t launch_xattn_rows(const XattnArgs& args, KeyMode mode, cudaStream_t s) {
     XattnArgs a = args;
-    a.vec = (on_16(a, a.q, a.Lq, a.Hq) ? kVecQ : 0) | (on_16(a, a.k, a.Lk, a.Hkv) ? kVecK : 0) |
-            (on_16(a, a.v, a.Lk, a.Hkv) ? kVecV : 0);
-    const int w = std::max(a.dk, a.dv);
-    cudaError_t e;
-    if (a.dtype == GS_BF16)
-        e = w <= 64 ? launch<__nv_bfloat16, 8>(a, s) : launch<__nv_bfloat16, 16>(a, s);
-    else
-        e = w <= 32 ? launch<float, 8>(a, s) : w <= 64 ? launch<float, 16>(a, s) : launch<float, 32>(a, s);
+    const bool paged = mode == kPagedKeys;
+    const int nb = paged ? a.pg.pages : a.B, nl = paged ? a.pg.page : a.Lk;
+    a.vec = (on_16(a, a.q, a.B, a.Lq, a.Hq) ? kVecQ : 0) | (on_16(a, a.k, nb, nl, a.Hkv) ? kVecK : 0) |
+            (on_16(a, a.v, nb, nl, a.Hkv) ? kVecV : 0);
+    const cudaError_t e = mode == kAllKeys      ? launch_mode<kAllKeys>(a, s)
+                          : mode == kWindowKeys ? launch_mode<kWindowKeys>(a, s)
+                                                : launch_mode<kPagedKeys>(a, s);
     if (e != cudaSuccess || a.splits == 1) return e;
     return launch_xattn_join(a, s);
 }

@@ -145,7 +145,8 @@ __device__ __forceinline__ int column(int q) {
     return D == 32 ? 2 * tx + q : 64 * (q / 4) + 4 * tx + q % 4;
 }
 // out[i][q] += sum_k W[ty + 16 i][k] X[k][column(q)] over a tile of K
-template <int D, int K = kTile, int RI>
+// (WIN: rows of a tile see different keys, and one that a row does not see stays out of its sum whatever it holds)
+template <int D, int K = kTile, bool WIN = false, int RI>
 __device__ __forceinline__ void weigh(float (&out)[RI][D / 16], const float* W, const float* X) {
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
 #pragma unroll 2
@@ -160,6 +161,7 @@ __device__ __forceinline__ void weigh(float (&out)[RI][D / 16], const float* W, 
 #pragma unroll
                 for (int i = 0; i < RI; ++i) {
                     const float p = q == 0 ? w[i].x : q == 1 ? w[i].y : q == 2 ? w[i].z : w[i].w;
+                    if (WIN && p == 0.f) continue;
                     out[i][0] = fmaf(p, x.x, out[i][0]);
                     out[i][1] = fmaf(p, x.y, out[i][1]);
                 }
@@ -173,6 +175,7 @@ __device__ __forceinline__ void weigh(float (&out)[RI][D / 16], const float* W, 
 #pragma unroll
                 for (int i = 0; i < RI; ++i) {
                     const float p = q == 0 ? w[i].x : q == 1 ? w[i].y : q == 2 ? w[i].z : w[i].w;
+                    if (WIN && p == 0.f) continue;
                     out[i][4 * c + 0] = fmaf(p, x.x, out[i][4 * c + 0]);
                     out[i][4 * c + 1] = fmaf(p, x.y, out[i][4 * c + 1]);
                     out[i][4 * c + 2] = fmaf(p, x.z, out[i][4 * c + 2]);
@@ -209,7 +212,43 @@ __device__ __forceinline__ Block block_of(long long tiles, int parts, int Hkv) {
     return k;
 }
 
-template <typename T, int DK, int DV>
+// Which keys a tile of packed rows [r0, r0 + R) reads: tiles [0, sinks) and [from, to) of 64, in this order.
+struct KeyTiles {
+    int sinks, from, count;
+    __device__ __forceinline__ int tile(int i) const { return i < sinks ? i : i - sinks + from; }
+};
+template <bool WIN, int R>
+__device__ __forceinline__ KeyTiles key_tiles(const XattnArgs& a, int b, long long r0, int n) {
+    KeyTiles t;
+    if constexpr (!WIN) {
+        t.sinks = t.from = 0;
+        t.count = (a.Lk + kTile - 1) / kTile;
+    } else {
+        const KeySpan s = key_span<kWindowKeys>(a, b, r0 / a.G, (min(a.rows, r0 + R) - 1) / a.G, n);
+        const int to = (s.hi + kTile - 1) / kTile;
+        t.from = s.lo / kTile;
+        t.sinks = min((s.sink + kTile - 1) / kTile, t.from);
+        t.count = t.sinks + max(0, to - t.from);
+    }
+    return t;
+}
+// The keys that the rows ty + 16 i of a tile see.
+template <bool WIN, int RI>
+__device__ __forceinline__ void row_spans(KeySpan (&span)[RI], const XattnArgs& a, int b, long long r0, int n) {
+    if constexpr (WIN) {
+#pragma unroll
+        for (int i = 0; i < RI; ++i) {
+            const long long l = min(a.rows - 1, r0 + (threadIdx.x >> 4) + 16 * i) / a.G;
+            span[i] = key_span<kWindowKeys>(a, b, l, l, n);
+        }
+    }
+}
+template <bool WIN>
+__device__ __forceinline__ bool sees(const KeySpan& s, int j) {
+    return !WIN || (j < s.hi && (j >= s.lo || j < s.sink));
+}
+
+template <typename T, int DK, int DV, bool WIN>
 __global__ void __launch_bounds__(kThreads) k_xattn(const XattnArgs a, long long tiles) {
     extern __shared__ float4 sm4[];
     float* Qs = reinterpret_cast<float*>(sm4);
@@ -221,9 +260,11 @@ __global__ void __launch_bounds__(kThreads) k_xattn(const XattnArgs a, long long
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
     const long long r0 = bl.tile * kTile;
     const int n = keys_of(a, bl.b);
-    const int ktiles = (a.Lk + kTile - 1) / kTile;
-    const int t0 = (int)((long long)ktiles * bl.part / a.splits), t1 = (int)((long long)ktiles * (bl.part + 1) / a.splits);
+    const KeyTiles kt = key_tiles<WIN, kTile>(a, bl.b, r0, n);
+    const int t0 = (int)((long long)kt.count * bl.part / a.splits), t1 = (int)((long long)kt.count * (bl.part + 1) / a.splits);
     const float c = a.scale * kLog2e;
+    [[maybe_unused]] KeySpan span[4];
+    row_spans<WIN>(span, a, bl.b, r0, n);
     load_rows<T, DK>(Qs, a, a.q, bl.b, bl.hk, r0, a.dk, a.vec & kVecQ);
     float m[4], l[4], o[4][DV / 16];
 #pragma unroll
@@ -233,7 +274,9 @@ __global__ void __launch_bounds__(kThreads) k_xattn(const XattnArgs a, long long
 #pragma unroll
         for (int q = 0; q < DV / 16; ++q) o[i][q] = 0.f;
     }
-    for (int t = t0; t < t1 && t * kTile < n; ++t) {
+    for (int i = t0; i < t1; ++i) {
+        const int t = kt.tile(i);
+        if (t * kTile >= n) break;
         __syncthreads();  // the last tile's weights and values have been read
         load_valid(ok, a, bl.b, t * kTile, n);
         __syncthreads();
@@ -248,7 +291,7 @@ __global__ void __launch_bounds__(kThreads) k_xattn(const XattnArgs a, long long
             float mx = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                s[i][j] = ok[tx + 16 * j] ? s[i][j] * c : -INFINITY;
+                s[i][j] = ok[tx + 16 * j] && sees<WIN>(span[i], t * kTile + tx + 16 * j) ? s[i][j] * c : -INFINITY;
                 mx = fmaxf(mx, s[i][j]);
             }
             const float mn = fmaxf(m[i], row_max(mx));
@@ -267,7 +310,7 @@ __global__ void __launch_bounds__(kThreads) k_xattn(const XattnArgs a, long long
             for (int q = 0; q < DV / 16; ++q) o[i][q] *= f;
         }
         __syncthreads();
-        weigh<DV>(o, Ks, Vs);
+        weigh<DV, kTile, WIN>(o, Ks, Vs);
     }
     const long long nrows = (long long)a.B * a.Hq * a.Lq;
 #pragma unroll
@@ -334,7 +377,8 @@ __global__ void __launch_bounds__(256) k_xattn_join(const XattnArgs a) {
 }
 
 // D_i = <dO_i, O_i>: one warp per row.  Under a mask that leaves few keys, from bf16: sum_j P dP (few_keys).
-template <typename T>
+// (WIN: what a row sees is its own; up to few_seen keys are taken one by one.)
+template <typename T, bool WIN>
 __global__ void __launch_bounds__(256) k_xattn_delta(const XattnArgs a) {
     const long long nrows = (long long)a.B * a.Hq * a.Lq;
     const long long at = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
@@ -350,7 +394,11 @@ __global__ void __launch_bounds__(256) k_xattn_delta(const XattnArgs a) {
     if constexpr (sizeof(T) == 2) {
         const int b = (int)(bh / a.Hq), h = (int)(bh % a.Hq), hk = h / a.G, n = keys_of(a, b);
         int key = 0;
-        const int few = a.mask && n > kTile ? few_keys(a, b, 0, n, key) : 0;  // (up to a tile's: k_xattn_dq sums D)
+        int few = 0;
+        if constexpr (WIN)
+            few = few_seen<32>(a, b, key_span<kWindowKeys>(a, b, i, i, n), key);
+        else
+            few = a.mask && n > kTile ? few_keys(a, b, 0, n, key) : 0;  // (up to a tile's: k_xattn_dq sums D)
         if (few > 0) {
             const T* q = reinterpret_cast<const T*>(a.q.p) + b * a.q.b + i * a.q.l + h * a.q.h;
             const float cs = a.scale * kLog2e, L = a.lse[at] * kLog2e;
@@ -375,16 +423,17 @@ __global__ void __launch_bounds__(256) k_xattn_delta(const XattnArgs a) {
 }
 
 // P and dS of a tile from S, dO V^T and the rows' statistics; a row without weight (lse = -inf) has P = 0
-template <int RI>
+// (WIN: key j0 + tx + 16 j is seen by the row as its span says)
+template <bool WIN, int RI>
 __device__ __forceinline__ void tile_grad(float (&s)[RI][4], float (&dp)[RI][4], const int* ok, const float* lse2,
-                                          const float* delta, float c) {
+                                          const float* delta, float c, const KeySpan (&span)[RI], int j0) {
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
 #pragma unroll
     for (int i = 0; i < RI; ++i) {
         const float L = lse2[ty + 16 * i], D = delta[ty + 16 * i];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const bool use = ok[tx + 16 * j] && L != INFINITY;
+            const bool use = ok[tx + 16 * j] && L != INFINITY && sees<WIN>(span[i], j0 + tx + 16 * j);
             s[i][j] = use ? exp2f(s[i][j] * c - L) : 0.f;
             dp[i][j] = use ? s[i][j] * (dp[i][j] - D) : 0.f;
         }
@@ -419,7 +468,7 @@ constexpr size_t bwd_smem() {  // weights: R x 64, or 64 keys x R
     return sizeof(float) * ((kTile + R) * ((DK + 4) + (DV + 4)) + (R * kPP > kTile * (R + 4) ? R * kPP : kTile * (R + 4)));
 }
 
-template <typename T, int DK, int DV, int R>
+template <typename T, int DK, int DV, int R, bool WIN>
 __global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long long tiles) {
     extern __shared__ float4 sm4[];
     float* Qs = reinterpret_cast<float*>(sm4);
@@ -434,13 +483,17 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long l
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
     const long long r0 = bl.tile * R;
     const int n = keys_of(a, bl.b);
-    const int ktiles = (a.Lk + kTile - 1) / kTile;
-    const int t0 = (int)((long long)ktiles * bl.part / a.splits), t1 = (int)((long long)ktiles * (bl.part + 1) / a.splits);
+    const KeyTiles kt = key_tiles<WIN, R>(a, bl.b, r0, n);
+    const int t0 = (int)((long long)kt.count * bl.part / a.splits), t1 = (int)((long long)kt.count * (bl.part + 1) / a.splits);
+    KeySpan span[RI];
+    row_spans<WIN>(span, a, bl.b, r0, n);
     load_rows<T, DK, R>(Qs, a, a.q, bl.b, bl.hk, r0, a.dk, a.vec & kVecQ);
     load_rows<T, DV, R>(Ds, a, a.dO, bl.b, bl.hk, r0, a.dv, a.vec & kVecDO);
-    if (t0 < t1 && t0 * kTile < n) load_stats<R>(lse2, delta, a, bl.b, bl.hk, r0);  // (the part that has the keys may write D)
+    if (t0 < t1 && kt.tile(t0) * kTile < n) load_stats<R>(lse2, delta, a, bl.b, bl.hk, r0);  // (the part that has the keys may write D)
     float o[RI][DK / 16] = {};
-    for (int t = t0; t < t1 && t * kTile < n; ++t) {
+    for (int i = t0; i < t1; ++i) {
+        const int t = kt.tile(i);
+        if (t * kTile >= n) break;
         __syncthreads();
         load_valid(ok, a, bl.b, t * kTile, n);
         __syncthreads();
@@ -450,7 +503,7 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long l
         float s[RI][4] = {}, dp[RI][4] = {};
         dots<DK>(s, Qs, Ks, a.dk);
         dots<DV>(dp, Ds, Vs, a.dv);
-        if (sizeof(T) == 2 && n <= kTile) {
+        if (!WIN && sizeof(T) == 2 && n <= kTile) {
             // every key of the sequence is here, whatever its padding (other parts have no tile): D = sum_j P dP, for this kernel
             // and the next (a bf16 O gives it to 2^-8 of the sum of |dO O|, which with a few keys is more than dP - D; an fp32 O gives
             // it more exactly than this sum, in which P is off by lse's rounding, |lse| 2^-24)
@@ -470,13 +523,13 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long l
             }
             __syncthreads();
         }
-        tile_grad(s, dp, ok, lse2, delta, a.scale * kLog2e);
+        tile_grad<WIN>(s, dp, ok, lse2, delta, a.scale * kLog2e, span, t * kTile);
 #pragma unroll
         for (int i = 0; i < RI; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) Ws[(ty + 16 * i) * kPP + tx + 16 * j] = dp[i][j];
         __syncthreads();
-        weigh<DK>(o, Ws, Ks);
+        weigh<DK, kTile, WIN>(o, Ws, Ks);
     }
     const long long nrows = (long long)a.B * a.Hq * a.Lq;
 #pragma unroll
@@ -495,7 +548,7 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long l
     }
 }
 
-template <typename T, int DK, int DV, int R>
+template <typename T, int DK, int DV, int R, bool WIN>
 __global__ void __launch_bounds__(kThreads) k_xattn_dkv(const XattnArgs a, int ktiles) {
     extern __shared__ float4 sm4[];
     float* Qs = reinterpret_cast<float*>(sm4);
@@ -512,6 +565,12 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dkv(const XattnArgs a, int k
     const int n = keys_of(a, bl.b);
     const long long rtiles = (a.rows + R - 1) / R;
     long long t0 = rtiles * bl.part / a.rsplits, t1 = rtiles * (bl.part + 1) / a.rsplits;
+    if constexpr (WIN) {
+        const RowSpan rs = row_span(a, bl.b, j0, min(n, j0 + kTile));
+        const long long first = rs.first * a.G / R, some = max(0ll, (rs.end * a.G + R - 1) / R - first);
+        t0 = first + some * bl.part / a.rsplits;
+        t1 = first + some * (bl.part + 1) / a.rsplits;
+    }
     if (j0 >= n) t1 = t0;  // no key of the tile is read
     load_valid(ok, a, bl.b, j0, n);
     __syncthreads();
@@ -527,20 +586,22 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dkv(const XattnArgs a, int k
         float s[RI][4] = {}, dp[RI][4] = {};
         dots<DK>(s, Qs, Ks, a.dk);
         dots<DV>(dp, Ds, Vs, a.dv);
-        tile_grad(s, dp, ok, lse2, delta, a.scale * kLog2e);
+        KeySpan span[RI];
+        row_spans<WIN>(span, a, bl.b, t * R, n);
+        tile_grad<WIN>(s, dp, ok, lse2, delta, a.scale * kLog2e, span, j0);
 #pragma unroll
         for (int i = 0; i < RI; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) Ws[(tx + 16 * j) * kPR + ty + 16 * i] = s[i][j];
         __syncthreads();
-        weigh<DV, R>(ov, Ws, Ds);
+        weigh<DV, R, WIN>(ov, Ws, Ds);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < RI; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) Ws[(tx + 16 * j) * kPR + ty + 16 * i] = dp[i][j];
         __syncthreads();
-        weigh<DK, R>(ok_, Ws, Qs);
+        weigh<DK, R, WIN>(ok_, Ws, Qs);
     }
     const long long nk = (long long)a.B * a.Hkv * a.Lk;
 #pragma unroll
@@ -590,30 +651,33 @@ cudaError_t allow_smem(F* f, size_t bytes) {
 }
 
 template <typename T, int DK, int DV>
-cudaError_t forward(const XattnArgs& a, cudaStream_t s) {
+cudaError_t forward(const XattnArgs& a, KeyMode mode, cudaStream_t s) {
     const long long tiles = (a.rows + kTile - 1) / kTile;
     const long long grid = tiles * a.splits * a.Hkv * a.B;
     const size_t smem = sizeof(float) * kTile * ((DK + 4) + (DK + 4 > kPP ? DK + 4 : kPP) + (DV + 4));
-    cudaError_t e = allow_smem(k_xattn<T, DK, DV>, smem);
+    const auto kernel = mode == kWindowKeys ? k_xattn<T, DK, DV, true> : k_xattn<T, DK, DV, false>;
+    cudaError_t e = allow_smem(kernel, smem);
     if (e != cudaSuccess) return e;
-    k_xattn<T, DK, DV><<<(unsigned)grid, kThreads, smem, s>>>(a, tiles);
+    kernel<<<(unsigned)grid, kThreads, smem, s>>>(a, tiles);
     return cudaGetLastError();
 }
 template <typename T, int DK, int DV, int R>
-cudaError_t backward_r(const XattnArgs& a, cudaStream_t s) {
+cudaError_t backward_r(const XattnArgs& a, KeyMode mode, cudaStream_t s) {
     const size_t smem = bwd_smem<DK, DV, R>();
     cudaError_t e = cudaSuccess;
     if (a.rows > 0) {
         const long long tiles = (a.rows + R - 1) / R;
-        if ((e = allow_smem(k_xattn_dq<T, DK, DV, R>, smem)) != cudaSuccess) return e;
-        k_xattn_dq<T, DK, DV, R><<<(unsigned)(tiles * a.splits * a.Hkv * a.B), kThreads, smem, s>>>(a, tiles);
+        const auto kernel = mode == kWindowKeys ? k_xattn_dq<T, DK, DV, R, true> : k_xattn_dq<T, DK, DV, R, false>;
+        if ((e = allow_smem(kernel, smem)) != cudaSuccess) return e;
+        kernel<<<(unsigned)(tiles * a.splits * a.Hkv * a.B), kThreads, smem, s>>>(a, tiles);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
         if (a.splits > 1 && (e = launch_xattn_join_dq(a, s)) != cudaSuccess) return e;
     }
     if (a.Lk > 0) {
         const int ktiles = (a.Lk + kTile - 1) / kTile;
-        if ((e = allow_smem(k_xattn_dkv<T, DK, DV, R>, smem)) != cudaSuccess) return e;
-        k_xattn_dkv<T, DK, DV, R><<<(unsigned)((long long)ktiles * a.rsplits * a.Hkv * a.B), kThreads, smem, s>>>(a, ktiles);
+        const auto kernel = mode == kWindowKeys ? k_xattn_dkv<T, DK, DV, R, true> : k_xattn_dkv<T, DK, DV, R, false>;
+        if ((e = allow_smem(kernel, smem)) != cudaSuccess) return e;
+        kernel<<<(unsigned)((long long)ktiles * a.rsplits * a.Hkv * a.B), kThreads, smem, s>>>(a, ktiles);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
         if (a.rsplits > 1) e = launch_xattn_join_dkv(a, s);
     }
@@ -621,8 +685,8 @@ cudaError_t backward_r(const XattnArgs& a, cudaStream_t s) {
 }
 
 template <typename T, int DK, int DV>
-cudaError_t backward(const XattnArgs& a, cudaStream_t s) {
-    return bwd_rows(a) == 16 ? backward_r<T, DK, DV, 16>(a, s) : backward_r<T, DK, DV, kTile>(a, s);
+cudaError_t backward(const XattnArgs& a, KeyMode mode, cudaStream_t s) {
+    return bwd_rows(a) == 16 ? backward_r<T, DK, DV, 16>(a, mode, s) : backward_r<T, DK, DV, kTile>(a, mode, s);
 }
 
 bool on_fours(const XattnArgs& a, const HeadView& v, int L, int H) {
@@ -631,56 +695,65 @@ bool on_fours(const XattnArgs& a, const HeadView& v, int L, int H) {
 }
 
 template <typename T>
-cudaError_t forward_t(XattnArgs a, cudaStream_t s) {
+cudaError_t forward_t(XattnArgs a, KeyMode mode, cudaStream_t s) {
     a.vec = (on_fours(a, a.q, a.Lq, a.Hq) ? kVecQ : 0) | (on_fours(a, a.k, a.Lk, a.Hkv) ? kVecK : 0) |
             (on_fours(a, a.v, a.Lk, a.Hkv) ? kVecV : 0);
     if (a.dk <= 64)
-        return a.dv <= 32 ? forward<T, 64, 32>(a, s) : a.dv <= 64 ? forward<T, 64, 64>(a, s) : forward<T, 64, 128>(a, s);
-    return a.dv <= 64 ? forward<T, 128, 64>(a, s) : forward<T, 128, 128>(a, s);
+        return a.dv <= 32 ? forward<T, 64, 32>(a, mode, s) : a.dv <= 64 ? forward<T, 64, 64>(a, mode, s) : forward<T, 64, 128>(a, mode, s);
+    return a.dv <= 64 ? forward<T, 128, 64>(a, mode, s) : forward<T, 128, 128>(a, mode, s);
 }
 template <typename T>
-cudaError_t backward_t(XattnArgs a, cudaStream_t s) {
+cudaError_t backward_t(XattnArgs a, KeyMode mode, cudaStream_t s) {
     a.vec = (on_fours(a, a.q, a.Lq, a.Hq) ? kVecQ : 0) | (on_fours(a, a.k, a.Lk, a.Hkv) ? kVecK : 0) |
             (on_fours(a, a.v, a.Lk, a.Hkv) ? kVecV : 0) | (on_fours(a, a.dO, a.Lq, a.Hq) ? kVecDO : 0);
-    if (a.dk <= 32 && a.dv <= 32) return backward<T, 32, 32>(a, s);
+    if (a.dk <= 32 && a.dv <= 32) return backward<T, 32, 32>(a, mode, s);
     if (a.dk <= 64)
-        return a.dv <= 32 ? backward<T, 64, 32>(a, s) : a.dv <= 64 ? backward<T, 64, 64>(a, s) : backward<T, 64, 128>(a, s);
-    return a.dv <= 64 ? backward<T, 128, 64>(a, s) : backward<T, 128, 128>(a, s);
+        return a.dv <= 32 ? backward<T, 64, 32>(a, mode, s) : a.dv <= 64 ? backward<T, 64, 64>(a, mode, s) : backward<T, 64, 128>(a, mode, s);
+    return a.dv <= 64 ? backward<T, 128, 64>(a, mode, s) : backward<T, 128, 128>(a, mode, s);
 }
 
 unsigned sum_grid(long long n) { return (unsigned)std::min<long long>((n + 255) / 256, 152 * 16); }
 
-cudaError_t launch_delta(const XattnArgs& a, cudaStream_t s) {
+cudaError_t launch_delta(const XattnArgs& a, KeyMode mode, cudaStream_t s) {
     const long long rows = (long long)a.B * a.Hq * a.Lq;
     if (rows == 0) return cudaSuccess;
+    const unsigned grid = (unsigned)((rows + 7) / 8);
     if (a.dtype == GS_F32)
-        k_xattn_delta<float><<<(unsigned)((rows + 7) / 8), 256, 0, s>>>(a);
+        k_xattn_delta<float, false><<<grid, 256, 0, s>>>(a);
+    else if (mode == kWindowKeys)
+        k_xattn_delta<__nv_bfloat16, true><<<grid, 256, 0, s>>>(a);
     else
-        k_xattn_delta<__nv_bfloat16><<<(unsigned)((rows + 7) / 8), 256, 0, s>>>(a);
+        k_xattn_delta<__nv_bfloat16, false><<<grid, 256, 0, s>>>(a);
     return cudaGetLastError();
 }
 
 }  // namespace
 
-void xattn_simt_plan(XattnArgs& a, bool backward, int sms) {
+void xattn_simt_plan(XattnArgs& a, bool backward, int sms, KeyMode mode) {
     const int R = backward ? bwd_rows(a) : kTile;
     const long long rt = (a.rows + R - 1) / R, kt = (a.Lk + kTile - 1) / kTile;
+    long long keys = kt, rows = rt;  // tiles that one of the other kind meets
+    if (mode == kWindowKeys) {
+        const long long w = a.win.window, k = w + a.win.sinks + R / a.G;
+        keys = std::min(kt, k / kTile + 2);
+        if (a.win.sinks == 0) rows = std::min(rt, (w + kTile) * a.G / R + 2);
+    }
     // up to four blocks a multiprocessor, and parts of two tiles or more
-    a.splits = xattn_parts(rt * a.Hkv * a.B, kt, 4 * sms, 2);
-    a.rsplits = backward ? xattn_parts(kt * a.Hkv * a.B, rt, 4 * sms, 2) : 1;
+    a.splits = xattn_parts(rt * a.Hkv * a.B, keys, 4 * sms, 2);
+    a.rsplits = backward ? xattn_parts(kt * a.Hkv * a.B, rows, 4 * sms, 2) : 1;
     a.stats = xattn_round4(xattn_rows(a));  // D_i
 }
 
-cudaError_t launch_xattn_simt(const XattnArgs& a, cudaStream_t s) {
-    cudaError_t e = a.dtype == GS_F32 ? forward_t<float>(a, s) : forward_t<__nv_bfloat16>(a, s);
+cudaError_t launch_xattn_simt(const XattnArgs& a, KeyMode mode, cudaStream_t s) {
+    cudaError_t e = a.dtype == GS_F32 ? forward_t<float>(a, mode, s) : forward_t<__nv_bfloat16>(a, mode, s);
     if (e != cudaSuccess || a.splits == 1) return e;
     return launch_xattn_join(a, s);
 }
 
-cudaError_t launch_xattn_simt_backward(const XattnArgs& a, cudaStream_t s) {
-    cudaError_t e = launch_delta(a, s);
+cudaError_t launch_xattn_simt_backward(const XattnArgs& a, KeyMode mode, cudaStream_t s) {
+    cudaError_t e = launch_delta(a, mode, s);
     if (e != cudaSuccess) return e;
-    return a.dtype == GS_F32 ? backward_t<float>(a, s) : backward_t<__nv_bfloat16>(a, s);
+    return a.dtype == GS_F32 ? backward_t<float>(a, mode, s) : backward_t<__nv_bfloat16>(a, mode, s);
 }
 
 cudaError_t launch_xattn_join(const XattnArgs& a, cudaStream_t s) {

@@ -560,14 +560,14 @@ unsigned take_device_error_xattn() {
     return v;
 }
 
-void xattn_tc_plan(XattnArgs& a, int sms) {
+void xattn_tc_plan(XattnArgs& a, KeyMode mode, int sms) {
     const long long tile_rows = (long long)(kTile / a.G) * a.G;
     const long long kt = (a.Lk + kTile - 1) / kTile;
     a.splits = take_pairs(a, sms) ? 1 : xattn_parts((a.rows + tile_rows - 1) / tile_rows * a.Hkv * a.B, kt, sms, 4);
     a.rsplits = 1;
 }
 
-cudaError_t launch_xattn_tc(const XattnArgs& a, int sms, int device, cudaStream_t s) {
+cudaError_t launch_xattn_tc(const XattnArgs& a, KeyMode mode, int sms, int device, cudaStream_t s) {
     if (device < 0 || device >= 64) return cudaErrorInvalidDevice;
     g_launched = true;
     const bool pair = take_pairs(a, sms);

@@ -10,8 +10,9 @@ Names follow the C ABI (gs_ prefix dropped): build_basis, build_basis_grouped,
 basis_groups, import_basis, project_similarity, project_similarity_host (with
 reserve_staging), project_similarity_static, similarity_coeffs, group_argmax,
 prob_vectorize, reconstruct, reconstruct_bind, bind, attention_scores,
-cross_attention, cross_attention_backward, sample_scores, stream_status,
-selftest_wait_timeout.
+cross_attention, cross_attention_backward, window_attention,
+window_attention_backward, page_slots, page_store, paged_attention, sample_scores,
+verify_drafts, stream_status, selftest_wait_timeout.
 """
 from __future__ import annotations
 
@@ -39,7 +40,9 @@ EXPORTS = ("gs_build_basis", "gs_basis_info", "gs_basis_destroy", "gs_project_si
            "gs_selftest_wait_timeout", "gs_basis_import", "gs_basis_reserve_staging",
            "gs_project_similarity_host", "gs_build_basis_grouped", "gs_basis_groups", "gs_group_argmax",
            "gs_bind", "gs_reconstruct_bind", "gs_cross_attention_workspace", "gs_cross_attention",
-           "gs_cross_attention_backward", "gs_sample_scores")
+           "gs_cross_attention_backward", "gs_sample_scores", "gs_window_attention_workspace", "gs_window_attention",
+           "gs_window_attention_backward", "gs_page_slots", "gs_page_store", "gs_paged_attention_workspace",
+           "gs_paged_attention", "gs_verify_drafts")
 
 
 class GramSpaceError(RuntimeError):
@@ -58,6 +61,18 @@ class _Attn(ctypes.Structure):  # gs_attn
                 ("Hq", ctypes.c_int), ("Hkv", ctypes.c_int), ("dk", ctypes.c_int), ("dv", ctypes.c_int),
                 ("scale", ctypes.c_float), ("key_lens", ctypes.c_void_p), ("key_mask", ctypes.c_void_p),
                 ("ld_mask", ctypes.c_longlong), ("flags", ctypes.c_uint)]
+
+
+class _Window(ctypes.Structure):  # gs_window
+    _fields_ = [("window", ctypes.c_int), ("sinks", ctypes.c_int), ("start", ctypes.c_int), ("starts", ctypes.c_void_p)]
+
+
+class _Paged(ctypes.Structure):  # gs_paged
+    _fields_ = [("dtype", ctypes.c_int), ("B", ctypes.c_int), ("Lq", ctypes.c_int), ("Hq", ctypes.c_int),
+                ("Hkv", ctypes.c_int), ("dk", ctypes.c_int), ("dv", ctypes.c_int), ("scale", ctypes.c_float),
+                ("pages", ctypes.c_int), ("page_size", ctypes.c_int), ("columns", ctypes.c_int), ("table", ctypes.c_void_p),
+                ("ld_table", ctypes.c_longlong), ("lens", ctypes.c_void_p), ("q_lens", ctypes.c_void_p),
+                ("window", ctypes.c_int), ("sinks", ctypes.c_int), ("flags", ctypes.c_uint)]
 
 
 class _Sampling(ctypes.Structure):  # gs_sampling
@@ -99,6 +114,15 @@ def load_library(path=LIB_PATH):
     L.gs_cross_attention_workspace.argtypes = [ap, ip, ctypes.POINTER(i64)]
     L.gs_cross_attention.argtypes = [ap, hp, hp, hp, hp, vp, vp, i64, vp]
     L.gs_cross_attention_backward.argtypes = [ap, hp, hp, hp, hp, vp, hp, hp, hp, hp, vp, i64, vp]
+    wp, pp = ctypes.POINTER(_Window), ctypes.POINTER(_Paged)
+    L.gs_window_attention_workspace.argtypes = [ap, wp, ip, ctypes.POINTER(i64)]
+    L.gs_window_attention.argtypes = [ap, wp, hp, hp, hp, hp, vp, vp, i64, vp]
+    L.gs_window_attention_backward.argtypes = [ap, wp, hp, hp, hp, hp, vp, hp, hp, hp, hp, vp, i64, vp]
+    L.gs_page_slots.argtypes = [vp, vp, ip, ip, ip, ip, vp, ip, vp, vp, i64, ip, vp, vp, vp, vp]
+    L.gs_page_store.argtypes = [ip, ip, ip, ip, ip, ip, hp, hp, vp, i64, ip, ip, hp, hp, vp]
+    L.gs_paged_attention_workspace.argtypes = [pp, ctypes.POINTER(i64)]
+    L.gs_paged_attention.argtypes = [pp, hp, hp, hp, hp, vp, vp, i64, vp]
+    L.gs_verify_drafts.argtypes = [vp, vp, ip, ip, ip, ip, i64, i64, i64, i64, vp, vp, vp, vp, vp, vp]
     L.gs_sample_scores.argtypes = [vp, ip, i64, ip, i64, ctypes.POINTER(_Sampling), vp, vp, vp, vp]
     L.gs_stream_status.argtypes = [vp]
     L.gs_selftest_wait_timeout.argtypes = [vp]
@@ -113,7 +137,9 @@ def load_library(path=LIB_PATH):
                  "gs_basis_reserve_staging", "gs_project_similarity_host", "gs_build_basis_grouped",
                  "gs_basis_groups", "gs_group_argmax", "gs_bind", "gs_reconstruct_bind",
                  "gs_cross_attention_workspace", "gs_cross_attention", "gs_cross_attention_backward",
-                 "gs_sample_scores"):
+                 "gs_sample_scores", "gs_window_attention_workspace", "gs_window_attention",
+                 "gs_window_attention_backward", "gs_page_slots", "gs_page_store", "gs_paged_attention_workspace",
+                 "gs_paged_attention", "gs_verify_drafts"):
         getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L
@@ -543,10 +569,14 @@ def _attn(Q, K, V, scale, key_lens, key_mask, path):
     return a, hs
 
 
-def _attn_workspace(L, a, backward, device):
+def _attn_workspace(L, a, backward, device, w=None):
     """(tensor to keep until the call has been made, its address, its bytes)"""
     n = ctypes.c_longlong()
-    _check(L.gs_cross_attention_workspace(ctypes.byref(a), backward, ctypes.byref(n)), "gs_cross_attention_workspace")
+    if w is None:
+        _check(L.gs_cross_attention_workspace(ctypes.byref(a), backward, ctypes.byref(n)), "gs_cross_attention_workspace")
+    else:
+        _check(L.gs_window_attention_workspace(ctypes.byref(a), ctypes.byref(w), backward, ctypes.byref(n)),
+               "gs_window_attention_workspace")
     if n.value == 0:
         return None, None, 0
     ws = torch.empty(n.value, dtype=torch.uint8, device=device)
@@ -569,10 +599,19 @@ def cross_attention(Q, K, V, scale=None, key_lens=None, key_mask=None, want_lse=
     bool B x Lk, False = not read.  Returns {"O": B x Lq x Hq x dv, "lse": B x Hq x Lq float32 with want_lse};
     `out` may supply them.  Like every call of this module it is not recorded by autograd: a graph's backward step calls
     cross_attention_backward (there is a warning where an input asks for its gradient)."""
-    if (Q.requires_grad or K.requires_grad or V.requires_grad) and torch.is_grad_enabled():
-        warnings.warn("cross_attention is not recorded by autograd, gradients do not pass through it: take them from "
-                      "cross_attention_backward, and call it under torch.no_grad() or on detached tensors", stacklevel=2)
+    _warn_unrecorded("cross_attention", Q, K, V)
     a, hs = _attn(Q, K, V, scale, key_lens, key_mask, path)
+    return _forward(a, hs, Q, want_lse, out, stream)
+
+
+def _warn_unrecorded(name, *inputs):
+    if torch.is_grad_enabled() and any(t.requires_grad for t in inputs):
+        warnings.warn(f"{name} is not recorded by autograd, gradients do not pass through it: take them from "
+                      f"{name}_backward, and call it under torch.no_grad() or on detached tensors", stacklevel=3)
+
+
+def _forward(a, hs, Q, want_lse, out, stream, w=None):
+    """cross_attention, or through a window window_attention."""
     L, dev, ref = load_library(), Q.device, ctypes.byref
     out = dict(out) if out else {}
     with _on_stream(dev, stream):
@@ -582,9 +621,10 @@ def cross_attention(Q, K, V, scale=None, key_lens=None, key_mask=None, want_lse=
             out["lse"] = torch.empty((a.B, a.Hq, a.Lq), dtype=torch.float32, device=dev)
         o = _heads(out["O"], "O", (a.B, a.Lq, a.Hq, a.dv), Q)
         lse = _attn_lse(out["lse"], (a.B, a.Hq, a.Lq), dev) if out.get("lse") is not None else None
-        keep, ws, size = _attn_workspace(L, a, 0, dev)
-        st = L.gs_cross_attention(ref(a), ref(hs[0]), ref(hs[1]), ref(hs[2]), ref(o), lse, ws, size, _stream(stream, dev))
-    _check(st, "gs_cross_attention")
+        keep, ws, size = _attn_workspace(L, a, 0, dev, w)
+        rest = (ref(hs[0]), ref(hs[1]), ref(hs[2]), ref(o), lse, ws, size, _stream(stream, dev))
+        st = L.gs_cross_attention(ref(a), *rest) if w is None else L.gs_window_attention(ref(a), ref(w), *rest)
+    _check(st, "gs_cross_attention" if w is None else "gs_window_attention")
     return out
 
 
@@ -594,6 +634,11 @@ def cross_attention_backward(Q, K, V, O, lse, dO, scale=None, key_lens=None, key
     call's (want_lse=True), dO the gradient of O; the other arguments as there.  Returns {"dQ", "dK", "dV"} with
     the shapes and type of Q, K and V; `out` may supply them."""
     a, hs = _attn(Q, K, V, scale, key_lens, key_mask, path)
+    return _backward(a, hs, Q, K, V, O, lse, dO, out, stream)
+
+
+def _backward(a, hs, Q, K, V, O, lse, dO, out, stream, w=None):
+    """cross_attention_backward, or through a window window_attention_backward."""
     L, dev, ref = load_library(), Q.device, ctypes.byref
     out = dict(out) if out else {}
     shape = (a.B, a.Lq, a.Hq, a.dv)
@@ -604,10 +649,224 @@ def cross_attention_backward(Q, K, V, O, lse, dO, scale=None, key_lens=None, key
             if name not in out:
                 out[name] = torch.empty(t.shape, dtype=t.dtype, device=dev)
         gq, gk, gv = _heads(out["dQ"], "dQ", Q.shape, Q), _heads(out["dK"], "dK", K.shape, Q), _heads(out["dV"], "dV", V.shape, Q)
-        keep, ws, size = _attn_workspace(L, a, 1, dev)
-        st = L.gs_cross_attention_backward(ref(a), ref(hs[0]), ref(hs[1]), ref(hs[2]), ref(o), logs, ref(do), ref(gq), ref(gk),
-                                           ref(gv), ws, size, _stream(stream, dev))
-    _check(st, "gs_cross_attention_backward")
+        keep, ws, size = _attn_workspace(L, a, 1, dev, w)
+        rest = (ref(hs[0]), ref(hs[1]), ref(hs[2]), ref(o), logs, ref(do), ref(gq), ref(gk), ref(gv), ws, size, _stream(stream, dev))
+        st = L.gs_cross_attention_backward(ref(a), *rest) if w is None else L.gs_window_attention_backward(ref(a), ref(w), *rest)
+    _check(st, "gs_cross_attention_backward" if w is None else "gs_window_attention_backward")
+    return out
+
+
+def _window(window, sinks, start, B, device):
+    """gs_window; start is a number or an int32 vector of B."""
+    window = 0x7fffffff if window is None else int(window)
+    if window < 1 or int(sinks) < 0:
+        raise ValueError(f"window must be at least 1 and sinks at least 0, got {window} and {sinks}")
+    w = _Window(min(window, 0x7fffffff), min(int(sinks), 0x7fffffff), 0, None)
+    if isinstance(start, torch.Tensor):
+        w.starts = _int_vector(start, "start", B, device)
+    else:
+        if abs(int(start)) > 0x7fffffff:
+            raise ValueError(f"start is no 32-bit position: {start}")
+        w.start = int(start)
+    return w
+
+
+def _int_vector(t, name, n, device):
+    if t.dtype is not torch.int32 or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 vector of {n}")
+    if t.device != device:
+        raise TypeError(f"{name} must be on {device}")
+    return t.data_ptr()
+
+
+def window_attention(Q, K, V, window, sinks=0, start=0, scale=None, key_lens=None, key_mask=None, want_lse=False, path="auto",
+                     out=None, stream=None):
+    """Causal attention over a sliding window; see gs_window_attention.
+
+    As cross_attention, where query row i stands at position start + i (start: a number, or an int32 CUDA vector with one per
+    sequence) and sees the keys up to it, the last `window` of them (None: all) and the first `sinks`."""
+    _warn_unrecorded("window_attention", Q, K, V)
+    a, hs = _attn(Q, K, V, scale, key_lens, key_mask, path)
+    return _forward(a, hs, Q, want_lse, out, stream, _window(window, sinks, start, a.B, Q.device))
+
+
+def window_attention_backward(Q, K, V, O, lse, dO, window, sinks=0, start=0, scale=None, key_lens=None, key_mask=None,
+                              path="auto", out=None, stream=None):
+    """The gradient of window_attention, as cross_attention_backward is of cross_attention; see
+    gs_window_attention_backward."""
+    a, hs = _attn(Q, K, V, scale, key_lens, key_mask, path)
+    return _backward(a, hs, Q, K, V, O, lse, dO, out, stream, _window(window, sinks, start, a.B, Q.device))
+
+
+def _table(table, device):
+    """(address, requests, columns, row stride) of a block table."""
+    if table.dim() != 2 or table.dtype is not torch.int32 or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError("table must be a 2-D int32 tensor (requests x columns) with unit column stride")
+    if table.device != device:
+        raise TypeError(f"table must be on {device}")
+    B, columns = table.shape
+    _c_int(B, columns)
+    return table.data_ptr(), B, columns, table.stride(0) if B > 1 else columns
+
+
+def page_slots(lens, added, table, free, page_size, max_new, pages, free_from=None, want_lens=True, want_taken=True, out=None,
+               stream=None):
+    """Slots of new tokens in a paged cache; see gs_page_slots.
+
+    lens, added: int32 CUDA vectors, tokens that each request holds and gets.  table: int32 requests x columns, the block table,
+    whose next columns are filled in place.  free: int32 vector, the free pages, taken from entry free_from (an int32 CUDA
+    tensor of one; None: 0) on.  max_new: columns of the result, pages: of the cache.  Returns {"slots": requests x max_new, "lens": the
+    requests' new lengths, "taken": pages asked for, one number}, int32."""
+    dev = lens.device
+    t, B, columns, ld = _table(table, dev)
+    _c_int(abs(int(page_size)), abs(int(max_new)), abs(int(pages)), free.numel())
+    if int(max_new) < 0:
+        raise ValueError(f"max_new must be at least 0, got {max_new}")
+    if free.dim() != 1:
+        raise ValueError("free must be a vector")
+    args = (_int_vector(lens, "lens", B, dev), _int_vector(added, "added", B, dev))
+    fr = _int_vector(free, "free", free.shape[0], dev)
+    ff = _int_vector(free_from.view(-1), "free_from", 1, dev) if free_from is not None else None
+    out = dict(out) if out else {}
+    for name, shape in (("slots", (B, max_new)), ("lens", (B,)), ("taken", (1,))):
+        x = out.get(name)
+        if x is not None and (x.dtype is not torch.int32 or x.shape != shape or not x.is_contiguous() or x.device != dev):
+            raise ValueError(f"out[{name!r}] must be a contiguous int32 {' x '.join(map(str, shape))} tensor on {dev}")
+    if not lens.is_cuda:
+        raise TypeError("lens, added, table and free must be CUDA tensors")
+    L = load_library()
+    with _on_stream(dev, stream):
+        for name, shape, want in (("slots", (B, max_new), True), ("lens", (B,), want_lens), ("taken", (1,), want_taken)):
+            if want and out.get(name) is None:
+                out[name] = torch.empty(shape, dtype=torch.int32, device=dev)
+        st = L.gs_page_slots(*args, B, int(max_new), int(page_size), int(pages), fr, free.shape[0], ff, t, ld, columns,
+                             _ptr(out["slots"]), _ptr(out.get("lens")), _ptr(out.get("taken")), _stream(stream, dev))
+    _check(st, "gs_page_slots")
+    return out
+
+
+def _cache(Kc, Vc, like):
+    """gs_heads of a cache's two arrays, its pages and page size."""
+    if Kc.dim() != 4 or Vc.dim() != 4:
+        raise ValueError("Kc and Vc must be 4-D (pages, page size, heads, width)")
+    pages, size, H, dk = Kc.shape
+    _c_int(pages, size, H, dk, Vc.shape[3])
+    return _heads(Kc, "Kc", Kc.shape, like), _heads(Vc, "Vc", (pages, size, H, Vc.shape[3]), like), pages, size
+
+
+def page_store(K, V, slots, Kc, Vc, stream=None):
+    """New keys and values (requests x tokens x heads x width) into the slots (int32 requests x tokens, negative: skipped) of the
+    cache Kc, Vc (pages x page size x heads x width), in place; see gs_page_store."""
+    if K.dim() != 4 or V.dim() != 4:
+        raise ValueError("K and V must be 4-D (requests, tokens, heads, width)")
+    code = _dtype_code(K)
+    kc, vc, pages, size = _cache(Kc, Vc, K)
+    B, n, H, dk = K.shape
+    dv = Vc.shape[3]
+    _c_int(B, n)
+    if Kc.shape[2] != H or Kc.shape[3] != dk:
+        raise ValueError(f"Kc must hold {H} heads of {dk}, got {Kc.shape[2]} of {Kc.shape[3]}")
+    k, v = _heads(K, "K", K.shape, K), _heads(V, "V", (B, n, H, dv), K)
+    dev = K.device
+    if slots.dtype is not torch.int32 or slots.shape != (B, n) or (n > 1 and slots.stride(1) != 1):
+        raise ValueError(f"slots must be an int32 {B} x {n} tensor with unit column stride")
+    if slots.device != dev:
+        raise TypeError(f"slots must be on {dev}")
+    if not K.is_cuda:
+        raise TypeError("K, V and the cache must be CUDA tensors")
+    L, ref = load_library(), ctypes.byref
+    with _on_stream(dev, stream):
+        st = L.gs_page_store(code, B, n, H, dk, dv, ref(k), ref(v), slots.data_ptr(), slots.stride(0) if B > 1 else n, pages, size,
+                             ref(kc), ref(vc), _stream(stream, dev))
+    _check(st, "gs_page_store")
+
+
+def paged_attention(Q, Kc, Vc, table, lens, scale=None, q_lens=None, window=None, sinks=0, want_lse=False, path="auto", out=None,
+                    stream=None):
+    """Attention of the requests' newest tokens over a paged cache; see gs_paged_attention.
+
+    Q: B x Lq x Hq x dk, the last q_lens[b] (int32 [B]; None: Lq) tokens of each request, Kc and Vc: the cache (pages x page size x
+    Hkv x width), table: int32 B x columns, lens: int32 [B], keys of each request with the newest ones.  A token sees the keys up to
+    itself, the last `window` (None: all) and the first `sinks`.  Returns {"O": B x Lq x Hq x dv, "lse": B x Hq x Lq float32 with
+    want_lse}; `out` may supply them."""
+    if Q.dim() != 4:
+        raise ValueError("Q must be 4-D (requests, tokens, heads, width)")
+    code = _dtype_code(Q)
+    B, Lq, Hq, dk = Q.shape
+    _c_int(B, Lq, Hq, dk)
+    q = _heads(Q, "Q", Q.shape, Q)
+    kc, vc, pages, size = _cache(Kc, Vc, Q)
+    if Kc.shape[3] != dk:
+        raise ValueError(f"Kc must be {dk} wide, got {Kc.shape[3]}")
+    dev = Q.device
+    t, rows, columns, ld = _table(table, dev)
+    if rows != B:
+        raise ValueError(f"table must have {B} rows, got {rows}")
+    w = _window(window, sinks, 0, B, dev)
+    if scale is None:
+        scale = dk ** -0.5 if dk else 1.0
+    a = _Paged(code, B, Lq, Hq, Kc.shape[2], dk, Vc.shape[3], scale, pages, size, columns, t, ld, _int_vector(lens, "lens", B, dev),
+               _int_vector(q_lens, "q_lens", B, dev) if q_lens is not None else None, w.window, w.sinks, PATHS[path])
+    if not Q.is_cuda:
+        raise TypeError("Q and the cache must be CUDA tensors")
+    L, ref = load_library(), ctypes.byref
+    out = dict(out) if out else {}
+    with _on_stream(dev, stream):
+        if "O" not in out:
+            out["O"] = torch.empty((B, Lq, Hq, a.dv), dtype=Q.dtype, device=dev)
+        if want_lse and out.get("lse") is None:
+            out["lse"] = torch.empty((B, Hq, Lq), dtype=torch.float32, device=dev)
+        o = _heads(out["O"], "O", (B, Lq, Hq, a.dv), Q)
+        lse = _attn_lse(out["lse"], (B, Hq, Lq), dev) if out.get("lse") is not None else None
+        n = ctypes.c_longlong()
+        _check(L.gs_paged_attention_workspace(ref(a), ref(n)), "gs_paged_attention_workspace")
+        ws = torch.empty(n.value, dtype=torch.uint8, device=dev) if n.value else None
+        st = L.gs_paged_attention(ref(a), ref(q), ref(kc), ref(vc), ref(o), lse, _ptr(ws), n.value, _stream(stream, dev))
+    _check(st, "gs_paged_attention")
+    return out
+
+
+def verify_drafts(P, D, drafts, U, draft_lens=None, out=None, stream=None):
+    """Which drafted tokens stand, and the token behind them; see gs_verify_drafts.
+
+    P: B x (K + 1) x M probabilities of the target (float32 or bfloat16, unit stride along M), D: B x K x M, those that the drafts
+    were drawn from (None: chosen without chance), drafts: int32 B x K, U: float32 B x (K + 1) numbers of [0, 1), draft_lens: int32
+    [B] or None (K each).  Returns {"accepted": int32 [B], "tokens": int32 B x (K + 1), -1 behind the drawn token}."""
+    if P.dim() != 3 or P.shape[1] < 1:
+        raise ValueError("P must be 3-D (requests, drafts + 1, entries)")
+    code = _dtype_code(P)
+    B, K, M = P.shape[0], P.shape[1] - 1, P.shape[2]
+    _c_int(B, K, M)
+    dev = P.device
+    if P.stride(2) != 1 and M > 1:
+        raise ValueError("P must have unit stride along its last axis")
+    if D is not None:
+        if D.shape != (B, K, M) or (D.stride(2) != 1 and M > 1):
+            raise ValueError(f"D must be {B} x {K} x {M} with unit stride along its last axis")
+        if D.dtype is not P.dtype or D.device != dev:
+            raise TypeError(f"D must be {P.dtype} on {dev}")
+    for name, t, dt, shape in (("drafts", drafts, torch.int32, (B, K)), ("U", U, torch.float32, (B, K + 1))):
+        if t.dtype is not dt or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dt} tensor of {shape[0]} x {shape[1]}")
+        if t.device != dev:
+            raise TypeError(f"{name} must be on {dev}")
+    n = _int_vector(draft_lens, "draft_lens", B, dev) if draft_lens is not None else None
+    out = dict(out) if out else {}
+    for name, shape in (("accepted", (B,)), ("tokens", (B, K + 1))):
+        t = out.get(name)
+        if t is not None and (t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous() or t.device != dev):
+            raise ValueError(f"out[{name!r}] must be a contiguous int32 {' x '.join(map(str, shape))} tensor on {dev}")
+    if not P.is_cuda:
+        raise TypeError("P must be a CUDA tensor")
+    L = load_library()
+    with _on_stream(dev, stream):
+        for name, shape in (("accepted", (B,)), ("tokens", (B, K + 1))):
+            if name not in out:
+                out[name] = torch.empty(shape, dtype=torch.int32, device=dev)
+        st = L.gs_verify_drafts(P.data_ptr(), _ptr(D) if K else None, code, B, K, M, P.stride(0), P.stride(1),
+                                D.stride(0) if D is not None else 0, D.stride(1) if D is not None else 0, drafts.data_ptr(), n,
+                                U.data_ptr(), _ptr(out.get("accepted")), _ptr(out.get("tokens")), _stream(stream, dev))
+    _check(st, "gs_verify_drafts")
     return out
 
 
