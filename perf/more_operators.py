@@ -379,8 +379,8 @@ def run(state):
             out = gs.page_slots(state["lens"], state["new"], state["table"], state["free"], c["page"], c["Lnew"],
                                 state["Kc"].shape[0], free_from=state["from"])
             gs.page_store(state["K"], state["V"], out["slots"], state["Kc"], state["Vc"])
-            return {"table": state["table"], "slots": out["slots"], "lens": out["lens"], "taken": out["taken"],
-                    "K": state["Kc"], "V": state["Vc"]}
+            return {"table": state["table"], "slots": out["slots"], "lens": out["lens"].long(), "taken": out["taken"],
+                    "K": state["Kc"], "V": state["Vc"]}  # (lengths in 64 bits, as the plain form has them)
         if c["kind"] == "paged":
             return gs.paged_attention(state["Q"], state["Kc"], state["Vc"], state["table"], state["lens"], _scale(c),
                                       q_lens=state["q_lens"], window=c["window"] or None, sinks=c["sinks"])
