@@ -1028,7 +1028,7 @@ gs_status attn_forward(const gs_attn* p, const gs_window* w, const gs_heads* Q, 
     a.ws = (float*)workspace;
     cudaStream_t s = (cudaStream_t)stream;
     int pack = 0;
-    const bool tc_ok = mode == gs::kAllKeys && attn_on_tensor(a, false, p->flags, pack);
+    const bool tc_ok = attn_on_tensor(a, false, p->flags, pack);
     if (p->flags == GS_PATH_TENSOR && !tc_ok)
         return a.dtype != GS_BF16 || a.G > 128 ? GS_ERR_UNSUPPORTED : GS_ERR_ALIGNMENT;
     const AttnPath path = attn_path(a, p->flags, tc_ok && a.Lk > 0);
@@ -1069,7 +1069,7 @@ gs_status attn_backward(const gs_attn* p, const gs_window* w, const gs_heads* Q,
     a.ws = (float*)workspace;
     cudaStream_t s = (cudaStream_t)stream;
     int pack = 0;
-    const bool tc_ok = mode == gs::kAllKeys && attn_on_tensor(a, true, p->flags, pack);
+    const bool tc_ok = attn_on_tensor(a, true, p->flags, pack);
     if (p->flags == GS_PATH_TENSOR && !tc_ok)
         return a.dtype != GS_BF16 || a.G > 128 ? GS_ERR_UNSUPPORTED : GS_ERR_ALIGNMENT;
     if (tc_ok && p->flags != GS_PATH_SIMT && a.Lq > 0 && a.Lk > 0) {

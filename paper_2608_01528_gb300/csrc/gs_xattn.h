@@ -43,6 +43,7 @@ struct XattnArgs {
     int rsplits;   // dK / dV: parts of the packed rows
     int vec;       // CUDA-core kernels: which arrays allow loads of four elements
     long long stats;  // backward: floats of the rows' statistics at the start of the workspace
+    bool flags;       // forward on tcgen05 through a window: a byte a row in the workspace
     KeyWindow win;
     KeyPages pg;
 };
@@ -82,9 +83,12 @@ static __device__ __forceinline__ KeySpan key_span(const XattnArgs& a, int b, lo
     }
     return s;
 }
-// Bits [c0, c1) of the 32 from `at` on.
 static __device__ __forceinline__ uint32_t bits_below(int x) { return x >= 32 ? 0xffffffffu : x <= 0 ? 0u : (1u << x) - 1u; }
 static __device__ __forceinline__ uint32_t bits_between(int c0, int c1) { return bits_below(c1) & ~bits_below(c0); }
+// bit i: key j + i is one of the span's
+static __device__ __forceinline__ uint32_t seen_word(const KeySpan& s, int j) {
+    return bits_between(s.lo - j, s.hi - j) | bits_below(s.sink - j);
+}
 
 // How many parts a kernel cuts its long axis into, so that about `want` blocks run: `base` blocks
 // exist without a split, `tiles` is the axis' length in tiles, and a part has `least` tiles or more.
@@ -104,7 +108,9 @@ GS_XWS xattn_round4(long long n) { return (n + 3) / 4 * 4; }
 GS_XWS xattn_rows(const XattnArgs& a) { return (long long)a.B * a.Hq * a.Lq; }
 GS_XWS xattn_keys(const XattnArgs& a) { return (long long)a.B * a.Hkv * a.Lk; }
 GS_XWS xattn_ws_ml(const XattnArgs& a) { return xattn_round4(a.splits * xattn_rows(a) * a.dv); }
-GS_XWS xattn_ws_forward(const XattnArgs& a) { return a.splits > 1 ? xattn_ws_ml(a) + a.splits * xattn_rows(a) * 2 : 0; }
+GS_XWS xattn_ws_forward(const XattnArgs& a) {
+    return a.splits > 1 ? xattn_ws_ml(a) + a.splits * xattn_rows(a) * 2 : a.flags ? xattn_round4((xattn_rows(a) + 3) / 4) : 0;
+}
 GS_XWS xattn_ws_dq(const XattnArgs& a) { return a.stats; }
 GS_XWS xattn_ws_dk(const XattnArgs& a) {
     return xattn_ws_dq(a) + (a.splits > 1 ? xattn_round4(a.splits * xattn_rows(a) * a.dk) : 0);
@@ -201,6 +207,8 @@ cudaError_t launch_xattn_rows(const XattnArgs& a, KeyMode mode, cudaStream_t s);
 void xattn_simt_plan(XattnArgs& a, bool backward, int sms, KeyMode mode);
 cudaError_t launch_xattn_simt(const XattnArgs& a, KeyMode mode, cudaStream_t s);
 cudaError_t launch_xattn_simt_backward(const XattnArgs& a, KeyMode mode, cudaStream_t s);
+cudaError_t launch_xattn_simt_window(const XattnArgs& a, cudaStream_t s);  // (gs_xattn_simt_window.cu, without the join)
+cudaError_t launch_xattn_simt_window_backward(const XattnArgs& a, cudaStream_t s);
 // O and lse from a.splits parts; dQ, dK, dV from theirs
 cudaError_t launch_xattn_join(const XattnArgs& a, cudaStream_t s);
 cudaError_t launch_xattn_join_dq(const XattnArgs& a, cudaStream_t s);

@@ -154,11 +154,54 @@ __device__ __forceinline__ float dot_eight(const uint4& x, const uint4& y, float
     return acc;
 }
 
+// D = sum_j P dP of the rows that see kFewKeys keys or fewer, instead of <dO, O> with a rounded O (few_keys): 16 threads a row, two rows
+// a warp in step.
+__device__ __forceinline__ void sum_few_seen(const XattnArgs& a, int b, int hk, long long rt, int nl, int grp, int ln, int n, float* dst) {
+    const __nv_bfloat16* keys = reinterpret_cast<const __nv_bfloat16*>(a.k.p) + b * a.k.b + hk * a.k.h;
+    const __nv_bfloat16* values = reinterpret_cast<const __nv_bfloat16*>(a.v.p) + b * a.v.b + hk * a.v.h;
+    const float cs = a.scale * kLog2e;
+    const int c0 = ln * 8;
+#pragma unroll 1
+    for (int r = grp; r < kTile; r += 16) {
+        if (r >= grp + 64) break;  // (a block's 64 slots)
+        const int l = r / a.G, h = hk * a.G + r - l * a.G;
+        const long long ql = rt * nl + l;
+        const bool row = l < nl && ql < a.Lq;
+        KeySpan sp{0, 0, 0};
+        if (row) sp = key_span<kWindowKeys>(a, b, ql, ql, n);
+        int key = 0;
+        const int few = few_seen<16>(a, b, sp, key), most = max(few, __shfl_xor_sync(0xffffffffu, few, 16));
+        if (most <= 0) continue;  // both rows of the warp
+        const bool on = few > 0;
+        const uint4 q = load_eight(reinterpret_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.b + (on ? ql : 0) * a.q.l + (on ? h : 0) * a.q.h,
+                                   c0, a.dk, on);
+        const uint4 d = load_eight(reinterpret_cast<const __nv_bfloat16*>(a.dO.p) + b * a.dO.b + (on ? ql : 0) * a.dO.l + (on ? h : 0) * a.dO.h,
+                                   c0, a.dv, on);
+        const float nl2 = on ? neg_lse2(a.lse[((long long)b * a.Hq + h) * a.Lq + ql]) : -INFINITY;
+        float sum = 0.f;
+        for (int f = 0; f < most; ++f) {
+            const long long j = __shfl_sync(0xffffffffu, key, f, 16);
+            const bool in = f < few;
+            float s = dot_eight(q, load_eight(keys + (in ? j : 0) * a.k.l, c0, a.dk, in), 0.f);
+            float dp = dot_eight(d, load_eight(values + (in ? j : 0) * a.v.l, c0, a.dv, in), 0.f);
+#pragma unroll
+            for (int o = 8; o; o >>= 1) {
+                s += __shfl_xor_sync(0xffffffffu, s, o);
+                dp += __shfl_xor_sync(0xffffffffu, dp, o);
+            }
+            if (in) sum = fmaf(ex2(fmaf(s, cs, nl2)), dp, sum);
+        }
+        if (on && ln == 0) dst[kTile + r] = nl2 == -INFINITY ? 0.f : -sum;
+    }
+}
+
 // Statistics of every row tile of a key head: slots without a row get (-inf, 0).  16 threads a row, 8 columns each, four rows
 // in flight a thread, 64 slots a block.  Bound by instructions, mostly addresses (issue 69 %; 8 x 1,024 rows of 16 heads of 64,
 // 34 MB: 15 us; two rows in flight and lse read last 17).  Where a mask leaves few keys, D is summed from them instead (9 of
 // 1,500 keys, 4 x 64 rows of 16 heads of 64: the whole gradient 59 -> 73 us).
+// Through a window (WIN), rows that see few keys are looked at one by one: the first rows of a sequence, or all of a short window.
 constexpr int kStatRows = 4, kStatBlocks = kTile / (16 * kStatRows);
+template <bool WIN>
 __global__ void __launch_bounds__(256) k_xattn_stats(const XattnArgs a, int nl, long long rtiles, int vec) {
     long long i = blockIdx.x / kStatBlocks;
     float* dst = a.ws + i * kStats;
@@ -200,6 +243,10 @@ __global__ void __launch_bounds__(256) k_xattn_stats(const XattnArgs a, int nl, 
         }
     }
     const int n = keys_of(a, b);
+    if constexpr (WIN) {
+        sum_few_seen(a, b, hk, rt, nl, grp, ln, n, dst);
+        return;
+    }
     if (!a.mask || n <= kTile) return;  // (up to a tile's keys: k_xattn_dq_tc sums D)
     // each warp looks through an eighth of the mask (65,536 keys, nine of them read: the whole call 305 us where each took all of it)
     __shared__ int counts[8], found[8][kFewKeys];
@@ -242,7 +289,7 @@ __global__ void __launch_bounds__(256) k_xattn_stats(const XattnArgs a, int nl, 
     }
 }
 
-template <int DKC, int DVC>
+template <int DKC, int DVC, bool WIN>
 __global__ void __launch_bounds__(kThreads, 1)
     k_xattn_dkv_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mo, const Params p) {
     using C = Cfg<DKC, DVC>;
@@ -259,14 +306,34 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31;
 
     long long i = blockIdx.x;
-    const int kt = (int)(i % p.ktiles);
-    i /= p.ktiles;
-    const int part = (int)(i % a.rsplits);
-    i /= a.rsplits;
-    const int hk = (int)(i % a.Hkv), b = (int)(i / a.Hkv);
+    int kt, part, hk, b;
+    if constexpr (WIN) {  // key tiles slowest: the first ones, which the most rows see, begin first
+        hk = (int)(i % a.Hkv);
+        i /= a.Hkv;
+        b = (int)(i % a.B);
+        i /= a.B;
+        part = (int)(i % a.rsplits);
+        kt = (int)(i / a.rsplits);
+    } else {
+        kt = (int)(i % p.ktiles);
+        i /= p.ktiles;
+        part = (int)(i % a.rsplits);
+        i /= a.rsplits;
+        hk = (int)(i % a.Hkv);
+        b = (int)(i / a.Hkv);
+    }
     const int tile_rows = p.nl * a.G;
     const int n = keys_of(a, b), j0 = kt * kTile;
-    const long long t0 = p.rtiles * part / a.rsplits, t1 = p.rtiles * (part + 1) / a.rsplits;
+    long long t0, t1;
+    if constexpr (WIN) {  // the row tiles that see some key of the tile
+        const RowSpan rows = row_span(a, b, j0, min(n, j0 + kTile));
+        const long long first = rows.first / p.nl, some = max(0ll, (rows.end + p.nl - 1) / p.nl - first);
+        t0 = first + some * part / a.rsplits;
+        t1 = first + some * (part + 1) / a.rsplits;
+    } else {
+        t0 = p.rtiles * part / a.rsplits;
+        t1 = p.rtiles * (part + 1) / a.rsplits;
+    }
     const int nt = uniform(j0 < n ? (int)(t1 - t0) : 0);  // row tiles
 
     // the softmax warps' parts of K and V, on their way while the CTA is set up
@@ -401,8 +468,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t ts = t_s + col, td = t_dp + col;
         const int j = j0 + quad * 32 + lane;
         const bool valid = j < n && (!a.mask || __ldg(a.mask + (long long)b * a.ldm + j) != 0);
-        const bool whole = __all_sync(0xffffffffu, valid);
+        const bool whole_keys = __all_sync(0xffffffffu, valid);
         const float cs = a.scale * kLog2e;
+        // through a window: the rows of the first tile, from its start, that see key j are first_row..end_row - 1 (before G)
+        [[maybe_unused]] long long first_row = 0, end_row = 0;
+        if constexpr (WIN) {
+            const RowSpan rows = row_span(a, b, j, j + 1);
+            first_row = rows.first - t0 * p.nl;
+            end_row = rows.end - t0 * p.nl;
+        }
         if (nt > 0) {
             keep_row(t_k + lane_base, kx, warp >> 2);
             keep_row(t_v + lane_base, vx, warp >> 2);
@@ -415,6 +489,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         bool ok = true;
         for (int t = 0; t < nt; ++t, rp.next(ST)) {
             const uint32_t ph = (uint32_t)t & 1u;
+            uint32_t see = valid ? 0xffffffffu : 0u;  // this warp's rows that see this lane's key
+            bool whole = whole_keys;
+            if constexpr (WIN) {
+                const long long l = (long long)t * p.nl;
+                const int x = (int)min(max(first_row - l, 0ll), (long long)p.nl) * a.G, y = (int)min(max(end_row - l, 0ll), (long long)p.nl) * a.G;
+                see &= bits_between(x - (kHalf * h + kCols * cw), y - (kHalf * h + kCols * cw));
+                whole = __all_sync(0xffffffffu, see == 0xffffffffu);
+            }
             if (!mbar_wait_warp_inline(&c.st_full[rp.idx], rp.phase, abort_flag, err) ||
                 !mbar_wait_warp_inline(&c.s_full[h], ph, abort_flag, err)) {
                 ok = false;
@@ -438,7 +520,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (!whole) {
 #pragma unroll
-                for (int q = 0; q < kCols; ++q) s[q] = valid ? s[q] : 0.f;
+                for (int q = 0; q < kCols; ++q) s[q] = (WIN ? (see >> q) & 1u : valid) ? s[q] : 0.f;
             }
 #pragma unroll
             for (int q = 0; q < kCols / 2; ++q) pk[q] = pack_bf16(s[2 * q], s[2 * q + 1]);
@@ -467,7 +549,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (!whole) {
 #pragma unroll
-                for (int q = 0; q < kCols; ++q) d[q] = valid ? d[q] : 0.f;
+                for (int q = 0; q < kCols; ++q) d[q] = (WIN ? (see >> q) & 1u : valid) ? d[q] : 0.f;
             }
 #pragma unroll
             for (int q = 0; q < kCols / 2; ++q) pk[q] = pack_bf16(d[2 * q], d[2 * q + 1]);
@@ -506,7 +588,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
 }
 
-template <int DKC, int DVC>
+template <int DKC, int DVC, bool WIN>
 __global__ void __launch_bounds__(kThreads, 1)
     k_xattn_dq_tc(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const Params p) {
     using C = Cfg<DKC, DVC>;
@@ -523,17 +605,43 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31;
 
     long long i = blockIdx.x;
-    const long long rt = i % p.rtiles;
-    i /= p.rtiles;
-    const int part = (int)(i % a.splits);
-    i /= a.splits;
-    const int hk = (int)(i % a.Hkv), b = (int)(i / a.Hkv);
+    long long rt;
+    int part, hk, b;
+    if constexpr (WIN) {  // row tiles slowest, from the last one on: without a window it sees the most keys
+        hk = (int)(i % a.Hkv);
+        i /= a.Hkv;
+        b = (int)(i % a.B);
+        i /= a.B;
+        part = (int)(i % a.splits);
+        rt = p.rtiles - 1 - i / a.splits;
+    } else {
+        rt = i % p.rtiles;
+        i /= p.rtiles;
+        part = (int)(i % a.splits);
+        i /= a.splits;
+        hk = (int)(i % a.Hkv);
+        b = (int)(i / a.Hkv);
+    }
     const int tile_rows = p.nl * a.G;
     const int n = keys_of(a, b);
-    const int t0 = (int)((long long)p.ktiles * part / a.splits);
-    const int t1 = min((int)((long long)p.ktiles * (part + 1) / a.splits), (n + kTile - 1) / kTile);
+    // the key tiles, or, through a window, those that some row of the tile sees: first sinks, then the window
+    int t0, t1, sinks = 0, skip = 0;
+    KeySpan span{0, 0, 0};
+    if constexpr (WIN) {
+        span = key_span<kWindowKeys>(a, b, rt * p.nl, min(rt * p.nl + p.nl, (long long)a.Lq) - 1, n);
+        const int from = span.lo / kTile;
+        sinks = min((span.sink + kTile - 1) / kTile, from);
+        skip = from - sinks;
+        const long long count = sinks + max(0, (span.hi + kTile - 1) / kTile - from);
+        t0 = (int)(count * part / a.splits);
+        t1 = (int)(count * (part + 1) / a.splits);
+    } else {
+        t0 = (int)((long long)p.ktiles * part / a.splits);
+        t1 = min((int)((long long)p.ktiles * (part + 1) / a.splits), (n + kTile - 1) / kTile);
+    }
     const int nt = uniform(max(0, t1 - t0));  // key tiles
-    const bool fix = a.lens != nullptr || a.mask != nullptr;
+    auto first_key = [&](int t) { return (WIN && t0 + t >= sinks ? t0 + t + skip : t0 + t) * kTile; };
+    const bool fix = WIN || a.lens != nullptr || a.mask != nullptr;
 
     // the softmax warps' parts of Q and dO, on their way while the CTA is set up
     uint32_t qx[DKC][8], ox[DVC][8];
@@ -585,13 +693,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                 mbar_arrive_expect_tx(&c.a_full[s], (uint32_t)(DKC * kChunkBytes));
                 for (int k = 0; k < DKC; ++k)
                     tma_load_4d(Kr + (size_t)(s * DKC + k) * kChunkBytes, &mk, &c.a_full[s], k * kChunk, hk * p.khmul,
-                                (t0 + t) * kTile, b * p.kmul);
+                                first_key(t), b * p.kmul);
                 ++sa;
                 if (!mbar_wait_1t(&c.b_empty[s], rp.phase ^ 1u, abort_flag, err)) break;
                 mbar_arrive_expect_tx(&c.b_full[s], (uint32_t)(DVC * kChunkBytes));
                 for (int k = 0; k < DVC; ++k)
                     tma_load_4d(Vr + (size_t)(s * DVC + k) * kChunkBytes, &mv, &c.b_full[s], k * kChunk, hk * p.vhmul,
-                                (t0 + t) * kTile, b * p.vmul);
+                                first_key(t), b * p.vmul);
                 ++sb;
             }
             for (int j = std::max(0, sa - ST); j < sa; ++j) mbar_drain(&c.a_full[j % ST], (uint32_t)(j / ST) & 1u, err);
@@ -602,7 +710,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         RingPos rp;
         for (int t = 0; t < nt && fix; ++t, rp.next(ST)) {
             uint32_t w[4];
-            valid_words(w, a, b, (t0 + t) * kTile, n);
+            valid_words(w, a, b, first_key(t), n);
+            if constexpr (WIN) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] &= seen_word(span, first_key(t) + 32 * e);
+            }
             if (!mbar_wait_warp(&c.a_full[rp.idx], rp.phase, abort_flag, err)) break;
             if ((w[0] & w[1] & w[2] & w[3]) != 0xffffffffu) {
                 zero_rows(Kr + (size_t)rp.idx * DKC * kChunkBytes, DKC, w);
@@ -675,7 +787,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         const float nl = stats[r];
         float nd = nt > 0 ? stats[kTile + r] : 0.f;  // (the part that has all keys may write it)
         const bool none = nl == -INFINITY;  // no row, or one without weight
-        const bool exact = n <= kTile && nt == 1;  // by the sequence, not by its padding: other parts have no tile then
+        [[maybe_unused]] KeySpan mine_sees{0, 0, 0};
+        if constexpr (WIN) {
+            if (mine) mine_sees = key_span<kWindowKeys>(a, b, ql, ql, n);
+        }
+        const bool exact = !WIN && n <= kTile && nt == 1;  // by the sequence, not by its padding: other parts have no tile then
         if (nt > 0) {
             keep_row(t_q + lane_base, qx, warp >> 2);
             keep_row(t_do + lane_base, ox, warp >> 2);
@@ -687,13 +803,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         bool ok = true;
         for (int t = 0; t < nt; ++t) {
             const uint32_t ph = (uint32_t)t & 1u;
-            const int j0 = (t0 + t) * kTile;
+            const int j0 = first_key(t);
             const bool whole = j0 + kTile <= n && !a.mask;
             uint32_t w = 0xffffffffu;
             if (!whole) {
                 const int j = j0 + kHalf * h + kCols * cw + lane;
                 w = __ballot_sync(0xffffffffu, j < n && (!a.mask || __ldg(a.mask + (long long)b * a.ldm + j) != 0));
             }
+            if constexpr (WIN) w &= seen_word(mine_sees, j0 + kHalf * h + kCols * cw);
             if (!mbar_wait_warp_inline(&c.s_full[h], ph, abort_flag, err)) {
                 if (exact) bar_sync_and(1, kSoftWarps * 32, false);
                 ok = false;
@@ -743,7 +860,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 add2(d[q], d[q + 1], nd, nd);
                 mul2(d[q], d[q + 1], s[q], s[q + 1]);
             }
-            if (w != 0xffffffffu) {
+            if (WIN ? __any_sync(0xffffffffu, w != 0xffffffffu) : w != 0xffffffffu) {
 #pragma unroll
                 for (int q = 0; q < kCols; ++q) d[q] = (w >> q) & 1u ? d[q] : 0.f;
             }
@@ -773,31 +890,43 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
 }
 
-std::atomic<bool> g_attr[64][4];
+std::atomic<bool> g_attr[64][8];
 std::atomic<bool> g_launched;  // the error word is read (a blocking copy of some 10 us) only once a kernel may have set it
 
-template <int DKC, int DVC>
+template <int DKC, int DVC, bool WIN>
 cudaError_t launch(const HeadMap& q, const HeadMap& o, const HeadMap& k, const HeadMap& v, const Params& p, int device,
                    cudaStream_t s) {
     using C = Cfg<DKC, DVC>;
     const XattnArgs& a = p.a;
-    std::atomic<bool>& set = g_attr[device][(DKC - 1) * 2 + DVC - 1];
+    std::atomic<bool>& set = g_attr[device][(DKC - 1) * 4 + (DVC - 1) * 2 + WIN];
     cudaError_t e = cudaSuccess;
     if (!set) {
-        e = cudaFuncSetAttribute(k_xattn_dkv_tc<DKC, DVC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
+        e = cudaFuncSetAttribute(k_xattn_dkv_tc<DKC, DVC, WIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
         if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(k_xattn_dq_tc<DKC, DVC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
+            e = cudaFuncSetAttribute(k_xattn_dq_tc<DKC, DVC, WIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
         if (e != cudaSuccess) return e;
         set = true;
     }
     // first dQ: for short sequences it leaves a more exact D to the other
-    k_xattn_dq_tc<DKC, DVC><<<(unsigned)(p.rtiles * a.splits * a.Hkv * a.B), kThreads, C::kSmem, s>>>(k.map, v.map, p);
+    k_xattn_dq_tc<DKC, DVC, WIN><<<(unsigned)(p.rtiles * a.splits * a.Hkv * a.B), kThreads, C::kSmem, s>>>(k.map, v.map, p);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     if (a.splits > 1 && (e = launch_xattn_join_dq(a, s)) != cudaSuccess) return e;
-    k_xattn_dkv_tc<DKC, DVC><<<(unsigned)((long long)p.ktiles * a.rsplits * a.Hkv * a.B), kThreads, C::kSmem, s>>>(
+    k_xattn_dkv_tc<DKC, DVC, WIN><<<(unsigned)((long long)p.ktiles * a.rsplits * a.Hkv * a.B), kThreads, C::kSmem, s>>>(
         q.map, o.map, p);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     return a.rsplits > 1 ? launch_xattn_join_dkv(a, s) : cudaSuccess;
+}
+
+template <bool WIN>
+cudaError_t launch_widths(const HeadMap& q, const HeadMap& o, const HeadMap& k, const HeadMap& v, const Params& p, int vec, int device,
+                          cudaStream_t s) {
+    const XattnArgs& a = p.a;
+    k_xattn_stats<WIN><<<(unsigned)(kStatBlocks * p.rtiles * a.Hkv * a.B), 256, 0, s>>>(a, p.nl, p.rtiles, vec);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    const bool k2 = a.dk > kChunk, v2 = a.dv > kChunk;
+    return k2 ? (v2 ? launch<2, 2, WIN>(q, o, k, v, p, device, s) : launch<2, 1, WIN>(q, o, k, v, p, device, s))
+              : (v2 ? launch<1, 2, WIN>(q, o, k, v, p, device, s) : launch<1, 1, WIN>(q, o, k, v, p, device, s));
 }
 
 bool on_vectors(const HeadView& v, int B, int L, int H, int w) {
@@ -818,9 +947,14 @@ unsigned take_device_error_xbwd() {
 void xattn_bwd_tc_plan(XattnArgs& a, KeyMode mode, int sms) {
     const long long nl = kTile / a.G;
     const long long kt = (a.Lk + kTile - 1) / kTile, rt = (a.Lq + nl - 1) / nl;
+    long long keys = kt, rows = rt;  // tiles that one of the other kind meets
+    if (mode == kWindowKeys) {
+        keys = std::min(kt, ((long long)a.win.window + std::min(a.win.sinks, a.Lk) + nl) / kTile + 1);
+        if (a.win.sinks == 0) rows = std::min(rt, ((long long)a.win.window + kTile) / nl + 1);
+    }
     // the keys (rows) are cut into parts of two tiles or more where one CTA per row (key) tile leaves multiprocessors idle
-    a.splits = xattn_parts(rt * a.Hkv * a.B, kt, sms, 2);
-    a.rsplits = xattn_parts(kt * a.Hkv * a.B, rt, sms, 2);
+    a.splits = xattn_parts(rt * a.Hkv * a.B, keys, sms, 2);
+    a.rsplits = xattn_parts(kt * a.Hkv * a.B, rows, sms, 2);
     a.stats = rt * a.Hkv * a.B * kStats;
 }
 
@@ -846,12 +980,7 @@ cudaError_t launch_xattn_bwd_tc(const XattnArgs& a, KeyMode mode, int device, cu
     p.vmul = v.bmul;
     p.vhmul = v.hmul;
     const int vec = on_vectors(a.o, a.B, a.Lq, a.Hq, a.dv) && on_vectors(a.dO, a.B, a.Lq, a.Hq, a.dv);
-    k_xattn_stats<<<(unsigned)(kStatBlocks * p.rtiles * a.Hkv * a.B), 256, 0, s>>>(a, p.nl, p.rtiles, vec);
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-    const bool k2 = a.dk > kChunk, v2 = a.dv > kChunk;
-    return k2 ? (v2 ? launch<2, 2>(q, o, k, v, p, device, s) : launch<2, 1>(q, o, k, v, p, device, s))
-              : (v2 ? launch<1, 2>(q, o, k, v, p, device, s) : launch<1, 1>(q, o, k, v, p, device, s));
+    return mode == kWindowKeys ? launch_widths<true>(q, o, k, v, p, vec, device, s) : launch_widths<false>(q, o, k, v, p, vec, device, s);
 }
 
 }  // namespace gs

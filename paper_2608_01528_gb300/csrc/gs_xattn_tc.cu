@@ -90,8 +90,16 @@ struct Item {
     long long row0;  // first packed row
     int part, hk, b, nq, n, t0, nt;
     long long unit;
+    int sinks, skip;  // through a window: tiles of first keys that stay visible, tiles between them and the window
+    KeySpan span;     // what some row of the item sees
 };
-template <bool PAIR>
+// the item's j-th tile of keys
+template <bool WIN>
+__device__ __forceinline__ int tile_of(const Item& m, int j) {
+    const int t = m.t0 + j;
+    return WIN && t >= m.sinks ? t + m.skip : t;
+}
+template <bool PAIR, bool WIN>
 __device__ __forceinline__ Item item_of(const Params& p, long long i) {
     const XattnArgs& a = p.a;
     Item m;
@@ -105,13 +113,24 @@ __device__ __forceinline__ Item item_of(const Params& p, long long i) {
     m.row0 = m.unit * (PAIR ? 2 : 1) * tile_rows;
     m.nq = PAIR && m.row0 + tile_rows < a.rows ? 2 : 1;
     m.n = keys_of(a, m.b);
+    if constexpr (WIN) {
+        const long long last = min(a.rows, m.row0 + (long long)m.nq * tile_rows) - 1;
+        m.span = key_span<kWindowKeys>(a, m.b, m.row0 / a.G, last / a.G, m.n);
+        const int from = m.span.lo / kTile;
+        m.sinks = min((m.span.sink + kTile - 1) / kTile, from);
+        m.skip = from - m.sinks;
+        const long long count = m.sinks + max(0, (m.span.hi + kTile - 1) / kTile - from);
+        m.t0 = (int)(count * m.part / a.splits);
+        m.nt = (int)(count * (m.part + 1) / a.splits) - m.t0;
+        return m;
+    }
     m.t0 = (int)((long long)p.ktiles * m.part / a.splits);
     const int t1 = min((int)((long long)p.ktiles * (m.part + 1) / a.splits), (m.n + kTile - 1) / kTile);
     m.nt = max(0, t1 - m.t0);  // key tiles
     return m;
 }
 
-template <int DKC, int DVC, bool PAIR>
+template <int DKC, int DVC, bool PAIR, bool WIN>
 __global__ void __launch_bounds__(kThreads, 1)
     k_xattn_tc(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                const __grid_constant__ CUtensorMap mv, const __grid_constant__ Params p) {
@@ -129,7 +148,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const XattnArgs& a = p.a;
     const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31;
     const int tile_rows = p.nl * a.G;
-    const bool fix = a.lens != nullptr || a.mask != nullptr;
+    const bool fix = WIN || a.lens != nullptr || a.mask != nullptr;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < QS; ++s) {
@@ -182,7 +201,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             int sent = 0, qsent = 0;
             bool ok = true;
             for (long long it = blockIdx.x; it < p.items && ok; it += gridDim.x) {
-                const Item m = item_of<PAIR>(p, it);
+                const Item m = item_of<PAIR, WIN>(p, it);
                 if (m.nt == 0) continue;
                 if (!(ok = mbar_wait_1t(&c.q_empty[rq.idx], rq.phase ^ 1u, abort_flag, err))) break;
                 mbar_arrive_expect_tx(&c.q_full[rq.idx], (uint32_t)(m.nq * DKC * kChunk * 2 * tile_rows));
@@ -198,7 +217,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     mbar_arrive_expect_tx(&c.full[rp.idx], (uint32_t)(chunks * kChunkBytes));
                     for (int k = 0; k < chunks; ++k)
                         tma_load_4d(ring + (size_t)rp.idx * C::kStageBytes + (size_t)k * kChunkBytes, key ? &mk : &mv,
-                                    &c.full[rp.idx], k * kChunk, m.hk * (key ? p.khmul : p.vhmul), (m.t0 + j) * kTile,
+                                    &c.full[rp.idx], k * kChunk, m.hk * (key ? p.khmul : p.vhmul), tile_of<WIN>(m, j) * kTile,
                                     m.b * (key ? p.kmul : p.vmul));
                     rp.next(ST);
                     ++sent;
@@ -218,10 +237,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         RingPos rp;
         bool ok = fix;
         for (long long it = blockIdx.x; it < p.items && ok; it += gridDim.x) {
-            const Item m = item_of<PAIR>(p, it);
+            const Item m = item_of<PAIR, WIN>(p, it);
             auto pass = [&](bool key, int j) {
                 uint32_t w[4];
-                if (!key) valid_words(w, a, m.b, (m.t0 + j) * kTile, m.n);
+                if (!key) {
+                    const int j0 = tile_of<WIN>(m, j) * kTile;
+                    valid_words(w, a, m.b, j0, m.n);
+                    if constexpr (WIN) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) w[i] &= seen_word(m.span, j0 + 32 * i);
+                    }
+                }
                 if (!mbar_wait_warp(&c.full[rp.idx], rp.phase, abort_flag, err)) return false;
                 if (!key && (w[0] & w[1] & w[2] & w[3]) != 0xffffffffu) {
                     zero_rows(ring + (size_t)rp.idx * C::kStageBytes, DVC, w);
@@ -248,7 +274,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             uint32_t done0 = 0, done1 = 0;  // weights consumed of each group
             bool ok = true;
             for (long long it = blockIdx.x; it < p.items && ok; it += gridDim.x) {
-                Item m = item_of<PAIR>(p, it);
+                Item m = item_of<PAIR, WIN>(p, it);
                 m.nt = uniform(m.nt);
                 m.nq = uniform(m.nq);
                 if (m.nt == 0) continue;
@@ -334,18 +360,37 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint32_t taken = 0, joins = 0;  // key tiles and joined items of this group so far
         bool ok = true;
         for (long long it = blockIdx.x; it < p.items && ok; it += gridDim.x) {
-            const Item im = item_of<PAIR>(p, it);
+            const Item im = item_of<PAIR, WIN>(p, it);
             if (PAIR && t >= im.nq) continue;
             const long long left = a.rows - (im.row0 + (long long)(PAIR ? t : 0) * tile_rows);
             const int nrows = (int)(left < tile_rows ? left : tile_rows);
             const bool busy = quad * 32 < nrows;  // a warp without a row only keeps the barriers' count
+            [[maybe_unused]] KeySpan sp;
+            if constexpr (WIN) {
+                sp.sink = sp.lo = 0;
+                sp.hi = 0x7fffffff;  // (a lane without a row keeps no tile from the unmasked path)
+                if (r < nrows) {
+                    const long long l = (im.row0 + (long long)(PAIR ? t : 0) * tile_rows + r) / a.G;
+                    sp = key_span<kWindowKeys>(a, im.b, l, l, im.n);
+                }
+            }
             const int steps = PAIR ? im.nt : (im.nt - t + 1) / 2;  // key tiles of this group
             float m = lowest, l = 0.f;  // m in units of the logits s
             for (int k = 0; k < steps; ++k, ++taken) {
-                const int j0 = (im.t0 + (PAIR ? k : 2 * k + t)) * kTile;
+                const int j0 = tile_of<WIN>(im, PAIR ? k : 2 * k + t) * kTile;
                 uint32_t w[4];
                 bool whole = j0 + kTile <= im.n && !a.mask;
-                if (busy && !whole) {
+                if constexpr (WIN) {
+                    if (busy) {
+                        whole = !a.mask && __all_sync(0xffffffffu, sp.lo <= j0 && sp.hi >= j0 + kTile);
+                        if (!whole) {
+                            valid_words(w, a, im.b, j0, im.n);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) w[i] &= seen_word(sp, j0 + 32 * i);
+                            whole = __all_sync(0xffffffffu, (w[0] & w[1] & w[2] & w[3]) == 0xffffffffu);
+                        }
+                    }
+                } else if (busy && !whole) {
                     valid_words(w, a, im.b, j0, im.n);
                     whole = (w[0] & w[1] & w[2] & w[3]) == 0xffffffffu;
                 }
@@ -377,8 +422,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (k == 0) {
                         m = mn;
                     } else if (__any_sync(0xffffffffu, (mn - m) * cs > kGrow)) {
-                        const float f = ex2((m - mn) * cs);
-                        m = mn;
+                        // through a window each row goes by its own keys: what only its neighbours see does not change its rounding
+                        const float to_m = WIN && !((mn - m) * cs > kGrow) ? m : mn;
+                        const float f = ex2((m - to_m) * cs);
+                        m = to_m;
                         l *= f;
                         if (!mbar_wait_warp_inline(&c.o_done[t], (taken - 1) & 1u, abort_flag, err)) {
                             ok = false;
@@ -458,6 +505,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const float inv = l == 0.f ? 0.f : 1.f / l;
                 __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.o.p) + im.b * a.o.b + ql * a.o.l + h * a.o.h;
                 float* po = a.ws + ((long long)im.part * all + at) * a.dv;
+                [[maybe_unused]] bool wild = false;
 #pragma unroll
                 for (int q = 0; q < DV / 32; ++q) {
                     if (32 * q >= a.dv) break;
@@ -478,6 +526,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const int w = a.dv - 32 * q;  // columns left
                     if (a.splits == 1) {
                         uint32_t u[16];
+                        if constexpr (WIN) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) wild |= !(fabsf(v[e] * inv) <= FLT_MAX);
+                        }
 #pragma unroll
                         for (int e = 0; e < 16; ++e) u[e] = pack_bf16(v[2 * e] * inv, v[2 * e + 1] * inv);
                         if (p.o_vec)
@@ -502,8 +554,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (a.splits > 1) {
                         float2* ml = reinterpret_cast<float2*>(a.ws + xattn_ws_ml(a)) + (long long)im.part * all + at;
                         *ml = make_float2(m2, l);
-                    } else if (a.lse) {
-                        a.lse[at] = l == 0.f ? -INFINITY : (m2 + log2f(l)) * kLn2;
+                    } else {
+                        if (a.lse) a.lse[at] = l == 0.f ? -INFINITY : (m2 + log2f(l)) * kLn2;
+                        if constexpr (WIN) reinterpret_cast<unsigned char*>(a.ws)[at] = wild;  // (for k_window_mend)
                     }
                 }
             }
@@ -524,22 +577,91 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
 }
 
-std::atomic<bool> g_attr[64][8];
+// Rows whose sum of values is not finite: a tile's rows see different keys, and 0 times what is not finite in a row of V that one of them
+// sees is NaN in the others'.  Such a row is taken again, over what it sees: a warp each.
+__device__ void mend_row(const XattnArgs& a, long long at, int lane) {
+    const long long l = at % a.Lq, bh = at / a.Lq;
+    const int b = (int)(bh / a.Hq), h = (int)(bh % a.Hq), hk = h / a.G, n = keys_of(a, b);
+    const KeySpan sp = key_span<kWindowKeys>(a, b, l, l, n);
+    const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.b + l * a.q.l + h * a.q.h;
+    const __nv_bfloat16* kp = reinterpret_cast<const __nv_bfloat16*>(a.k.p) + b * a.k.b + hk * a.k.h;
+    const __nv_bfloat16* vp = reinterpret_cast<const __nv_bfloat16*>(a.v.p) + b * a.v.b + hk * a.v.h;
+    float m = -INFINITY, sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 < sp.count(); i0 += 32) {
+        const int i = i0 + lane;
+        const long long j = i < sp.count() ? sp.key(i) : -1;
+        const bool in = j >= 0 && (!a.mask || a.mask[b * a.ldm + j] != 0);
+        float s = 0.f;
+        for (int c = 0; c < a.dk && in; ++c) s = fmaf(__bfloat162float(q[c]), __bfloat162float(kp[j * a.k.l + c]), s);
+        s = in ? s * a.scale * kLog2e : -INFINITY;
+        float mn = fmaxf(m, s);
+#pragma unroll
+        for (int x = 16; x; x >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, x));
+        const float ms = mn == -INFINITY ? 0.f : mn, f = ex2(m - ms), p = ex2(s - ms);
+        m = mn;
+        sum *= f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] *= f;
+        for (int x = 0; x < 32; ++x) {
+            const float w = __shfl_sync(0xffffffffu, p, x);
+            const long long jj = __shfl_sync(0xffffffffu, j, x);
+            if (w == 0.f) continue;
+            sum += w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (lane + 32 * e < a.dv) o[e] = fmaf(w, __bfloat162float(vp[jj * a.v.l + lane + 32 * e]), o[e]);
+        }
+    }
+    __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.o.p) + b * a.o.b + l * a.o.l + h * a.o.h;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (lane + 32 * e < a.dv) out[lane + 32 * e] = __float2bfloat16_rn(sum == 0.f ? 0.f : o[e] / sum);
+}
+// Flagged rows (a byte each), or, where parts were joined, the rows of O themselves: 256 rows a block.  4 x 4,096 rows of 32 heads
+// without a flag: 2 us.
+__global__ void __launch_bounds__(256) k_window_mend(const XattnArgs a) {
+    const long long rows = xattn_rows(a), at = (long long)blockIdx.x * 256 + threadIdx.x;
+    const int lane = threadIdx.x & 31;
+    bool wild = false;
+    if (at < rows) {
+        if (a.splits == 1) {
+            wild = reinterpret_cast<const unsigned char*>(a.ws)[at] != 0;
+        } else {
+            const long long l = at % a.Lq, bh = at / a.Lq;
+            const __nv_bfloat16* o = reinterpret_cast<const __nv_bfloat16*>(a.o.p) + (bh / a.Hq) * a.o.b + l * a.o.l + (bh % a.Hq) * a.o.h;
+            for (int c = 0; c < a.dv; ++c) wild |= !(fabsf(__bfloat162float(o[c])) <= FLT_MAX);
+        }
+    }
+    unsigned todo = __ballot_sync(0xffffffffu, wild);
+    for (; todo; todo &= todo - 1) mend_row(a, at - lane + __ffs(todo) - 1, lane);
+}
+
+std::atomic<bool> g_attr[64][16];
 std::atomic<bool> g_launched;  // the error word is read (a blocking copy of some 10 us) only once a kernel may have set it
 
-template <int DKC, int DVC, bool PAIR>
+template <int DKC, int DVC, bool PAIR, bool WIN>
 cudaError_t launch(const HeadMap& q, const HeadMap& k, const HeadMap& v, const Params& p, int sms, int device, cudaStream_t s) {
     using C = Cfg<DKC, DVC, PAIR>;
-    std::atomic<bool>& set = g_attr[device][(DKC - 1) * 4 + (DVC - 1) * 2 + PAIR];
+    std::atomic<bool>& set = g_attr[device][(DKC - 1) * 8 + (DVC - 1) * 4 + PAIR * 2 + WIN];
     if (!set) {
-        cudaError_t e = cudaFuncSetAttribute(k_xattn_tc<DKC, DVC, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        cudaError_t e = cudaFuncSetAttribute(k_xattn_tc<DKC, DVC, PAIR, WIN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                              (int)C::kSmem);
         if (e != cudaSuccess) return e;
         set = true;
     }
     const long long grid = std::min<long long>(p.items, sms);
-    k_xattn_tc<DKC, DVC, PAIR><<<(unsigned)grid, kThreads, C::kSmem, s>>>(q.map, k.map, v.map, p);
+    k_xattn_tc<DKC, DVC, PAIR, WIN><<<(unsigned)grid, kThreads, C::kSmem, s>>>(q.map, k.map, v.map, p);
     return cudaGetLastError();
+}
+template <bool WIN>
+cudaError_t launch_widths(bool pair, const HeadMap& q, const HeadMap& k, const HeadMap& v, const Params& p, int sms, int device,
+                          cudaStream_t s) {
+    const bool k2 = p.a.dk > kChunk, v2 = p.a.dv > kChunk;
+    if (pair)
+        return k2 ? (v2 ? launch<2, 2, true, WIN>(q, k, v, p, sms, device, s) : launch<2, 1, true, WIN>(q, k, v, p, sms, device, s))
+                  : (v2 ? launch<1, 2, true, WIN>(q, k, v, p, sms, device, s) : launch<1, 1, true, WIN>(q, k, v, p, sms, device, s));
+    return k2 ? (v2 ? launch<2, 2, false, WIN>(q, k, v, p, sms, device, s) : launch<2, 1, false, WIN>(q, k, v, p, sms, device, s))
+              : (v2 ? launch<1, 2, false, WIN>(q, k, v, p, sms, device, s) : launch<1, 1, false, WIN>(q, k, v, p, sms, device, s));
 }
 
 // Row tiles come in pairs when pairs alone fill the multiprocessors; else one row tile a CTA, the keys
@@ -562,7 +684,10 @@ unsigned take_device_error_xattn() {
 
 void xattn_tc_plan(XattnArgs& a, KeyMode mode, int sms) {
     const long long tile_rows = (long long)(kTile / a.G) * a.G;
-    const long long kt = (a.Lk + kTile - 1) / kTile;
+    long long kt = (a.Lk + kTile - 1) / kTile;
+    if (mode == kWindowKeys)  // that a row tile meets
+        kt = std::min(kt, ((long long)a.win.window + std::min(a.win.sinks, a.Lk) + kTile / a.G) / kTile + 1);
+    a.flags = mode == kWindowKeys;
     a.splits = take_pairs(a, sms) ? 1 : xattn_parts((a.rows + tile_rows - 1) / tile_rows * a.Hkv * a.B, kt, sms, 4);
     a.rsplits = 1;
 }
@@ -590,16 +715,12 @@ cudaError_t launch_xattn_tc(const XattnArgs& a, KeyMode mode, int sms, int devic
     p.khmul = k.hmul;
     p.vmul = v.bmul;
     p.vhmul = v.hmul;
-    const bool k2 = a.dk > kChunk, v2 = a.dv > kChunk;
-    cudaError_t e;
-    if (pair)
-        e = k2 ? (v2 ? launch<2, 2, true>(q, k, v, p, sms, device, s) : launch<2, 1, true>(q, k, v, p, sms, device, s))
-               : (v2 ? launch<1, 2, true>(q, k, v, p, sms, device, s) : launch<1, 1, true>(q, k, v, p, sms, device, s));
-    else
-        e = k2 ? (v2 ? launch<2, 2, false>(q, k, v, p, sms, device, s) : launch<2, 1, false>(q, k, v, p, sms, device, s))
-               : (v2 ? launch<1, 2, false>(q, k, v, p, sms, device, s) : launch<1, 1, false>(q, k, v, p, sms, device, s));
-    if (e != cudaSuccess || a.splits == 1) return e;
-    return launch_xattn_join(a, s);
+    cudaError_t e = mode == kWindowKeys ? launch_widths<true>(pair, q, k, v, p, sms, device, s)
+                                        : launch_widths<false>(pair, q, k, v, p, sms, device, s);
+    if (e == cudaSuccess && a.splits > 1) e = launch_xattn_join(a, s);
+    if (e != cudaSuccess || mode != kWindowKeys) return e;
+    k_window_mend<<<(unsigned)((xattn_rows(a) + 255) / 256), 256, 0, s>>>(a);
+    return cudaGetLastError();
 }
 
 }  // namespace gs
