@@ -10,6 +10,7 @@
 // integers run at an eighth of that rate.
 
 #include <algorithm>
+#include <type_traits>
 
 #include "gs_paged.h"
 #include "gs_tc_ptx.cuh"
@@ -19,18 +20,17 @@ namespace {
 
 using u64 = unsigned long long;
 
-constexpr int kWarps = 16, kThreads = kWarps * 32;
-constexpr int kMaxCtas = 8;
+constexpr int kWarps = 4, kThreads = kWarps * 32;
+constexpr int kMaxCtas = 8, kResident = 8;  // CTAs of a row; of a multiprocessor
+constexpr int kAhead = 4;                   // 16-byte loads of a lane in flight, of P and of D each
 constexpr float kHigh = 2097152.f, kLow = 8388608.f, kMagic = 12582912.f;  // 2^21, 2^23, 1.5 * 2^23
 constexpr int kMagicBits = 0x4B400000;
 
-struct Parts {
-    int hi, lo;  // (hi 2^23 + lo) units
-};
-__device__ __forceinline__ Parts parts_of(float p) {  // p in [0, 1]
+// hi 2^23 + lo units, the sums of p's parts (kMagicBits over in each term), less those of d
+__device__ __forceinline__ void split(float p, int& hi, int& lo) {  // p in [0, 1]
     const float a = fmaf(p, kHigh, kMagic), t = a - kMagic;
-    const float b = fmaf(fmaf(p, kHigh, -t), kLow, kMagic);  // (the inner one is exact)
-    return {__float_as_int(a) - kMagicBits, __float_as_int(b) - kMagicBits};
+    hi = __float_as_int(a);
+    lo = __float_as_int(fmaf(fmaf(p, kHigh, -t), kLow, kMagic));  // (the inner one is exact)
 }
 
 // What the rows weigh: P alone, P without one entry, or P less D.
@@ -46,14 +46,20 @@ __device__ __forceinline__ float read(const void* row, int j) {
     else
         return __uint_as_float((uint32_t)__ldg(static_cast<const unsigned short*>(row) + j) << 16);
 }
-__device__ __forceinline__ void add(float p, float d, int& hi, int& lo) {  // NaN counts as 0, what is above 1 as 1
+// NaN counts as 0, what is above 1 as 1; below d nothing is left, d's parts less d's parts
+__device__ __forceinline__ void add(float p, float d, int& hi, int& lo) {
     p = __saturatef(p);
-    d = __saturatef(d);
-    const Parts x = parts_of(p), y = parts_of(d);
-    if (p > d) {
-        hi += x.hi - y.hi;
-        lo += x.lo - y.lo;
-    }
+    int ph, pl, dh, dl;
+    split(p, ph, pl);
+    split(fminf(__saturatef(d), p), dh, dl);
+    hi += ph - dh;
+    lo += pl - dl;
+}
+__device__ __forceinline__ void add(float p, int& hi, int& lo) {
+    int ph, pl;
+    split(__saturatef(p), ph, pl);
+    hi += ph - kMagicBits;
+    lo += pl - kMagicBits;
 }
 __device__ __forceinline__ long long units(int hi, int lo) { return (long long)hi * 8388608ll + lo; }
 template <typename T>
@@ -64,66 +70,94 @@ __device__ __forceinline__ u64 weight(const Row& r, int j) {
     return (u64)units(hi, lo);
 }
 
-// Sum of the weights [j0, j1) (a warp).
+// What 16 bytes of P (and D) weigh, added to hi and lo.
+template <typename T, bool LESS>
+__device__ __forceinline__ void add16(const uint4& a, const uint4& b, int& hi, int& lo) {
+    const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+    auto one = [&](uint32_t u, uint32_t v) {
+        if constexpr (LESS)
+            add(__uint_as_float(u), __uint_as_float(v), hi, lo);
+        else
+            add(__uint_as_float(u), hi, lo);
+    };
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if constexpr (sizeof(T) == 4) {
+            one(x[e], y[e]);
+        } else {
+            one(x[e] << 16, y[e] << 16);
+            one(x[e] & 0xffff0000u, y[e] & 0xffff0000u);
+        }
+    }
+}
+// Steps of 16 bytes at p (and d), `step` entries apart, kAhead in flight.
+template <typename T, bool LESS>
+__device__ __forceinline__ long long sum_steps(const T* p, const T* d, int steps, int step) {
+    long long sum = 0;
+    int w = 0;
+    auto some = [&](auto n) {
+        constexpr int kN = decltype(n)::value;
+        uint4 a[kN], b[kN];
+#pragma unroll
+        for (int u = 0; u < kN; ++u) {
+            a[u] = __ldg(reinterpret_cast<const uint4*>(p + (long long)(w + u) * step));
+            b[u] = LESS ? __ldg(reinterpret_cast<const uint4*>(d + (long long)(w + u) * step)) : make_uint4(0, 0, 0, 0);
+        }
+        int hi = 0, lo = 0;
+#pragma unroll
+        for (int u = 0; u < kN; ++u) add16<T, LESS>(a[u], b[u], hi, lo);
+        sum += units(hi, lo);
+        w += kN;
+    };
+    while (w + kAhead <= steps) some(std::integral_constant<int, kAhead>());
+    while (w < steps) some(std::integral_constant<int, 1>());
+    return sum;
+}
+// Sum of the weights [j0, j1): entries j0 + first, .. + 16 bytes, then `step` entries on, as long as they lie inside; then those that
+// are left, one to each of `lanes` lanes.
 template <typename T>
-__device__ __forceinline__ u64 sum_piece(const Row& r, int j0, int j1, bool vec) {
-    constexpr int N = 16 / sizeof(T), kAhead = 2;
-    const int lane = threadIdx.x & 31;
+__device__ __forceinline__ u64 sum_of(const Row& r, int j0, int j1, int first, int step, int lanes, bool vec) {
+    constexpr int N = 16 / sizeof(T);
     long long sum = 0;
     int j = j0;
     if (vec) {
-        for (; j + 32 * N <= j1; j += 32 * N * kAhead) {
-            uint4 a[kAhead], b[kAhead];
-            bool in[kAhead];
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const int at = j + 32 * N * u + lane * N;
-                in[u] = j + 32 * N * (u + 1) <= j1;
-                a[u] = in[u] ? __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(r.p) + at)) : make_uint4(0, 0, 0, 0);
-                b[u] = in[u] && r.rest == kLess ? __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(r.d) + at))
-                                                : make_uint4(0, 0, 0, 0);
-            }
+        const int steps = (j1 - j0) / step;
+        const T *p = static_cast<const T*>(r.p) + j0 + first, *d = static_cast<const T*>(r.d) + j0 + first;
+        sum = r.rest == kLess ? sum_steps<T, true>(p, d, steps, step) : sum_steps<T, false>(p, p, steps, step);
+        j += steps * step;
+        const int x = r.x - j0;  // the entry that is left out is taken off again by the lane that added it
+        if (r.rest == kWithout && x >= 0 && x < j - j0 && x % step >= first && x % step < first + N) {
             int hi = 0, lo = 0;
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const uint32_t x[4] = {a[u].x, a[u].y, a[u].z, a[u].w}, y[4] = {b[u].x, b[u].y, b[u].z, b[u].w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if constexpr (sizeof(T) == 4) {
-                        add(__uint_as_float(x[e]), __uint_as_float(y[e]), hi, lo);
-                    } else {
-                        add(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), hi, lo);
-                        add(__uint_as_float(x[e] & 0xffff0000u), __uint_as_float(y[e] & 0xffff0000u), hi, lo);
-                    }
-                }
-            }
-            sum += units(hi, lo);
-            if (!in[kAhead - 1]) {
-                j += 32 * N;
-                break;
-            }
-        }
-        if (r.rest == kWithout && lane == 0 && r.x >= j0 && r.x < j) {  // the entry that is left out, taken off again
-            int hi = 0, lo = 0;
-            add(read<T>(r.p, r.x), 0.f, hi, lo);
+            add(read<T>(r.p, r.x), hi, lo);
             sum -= units(hi, lo);
         }
     }
-    for (j += lane; j < j1; j += 32) sum += (long long)weight<T>(r, j);
-    u64 v = (u64)sum;
+    for (j += first / N; j < j1; j += lanes) sum += (long long)weight<T>(r, j);
+    return (u64)sum;
+}
+// of a warp: every lane gets it
+template <typename T>
+__device__ __forceinline__ u64 sum_piece(const Row& r, int j0, int j1, bool vec) {
+    constexpr int N = 16 / sizeof(T);
+    u64 v = sum_of<T>(r, j0, j1, (threadIdx.x & 31) * N, 32 * N, 32, vec);
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
 
-// The first index of [j0, j1) whose running weight is above t (there is one); a warp.
+// The first index of [j0, j1) whose running weight is above t (there is one); a warp.  Each lane sums a 32nd, and the one whose part
+// crosses t is cut into 32 again: 8,192 entries take three rounds.
 template <typename T>
-__device__ int locate(const Row& r, int j0, int j1, u64 t) {
+__device__ int locate(const Row& r, int j0, int j1, u64 t, bool vec) {
+    constexpr int N = 16 / sizeof(T);
     const int lane = threadIdx.x & 31;
     for (;;) {
-        const int n = j1 - j0, per = (n + 31) / 32, a = min(j1, j0 + lane * per), b = min(j1, a + per);
-        u64 v = 0;
-        for (int j = a; j < b; ++j) v += weight<T>(r, j);
+        const int n = j1 - j0;
+        int per = (n + 31) / 32;
+        const bool wide = vec && per >= N;  // (j0 is a multiple of N then)
+        if (wide) per = (per + N - 1) / N * N;
+        const int a = min(j1, j0 + lane * per), b = min(j1, a + per);
+        const u64 v = sum_of<T>(r, a, b, 0, N, 1, wide);
         u64 run = v;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -150,7 +184,7 @@ __device__ __forceinline__ void put_remote(uint64_t* at, unsigned rank, u64 v) {
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) k_verify(const VerifyArgs a, int ctas) {
+__global__ void __launch_bounds__(kThreads, kResident) k_verify(const VerifyArgs a, int ctas) {
     __shared__ uint64_t totals[2][kMaxCtas];
     __shared__ u64 sums[kWarps];
     __shared__ int s_kept;
@@ -161,14 +195,15 @@ __global__ void __launch_bounds__(kThreads) k_verify(const VerifyArgs a, int cta
     const float* U = a.U + (long long)b * (a.K + 1);
     const T* P = static_cast<const T*>(a.P) + b * a.pb;
     const T* D = a.D ? static_cast<const T*>(a.D) + b * a.db : nullptr;
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     if (warp == 0) {
         int kept = 0;
-        for (int i0 = 0; i0 < n; i0 += 32) {
+        for (int i0 = 0; i0 < a.K; i0 += 32) {  // (up to K, so that the draft does not wait for the request's length)
             const int i = i0 + lane;
             bool ok = false;
-            if (i < n) {
+            if (i < a.K) {
                 const int x = __ldg(drafts + i);
-                if (x >= 0 && x < a.M) {
+                if (i < n && x >= 0 && x < a.M) {
                     const double d = D ? (double)read<T>(D + i * a.dr, x) : 1.0;
                     ok = (double)unit_of(__ldg(U + i)) * d < (double)read<T>(P + i * a.pr, x);
                 }
@@ -179,7 +214,6 @@ __global__ void __launch_bounds__(kThreads) k_verify(const VerifyArgs a, int cta
         }
         if (lane == 0) s_kept = min(kept, n);
     }
-    ptx::cluster_sync_all();  // every CTA of the cluster runs from here on
     __syncthreads();
     const int kept = s_kept;
     Row row;
@@ -191,11 +225,13 @@ __global__ void __launch_bounds__(kThreads) k_verify(const VerifyArgs a, int cta
     const int steps = (a.M + kStep - 1) / kStep, me = rank * kWarps + warp, all = ctas * kWarps;
     const int j0 = min(a.M, (int)((long long)steps * me / all) * kStep), j1 = min(a.M, (int)((long long)steps * (me + 1) / all) * kStep);
     u64 mine = 0, before = 0, total = 0;
+    bool vec = false;
     for (int turn = 0; turn < 2; ++turn) {  // (again with P alone where nothing is left of it)
-        const bool vec = ((uintptr_t)row.p | (row.rest == kLess ? (uintptr_t)row.d : 0)) % 16 == 0;
+        vec = ((uintptr_t)row.p | (row.rest == kLess ? (uintptr_t)row.d : 0)) % 16 == 0;
         mine = sum_piece<T>(row, j0, j1, vec);
         if (lane == 0) sums[warp] = mine;
         __syncthreads();
+        if (turn == 0) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");  // every CTA of the cluster runs
         if (warp == 0) {
             u64 v = lane < kWarps ? sums[lane] : 0;
 #pragma unroll
@@ -222,7 +258,7 @@ __global__ void __launch_bounds__(kThreads) k_verify(const VerifyArgs a, int cta
         if (me != 0) return;
     } else {
         if (t < before || t >= before + mine) return;  // another warp's
-        drawn = locate<T>(row, j0, j1, t - before);
+        drawn = locate<T>(row, j0, j1, t - before, vec);
     }
     if (lane == 0 && a.accepted) a.accepted[b] = kept;
     if (a.tokens)
@@ -233,10 +269,10 @@ __global__ void __launch_bounds__(kThreads) k_verify(const VerifyArgs a, int cta
 }  // namespace
 
 cudaError_t launch_verify(const VerifyArgs& a, int sms, cudaStream_t s) {
-    // a warp's piece of four loads or more, and no more CTAs than run at once while one a row fills the GPU
+    // a warp's piece of four loads or more, and no more CTAs than run at once where there are more rows than that
     const long long steps = ((long long)a.M * (a.bf16 ? 2 : 4) + 511) / 512;
     int ctas = 1;
-    while (ctas < kMaxCtas && steps >= 4ll * kWarps * ctas && (long long)a.B * ctas < 4ll * sms) ctas *= 2;
+    while (ctas < kMaxCtas && steps >= 4ll * kWarps * ctas && 2ll * a.B * ctas <= (long long)kResident * sms) ctas *= 2;
     if ((long long)a.B * ctas > 0x7fffffffLL) ctas = 1;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(a.B * (long long)ctas));
