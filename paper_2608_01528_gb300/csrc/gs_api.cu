@@ -909,6 +909,7 @@ gs_status attn_args(const gs_attn* p, gs::XattnArgs& a) {
     a.mask = p->key_mask;
     a.ldm = p->ld_mask;
     a.splits = a.rsplits = 1;
+    a.pkeys = a.Lk;
     return GS_OK;
 }
 
@@ -1107,6 +1108,7 @@ gs_status paged_args(const gs_paged* p, gs::XattnArgs& a) {
     a.scale = p->scale;
     a.lens = p->lens;
     a.splits = a.rsplits = 1;
+    a.pkeys = a.Lk;
     a.win = {p->window, p->sinks, 0, nullptr};
     int shift = 0;
     while (1 << shift < p->page_size && shift < 30) ++shift;

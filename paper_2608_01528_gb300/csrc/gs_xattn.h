@@ -5,6 +5,8 @@
 // across the group and the gradients of a shared key head sum over its rows by themselves.
 #pragma once
 
+#include <algorithm>
+
 #include "gs_internal.h"
 
 namespace gs {
@@ -41,6 +43,7 @@ struct XattnArgs {
     float* ws;     // workspace
     int splits;    // forward, dQ: parts of the key axis
     int rsplits;   // dK / dV: parts of the packed rows
+    int pkeys;     // .. of the keys before this one (Lk, or a whole number of tiles): the others' rows are one part
     int vec;       // CUDA-core kernels: which arrays allow loads of four elements
     long long stats;  // backward: floats of the rows' statistics at the start of the workspace
     bool flags;       // forward on tcgen05 through a window: a byte a row in the workspace
@@ -100,13 +103,22 @@ inline int xattn_parts(long long base, long long tiles, int want, int least) {
     return s < 1 ? 1 : (int)s;
 }
 
+// Parts of the rows for the key tiles that sinks show to every row, where all tiles are in one part so far (`base` of them, with all
+// heads and sequences): such a tile meets `rows` row tiles, others about `typical`, and is the last to end where that is more than a slot
+// (there are `slots`; `more` steps besides) has in all.
+inline int xattn_sink_parts(long long base, long long rows, long long typical, long long more, long long slots) {
+    const long long share = std::max(typical, (base * typical + more) / std::max(slots, 1ll));
+    if (4 * rows <= 5 * share) return 1;
+    return (int)std::min({16ll, (rows + share - 1) / share, std::max(1ll, rows / 2)});
+}
+
 // Workspace in floats; every section starts on a 16-byte boundary.
 // Forward (splits > 1): per part and row dv sums, then the row's maximum (base 2) and sum.
 // Backward: the rows' statistics (a.stats), then the parts of dQ (splits > 1), of dK and of dV (rsplits > 1).
 #define GS_XWS __host__ __device__ inline long long
 GS_XWS xattn_round4(long long n) { return (n + 3) / 4 * 4; }
 GS_XWS xattn_rows(const XattnArgs& a) { return (long long)a.B * a.Hq * a.Lq; }
-GS_XWS xattn_keys(const XattnArgs& a) { return (long long)a.B * a.Hkv * a.Lk; }
+GS_XWS xattn_keys(const XattnArgs& a) { return (long long)a.B * a.Hkv * a.pkeys; }  // in parts
 GS_XWS xattn_ws_ml(const XattnArgs& a) { return xattn_round4(a.splits * xattn_rows(a) * a.dv); }
 GS_XWS xattn_ws_forward(const XattnArgs& a) {
     return a.splits > 1 ? xattn_ws_ml(a) + a.splits * xattn_rows(a) * 2 : a.flags ? xattn_round4((xattn_rows(a) + 3) / 4) : 0;

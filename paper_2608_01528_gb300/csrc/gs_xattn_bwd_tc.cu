@@ -161,6 +161,11 @@ __device__ __forceinline__ void sum_few_seen(const XattnArgs& a, int b, int hk, 
     const __nv_bfloat16* values = reinterpret_cast<const __nv_bfloat16*>(a.v.p) + b * a.v.b + hk * a.v.h;
     const float cs = a.scale * kLog2e;
     const int c0 = ln * 8;
+    if (!a.mask) {  // along a tile the number of keys grows, then falls: the first and the last row see the fewest
+        const long long first = rt * nl, last = min(first + nl, (long long)a.Lq) - 1;
+        const int x = key_span<kWindowKeys>(a, b, first, first, n).count(), y = key_span<kWindowKeys>(a, b, last, last, n).count();
+        if (min(x, y) > kFewKeys) return;
+    }
 #pragma unroll 1
     for (int r = grp; r < kTile; r += 16) {
         if (r >= grp + 64) break;  // (a block's 64 slots)
@@ -306,14 +311,21 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31;
 
     long long i = blockIdx.x;
-    int kt, part, hk, b;
+    int kt, part, hk, b, parts = a.rsplits;
     if constexpr (WIN) {  // key tiles slowest: the first ones, which the most rows see, begin first
         hk = (int)(i % a.Hkv);
         i /= a.Hkv;
         b = (int)(i % a.B);
         i /= a.B;
-        part = (int)(i % a.rsplits);
-        kt = (int)(i / a.rsplits);
+        const int in_parts = (a.pkeys + kTile - 1) / kTile;
+        if (i < (long long)in_parts * parts) {
+            part = (int)(i % parts);
+            kt = (int)(i / parts);
+        } else {
+            part = 0;
+            kt = (int)(i - (long long)in_parts * (parts - 1));
+            parts = 1;
+        }
     } else {
         kt = (int)(i % p.ktiles);
         i /= p.ktiles;
@@ -328,11 +340,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     if constexpr (WIN) {  // the row tiles that see some key of the tile
         const RowSpan rows = row_span(a, b, j0, min(n, j0 + kTile));
         const long long first = rows.first / p.nl, some = max(0ll, (rows.end + p.nl - 1) / p.nl - first);
-        t0 = first + some * part / a.rsplits;
-        t1 = first + some * (part + 1) / a.rsplits;
+        t0 = first + some * part / parts;
+        t1 = first + some * (part + 1) / parts;
     } else {
-        t0 = p.rtiles * part / a.rsplits;
-        t1 = p.rtiles * (part + 1) / a.rsplits;
+        t0 = p.rtiles * part / parts;
+        t1 = p.rtiles * (part + 1) / parts;
     }
     const int nt = uniform(j0 < n ? (int)(t1 - t0) : 0);  // row tiles
 
@@ -567,17 +579,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (ok) {  // group 0 writes dV, group 1 dK, 64 columns a warp
             const bool mine = j < a.Lk;
             const long long jj = mine ? j : 0;
-            const long long at = (long long)part * xattn_keys(a) + ((long long)b * a.Hkv + hk) * a.Lk + jj;
-            const bool parts = a.rsplits > 1;
+            const long long at = (long long)part * xattn_keys(a) + ((long long)b * a.Hkv + hk) * a.pkeys + jj;
+            const bool sums = parts > 1;
             const int c0 = cw * 64;
             if (h == 0)
                 drain_acc(t_dv + lane_base, c0, c0 + 64, a.dv, nt > 0, valid, mine, 1.f,
                           reinterpret_cast<__nv_bfloat16*>(a.dV.p) + b * a.dV.b + jj * a.dV.l + hk * a.dV.h, p.vec_v != 0,
-                          parts ? a.ws + xattn_ws_dv(a) + at * a.dv : nullptr);
+                          sums ? a.ws + xattn_ws_dv(a) + at * a.dv : nullptr);
             else
-                drain_acc(t_dk + lane_base, c0, c0 + 64, a.dk, nt > 0, valid, mine, parts ? 1.f : a.scale,
+                drain_acc(t_dk + lane_base, c0, c0 + 64, a.dk, nt > 0, valid, mine, sums ? 1.f : a.scale,
                           reinterpret_cast<__nv_bfloat16*>(a.dK.p) + b * a.dK.b + jj * a.dK.l + hk * a.dK.h, p.vec_k != 0,
-                          parts ? a.ws + xattn_ws_dk(a) + at * a.dk : nullptr);
+                          sums ? a.ws + xattn_ws_dk(a) + at * a.dk : nullptr);
         }
     }
     tc_fence_before();
@@ -911,7 +923,7 @@ cudaError_t launch(const HeadMap& q, const HeadMap& o, const HeadMap& k, const H
     k_xattn_dq_tc<DKC, DVC, WIN><<<(unsigned)(p.rtiles * a.splits * a.Hkv * a.B), kThreads, C::kSmem, s>>>(k.map, v.map, p);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     if (a.splits > 1 && (e = launch_xattn_join_dq(a, s)) != cudaSuccess) return e;
-    k_xattn_dkv_tc<DKC, DVC, WIN><<<(unsigned)((long long)p.ktiles * a.rsplits * a.Hkv * a.B), kThreads, C::kSmem, s>>>(
+    k_xattn_dkv_tc<DKC, DVC, WIN><<<(unsigned)((p.ktiles + (a.pkeys + kTile - 1ll) / kTile * (a.rsplits - 1)) * a.Hkv * a.B), kThreads, C::kSmem, s>>>(
         q.map, o.map, p);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     return a.rsplits > 1 ? launch_xattn_join_dkv(a, s) : cudaSuccess;
@@ -955,6 +967,11 @@ void xattn_bwd_tc_plan(XattnArgs& a, KeyMode mode, int sms) {
     // the keys (rows) are cut into parts of two tiles or more where one CTA per row (key) tile leaves multiprocessors idle
     a.splits = xattn_parts(rt * a.Hkv * a.B, keys, sms, 2);
     a.rsplits = xattn_parts(kt * a.Hkv * a.B, rows, sms, 2);
+    a.pkeys = a.Lk;
+    if (mode == kWindowKeys && a.win.sinks > 0 && a.rsplits == 1) {
+        a.rsplits = xattn_sink_parts(kt * a.Hkv * a.B, rt, std::min(rt, ((long long)a.win.window + kTile) / nl + 1), 0, sms);
+        if (a.rsplits > 1) a.pkeys = (int)std::min<long long>(a.Lk, (a.win.sinks + kTile - 1ll) / kTile * kTile);
+    }
     a.stats = rt * a.Hkv * a.B * kStats;
 }
 

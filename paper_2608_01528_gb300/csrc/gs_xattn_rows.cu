@@ -65,12 +65,12 @@ struct Vec {
 };
 
 template <typename T, int LK, int R, int MODE>
-__global__ void __launch_bounds__(kThreads, R == 1 ? 3 : 2) k_xattn_rows(const XattnArgs a, long long chunks) {
+__global__ void __launch_bounds__(kThreads, R == 1 && MODE != kPagedKeys ? 3 : 2) k_xattn_rows(const XattnArgs a, long long chunks) {
     using V = Vec<T>;
     constexpr int N = V::N, W = LK * N, KS = 32 / LK;
     // Two rows leave registers for the next four keys on their way as well (8 x 8,192 keys, 16 heads of 128, fp32: 209 -> 195 us);
-    // one row does better with a third block a multiprocessor (242 against 297 us).
-    constexpr bool kAhead = R == 2;
+    // one row does better with a third block a multiprocessor (242 against 297 us), but not where the keys wait for the table.
+    constexpr bool kAhead = R == 2 || (R == 1 && MODE == kPagedKeys);
     __shared__ float acc_s[kWarps][R][W];
     __shared__ float2 ml_s[kWarps][R];
     long long i = blockIdx.x;
@@ -121,11 +121,12 @@ __global__ void __launch_bounds__(kThreads, R == 1 ? 3 : 2) k_xattn_rows(const X
         mine = key_span<MODE>(a, b, l, l, n);
     }
     const unsigned char* mask = a.mask ? a.mask + (long long)b * a.ldm : nullptr;
+    constexpr int kStep = kWarps * KS * kBatch;
     V kx[kBatch], vx[kBatch], kn[kBatch], vn[kBatch];
     bool ok[kBatch], okn[kBatch];
-    auto fetch = [&](int j0, V(&kk)[kBatch], V(&vv)[kBatch], bool(&o)[kBatch]) {
+    [[maybe_unused]] int entry[kBatch], row[kBatch];  // of the table, read a batch ahead: the next keys' pages and their rows in them
+    auto entries = [&](int j0) {
         if constexpr (MODE == kPagedKeys) {
-            int entry[kBatch], row[kBatch];
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
                 const int i = j0 + u * KS + slot, j = i < k1 ? span.key(i) : 0;
@@ -133,6 +134,10 @@ __global__ void __launch_bounds__(kThreads, R == 1 ? 3 : 2) k_xattn_rows(const X
                 row[u] = j - col * a.pg.page;
                 entry[u] = i < k1 ? __ldg(a.pg.table + (long long)b * a.pg.ldt + col) : -1;
             }
+        }
+    };
+    auto fetch = [&](int j0, V(&kk)[kBatch], V(&vv)[kBatch], bool(&o)[kBatch]) {
+        if constexpr (MODE == kPagedKeys) {
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
                 o[u] = entry[u] >= 0 && entry[u] < a.pg.pages;
@@ -141,20 +146,21 @@ __global__ void __launch_bounds__(kThreads, R == 1 ? 3 : 2) k_xattn_rows(const X
                 vv[u].load(vp + (o[u] ? (long long)entry[u] * a.v.b + (long long)row[u] * a.v.l : 0), o[u] ? a.dv - e0 : 0,
                            a.vec & kVecV);
             }
-            return;
-        }
+            entries(j0 + kStep);
+        } else {
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            int j = j0 + u * KS + slot;
-            const bool in = j < k1;
-            if constexpr (MODE == kWindowKeys) j = span.key(j);
-            o[u] = in && (!mask || __ldg(mask + j) != 0);
-            kk[u].load(kp + (o[u] ? (long long)j * a.k.l : 0), o[u] ? a.dk - e0 : 0, a.vec & kVecK);
-            vv[u].load(vp + (o[u] ? (long long)j * a.v.l : 0), o[u] ? a.dv - e0 : 0, a.vec & kVecV);
+            for (int u = 0; u < kBatch; ++u) {
+                int j = j0 + u * KS + slot;
+                const bool in = j < k1;
+                if constexpr (MODE == kWindowKeys) j = span.key(j);
+                o[u] = in && (!mask || __ldg(mask + j) != 0);
+                kk[u].load(kp + (o[u] ? (long long)j * a.k.l : 0), o[u] ? a.dk - e0 : 0, a.vec & kVecK);
+                vv[u].load(vp + (o[u] ? (long long)j * a.v.l : 0), o[u] ? a.dv - e0 : 0, a.vec & kVecV);
+            }
         }
     };
-    constexpr int kStep = kWarps * KS * kBatch;
     int j0 = k0 + warp * (KS * kBatch);
+    entries(j0);
     if (kAhead && j0 < k1) fetch(j0, kn, vn, okn);
     for (; j0 < k1; j0 += kStep) {
         if constexpr (kAhead) {
@@ -345,8 +351,9 @@ void xattn_rows_plan(XattnArgs& a, int sms, KeyMode mode) {
     const int R = rows_per_block(a.rows);
     // through a window, a block's rows see no more than this
     const long long keys = mode == kAllKeys ? a.Lk : std::min<long long>(a.Lk, (long long)a.win.window + a.win.sinks + R);
-    // parts of 256 keys or more, up to four blocks a multiprocessor (three of one row or two of more are resident at a time)
-    a.splits = xattn_parts((a.rows + R - 1) / R * a.Hkv * a.B, keys / 256, 4 * sms, 1);
+    // parts of 256 keys or more, up to four blocks a multiprocessor (three of one row or two of more are resident at a time); over
+    // pages two, so that parts that have to be joined come only where blocks are few
+    a.splits = xattn_parts((a.rows + R - 1) / R * a.Hkv * a.B, keys / 256, (mode == kPagedKeys ? 2 : 4) * sms, 1);
     a.rsplits = 1;
 }
 

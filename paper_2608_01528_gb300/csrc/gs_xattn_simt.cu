@@ -38,16 +38,23 @@ __global__ void __launch_bounds__(256) k_xattn_join(const XattnArgs a) {
     if (lane == 0 && a.lse) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-// out (B x L x H x w) = mul * the sum, in order, of `parts` arrays (B, H, L, w)
+// out (B x L x H x w, of longer sequences perhaps) = mul * the sum, in order, of `parts` arrays (B, H, L, w): one, or dK and dV at once
+struct Sum {
+    const float* src;
+    long long n;
+    HeadView out;
+    int w;
+    float mul;
+};
 template <typename T>
-__global__ void __launch_bounds__(256) k_xattn_sum(const float* src, int parts, long long n, HeadView out, int H, int L,
-                                                   int w, float mul) {
-    for (long long e = (long long)blockIdx.x * 256 + threadIdx.x; e < n; e += (long long)gridDim.x * 256) {
+__global__ void __launch_bounds__(256) k_xattn_sum(const Sum first, const Sum second, int parts, int H, int L) {
+    const Sum& x = blockIdx.y ? second : first;
+    for (long long e = (long long)blockIdx.x * 256 + threadIdx.x; e < x.n; e += (long long)gridDim.x * 256) {
         float v = 0.f;
-        for (int s = 0; s < parts; ++s) v += src[(long long)s * n + e];
-        const int c = (int)(e % w);
-        const long long at = e / w, l = at % L, bh = at / L;
-        (reinterpret_cast<T*>(out.p) + (bh / H) * out.b + l * out.l + (bh % H) * out.h)[c] = from_f32<T>(v * mul);
+        for (int s = 0; s < parts; ++s) v += x.src[(long long)s * x.n + e];
+        const int c = (int)(e % x.w);
+        const long long at = e / x.w, l = at % L, bh = at / L;
+        (reinterpret_cast<T*>(x.out.p) + (bh / H) * x.out.b + l * x.out.l + (bh % H) * x.out.h)[c] = from_f32<T>(v * x.mul);
     }
 }
 
@@ -65,8 +72,16 @@ void xattn_simt_plan(XattnArgs& a, bool backward, int sms, KeyMode mode) {
         if (a.win.sinks == 0) rows = std::min(rt, (w + kTile) * a.G / R + 2);
     }
     // up to four blocks a multiprocessor, and parts of two tiles or more
-    a.splits = xattn_parts(rt * a.Hkv * a.B, keys, 4 * sms, 2);
-    a.rsplits = backward ? xattn_parts(kt * a.Hkv * a.B, rows, 4 * sms, 2) : 1;
+    long long base = rt, kbase = kt;
+    if (mode == kWindowKeys && backward) base = kbase = rt + kt;  // (one launch; 160 blocks of keys and 288 of rows leave nothing to sum)
+    a.splits = xattn_parts(base * a.Hkv * a.B, keys, 4 * sms, 2);
+    a.rsplits = backward ? xattn_parts(kbase * a.Hkv * a.B, rows, 4 * sms, 2) : 1;
+    a.pkeys = a.Lk;
+    if (backward && mode == kWindowKeys && a.win.sinks > 0 && a.rsplits == 1) {
+        const long long some = std::min(rt, ((long long)a.win.window + kTile) * a.G / R + 1);
+        a.rsplits = xattn_sink_parts(kt * a.Hkv * a.B, rt, some, rt * keys * a.Hkv * a.B, 2 * sms);
+        if (a.rsplits > 1) a.pkeys = (int)std::min<long long>(a.Lk, (a.win.sinks + kTile - 1ll) / kTile * kTile);
+    }
     a.stats = xattn_round4(xattn_rows(a));  // D_i
 }
 
@@ -90,26 +105,22 @@ cudaError_t launch_xattn_join(const XattnArgs& a, cudaStream_t s) {
 }
 
 cudaError_t launch_xattn_join_dq(const XattnArgs& a, cudaStream_t s) {
-    const long long n = (long long)a.B * a.Hq * a.Lq * a.dk;
-    const float* src = a.ws + xattn_ws_dq(a);
+    const Sum q{a.ws + xattn_ws_dq(a), (long long)a.B * a.Hq * a.Lq * a.dk, a.dQ, a.dk, a.scale};
     if (a.dtype == GS_F32)
-        k_xattn_sum<float><<<sum_grid(n), 256, 0, s>>>(src, a.splits, n, a.dQ, a.Hq, a.Lq, a.dk, a.scale);
+        k_xattn_sum<float><<<sum_grid(q.n), 256, 0, s>>>(q, q, a.splits, a.Hq, a.Lq);
     else
-        k_xattn_sum<__nv_bfloat16><<<sum_grid(n), 256, 0, s>>>(src, a.splits, n, a.dQ, a.Hq, a.Lq, a.dk, a.scale);
+        k_xattn_sum<__nv_bfloat16><<<sum_grid(q.n), 256, 0, s>>>(q, q, a.splits, a.Hq, a.Lq);
     return cudaGetLastError();
 }
 
 cudaError_t launch_xattn_join_dkv(const XattnArgs& a, cudaStream_t s) {
-    const long long rows = (long long)a.B * a.Hkv * a.Lk;
-    const float *src = a.ws + xattn_ws_dk(a), *srcv = a.ws + xattn_ws_dv(a);
-    const long long nk = rows * a.dk, nv = rows * a.dv;
-    if (a.dtype == GS_F32) {
-        k_xattn_sum<float><<<sum_grid(nk), 256, 0, s>>>(src, a.rsplits, nk, a.dK, a.Hkv, a.Lk, a.dk, a.scale);
-        k_xattn_sum<float><<<sum_grid(nv), 256, 0, s>>>(srcv, a.rsplits, nv, a.dV, a.Hkv, a.Lk, a.dv, 1.f);
-    } else {
-        k_xattn_sum<__nv_bfloat16><<<sum_grid(nk), 256, 0, s>>>(src, a.rsplits, nk, a.dK, a.Hkv, a.Lk, a.dk, a.scale);
-        k_xattn_sum<__nv_bfloat16><<<sum_grid(nv), 256, 0, s>>>(srcv, a.rsplits, nv, a.dV, a.Hkv, a.Lk, a.dv, 1.f);
-    }
+    const long long rows = xattn_keys(a);
+    const Sum k{a.ws + xattn_ws_dk(a), rows * a.dk, a.dK, a.dk, a.scale}, v{a.ws + xattn_ws_dv(a), rows * a.dv, a.dV, a.dv, 1.f};
+    const dim3 grid(sum_grid(std::max(k.n, v.n)), 2);
+    if (a.dtype == GS_F32)
+        k_xattn_sum<float><<<grid, 256, 0, s>>>(k, v, a.rsplits, a.Hkv, a.pkeys);
+    else
+        k_xattn_sum<__nv_bfloat16><<<grid, 256, 0, s>>>(k, v, a.rsplits, a.Hkv, a.pkeys);
     return cudaGetLastError();
 }
 

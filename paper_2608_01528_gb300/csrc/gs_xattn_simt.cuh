@@ -33,7 +33,7 @@ constexpr int kPP = kTile + 4; // pitch of a tile of weights
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // bits of XattnArgs::vec: the array's rows start on boundaries of four elements
-constexpr int kVecQ = 1, kVecK = 2, kVecV = 4, kVecDO = 8;
+constexpr int kVecQ = 1, kVecK = 2, kVecV = 4, kVecDO = 8, kVecO = 16;
 
 template <typename T>
 __device__ __forceinline__ float to_f32(T v);
@@ -101,20 +101,29 @@ __device__ __forceinline__ void load_rows(float* dst, const XattnArgs& a, const 
     for (int c = 0; c < D; c += 16)
         *reinterpret_cast<float4*>(dst + i * (D + 4) + c + c0) = load4(p + c + c0, has ? w - c - c0 : 0, vec);
 }
-// 64 keys from j0 (zero where ok[] says that a key is not read).
+// 64 keys from j0 (zero where ok[] says that a key is not read); true where one of this thread's entries is not finite.
 template <typename T, int D>
-__device__ __forceinline__ void load_keys(float* dst, const HeadView& v, int b, int hk, int j0, int w, const int* ok, bool vec) {
+__device__ __forceinline__ bool load_keys(float* dst, const HeadView& v, int b, int hk, int j0, int w, const int* ok, bool vec) {
     const int i = threadIdx.x >> 2, c0 = (threadIdx.x & 3) * 4;
     const bool has = ok[i] != 0;
     const T* p = reinterpret_cast<const T*>(v.p) + b * v.b + hk * v.h + (has ? (long long)(j0 + i) * v.l : 0);
+    float odd = 0.f;  // NaN as soon as an entry is an infinity or a NaN
 #pragma unroll
-    for (int c = 0; c < D; c += 16)
-        *reinterpret_cast<float4*>(dst + i * (D + 4) + c + c0) = load4(p + c + c0, has ? w - c - c0 : 0, vec);
+    for (int c = 0; c < D; c += 16) {
+        const float4 x = load4(p + c + c0, has ? w - c - c0 : 0, vec);
+        odd = fmaf(x.x, 0.f, fmaf(x.y, 0.f, fmaf(x.z, 0.f, fmaf(x.w, 0.f, odd))));
+        *reinterpret_cast<float4*>(dst + i * (D + 4) + c + c0) = x;
+    }
+    return odd != 0.f;
 }
-__device__ __forceinline__ void load_valid(int* ok, const XattnArgs& a, int b, int j0, int n) {
+// (WIN: of those that `seen`, the keys of the tile's rows, has)
+template <bool WIN>
+__device__ __forceinline__ void load_valid(int* ok, const XattnArgs& a, int b, int j0, int n, const KeySpan& seen) {
     if (threadIdx.x < kTile) {
         const int j = j0 + threadIdx.x;
-        ok[threadIdx.x] = j < n && (!a.mask || a.mask[b * a.ldm + j] != 0);
+        bool in = j < n && (!a.mask || a.mask[b * a.ldm + j] != 0);
+        if constexpr (WIN) in = in && j < seen.hi && (j >= seen.lo || j < seen.sink);
+        ok[threadIdx.x] = in;
     }
 }
 
@@ -147,8 +156,8 @@ __device__ __forceinline__ int column(int q) {
     return D == 32 ? 2 * tx + q : 64 * (q / 4) + 4 * tx + q % 4;
 }
 // out[i][q] += sum_k W[ty + 16 i][k] X[k][column(q)] over a tile of K
-// (WIN: rows of a tile see different keys, and one that a row does not see stays out of its sum whatever it holds)
-template <int D, int K = kTile, bool WIN = false, int RI>
+// (OWN: a zero weight keeps out whatever X holds there, for tiles whose rows see different keys that are not all finite)
+template <int D, int K = kTile, bool OWN = false, int RI>
 __device__ __forceinline__ void weigh(float (&out)[RI][D / 16], const float* W, const float* X) {
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
 #pragma unroll 2
@@ -163,7 +172,7 @@ __device__ __forceinline__ void weigh(float (&out)[RI][D / 16], const float* W, 
 #pragma unroll
                 for (int i = 0; i < RI; ++i) {
                     const float p = q == 0 ? w[i].x : q == 1 ? w[i].y : q == 2 ? w[i].z : w[i].w;
-                    if (WIN && p == 0.f) continue;
+                    if (OWN && p == 0.f) continue;
                     out[i][0] = fmaf(p, x.x, out[i][0]);
                     out[i][1] = fmaf(p, x.y, out[i][1]);
                 }
@@ -177,7 +186,7 @@ __device__ __forceinline__ void weigh(float (&out)[RI][D / 16], const float* W, 
 #pragma unroll
                 for (int i = 0; i < RI; ++i) {
                     const float p = q == 0 ? w[i].x : q == 1 ? w[i].y : q == 2 ? w[i].z : w[i].w;
-                    if (WIN && p == 0.f) continue;
+                    if (OWN && p == 0.f) continue;
                     out[i][4 * c + 0] = fmaf(p, x.x, out[i][4 * c + 0]);
                     out[i][4 * c + 1] = fmaf(p, x.y, out[i][4 * c + 1]);
                     out[i][4 * c + 2] = fmaf(p, x.z, out[i][4 * c + 2]);
@@ -202,8 +211,7 @@ struct Block {  // which tile, part, key head and sequence a block has
     long long tile;
     int part, hk, b;
 };
-__device__ __forceinline__ Block block_of(long long tiles, int parts, int Hkv) {
-    long long i = blockIdx.x;
+__device__ __forceinline__ Block block_of(long long i, long long tiles, int parts, int Hkv) {
     Block k;
     k.tile = i % tiles;
     i /= tiles;
@@ -217,6 +225,7 @@ __device__ __forceinline__ Block block_of(long long tiles, int parts, int Hkv) {
 // Which keys a tile of packed rows [r0, r0 + R) reads: tiles [0, sinks) and [from, to) of 64, in this order.
 struct KeyTiles {
     int sinks, from, count;
+    KeySpan seen;  // by some row
     __device__ __forceinline__ int tile(int i) const { return i < sinks ? i : i - sinks + from; }
 };
 template <bool WIN, int R>
@@ -226,7 +235,7 @@ __device__ __forceinline__ KeyTiles key_tiles(const XattnArgs& a, int b, long lo
         t.sinks = t.from = 0;
         t.count = (a.Lk + kTile - 1) / kTile;
     } else {
-        const KeySpan s = key_span<kWindowKeys>(a, b, r0 / a.G, (min(a.rows, r0 + R) - 1) / a.G, n);
+        const KeySpan s = t.seen = key_span<kWindowKeys>(a, b, r0 / a.G, (min(a.rows, r0 + R) - 1) / a.G, n);
         const int to = (s.hi + kTile - 1) / kTile;
         t.from = s.lo / kTile;
         t.sinks = min((s.sink + kTile - 1) / kTile, t.from);
@@ -234,38 +243,44 @@ __device__ __forceinline__ KeyTiles key_tiles(const XattnArgs& a, int b, long lo
     }
     return t;
 }
-// The keys that the rows ty + 16 i of a tile see.
+// The keys that the rows ty + 16 i of a tile see: those of [lo, hi), and the sinks.
+struct RowKeys {
+    int lo, hi;
+};
 template <bool WIN, int RI>
-__device__ __forceinline__ void row_spans(KeySpan (&span)[RI], const XattnArgs& a, int b, long long r0, int n) {
+__device__ __forceinline__ void row_spans(RowKeys (&span)[RI], const XattnArgs& a, int b, long long r0, int n) {
     if constexpr (WIN) {
 #pragma unroll
         for (int i = 0; i < RI; ++i) {
             const long long l = min(a.rows - 1, r0 + (threadIdx.x >> 4) + 16 * i) / a.G;
-            span[i] = key_span<kWindowKeys>(a, b, l, l, n);
+            const KeySpan s = key_span<kWindowKeys>(a, b, l, l, n);
+            span[i] = {s.lo, s.hi};
         }
     }
 }
 template <bool WIN>
-__device__ __forceinline__ bool sees(const KeySpan& s, int j) {
-    return !WIN || (j < s.hi && (j >= s.lo || j < s.sink));
+__device__ __forceinline__ bool sees(const RowKeys& s, int j, int sinks) {
+    return !WIN || (j < s.hi && (j >= s.lo || j < sinks));
 }
 
+// (WIN: the spans take the registers of a second block of a multiprocessor unless told; 16 x 200 rows, 4 / 2 heads of 40 and 30:
+// 41 us with one)
 template <typename T, int DK, int DV, bool WIN>
-__global__ void __launch_bounds__(kThreads) k_xattn(const XattnArgs a, long long tiles) {
+__global__ void __launch_bounds__(kThreads, WIN ? 2 : 1) k_xattn(const XattnArgs a, long long tiles) {
     extern __shared__ float4 sm4[];
     float* Qs = reinterpret_cast<float*>(sm4);
     float* Ks = Qs + kTile * (DK + 4);  // then the weights
     constexpr int kKs = (DK + 4 > kPP ? DK + 4 : kPP) * kTile;
     float* Vs = Ks + kKs;
     __shared__ int ok[kTile];
-    const Block bl = block_of(tiles, a.splits, a.Hkv);
+    const Block bl = block_of(blockIdx.x, tiles, a.splits, a.Hkv);
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
     const long long r0 = bl.tile * kTile;
     const int n = keys_of(a, bl.b);
     const KeyTiles kt = key_tiles<WIN, kTile>(a, bl.b, r0, n);
     const int t0 = (int)((long long)kt.count * bl.part / a.splits), t1 = (int)((long long)kt.count * (bl.part + 1) / a.splits);
     const float c = a.scale * kLog2e;
-    [[maybe_unused]] KeySpan span[4];
+    [[maybe_unused]] RowKeys span[4];
     row_spans<WIN>(span, a, bl.b, r0, n);
     load_rows<T, DK>(Qs, a, a.q, bl.b, bl.hk, r0, a.dk, a.vec & kVecQ);
     float m[4], l[4], o[4][DV / 16];
@@ -280,11 +295,15 @@ __global__ void __launch_bounds__(kThreads) k_xattn(const XattnArgs a, long long
         const int t = kt.tile(i);
         if (t * kTile >= n) break;
         __syncthreads();  // the last tile's weights and values have been read
-        load_valid(ok, a, bl.b, t * kTile, n);
+        load_valid<WIN>(ok, a, bl.b, t * kTile, n, kt.seen);
         __syncthreads();
         load_keys<T, DK>(Ks, a.k, bl.b, bl.hk, t * kTile, a.dk, ok, a.vec & kVecK);
-        load_keys<T, DV>(Vs, a.v, bl.b, bl.hk, t * kTile, a.dv, ok, a.vec & kVecV);
-        __syncthreads();
+        const bool odd = load_keys<T, DV>(Vs, a.v, bl.b, bl.hk, t * kTile, a.dv, ok, a.vec & kVecV);
+        bool own = false;  // through a window 0 * NaN of a value that only other rows of the tile see is kept out
+        if constexpr (WIN)
+            own = __syncthreads_or(odd);
+        else
+            __syncthreads();
         float s[4][4] = {};
         dots<DK>(s, Qs, Ks, a.dk);
         __syncthreads();  // K has been read: the weights go over it
@@ -293,7 +312,7 @@ __global__ void __launch_bounds__(kThreads) k_xattn(const XattnArgs a, long long
             float mx = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                s[i][j] = ok[tx + 16 * j] && sees<WIN>(span[i], t * kTile + tx + 16 * j) ? s[i][j] * c : -INFINITY;
+                s[i][j] = ok[tx + 16 * j] && sees<WIN>(span[i], t * kTile + tx + 16 * j, a.win.sinks) ? s[i][j] * c : -INFINITY;
                 mx = fmaxf(mx, s[i][j]);
             }
             const float mn = fmaxf(m[i], row_max(mx));
@@ -312,7 +331,10 @@ __global__ void __launch_bounds__(kThreads) k_xattn(const XattnArgs a, long long
             for (int q = 0; q < DV / 16; ++q) o[i][q] *= f;
         }
         __syncthreads();
-        weigh<DV, kTile, WIN>(o, Ks, Vs);
+        if (WIN && own)
+            weigh<DV, kTile, true>(o, Ks, Vs);
+        else
+            weigh<DV>(o, Ks, Vs);
     }
     const long long nrows = (long long)a.B * a.Hq * a.Lq;
 #pragma unroll
@@ -395,21 +417,21 @@ __global__ void __launch_bounds__(256) k_xattn_delta(const XattnArgs a) {
 // (WIN: key j0 + tx + 16 j is seen by the row as its span says)
 template <bool WIN, int RI>
 __device__ __forceinline__ void tile_grad(float (&s)[RI][4], float (&dp)[RI][4], const int* ok, const float* lse2,
-                                          const float* delta, float c, const KeySpan (&span)[RI], int j0) {
+                                          const float* delta, float c, const RowKeys (&span)[RI], int j0, int sinks) {
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
 #pragma unroll
     for (int i = 0; i < RI; ++i) {
         const float L = lse2[ty + 16 * i], D = delta[ty + 16 * i];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const bool use = ok[tx + 16 * j] && L != INFINITY && sees<WIN>(span[i], j0 + tx + 16 * j);
+            const bool use = ok[tx + 16 * j] && L != INFINITY && sees<WIN>(span[i], j0 + tx + 16 * j, sinks);
             s[i][j] = use ? exp2f(s[i][j] * c - L) : 0.f;
             dp[i][j] = use ? s[i][j] * (dp[i][j] - D) : 0.f;
         }
     }
 }
-// lse (base 2; +inf: the row has no weight) and D of R packed rows
-template <int R>
+// lse (base 2; +inf: the row has no weight) and D (OWN: not here) of R packed rows
+template <int R, bool OWN>
 __device__ __forceinline__ void load_stats(float* lse2, float* delta, const XattnArgs& a, int b, int hk, long long r0) {
     if (threadIdx.x < R) {
         const long long r = r0 + threadIdx.x;
@@ -420,12 +442,31 @@ __device__ __forceinline__ void load_stats(float* lse2, float* delta, const Xatt
             if (v != -INFINITY) {
                 // (a +inf here is a row whose forward result is NaN: P = NaN, as there)
                 L = v == INFINITY ? NAN : v * kLog2e;
-                D = a.ws[at];
+                if constexpr (!OWN) D = a.ws[at];
             }
         }
         lse2[threadIdx.x] = L;
-        delta[threadIdx.x] = D;
+        if constexpr (!OWN) delta[threadIdx.x] = D;
     }
+}
+
+// In fp32 a window's kernels take D = <dO, O> of their R rows themselves, which spares a launch: rows of dO go to dst as by load_rows,
+// four threads a row, and D to delta.
+template <typename T, int D, int R>
+__device__ __forceinline__ void load_rows_delta(float* dst, float* delta, const XattnArgs& a, int b, int hk, long long r0) {
+    const int i = threadIdx.x >> 2, c0 = (threadIdx.x & 3) * 4;
+    const bool has = i < R && r0 + i < a.rows;
+    const T *p = row_at<T>(a, a.dO, b, hk, has ? r0 + i : 0), *o = row_at<T>(a, a.o, b, hk, has ? r0 + i : 0);
+    float sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < D; c += 16) {
+        const float4 x = load4(p + c + c0, has ? a.dv - c - c0 : 0, a.vec & kVecDO), y = load4(o + c + c0, has ? a.dv - c - c0 : 0, a.vec & kVecO);
+        if (i < R) *reinterpret_cast<float4*>(dst + i * (D + 4) + c + c0) = x;
+        sum = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, sum))));
+    }
+    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+    if (i < R && (threadIdx.x & 3) == 0) delta[i] = sum;
 }
 
 // Tiles of R rows: 64, or 16 where a key head has few (a tile's products are taken whole).  fp32, 17 x 832 keys, 16 / 64: 14 rows,
@@ -438,8 +479,9 @@ constexpr size_t bwd_smem() {  // weights: R x 64, or 64 keys x R
 }
 
 template <typename T, int DK, int DV, int R, bool WIN>
-__global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long long tiles) {
+__device__ __forceinline__ void dq_block(const XattnArgs& a, long long block, long long tiles) {
     extern __shared__ float4 sm4[];
+    constexpr bool kOwn = WIN && sizeof(T) == 4;
     float* Qs = reinterpret_cast<float*>(sm4);
     float* Ks = Qs + R * (DK + 4);
     float* Vs = Ks + kTile * (DK + 4);
@@ -448,23 +490,26 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long l
     __shared__ int ok[kTile];
     __shared__ float lse2[R], delta[R];
     constexpr int RI = R / 16;
-    const Block bl = block_of(tiles, a.splits, a.Hkv);
+    const Block bl = block_of(block, tiles, a.splits, a.Hkv);
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
     const long long r0 = bl.tile * R;
     const int n = keys_of(a, bl.b);
     const KeyTiles kt = key_tiles<WIN, R>(a, bl.b, r0, n);
     const int t0 = (int)((long long)kt.count * bl.part / a.splits), t1 = (int)((long long)kt.count * (bl.part + 1) / a.splits);
-    KeySpan span[RI];
+    RowKeys span[RI];
     row_spans<WIN>(span, a, bl.b, r0, n);
     load_rows<T, DK, R>(Qs, a, a.q, bl.b, bl.hk, r0, a.dk, a.vec & kVecQ);
-    load_rows<T, DV, R>(Ds, a, a.dO, bl.b, bl.hk, r0, a.dv, a.vec & kVecDO);
-    if (t0 < t1 && kt.tile(t0) * kTile < n) load_stats<R>(lse2, delta, a, bl.b, bl.hk, r0);  // (the part that has the keys may write D)
+    if constexpr (kOwn)
+        load_rows_delta<T, DV, R>(Ds, delta, a, bl.b, bl.hk, r0);
+    else
+        load_rows<T, DV, R>(Ds, a, a.dO, bl.b, bl.hk, r0, a.dv, a.vec & kVecDO);
+    if (t0 < t1 && kt.tile(t0) * kTile < n) load_stats<R, kOwn>(lse2, delta, a, bl.b, bl.hk, r0);  // (the part that has the keys may write D)
     float o[RI][DK / 16] = {};
     for (int i = t0; i < t1; ++i) {
         const int t = kt.tile(i);
         if (t * kTile >= n) break;
         __syncthreads();
-        load_valid(ok, a, bl.b, t * kTile, n);
+        load_valid<WIN>(ok, a, bl.b, t * kTile, n, kt.seen);
         __syncthreads();
         load_keys<T, DK>(Ks, a.k, bl.b, bl.hk, t * kTile, a.dk, ok, a.vec & kVecK);
         load_keys<T, DV>(Vs, a.v, bl.b, bl.hk, t * kTile, a.dv, ok, a.vec & kVecV);
@@ -492,13 +537,13 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long l
             }
             __syncthreads();
         }
-        tile_grad<WIN>(s, dp, ok, lse2, delta, a.scale * kLog2e, span, t * kTile);
+        tile_grad<WIN>(s, dp, ok, lse2, delta, a.scale * kLog2e, span, t * kTile, a.win.sinks);
 #pragma unroll
         for (int i = 0; i < RI; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) Ws[(ty + 16 * i) * kPP + tx + 16 * j] = dp[i][j];
         __syncthreads();
-        weigh<DK, kTile, WIN>(o, Ws, Ks);
+        weigh<DK>(o, Ws, Ks);
     }
     const long long nrows = (long long)a.B * a.Hq * a.Lq;
 #pragma unroll
@@ -518,8 +563,9 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long l
 }
 
 template <typename T, int DK, int DV, int R, bool WIN>
-__global__ void __launch_bounds__(kThreads) k_xattn_dkv(const XattnArgs a, int ktiles) {
+__device__ __forceinline__ void dkv_block(const XattnArgs& a, long long block, int ktiles) {
     extern __shared__ float4 sm4[];
+    constexpr bool kOwn = WIN && sizeof(T) == 4;
     float* Qs = reinterpret_cast<float*>(sm4);
     float* Ks = Qs + R * (DK + 4);
     float* Vs = Ks + kTile * (DK + 4);
@@ -528,20 +574,35 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dkv(const XattnArgs a, int k
     __shared__ int ok[kTile];
     __shared__ float lse2[R], delta[R];
     constexpr int RI = R / 16, kPR = R + 4;
-    const Block bl = block_of(ktiles, a.rsplits, a.Hkv);
+    Block bl;
+    int parts = a.rsplits;
+    if constexpr (WIN) {  // key tiles slowest: the first ones, which sinks show to all rows, begin first
+        const int per = a.Hkv * a.B;
+        bl = block_of(block % per, 1, 1, a.Hkv);
+        const long long at = block / per, in_parts = (a.pkeys + kTile - 1) / kTile;
+        if (at < in_parts * parts) {
+            bl.tile = at / parts;
+            bl.part = (int)(at % parts);
+        } else {
+            bl.tile = at - in_parts * (parts - 1);
+            parts = 1;
+        }
+    } else {
+        bl = block_of(block, ktiles, a.rsplits, a.Hkv);
+    }
     const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
     const int j0 = (int)bl.tile * kTile;
     const int n = keys_of(a, bl.b);
     const long long rtiles = (a.rows + R - 1) / R;
-    long long t0 = rtiles * bl.part / a.rsplits, t1 = rtiles * (bl.part + 1) / a.rsplits;
+    long long t0 = rtiles * bl.part / parts, t1 = rtiles * (bl.part + 1) / parts;
     if constexpr (WIN) {
         const RowSpan rs = row_span(a, bl.b, j0, min(n, j0 + kTile));
         const long long first = rs.first * a.G / R, some = max(0ll, (rs.end * a.G + R - 1) / R - first);
-        t0 = first + some * bl.part / a.rsplits;
-        t1 = first + some * (bl.part + 1) / a.rsplits;
+        t0 = first + some * bl.part / parts;
+        t1 = first + some * (bl.part + 1) / parts;
     }
     if (j0 >= n) t1 = t0;  // no key of the tile is read
-    load_valid(ok, a, bl.b, j0, n);
+    load_valid<false>(ok, a, bl.b, j0, n, KeySpan());
     __syncthreads();
     load_keys<T, DK>(Ks, a.k, bl.b, bl.hk, j0, a.dk, ok, a.vec & kVecK);
     load_keys<T, DV>(Vs, a.v, bl.b, bl.hk, j0, a.dv, ok, a.vec & kVecV);
@@ -549,40 +610,43 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dkv(const XattnArgs a, int k
     for (long long t = t0; t < t1; ++t) {
         __syncthreads();
         load_rows<T, DK, R>(Qs, a, a.q, bl.b, bl.hk, t * R, a.dk, a.vec & kVecQ);
-        load_rows<T, DV, R>(Ds, a, a.dO, bl.b, bl.hk, t * R, a.dv, a.vec & kVecDO);
-        load_stats<R>(lse2, delta, a, bl.b, bl.hk, t * R);
+        if constexpr (kOwn)
+            load_rows_delta<T, DV, R>(Ds, delta, a, bl.b, bl.hk, t * R);
+        else
+            load_rows<T, DV, R>(Ds, a, a.dO, bl.b, bl.hk, t * R, a.dv, a.vec & kVecDO);
+        load_stats<R, kOwn>(lse2, delta, a, bl.b, bl.hk, t * R);
         __syncthreads();
         float s[RI][4] = {}, dp[RI][4] = {};
         dots<DK>(s, Qs, Ks, a.dk);
         dots<DV>(dp, Ds, Vs, a.dv);
-        KeySpan span[RI];
+        RowKeys span[RI];
         row_spans<WIN>(span, a, bl.b, t * R, n);
-        tile_grad<WIN>(s, dp, ok, lse2, delta, a.scale * kLog2e, span, j0);
+        tile_grad<WIN>(s, dp, ok, lse2, delta, a.scale * kLog2e, span, j0, a.win.sinks);
 #pragma unroll
         for (int i = 0; i < RI; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) Ws[(tx + 16 * j) * kPR + ty + 16 * i] = s[i][j];
         __syncthreads();
-        weigh<DV, R, WIN>(ov, Ws, Ds);
+        weigh<DV, R>(ov, Ws, Ds);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < RI; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) Ws[(tx + 16 * j) * kPR + ty + 16 * i] = dp[i][j];
         __syncthreads();
-        weigh<DK, R, WIN>(ok_, Ws, Qs);
+        weigh<DK, R>(ok_, Ws, Qs);
     }
-    const long long nk = (long long)a.B * a.Hkv * a.Lk;
+    const long long nk = xattn_keys(a);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int j = j0 + ty + 16 * i;
         if (j >= a.Lk) continue;
-        const long long at = ((long long)bl.b * a.Hkv + bl.hk) * a.Lk + j;
+        const long long at = ((long long)bl.b * a.Hkv + bl.hk) * a.pkeys + j;
 #pragma unroll
         for (int q = 0; q < DK / 16; ++q) {
             const int col = column<DK>(q);
             if (col >= a.dk) continue;
-            if (a.rsplits > 1)
+            if (parts > 1)
                 a.ws[xattn_ws_dk(a) + ((long long)bl.part * nk + at) * a.dk + col] = ok_[i][q];
             else
                 (reinterpret_cast<T*>(a.dK.p) + bl.b * a.dK.b + j * a.dK.l + bl.hk * a.dK.h)[col] =
@@ -592,7 +656,7 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dkv(const XattnArgs a, int k
         for (int q = 0; q < DV / 16; ++q) {
             const int col = column<DV>(q);
             if (col >= a.dv) continue;
-            if (a.rsplits > 1)
+            if (parts > 1)
                 a.ws[xattn_ws_dv(a) + ((long long)bl.part * nk + at) * a.dv + col] = ov[i][q];
             else
                 (reinterpret_cast<T*>(a.dV.p) + bl.b * a.dV.b + j * a.dV.l + bl.hk * a.dV.h)[col] = from_f32<T>(ov[i][q]);
@@ -600,9 +664,27 @@ __global__ void __launch_bounds__(kThreads) k_xattn_dkv(const XattnArgs a, int k
     }
 }
 
+template <typename T, int DK, int DV, int R, bool WIN>
+__global__ void __launch_bounds__(kThreads) k_xattn_dq(const XattnArgs a, long long tiles) {
+    dq_block<T, DK, DV, R, WIN>(a, blockIdx.x, tiles);
+}
+template <typename T, int DK, int DV, int R, bool WIN>
+__global__ void __launch_bounds__(kThreads) k_xattn_dkv(const XattnArgs a, int ktiles) {
+    dkv_block<T, DK, DV, R, WIN>(a, blockIdx.x, ktiles);
+}
+// Through a window both in one launch, as a row or key tile alone meets few of the other kind: first `keys` blocks of keys, then
+// those of rows.
+template <typename T, int DK, int DV, int R>
+__global__ void __launch_bounds__(kThreads, 2) k_xattn_bwd(const XattnArgs a, long long keys, int ktiles, long long tiles) {
+    if (blockIdx.x < keys)
+        dkv_block<T, DK, DV, R, true>(a, blockIdx.x, ktiles);
+    else
+        dq_block<T, DK, DV, R, true>(a, blockIdx.x - keys, tiles);
+}
+
 template <typename F>
 cudaError_t allow_smem(F* f, size_t bytes) {
-    return bytes <= 48 * 1024 ? cudaSuccess
+    return bytes <= 47 * 1024 ? cudaSuccess  // (48 KB with the static arrays)
                               : cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
@@ -621,23 +703,38 @@ template <typename T, int DK, int DV, int R, bool WIN>
 cudaError_t backward_r(const XattnArgs& a, cudaStream_t s) {
     const size_t smem = bwd_smem<DK, DV, R>();
     cudaError_t e = cudaSuccess;
-    if (a.rows > 0) {
-        const long long tiles = (a.rows + R - 1) / R;
-        const auto kernel = k_xattn_dq<T, DK, DV, R, WIN>;
+    if constexpr (WIN) {
+        const long long tiles = (a.rows + R - 1) / R, per = (long long)a.Hkv * a.B;
+        const int ktiles = (a.Lk + kTile - 1) / kTile;
+        const long long in_parts = (a.pkeys + kTile - 1) / kTile;
+        const long long keys = (ktiles + in_parts * (a.rsplits - 1)) * per, grid = keys + tiles * a.splits * per;
+        if (grid == 0) return e;
+        if (grid > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+        const auto kernel = k_xattn_bwd<T, DK, DV, R>;
         if ((e = allow_smem(kernel, smem)) != cudaSuccess) return e;
-        kernel<<<(unsigned)(tiles * a.splits * a.Hkv * a.B), kThreads, smem, s>>>(a, tiles);
+        kernel<<<(unsigned)grid, kThreads, smem, s>>>(a, keys, ktiles, tiles);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
         if (a.splits > 1 && (e = launch_xattn_join_dq(a, s)) != cudaSuccess) return e;
+        return a.rsplits > 1 ? launch_xattn_join_dkv(a, s) : cudaSuccess;
+    } else {
+        if (a.rows > 0) {
+            const long long tiles = (a.rows + R - 1) / R;
+            const auto kernel = k_xattn_dq<T, DK, DV, R, WIN>;
+            if ((e = allow_smem(kernel, smem)) != cudaSuccess) return e;
+            kernel<<<(unsigned)(tiles * a.splits * a.Hkv * a.B), kThreads, smem, s>>>(a, tiles);
+            if ((e = cudaGetLastError()) != cudaSuccess) return e;
+            if (a.splits > 1 && (e = launch_xattn_join_dq(a, s)) != cudaSuccess) return e;
+        }
+        if (a.Lk > 0) {
+            const int ktiles = (a.Lk + kTile - 1) / kTile;
+            const auto kernel = k_xattn_dkv<T, DK, DV, R, WIN>;
+            if ((e = allow_smem(kernel, smem)) != cudaSuccess) return e;
+            kernel<<<(unsigned)((long long)ktiles * a.rsplits * a.Hkv * a.B), kThreads, smem, s>>>(a, ktiles);
+            if ((e = cudaGetLastError()) != cudaSuccess) return e;
+            if (a.rsplits > 1) e = launch_xattn_join_dkv(a, s);
+        }
+        return e;
     }
-    if (a.Lk > 0) {
-        const int ktiles = (a.Lk + kTile - 1) / kTile;
-        const auto kernel = k_xattn_dkv<T, DK, DV, R, WIN>;
-        if ((e = allow_smem(kernel, smem)) != cudaSuccess) return e;
-        kernel<<<(unsigned)((long long)ktiles * a.rsplits * a.Hkv * a.B), kThreads, smem, s>>>(a, ktiles);
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
-        if (a.rsplits > 1) e = launch_xattn_join_dkv(a, s);
-    }
-    return e;
 }
 
 template <typename T, int DK, int DV, bool WIN>
@@ -661,7 +758,8 @@ cudaError_t forward_t(XattnArgs a, cudaStream_t s) {
 template <typename T, bool WIN>
 cudaError_t backward_t(XattnArgs a, cudaStream_t s) {
     a.vec = (on_fours(a, a.q, a.Lq, a.Hq) ? kVecQ : 0) | (on_fours(a, a.k, a.Lk, a.Hkv) ? kVecK : 0) |
-            (on_fours(a, a.v, a.Lk, a.Hkv) ? kVecV : 0) | (on_fours(a, a.dO, a.Lq, a.Hq) ? kVecDO : 0);
+            (on_fours(a, a.v, a.Lk, a.Hkv) ? kVecV : 0) | (on_fours(a, a.dO, a.Lq, a.Hq) ? kVecDO : 0) |
+            (on_fours(a, a.o, a.Lq, a.Hq) ? kVecO : 0);
     if (a.dk <= 32 && a.dv <= 32) return backward<T, 32, 32, WIN>(a, s);
     if (a.dk <= 64)
         return a.dv <= 32 ? backward<T, 64, 32, WIN>(a, s) : a.dv <= 64 ? backward<T, 64, 64, WIN>(a, s) : backward<T, 64, 128, WIN>(a, s);
@@ -682,7 +780,7 @@ cudaError_t forward_all(const XattnArgs& a, cudaStream_t s) {
 }
 template <bool WIN>
 cudaError_t backward_all(const XattnArgs& a, cudaStream_t s) {
-    const cudaError_t e = a.dtype == GS_F32 ? launch_delta<float, WIN>(a, s) : launch_delta<__nv_bfloat16, WIN>(a, s);
+    const cudaError_t e = a.dtype != GS_F32 ? launch_delta<__nv_bfloat16, WIN>(a, s) : WIN ? cudaSuccess : launch_delta<float, WIN>(a, s);
     if (e != cudaSuccess) return e;
     return a.dtype == GS_F32 ? backward_t<float, WIN>(a, s) : backward_t<__nv_bfloat16, WIN>(a, s);
 }

@@ -110,6 +110,20 @@ def test_pairs_of_row_tiles(gs, shape):
     assert torch.equal(a[0]["O"], b["O"]) and torch.equal(a[0]["lse"], b["lse"])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(4, 1200, 1200, 8, 8, 32, 24, 20, 5, 0), (2, 1100, 1300, 16, 8, 64, 64, 33, 130, 200),
+                                   (1, 2000, 70, 32, 32, 40, 40, 9, 300, 0)], ids=lambda s: "x".join(map(str, s)))
+def test_sinks_that_every_row_sees(gs, shape, dtype):
+    """The gradients of the first tiles of keys come in parts, those of the others do not; the same bits again."""
+    Q, K, V, dO = make(*shape[:7], dtype)
+    lens, _ = masks("lens", shape[0], shape[2])
+    for n in (None, lens):
+        out, got = check(gs, Q, K, V, dO, *shape[7:], n)
+        O = out["O"]
+        a, b = (gs.window_attention_backward(Q, K, V, O, out["lse"], dO, *shape[7:], key_lens=n) for _ in range(2))
+        assert all(torch.equal(a[k], b[k]) for k in a)
+
+
 @pytest.mark.parametrize("path", ["auto", "simt"])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_starts_of_their_own(gs, dtype, path):
