@@ -208,11 +208,11 @@ __device__ __forceinline__ void sum_few_seen(const XattnArgs& a, int b, int hk, 
 constexpr int kStatRows = 4, kStatBlocks = kTile / (16 * kStatRows);
 template <bool WIN>
 __global__ void __launch_bounds__(256) k_xattn_stats(const XattnArgs a, int nl, long long rtiles, int vec) {
-    long long i = blockIdx.x / kStatBlocks;
-    float* dst = a.ws + i * kStats;
-    const long long rt = i % rtiles;
-    i /= rtiles;
-    const int hk = (int)(i % a.Hkv), b = (int)(i / a.Hkv);
+    unsigned i = blockIdx.x / kStatBlocks;  // (in 32 bits, as all of these kernels' places: a grid has no more blocks)
+    float* dst = a.ws + (long long)i * kStats;
+    const long long rt = i % (unsigned)rtiles;
+    i /= (unsigned)rtiles;
+    const int b = (int)(i / (unsigned)a.Hkv), hk = (int)i - b * a.Hkv;
     const int grp = (blockIdx.x % kStatBlocks) * (16 * kStatRows) + (threadIdx.x >> 4), ln = threadIdx.x & 15, c0 = ln * 8;
     float L[kStatRows], acc[kStatRows];
     uint4 x[kStatRows], y[kStatRows];
@@ -310,43 +310,48 @@ __global__ void __launch_bounds__(kThreads, 1)
     const XattnArgs& a = p.a;
     const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31;
 
-    long long i = blockIdx.x;
+    unsigned i = blockIdx.x;
+    const unsigned rtiles = (unsigned)p.rtiles;
     int kt, part, hk, b, parts = a.rsplits;
     if constexpr (WIN) {  // key tiles slowest: the first ones, which the most rows see, begin first
-        hk = (int)(i % a.Hkv);
-        i /= a.Hkv;
-        b = (int)(i % a.B);
-        i /= a.B;
-        const int in_parts = (a.pkeys + kTile - 1) / kTile;
-        if (i < (long long)in_parts * parts) {
-            part = (int)(i % parts);
-            kt = (int)(i / parts);
-        } else {
-            part = 0;
-            kt = (int)(i - (long long)in_parts * (parts - 1));
-            parts = 1;
+        hk = (int)(i % (unsigned)a.Hkv);
+        i /= (unsigned)a.Hkv;
+        b = (int)(i % (unsigned)a.B);
+        i /= (unsigned)a.B;
+        part = 0;
+        kt = (int)i;
+        if (parts > 1) {
+            const int in_parts = (a.pkeys + kTile - 1) / kTile;
+            if ((int)i < in_parts * parts) {
+                kt = (int)i / parts;
+                part = (int)i - kt * parts;
+            } else {
+                kt = (int)i - in_parts * (parts - 1);
+                parts = 1;
+            }
         }
     } else {
-        kt = (int)(i % p.ktiles);
-        i /= p.ktiles;
-        part = (int)(i % a.rsplits);
-        i /= a.rsplits;
-        hk = (int)(i % a.Hkv);
-        b = (int)(i / a.Hkv);
+        kt = (int)(i % (unsigned)p.ktiles);
+        i /= (unsigned)p.ktiles;
+        part = (int)(i % (unsigned)parts);
+        i /= (unsigned)parts;
+        hk = (int)(i % (unsigned)a.Hkv);
+        b = (int)(i / (unsigned)a.Hkv);
     }
     const int tile_rows = p.nl * a.G;
     const int n = keys_of(a, b), j0 = kt * kTile;
-    long long t0, t1;
+    int t0 = 0, t1 = (int)rtiles;
     if constexpr (WIN) {  // the row tiles that see some key of the tile
         const RowSpan rows = row_span(a, b, j0, min(n, j0 + kTile));
-        const long long first = rows.first / p.nl, some = max(0ll, (rows.end + p.nl - 1) / p.nl - first);
-        t0 = first + some * part / parts;
-        t1 = first + some * (part + 1) / parts;
-    } else {
-        t0 = p.rtiles * part / parts;
-        t1 = p.rtiles * (part + 1) / parts;
+        t0 = (int)rows.first / p.nl;
+        t1 = max(t0, (int)((unsigned)rows.end + p.nl - 1) / p.nl);
     }
-    const int nt = uniform(j0 < n ? (int)(t1 - t0) : 0);  // row tiles
+    if (parts > 1) {
+        const long long first = t0, some = t1 - t0;
+        t0 = (int)(first + some * part / parts);
+        t1 = (int)(first + some * (part + 1) / parts);
+    }
+    const int nt = uniform(j0 < n ? t1 - t0 : 0);  // row tiles
 
     // the softmax warps' parts of K and V, on their way while the CTA is set up
     uint32_t kx[DKC][8], vx[DVC][8];
@@ -400,7 +405,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             RingPos rp;
             int sa = 0, sb = 0, ss = 0;
             for (int t = 0; t < nt; ++t, rp.next(ST)) {
-                const int s = rp.idx, l0 = (int)(t0 + t) * p.nl;
+                const int s = rp.idx, l0 = (t0 + t) * p.nl;
                 if (!mbar_wait_1t(&c.a_empty[s], rp.phase ^ 1u, abort_flag, err)) break;
                 mbar_arrive_expect_tx(&c.a_full[s], (uint32_t)(DKC * kChunk * 2 * tile_rows));
                 for (int k = 0; k < DKC; ++k)
@@ -483,11 +488,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool whole_keys = __all_sync(0xffffffffu, valid);
         const float cs = a.scale * kLog2e;
         // through a window: the rows of the first tile, from its start, that see key j are first_row..end_row - 1 (before G)
-        [[maybe_unused]] long long first_row = 0, end_row = 0;
+        [[maybe_unused]] int first_row = 0, end_row = 0;
         if constexpr (WIN) {
             const RowSpan rows = row_span(a, b, j, j + 1);
-            first_row = rows.first - t0 * p.nl;
-            end_row = rows.end - t0 * p.nl;
+            first_row = (int)rows.first - t0 * p.nl;
+            end_row = (int)rows.end - t0 * p.nl;
         }
         if (nt > 0) {
             keep_row(t_k + lane_base, kx, warp >> 2);
@@ -504,8 +509,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             uint32_t see = valid ? 0xffffffffu : 0u;  // this warp's rows that see this lane's key
             bool whole = whole_keys;
             if constexpr (WIN) {
-                const long long l = (long long)t * p.nl;
-                const int x = (int)min(max(first_row - l, 0ll), (long long)p.nl) * a.G, y = (int)min(max(end_row - l, 0ll), (long long)p.nl) * a.G;
+                const int l = t * p.nl, x = min(max(first_row - l, 0), p.nl) * a.G, y = min(max(end_row - l, 0), p.nl) * a.G;
                 see &= bits_between(x - (kHalf * h + kCols * cw), y - (kHalf * h + kCols * cw));
                 whole = __all_sync(0xffffffffu, see == 0xffffffffu);
             }
@@ -616,23 +620,23 @@ __global__ void __launch_bounds__(kThreads, 1)
     const XattnArgs& a = p.a;
     const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31;
 
-    long long i = blockIdx.x;
-    long long rt;
+    unsigned i = blockIdx.x;
+    int rt;
     int part, hk, b;
     if constexpr (WIN) {  // row tiles slowest, from the last one on: without a window it sees the most keys
-        hk = (int)(i % a.Hkv);
-        i /= a.Hkv;
-        b = (int)(i % a.B);
-        i /= a.B;
-        part = (int)(i % a.splits);
-        rt = p.rtiles - 1 - i / a.splits;
+        hk = (int)(i % (unsigned)a.Hkv);
+        i /= (unsigned)a.Hkv;
+        b = (int)(i % (unsigned)a.B);
+        i /= (unsigned)a.B;
+        part = (int)(i % (unsigned)a.splits);
+        rt = (int)((unsigned)p.rtiles - 1 - i / (unsigned)a.splits);
     } else {
-        rt = i % p.rtiles;
-        i /= p.rtiles;
-        part = (int)(i % a.splits);
-        i /= a.splits;
-        hk = (int)(i % a.Hkv);
-        b = (int)(i / a.Hkv);
+        rt = (int)(i % (unsigned)p.rtiles);
+        i /= (unsigned)p.rtiles;
+        part = (int)(i % (unsigned)a.splits);
+        i /= (unsigned)a.splits;
+        hk = (int)(i % (unsigned)a.Hkv);
+        b = (int)(i / (unsigned)a.Hkv);
     }
     const int tile_rows = p.nl * a.G;
     const int n = keys_of(a, b);
@@ -640,13 +644,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     int t0, t1, sinks = 0, skip = 0;
     KeySpan span{0, 0, 0};
     if constexpr (WIN) {
-        span = key_span<kWindowKeys>(a, b, rt * p.nl, min(rt * p.nl + p.nl, (long long)a.Lq) - 1, n);
+        span = key_span<kWindowKeys>(a, b, rt * p.nl, min(rt * p.nl + p.nl, a.Lq) - 1, n);
         const int from = span.lo / kTile;
         sinks = min((span.sink + kTile - 1) / kTile, from);
         skip = from - sinks;
         const long long count = sinks + max(0, (span.hi + kTile - 1) / kTile - from);
-        t0 = (int)(count * part / a.splits);
-        t1 = (int)(count * (part + 1) / a.splits);
+        t0 = 0;
+        t1 = (int)count;
+        if (a.splits > 1) {
+            t0 = (int)(count * part / a.splits);
+            t1 = (int)(count * (part + 1) / a.splits);
+        }
     } else {
         t0 = (int)((long long)p.ktiles * part / a.splits);
         t1 = min((int)((long long)p.ktiles * (part + 1) / a.splits), (n + kTile - 1) / kTile);
@@ -789,7 +797,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t col = lane_base + 64u * h + (uint32_t)(kCols * cw);
         const uint32_t ts = t_s + col, td = t_dp + col;
         const int r = quad * 32 + lane;
-        const long long pr = rt * tile_rows + r;
+        const long long pr = (long long)rt * tile_rows + r;
         const bool mine = r < tile_rows && pr < a.rows;
         const int l = r / a.G;
         const long long ql = mine ? rt * p.nl + l : 0;

@@ -53,7 +53,7 @@ constexpr float kGrow = 8.f;  // the maximum moves when it grew by more than 2^k
 
 struct Ctl {
     uint64_t q_full[2], q_empty[2];
-    uint64_t full[kMaxStages], empty[kMaxStages], ready[kMaxStages];
+    uint64_t full[kMaxStages], vfull[kMaxStages], empty[kMaxStages], ready[kMaxStages];  // keys there, values, free, values mended
     uint64_t s_full[2], p_full[2], o_done[2];
     uint64_t posted, joined;  // group 1's statistics are in ml; group 0 has read its O
     uint64_t mma_done;
@@ -87,9 +87,8 @@ struct Cfg {
 
 // A work item.
 struct Item {
-    long long row0;  // first packed row
     int part, hk, b, nq, n, t0, nt;
-    long long unit;
+    int l0;           // first query position
     int sinks, skip;  // through a window: tiles of first keys that stay visible, tiles between them and the window
     KeySpan span;     // what some row of the item sees
 };
@@ -100,28 +99,39 @@ __device__ __forceinline__ int tile_of(const Item& m, int j) {
     return WIN && t >= m.sinks ? t + m.skip : t;
 }
 template <bool PAIR, bool WIN>
-__device__ __forceinline__ Item item_of(const Params& p, long long i) {
+// (In 32 bits: items are few enough, and the divisions of 64 bits were half of an item of one key tile's 11 us.)
+__device__ __forceinline__ Item item_of(const Params& p, unsigned i) {
     const XattnArgs& a = p.a;
     Item m;
-    m.unit = i % p.units;
-    i /= p.units;
-    m.part = (int)(i % a.splits);
-    i /= a.splits;
-    m.hk = (int)(i % a.Hkv);
-    m.b = (int)(i / a.Hkv);
-    const int tile_rows = p.nl * a.G;
-    m.row0 = m.unit * (PAIR ? 2 : 1) * tile_rows;
-    m.nq = PAIR && m.row0 + tile_rows < a.rows ? 2 : 1;
+    const unsigned units = (unsigned)p.units;
+    m.l0 = (int)(i % units) * (PAIR ? 2 : 1) * p.nl;
+    i /= units;
+    m.part = 0;
+    if (a.splits > 1) {
+        m.part = (int)(i % (unsigned)a.splits);
+        i /= (unsigned)a.splits;
+    }
+    m.b = (int)(i / (unsigned)a.Hkv);
+    m.hk = (int)i - m.b * a.Hkv;
+    m.nq = PAIR && m.l0 + p.nl < a.Lq ? 2 : 1;
     m.n = keys_of(a, m.b);
     if constexpr (WIN) {
-        const long long last = min(a.rows, m.row0 + (long long)m.nq * tile_rows) - 1;
-        m.span = key_span<kWindowKeys>(a, m.b, m.row0 / a.G, last / a.G, m.n);
+        m.span = key_span<kWindowKeys>(a, m.b, m.l0, min(a.Lq, m.l0 + m.nq * p.nl) - 1, m.n);
         const int from = m.span.lo / kTile;
         m.sinks = min((m.span.sink + kTile - 1) / kTile, from);
         m.skip = from - m.sinks;
-        const long long count = m.sinks + max(0, (m.span.hi + kTile - 1) / kTile - from);
-        m.t0 = (int)(count * m.part / a.splits);
-        m.nt = (int)(count * (m.part + 1) / a.splits) - m.t0;
+        const int count = m.sinks + max(0, (m.span.hi + kTile - 1) / kTile - from);
+        m.t0 = 0;
+        m.nt = count;
+        if (a.splits > 1) {
+            m.t0 = (int)((long long)count * m.part / a.splits);
+            m.nt = (int)((long long)count * (m.part + 1) / a.splits) - m.t0;
+        }
+        return m;
+    }
+    if (a.splits == 1) {
+        m.t0 = 0;
+        m.nt = (m.n + kTile - 1) / kTile;
         return m;
     }
     m.t0 = (int)((long long)p.ktiles * m.part / a.splits);
@@ -148,7 +158,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const XattnArgs& a = p.a;
     const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31;
     const int tile_rows = p.nl * a.G;
-    const bool fix = WIN || a.lens != nullptr || a.mask != nullptr;
+    // (What lies outside the window is not zeroed: where it is not finite, the rows that met it are taken again, k_window_mend.)
+    const bool fix = a.lens != nullptr || a.mask != nullptr;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < QS; ++s) {
@@ -157,6 +168,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         for (int s = 0; s < ST; ++s) {
             mbar_init(&c.full[s], 1);
+            mbar_init(&c.vfull[s], 1);
             mbar_init(&c.empty[s], 1);
             mbar_init(&c.ready[s], 1);
         }
@@ -198,9 +210,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         // ------------------------------------------------------------- Q, then K and V tiles
         if (lane == 0) {
             RingPos rp, rq;
-            int sent = 0, qsent = 0;
+            int qsent = 0;
+            uint32_t kph = 0, vph = 0, used = 0, last = 0;  // a bit a stage: phases, whether it was filled, and with values
             bool ok = true;
-            for (long long it = blockIdx.x; it < p.items && ok; it += gridDim.x) {
+            for (unsigned it = blockIdx.x; it < (unsigned)p.items && ok; it += gridDim.x) {
                 const Item m = item_of<PAIR, WIN>(p, it);
                 if (m.nt == 0) continue;
                 if (!(ok = mbar_wait_1t(&c.q_empty[rq.idx], rq.phase ^ 1u, abort_flag, err))) break;
@@ -208,19 +221,23 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int t = 0; t < m.nq; ++t)
                     for (int k = 0; k < DKC; ++k)
                         tma_load_4d(Qs + (size_t)rq.idx * C::kQBytes + (size_t)(t * DKC + k) * kChunkBytes, &mq, &c.q_full[rq.idx],
-                                    k * kChunk, m.hk * a.G, (int)(m.unit * C::kQTiles + t) * p.nl, m.b * p.qmul);
+                                    k * kChunk, m.hk * a.G, m.l0 + t * p.nl, m.b * p.qmul);
                 rq.next(QS);
                 ++qsent;
                 auto load = [&](bool key, int j) {
                     if (!mbar_wait_1t(&c.empty[rp.idx], rp.phase ^ 1u, abort_flag, err)) return false;
                     const int chunks = key ? DKC : DVC;
-                    mbar_arrive_expect_tx(&c.full[rp.idx], (uint32_t)(chunks * kChunkBytes));
+                    const uint32_t bit = 1u << rp.idx;
+                    uint64_t* there = key ? &c.full[rp.idx] : &c.vfull[rp.idx];
+                    mbar_arrive_expect_tx(there, (uint32_t)(chunks * kChunkBytes));
                     for (int k = 0; k < chunks; ++k)
                         tma_load_4d(ring + (size_t)rp.idx * C::kStageBytes + (size_t)k * kChunkBytes, key ? &mk : &mv,
-                                    &c.full[rp.idx], k * kChunk, m.hk * (key ? p.khmul : p.vhmul), tile_of<WIN>(m, j) * kTile,
+                                    there, k * kChunk, m.hk * (key ? p.khmul : p.vhmul), tile_of<WIN>(m, j) * kTile,
                                     m.b * (key ? p.kmul : p.vmul));
+                    (key ? kph : vph) ^= bit;
+                    used |= bit;
+                    last = key ? last & ~bit : last | bit;
                     rp.next(ST);
-                    ++sent;
                     return true;
                 };
                 for (int j = 0; j < C::kLead && j < m.nt && ok; ++j) ok = load(true, j);
@@ -230,31 +247,29 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
             for (int j = std::max(0, qsent - QS); j < qsent; ++j) mbar_drain(&c.q_full[j % QS], (uint32_t)(j / QS) & 1u, err);
-            for (int j = std::max(0, sent - ST); j < sent; ++j) mbar_drain(&c.full[j % ST], (uint32_t)(j / ST) & 1u, err);
+            for (int s = 0; s < ST; ++s)
+                if (used >> s & 1u) mbar_drain(last >> s & 1u ? &c.vfull[s] : &c.full[s], ((last >> s & 1u ? vph : kph) >> s & 1u) ^ 1u, err);
         }
     } else if (warp == kMaskWarp) {
         // ------------------------------------------------------------- rows of V that are not read
         RingPos rp;
+        uint32_t vph = 0;
         bool ok = fix;
-        for (long long it = blockIdx.x; it < p.items && ok; it += gridDim.x) {
+        for (unsigned it = blockIdx.x; it < (unsigned)p.items && ok; it += gridDim.x) {
             const Item m = item_of<PAIR, WIN>(p, it);
             auto pass = [&](bool key, int j) {
-                uint32_t w[4];
                 if (!key) {
-                    const int j0 = tile_of<WIN>(m, j) * kTile;
-                    valid_words(w, a, m.b, j0, m.n);
-                    if constexpr (WIN) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) w[i] &= seen_word(m.span, j0 + 32 * i);
+                    uint32_t w[4];
+                    valid_words(w, a, m.b, tile_of<WIN>(m, j) * kTile, m.n);
+                    if (!mbar_wait_warp(&c.vfull[rp.idx], vph >> rp.idx & 1u, abort_flag, err)) return false;
+                    vph ^= 1u << rp.idx;
+                    if ((w[0] & w[1] & w[2] & w[3]) != 0xffffffffu) {
+                        zero_rows(ring + (size_t)rp.idx * C::kStageBytes, DVC, w);
+                        fence_proxy_async();
                     }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&c.ready[rp.idx]);
                 }
-                if (!mbar_wait_warp(&c.full[rp.idx], rp.phase, abort_flag, err)) return false;
-                if (!key && (w[0] & w[1] & w[2] & w[3]) != 0xffffffffu) {
-                    zero_rows(ring + (size_t)rp.idx * C::kStageBytes, DVC, w);
-                    fence_proxy_async();
-                }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&c.ready[rp.idx]);
                 rp.next(ST);
                 return true;
             };
@@ -272,15 +287,19 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint32_t ringa = smem_u32(ring);
             RingPos rp, rq;
             uint32_t done0 = 0, done1 = 0;  // weights consumed of each group
+            uint32_t kph = 0, vph = 0;      // phases of the stages' keys and values, a bit each
             bool ok = true;
-            for (long long it = blockIdx.x; it < p.items && ok; it += gridDim.x) {
+            for (unsigned it = blockIdx.x; it < (unsigned)p.items && ok; it += gridDim.x) {
                 Item m = item_of<PAIR, WIN>(p, it);
                 m.nt = uniform(m.nt);
                 m.nq = uniform(m.nq);
                 if (m.nt == 0) continue;
                 const uint32_t qa = smem_u32(Qs) + (uint32_t)(rq.idx * C::kQBytes);
-                auto arrived = [&]() {
-                    const bool in = mbar_wait_warp_inline(fix ? &c.ready[rp.idx] : &c.full[rp.idx], rp.phase, abort_flag, err);
+                auto arrived = [&](bool key) {  // each kind has barriers of its own, so that the mask warp need not follow the keys
+                    uint32_t& ph = key ? kph : vph;
+                    const bool in = mbar_wait_warp_inline(key ? &c.full[rp.idx] : fix ? &c.ready[rp.idx] : &c.vfull[rp.idx],
+                                                          ph >> rp.idx & 1u, abort_flag, err);
+                    ph ^= 1u << rp.idx;
                     tc_fence_after();
                     return in;
                 };
@@ -299,19 +318,19 @@ __global__ void __launch_bounds__(kThreads, 1)
                 };
                 if (!(ok = mbar_wait_warp_inline(&c.q_full[rq.idx], rq.phase, abort_flag, err))) break;
                 if (PAIR) {
-                    if (!(ok = arrived())) break;
+                    if (!(ok = arrived(true))) break;
                     for (int t = 0; t < m.nq; ++t) scores(t);
                     commit_to(&c.empty[rp.idx], el);
                     if (m.nt == 1) commit_to(&c.q_empty[rq.idx], el);
                     rp.next(ST);
                     for (int j = 0; j < m.nt && ok; ++j) {
-                        if (!(ok = arrived())) break;
+                        if (!(ok = arrived(false))) break;
                         const uint32_t v = stage();
                         const int vs = rp.idx;
                         rp.next(ST);
                         for (int t = 0; t < m.nq && ok; ++t) {
                             ok = values(t, j == 0, v);
-                            if (ok && j + 1 < m.nt && (t != 0 || (ok = arrived()))) scores(t);
+                            if (ok && j + 1 < m.nt && (t != 0 || (ok = arrived(true)))) scores(t);
                         }
                         if (!ok) break;
                         commit_to(&c.empty[vs], el);
@@ -323,18 +342,18 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 } else {
                     for (int j = 0; j < 2 && j < m.nt && ok; ++j) {
-                        if (!(ok = arrived())) break;
+                        if (!(ok = arrived(true))) break;
                         scores(j);
                         commit_to(&c.empty[rp.idx], el);
                         if (j + 1 == m.nt) commit_to(&c.q_empty[rq.idx], el);
                         rp.next(ST);
                     }
                     for (int j = 0; j < m.nt && ok; ++j) {
-                        if (!(ok = arrived()) || !(ok = values(j & 1, j < 2, stage()))) break;
+                        if (!(ok = arrived(false)) || !(ok = values(j & 1, j < 2, stage()))) break;
                         commit_to(&c.empty[rp.idx], el);
                         rp.next(ST);
                         if (j + 2 < m.nt) {
-                            if (!(ok = arrived())) break;
+                            if (!(ok = arrived(true))) break;
                             scores(j & 1);
                             commit_to(&c.empty[rp.idx], el);
                             if (j + 3 == m.nt) commit_to(&c.q_empty[rq.idx], el);
@@ -352,27 +371,23 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int t = warp >> 2, quad = warp & 3;
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
         const uint32_t ts = tmem + lane_base + (t ? 128u : 0u), to0 = tmem + lane_base + 256u, to = to0 + (t ? (uint32_t)DV : 0u);
-        const int r = quad * 32 + lane;  // row of the tile
+        const int r = quad * 32 + lane, rl = r / a.G;  // row of the tile, its query position there
         const float cs = a.scale * kLog2e;
         // The lowest maximum, instead of -inf: its product with cs is finite, so that what lies below (a dot product of -inf, a key
         // that is not read, a dot product that only the scale takes to -inf) weighs 0 without a test a tile.
         const float lowest = fmaxf(-3.3e38f / cs, -FLT_MAX);
         uint32_t taken = 0, joins = 0;  // key tiles and joined items of this group so far
         bool ok = true;
-        for (long long it = blockIdx.x; it < p.items && ok; it += gridDim.x) {
+        for (unsigned it = blockIdx.x; it < (unsigned)p.items && ok; it += gridDim.x) {
             const Item im = item_of<PAIR, WIN>(p, it);
             if (PAIR && t >= im.nq) continue;
-            const long long left = a.rows - (im.row0 + (long long)(PAIR ? t : 0) * tile_rows);
-            const int nrows = (int)(left < tile_rows ? left : tile_rows);
+            const int l0 = im.l0 + (PAIR ? t : 0) * p.nl, nrows = min(p.nl, a.Lq - l0) * a.G;
             const bool busy = quad * 32 < nrows;  // a warp without a row only keeps the barriers' count
             [[maybe_unused]] KeySpan sp;
             if constexpr (WIN) {
                 sp.sink = sp.lo = 0;
                 sp.hi = 0x7fffffff;  // (a lane without a row keeps no tile from the unmasked path)
-                if (r < nrows) {
-                    const long long l = (im.row0 + (long long)(PAIR ? t : 0) * tile_rows + r) / a.G;
-                    sp = key_span<kWindowKeys>(a, im.b, l, l, im.n);
-                }
+                if (r < nrows) sp = key_span<kWindowKeys>(a, im.b, l0 + rl, l0 + rl, im.n);
             }
             const int steps = PAIR ? im.nt : (im.nt - t + 1) / 2;  // key tiles of this group
             float m = lowest, l = 0.f;  // m in units of the logits s
@@ -497,15 +512,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (busy && (PAIR || t == 0)) {  // a whole warp, or none
                 const bool mine = r < nrows;
-                const long long pr = im.row0 + (long long)(PAIR ? t : 0) * tile_rows + (mine ? r : 0);
-                const long long ql = pr / a.G;
-                const int h = im.hk * a.G + (int)(pr - ql * a.G);
+                const long long ql = l0 + (mine ? rl : 0);
+                const int h = im.hk * a.G + (mine ? r - rl * a.G : 0);
                 const long long at = ((long long)im.b * a.Hq + h) * a.Lq + ql;
                 const long long all = xattn_rows(a);
                 const float inv = l == 0.f ? 0.f : 1.f / l;
                 __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.o.p) + im.b * a.o.b + ql * a.o.l + h * a.o.h;
                 float* po = a.ws + ((long long)im.part * all + at) * a.dv;
-                [[maybe_unused]] bool wild = false;
+                [[maybe_unused]] float wild = 0.f;  // NaN once a sum is not finite
 #pragma unroll
                 for (int q = 0; q < DV / 32; ++q) {
                     if (32 * q >= a.dv) break;
@@ -528,7 +542,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         uint32_t u[16];
                         if constexpr (WIN) {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) wild |= !(fabsf(v[e] * inv) <= FLT_MAX);
+                            for (int e = 0; e < 32; ++e) wild = fmaf(v[e], 0.f, wild);
                         }
 #pragma unroll
                         for (int e = 0; e < 16; ++e) u[e] = pack_bf16(v[2 * e] * inv, v[2 * e + 1] * inv);
@@ -556,7 +570,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         *ml = make_float2(m2, l);
                     } else {
                         if (a.lse) a.lse[at] = l == 0.f ? -INFINITY : (m2 + log2f(l)) * kLn2;
-                        if constexpr (WIN) reinterpret_cast<unsigned char*>(a.ws)[at] = wild;  // (for k_window_mend)
+                        if constexpr (WIN) reinterpret_cast<unsigned char*>(a.ws)[at] = wild != 0.f;  // (for k_window_mend)
                     }
                 }
             }
