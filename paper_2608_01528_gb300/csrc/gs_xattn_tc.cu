@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int t = warp >> 2, quad = warp & 3;
         const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
         const uint32_t ts = tmem + lane_base + (t ? 128u : 0u), to0 = tmem + lane_base + 256u, to = to0 + (t ? (uint32_t)DV : 0u);
-        const int r = quad * 32 + lane, rl = r / a.G;  // row of the tile, its query position there
+        const int r = quad * 32 + lane;  // row of the tile
         const float cs = a.scale * kLog2e;
         // The lowest maximum, instead of -inf: its product with cs is finite, so that what lies below (a dot product of -inf, a key
         // that is not read, a dot product that only the scale takes to -inf) weighs 0 without a test a tile.
@@ -387,7 +387,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             if constexpr (WIN) {
                 sp.sink = sp.lo = 0;
                 sp.hi = 0x7fffffff;  // (a lane without a row keeps no tile from the unmasked path)
-                if (r < nrows) sp = key_span<kWindowKeys>(a, im.b, l0 + rl, l0 + rl, im.n);
+                const int l = l0 + r / a.G;
+                if (r < nrows) sp = key_span<kWindowKeys>(a, im.b, l, l, im.n);
             }
             const int steps = PAIR ? im.nt : (im.nt - t + 1) / 2;  // key tiles of this group
             float m = lowest, l = 0.f;  // m in units of the logits s
@@ -512,8 +513,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (busy && (PAIR || t == 0)) {  // a whole warp, or none
                 const bool mine = r < nrows;
-                const long long ql = l0 + (mine ? rl : 0);
-                const int h = im.hk * a.G + (mine ? r - rl * a.G : 0);
+                const int rr = mine ? r : 0, rl = rr / a.G, h = im.hk * a.G + rr - rl * a.G;
+                const long long ql = l0 + rl;
                 const long long at = ((long long)im.b * a.Hq + h) * a.Lq + ql;
                 const long long all = xattn_rows(a);
                 const float inv = l == 0.f ? 0.f : 1.f / l;
