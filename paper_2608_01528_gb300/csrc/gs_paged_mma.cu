@@ -581,23 +581,46 @@ __global__ void __launch_bounds__(256) k_paged_join(const Params p, int R) {
     // the last worker w that begins at or before step x: total w / all < x + 1
     const long long w0 = ((u0 + 1) * all - 1) / total, w1 = (u1 * all - 1) / total;
     if (w0 == w1) return;  // written already
-    auto slot_of = [&](long long w) { return (w * p.heads + hk % p.heads) * 2 + (total * w / all < u0); };
+    // (only the first of them can have begun before the unit: it is a later piece of that worker's then)
+    const long long slot0 = (w0 * p.heads + hk % p.heads) * 2;
+    const bool later = total * w0 / all < u0;
+    const int n = (int)(w1 - w0 + 1);
+    auto slot_of = [&](int i) { return slot0 + (long long)i * p.heads * 2 + (i == 0 && later); };
     float m = -INFINITY;
-    for (long long w = w0; w <= w1; ++w) m = fmaxf(m, p.ml[slot_of(w) * R + r].x);
+    for (int i = lane; i < n; i += 32) m = fmaxf(m, p.ml[slot_of(i) * R + r].x);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
     const float ms = m == -INFINITY ? 0.f : m;
     float l = 0.f, acc[DV / 32];
 #pragma unroll
     for (int q = 0; q < DV / 32; ++q) acc[q] = 0.f;
-    for (long long w = w0; w <= w1; ++w) {
-        const long long slot = slot_of(w);
-        const float2 x = p.ml[slot * R + r];
-        if (x.y == 0.f) continue;  // nothing in this piece (NaN is not 0)
-        const float f = ex2(x.x - ms);
-        l = fmaf(x.y, f, l);
-        const float* from = p.part + (slot * R + r) * DV;
+    for (int i0 = 0; i0 < n; i0 += 32) {
+        const float2 mine = i0 + lane < n ? p.ml[slot_of(i0 + lane) * R + r] : make_float2(0.f, 0.f);
+        const bool some = mine.y != 0.f;  // (else nothing in this piece; NaN is not 0)
+        const float f = some ? ex2(mine.x - ms) : 0.f;
+        if (some) l = fmaf(mine.y, f, l);
+        const unsigned which = __ballot_sync(0xffffffffu, some);
+        const int count = min(32, n - i0);
+        constexpr int kAhead = 4;  // pieces in flight
+        for (int c = 0; c < count; c += kAhead) {
+            float v[kAhead][DV / 32], w[kAhead];
 #pragma unroll
-        for (int q = 0; q < DV / 32; ++q) acc[q] = fmaf(from[lane + 32 * q], f, acc[q]);
+            for (int u = 0; u < kAhead; ++u) {
+                w[u] = __shfl_sync(0xffffffffu, f, (c + u) & 31);
+                const bool in = c + u < count && (which >> ((c + u) & 31) & 1u);
+                const float* from = p.part + (slot_of(i0 + (in ? c + u : 0)) * R + r) * DV;
+#pragma unroll
+                for (int q = 0; q < DV / 32; ++q) v[u][q] = in ? from[lane + 32 * q] : 0.f;
+                if (!in) w[u] = 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                for (int q = 0; q < DV / 32; ++q) acc[q] = fmaf(v[u][q], w[u], acc[q]);
+        }
     }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const long long ql = pr / a.G;
     const int head = hk * a.G + (int)(pr - ql * a.G);
