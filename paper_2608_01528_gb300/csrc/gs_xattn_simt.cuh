@@ -63,14 +63,12 @@ __device__ __forceinline__ int keys_of(const XattnArgs& a, int b) {
 // Address of packed row r of (b, key head hk) in a query-side array.
 template <typename T>
 __device__ __forceinline__ T* row_at(const XattnArgs& a, const HeadView& v, int b, int hk, long long r) {
-    const long long l = r / a.G;
-    const int g = (int)(r - l * a.G);
+    const int l = (int)((unsigned)r / (unsigned)a.G), g = (int)r - l * a.G;  // (rows are fewer than 2^31)
     return reinterpret_cast<T*>(v.p) + b * v.b + l * v.l + (long long)(hk * a.G + g) * v.h;
 }
 // Index of packed row r in the (B, Hq, Lq) arrays.
 __device__ __forceinline__ long long row_index(const XattnArgs& a, int b, int hk, long long r) {
-    const long long l = r / a.G;
-    const int g = (int)(r - l * a.G);
+    const int l = (int)((unsigned)r / (unsigned)a.G), g = (int)r - l * a.G;  // (rows are fewer than 2^31)
     return ((long long)b * a.Hq + hk * a.G + g) * a.Lq + l;
 }
 
@@ -101,30 +99,39 @@ __device__ __forceinline__ void load_rows(float* dst, const XattnArgs& a, const 
     for (int c = 0; c < D; c += 16)
         *reinterpret_cast<float4*>(dst + i * (D + 4) + c + c0) = load4(p + c + c0, has ? w - c - c0 : 0, vec);
 }
-// 64 keys from j0 (zero where ok[] says that a key is not read); true where one of this thread's entries is not finite.
-template <typename T, int D>
-__device__ __forceinline__ bool load_keys(float* dst, const HeadView& v, int b, int hk, int j0, int w, const int* ok, bool vec) {
-    const int i = threadIdx.x >> 2, c0 = (threadIdx.x & 3) * 4;
-    const bool has = ok[i] != 0;
-    const T* p = reinterpret_cast<const T*>(v.p) + b * v.b + hk * v.h + (has ? (long long)(j0 + i) * v.l : 0);
-    float odd = 0.f;  // NaN as soon as an entry is an infinity or a NaN
-#pragma unroll
-    for (int c = 0; c < D; c += 16) {
-        const float4 x = load4(p + c + c0, has ? w - c - c0 : 0, vec);
-        odd = fmaf(x.x, 0.f, fmaf(x.y, 0.f, fmaf(x.z, 0.f, fmaf(x.w, 0.f, odd))));
-        *reinterpret_cast<float4*>(dst + i * (D + 4) + c + c0) = x;
-    }
-    return odd != 0.f;
-}
+// Whether key j0 + threadIdx.x / 4 is read, also in ok[] for the others.
 // (WIN: of those that `seen`, the keys of the tile's rows, has)
 template <bool WIN>
-__device__ __forceinline__ void load_valid(int* ok, const XattnArgs& a, int b, int j0, int n, const KeySpan& seen) {
-    if (threadIdx.x < kTile) {
-        const int j = j0 + threadIdx.x;
-        bool in = j < n && (!a.mask || a.mask[b * a.ldm + j] != 0);
-        if constexpr (WIN) in = in && j < seen.hi && (j >= seen.lo || j < seen.sink);
-        ok[threadIdx.x] = in;
+__device__ __forceinline__ bool load_valid(int* ok, const XattnArgs& a, int b, int j0, int n, const KeySpan& seen) {
+    const int i = threadIdx.x >> 2, j = j0 + i;
+    bool in = j < n;
+    if constexpr (WIN) in = in && j < seen.hi && (j >= seen.lo || j < seen.sink);
+    if (in && a.mask) in = a.mask[b * a.ldm + j] != 0;
+    if ((threadIdx.x & 3) == 0) ok[i] = in;
+    return in;
+}
+// This thread's part of 64 keys and values from j0, four threads a key (zero where it is not read): all on their way before the first
+// goes to shared memory.  True where an entry of V is not finite.
+template <typename T, int DK, int DV>
+__device__ __forceinline__ bool load_keys(float* Ks, float* Vs, const XattnArgs& a, int b, int hk, int j0, bool has) {
+    const int i = threadIdx.x >> 2, c0 = (threadIdx.x & 3) * 4;
+    const long long j = has ? j0 + i : 0;
+    const T *k = reinterpret_cast<const T*>(a.k.p) + b * a.k.b + hk * a.k.h + j * a.k.l;
+    const T *v = reinterpret_cast<const T*>(a.v.p) + b * a.v.b + hk * a.v.h + j * a.v.l;
+    float4 x[DK / 16], y[DV / 16];
+#pragma unroll
+    for (int c = 0; c < DK / 16; ++c) x[c] = load4(k + 16 * c + c0, has ? a.dk - 16 * c - c0 : 0, a.vec & kVecK);
+#pragma unroll
+    for (int c = 0; c < DV / 16; ++c) y[c] = load4(v + 16 * c + c0, has ? a.dv - 16 * c - c0 : 0, a.vec & kVecV);
+    float odd = 0.f;  // NaN as soon as an entry is an infinity or a NaN
+#pragma unroll
+    for (int c = 0; c < DK / 16; ++c) *reinterpret_cast<float4*>(Ks + i * (DK + 4) + 16 * c + c0) = x[c];
+#pragma unroll
+    for (int c = 0; c < DV / 16; ++c) {
+        odd = fmaf(y[c].x, 0.f, fmaf(y[c].y, 0.f, fmaf(y[c].z, 0.f, fmaf(y[c].w, 0.f, odd))));
+        *reinterpret_cast<float4*>(Vs + i * (DV + 4) + 16 * c + c0) = y[c];
     }
+    return odd != 0.f;
 }
 
 // acc[i][j] += <A row ty + 16 i, B row tx + 16 j>
@@ -252,7 +259,7 @@ __device__ __forceinline__ void row_spans(RowKeys (&span)[RI], const XattnArgs& 
     if constexpr (WIN) {
 #pragma unroll
         for (int i = 0; i < RI; ++i) {
-            const long long l = min(a.rows - 1, r0 + (threadIdx.x >> 4) + 16 * i) / a.G;
+            const long long l = (unsigned)min(a.rows - 1, r0 + (threadIdx.x >> 4) + 16 * i) / (unsigned)a.G;
             const KeySpan s = key_span<kWindowKeys>(a, b, l, l, n);
             span[i] = {s.lo, s.hi};
         }
@@ -295,10 +302,7 @@ __global__ void __launch_bounds__(kThreads, WIN ? 2 : 1) k_xattn(const XattnArgs
         const int t = kt.tile(i);
         if (t * kTile >= n) break;
         __syncthreads();  // the last tile's weights and values have been read
-        load_valid<WIN>(ok, a, bl.b, t * kTile, n, kt.seen);
-        __syncthreads();
-        load_keys<T, DK>(Ks, a.k, bl.b, bl.hk, t * kTile, a.dk, ok, a.vec & kVecK);
-        const bool odd = load_keys<T, DV>(Vs, a.v, bl.b, bl.hk, t * kTile, a.dv, ok, a.vec & kVecV);
+        const bool has = load_valid<WIN>(ok, a, bl.b, t * kTile, n, kt.seen), odd = load_keys<T, DK, DV>(Ks, Vs, a, bl.b, bl.hk, t * kTile, has);
         bool own = false;  // through a window 0 * NaN of a value that only other rows of the tile see is kept out
         if constexpr (WIN)
             own = __syncthreads_or(odd);
@@ -509,10 +513,7 @@ __device__ __forceinline__ void dq_block(const XattnArgs& a, long long block, lo
         const int t = kt.tile(i);
         if (t * kTile >= n) break;
         __syncthreads();
-        load_valid<WIN>(ok, a, bl.b, t * kTile, n, kt.seen);
-        __syncthreads();
-        load_keys<T, DK>(Ks, a.k, bl.b, bl.hk, t * kTile, a.dk, ok, a.vec & kVecK);
-        load_keys<T, DV>(Vs, a.v, bl.b, bl.hk, t * kTile, a.dv, ok, a.vec & kVecV);
+        load_keys<T, DK, DV>(Ks, Vs, a, bl.b, bl.hk, t * kTile, load_valid<WIN>(ok, a, bl.b, t * kTile, n, kt.seen));
         __syncthreads();
         float s[RI][4] = {}, dp[RI][4] = {};
         dots<DK>(s, Qs, Ks, a.dk);
@@ -602,10 +603,7 @@ __device__ __forceinline__ void dkv_block(const XattnArgs& a, long long block, i
         t1 = first + some * (bl.part + 1) / parts;
     }
     if (j0 >= n) t1 = t0;  // no key of the tile is read
-    load_valid<false>(ok, a, bl.b, j0, n, KeySpan());
-    __syncthreads();
-    load_keys<T, DK>(Ks, a.k, bl.b, bl.hk, j0, a.dk, ok, a.vec & kVecK);
-    load_keys<T, DV>(Vs, a.v, bl.b, bl.hk, j0, a.dv, ok, a.vec & kVecV);
+    load_keys<T, DK, DV>(Ks, Vs, a, bl.b, bl.hk, j0, load_valid<false>(ok, a, bl.b, j0, n, KeySpan()));
     float ok_[4][DK / 16] = {}, ov[4][DV / 16] = {};
     for (long long t = t0; t < t1; ++t) {
         __syncthreads();
