@@ -593,21 +593,65 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // Rows whose sum of values is not finite: a tile's rows see different keys, and 0 times what is not finite in a row of V that one of them
-// sees is NaN in the others'.  Such a row is taken again, over what it sees: a warp each.
-__device__ void mend_row(const XattnArgs& a, long long at, int lane) {
+// sees is NaN in the others'.  Such a row is taken again, over what it sees: a warp each.  First its item's tiles are searched for a
+// value that it does not see and that is not finite (some hundred keys); where there is none, its sum is what it should be.
+// (Inputs lie on 16-byte boundaries here, as for the tensor maps.)
+__device__ __forceinline__ bool odd8(const uint4& x) {  // an infinity or NaN among eight
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) odd |= (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
+    return odd;
+}
+// some value of the keys [j0, j1) is not finite (a warp)
+__device__ bool odd_values(const __nv_bfloat16* vp, const XattnArgs& a, int j0, int j1) {
+    const int lane = threadIdx.x & 31;
+    bool odd = false;
+    for (long long e = lane; e < (j1 - j0) * 16ll; e += 32) {
+        const int c = (int)(e & 15) * 8;
+        const __nv_bfloat16* p = vp + (j0 + (e >> 4)) * a.v.l + c;
+        if (c + 8 <= a.dv)
+            odd |= odd8(__ldg(reinterpret_cast<const uint4*>(p)));
+        else
+            for (int x = 0; c + x < a.dv; ++x) odd |= !(fabsf(__bfloat162float(p[x])) <= FLT_MAX);
+    }
+    return __any_sync(0xffffffffu, odd);
+}
+__device__ void mend_row(const XattnArgs& a, long long at, int lane, int item_rows) {
     const long long l = at % a.Lq, bh = at / a.Lq;
     const int b = (int)(bh / a.Hq), h = (int)(bh % a.Hq), hk = h / a.G, n = keys_of(a, b);
     const KeySpan sp = key_span<kWindowKeys>(a, b, l, l, n);
     const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.q.p) + b * a.q.b + l * a.q.l + h * a.q.h;
     const __nv_bfloat16* kp = reinterpret_cast<const __nv_bfloat16*>(a.k.p) + b * a.k.b + hk * a.k.h;
     const __nv_bfloat16* vp = reinterpret_cast<const __nv_bfloat16*>(a.v.p) + b * a.v.b + hk * a.v.h;
+    {
+        const long long l0 = l / item_rows * item_rows, l1 = min(l0 + item_rows, (long long)a.Lq) - 1;
+        const KeySpan all = key_span<kWindowKeys>(a, b, l0, l1, n);
+        const int from = all.lo / kTile, sinks = min((all.sink + kTile - 1) / kTile, from);
+        const int end = (int)min((long long)n, (all.hi + kTile - 1ll) / kTile * kTile);
+        if (!odd_values(vp, a, sp.sink, min(sinks * kTile, n)) && !odd_values(vp, a, from * kTile, min(sp.lo, n)) &&
+            !odd_values(vp, a, max(sp.hi, from * kTile), end))
+            return;
+    }
     float m = -INFINITY, sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
     for (int i0 = 0; i0 < sp.count(); i0 += 32) {
         const int i = i0 + lane;
         const long long j = i < sp.count() ? sp.key(i) : -1;
         const bool in = j >= 0 && (!a.mask || a.mask[b * a.ldm + j] != 0);
         float s = 0.f;
-        for (int c = 0; c < a.dk && in; ++c) s = fmaf(__bfloat162float(q[c]), __bfloat162float(kp[j * a.k.l + c]), s);
+        for (int c = 0; c < a.dk && in; c += 8) {
+            if (c + 8 <= a.dk) {
+                const uint4 x = __ldg(reinterpret_cast<const uint4*>(q + c)), y = __ldg(reinterpret_cast<const uint4*>(kp + j * a.k.l + c));
+                const uint32_t u[4] = {x.x, x.y, x.z, x.w}, w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s = fmaf(__uint_as_float(u[e] << 16), __uint_as_float(w[e] << 16), s);
+                    s = fmaf(__uint_as_float(u[e] & 0xffff0000u), __uint_as_float(w[e] & 0xffff0000u), s);
+                }
+            } else {
+                for (int e = c; e < a.dk; ++e) s = fmaf(__bfloat162float(q[e]), __bfloat162float(kp[j * a.k.l + e]), s);
+            }
+        }
         s = in ? s * a.scale * kLog2e : -INFINITY;
         float mn = fmaxf(m, s);
 #pragma unroll
@@ -634,7 +678,7 @@ __device__ void mend_row(const XattnArgs& a, long long at, int lane) {
 }
 // Flagged rows (a byte each), or, where parts were joined, the rows of O themselves: 256 rows a block.  4 x 4,096 rows of 32 heads
 // without a flag: 2 us.
-__global__ void __launch_bounds__(256) k_window_mend(const XattnArgs a) {
+__global__ void __launch_bounds__(256) k_window_mend(const XattnArgs a, int item_rows) {
     const long long rows = xattn_rows(a), at = (long long)blockIdx.x * 256 + threadIdx.x;
     const int lane = threadIdx.x & 31;
     bool wild = false;
@@ -648,7 +692,7 @@ __global__ void __launch_bounds__(256) k_window_mend(const XattnArgs a) {
         }
     }
     unsigned todo = __ballot_sync(0xffffffffu, wild);
-    for (; todo; todo &= todo - 1) mend_row(a, at - lane + __ffs(todo) - 1, lane);
+    for (; todo; todo &= todo - 1) mend_row(a, at - lane + __ffs(todo) - 1, lane, item_rows);
 }
 
 std::atomic<bool> g_attr[64][16];
@@ -734,7 +778,7 @@ cudaError_t launch_xattn_tc(const XattnArgs& a, KeyMode mode, int sms, int devic
                                         : launch_widths<false>(pair, q, k, v, p, sms, device, s);
     if (e == cudaSuccess && a.splits > 1) e = launch_xattn_join(a, s);
     if (e != cudaSuccess || mode != kWindowKeys) return e;
-    k_window_mend<<<(unsigned)((xattn_rows(a) + 255) / 256), 256, 0, s>>>(a);
+    k_window_mend<<<(unsigned)((xattn_rows(a) + 255) / 256), 256, 0, s>>>(a, p.nl * (pair ? 2 : 1));
     return cudaGetLastError();
 }
 

@@ -181,6 +181,21 @@ def test_keys_that_no_row_sees_may_hold_anything(gs, dtype):
         assert all(torch.equal(a[1][k], b[1][k]) for k in a[1])
 
 
+@pytest.mark.parametrize("path", ["auto", "simt"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_an_infinite_value_goes_to_the_rows_that_see_it(gs, dtype, path):
+    """In its column and nowhere else, also where its tile holds rows of both kinds (and where all rows of most tiles see it)."""
+    for window, sinks, j in ((None, 0, 5), (100, 2, 300), (1, 6, 4), (40, 0, 511)):
+        Q, K, V, _ = make(2, 700, 700, 8, 2, 64, 72, dtype)
+        V[1, j, 1, 70] = math.inf
+        O = gs.window_attention(Q, K, V, window, sinks, path=path)["O"].float().cpu()
+        gs.stream_status()
+        see = sees(1, 700, 700, window or 2 ** 40, sinks, 0)[0, :, j]
+        hit = torch.zeros(2, 700, 8, 72, dtype=torch.bool)
+        hit[1, :, 4:, 70] = see[:, None]
+        assert (O[hit] == math.inf).all() and torch.isfinite(O[~hit]).all()
+
+
 def test_gradient_against_differences(gs):
     Q, K, V, dO = make(1, 40, 60, 2, 1, 24, 16, "f32")
     args = (13, 2, 20)
