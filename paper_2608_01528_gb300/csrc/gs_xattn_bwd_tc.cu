@@ -154,6 +154,25 @@ __device__ __forceinline__ float dot_eight(const uint4& x, const uint4& y, float
     return acc;
 }
 
+// The key tiles that some row of a row tile sees through a window: first sinks, then the window.  Where the window's are two or fewer,
+// the dQ kernel sums D = sum_j P dP itself, in a pass of its own ahead (few): with some ten keys a D from a bf16 O adds half as much
+// error to dQ as the rounding of dS does.
+struct RowTile {
+    KeySpan span;
+    int sinks, skip, count;
+    bool few;
+};
+__device__ __forceinline__ RowTile row_tile(const XattnArgs& a, int b, int rt, int nl, int n) {
+    RowTile t;
+    t.span = key_span<kWindowKeys>(a, b, rt * nl, min(rt * nl + nl, a.Lq) - 1, n);
+    const int from = t.span.lo / kTile, window = max(0, (t.span.hi + kTile - 1) / kTile - from);
+    t.sinks = min((t.span.sink + kTile - 1) / kTile, from);
+    t.skip = from - t.sinks;
+    t.count = t.sinks + window;
+    t.few = window <= 2 && t.sinks <= 1;
+    return t;
+}
+
 // D = sum_j P dP of the rows that see kFewKeys keys or fewer, instead of <dO, O> with a rounded O (few_keys): 16 threads a row, two rows
 // a warp in step.
 __device__ __forceinline__ void sum_few_seen(const XattnArgs& a, int b, int hk, long long rt, int nl, int grp, int ln, int n, float* dst) {
@@ -161,6 +180,7 @@ __device__ __forceinline__ void sum_few_seen(const XattnArgs& a, int b, int hk, 
     const __nv_bfloat16* values = reinterpret_cast<const __nv_bfloat16*>(a.v.p) + b * a.v.b + hk * a.v.h;
     const float cs = a.scale * kLog2e;
     const int c0 = ln * 8;
+    if (row_tile(a, b, (int)rt, nl, n).few) return;  // (the dQ kernel sums D)
     if (!a.mask) {  // along a tile the number of keys grows, then falls: the first and the last row see the fewest
         const long long first = rt * nl, last = min(first + nl, (long long)a.Lq) - 1;
         const int x = key_span<kWindowKeys>(a, b, first, first, n).count(), y = key_span<kWindowKeys>(a, b, last, last, n).count();
@@ -640,27 +660,35 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     const int tile_rows = p.nl * a.G;
     const int n = keys_of(a, b);
-    // the key tiles, or, through a window, those that some row of the tile sees: first sinks, then the window
-    int t0, t1, sinks = 0, skip = 0;
+    // the key tiles, or, through a window, those that some row of the tile sees, the first `ahead` of them D's (t0 is theirs then too)
+    int t0, t1, sinks = 0, skip = 0, ahead = 0;
+    bool few = false;
     KeySpan span{0, 0, 0};
     if constexpr (WIN) {
-        span = key_span<kWindowKeys>(a, b, rt * p.nl, min(rt * p.nl + p.nl, a.Lq) - 1, n);
-        const int from = span.lo / kTile;
-        sinks = min((span.sink + kTile - 1) / kTile, from);
-        skip = from - sinks;
-        const long long count = sinks + max(0, (span.hi + kTile - 1) / kTile - from);
+        const RowTile tile = row_tile(a, b, rt, p.nl, n);
+        span = tile.span;
+        sinks = tile.sinks;
+        skip = tile.skip;
+        few = tile.few;
         t0 = 0;
-        t1 = (int)count;
-        if (a.splits > 1) {
-            t0 = (int)(count * part / a.splits);
-            t1 = (int)(count * (part + 1) / a.splits);
+        t1 = tile.count;
+        if (few) {  // all in one part
+            if (part != 0) t1 = 0;
+            if (t1 > 1) ahead = t1;
+        } else if (a.splits > 1) {
+            t0 = (int)((long long)tile.count * part / a.splits);
+            t1 = (int)((long long)tile.count * (part + 1) / a.splits);
         }
     } else {
         t0 = (int)((long long)p.ktiles * part / a.splits);
         t1 = min((int)((long long)p.ktiles * (part + 1) / a.splits), (n + kTile - 1) / kTile);
     }
-    const int nt = uniform(max(0, t1 - t0));  // key tiles
-    auto first_key = [&](int t) { return (WIN && t0 + t >= sinks ? t0 + t + skip : t0 + t) * kTile; };
+    if constexpr (WIN) ahead = uniform(ahead);
+    const int nt = uniform(max(0, t1 - t0)) + ahead;  // key tiles to go through
+    auto first_key = [&](int t) {
+        if (WIN && t >= ahead) t -= ahead;
+        return (WIN && t0 + t >= sinks ? t0 + t + skip : t0 + t) * kTile;
+    };
     const bool fix = WIN || a.lens != nullptr || a.mask != nullptr;
 
     // the softmax warps' parts of Q and dO, on their way while the CTA is set up
@@ -780,7 +808,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (u + 2 < steps && !(ok = mbar_wait_warp_inline(&c.s_free[h], ph, abort_flag, err) && scores(u + 2))) break;
                 if (!(ok = mbar_wait_warp_inline(&c.ds_full[h], ph, abort_flag, err))) break;
                 tc_fence_after();
-                mma_tile_ts<32, 4>(t_dq, t_dp + 64u * h, ka + (uint32_t)(cur.idx * DKC * kChunkBytes) + h * kHalfBytes, id_q, u != 0, el);
+                if (!WIN || u >= 2 * ahead)
+                    mma_tile_ts<32, 4>(t_dq, t_dp + 64u * h, ka + (uint32_t)(cur.idx * DKC * kChunkBytes) + h * kHalfBytes, id_q,
+                                       u != (WIN ? 2 * ahead : 0), el);
                 if (h == 1) {
                     commit_to(&c.a_empty[cur.idx], el);
                     cur.next(ST);
@@ -811,7 +841,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         if constexpr (WIN) {
             if (mine) mine_sees = key_span<kWindowKeys>(a, b, ql, ql, n);
         }
-        const bool exact = !WIN && n <= kTile && nt == 1;  // by the sequence, not by its padding: other parts have no tile then
+        // D is summed here: by the sequence, not by its padding (other parts have no tile then)
+        const bool exact = WIN ? few && nt > 0 : n <= kTile && nt == 1;
+        [[maybe_unused]] float dsum = 0.f;
+        [[maybe_unused]] const int last_sum = max(ahead - 1, 0);  // the last tile of D's pass
         if (nt > 0) {
             keep_row(t_q + lane_base, qx, warp >> 2);
             keep_row(t_do + lane_base, ox, warp >> 2);
@@ -832,7 +865,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if constexpr (WIN) w &= seen_word(mine_sees, j0 + kHalf * h + kCols * cw);
             if (!mbar_wait_warp_inline(&c.s_full[h], ph, abort_flag, err)) {
-                if (exact) bar_sync_and(1, kSoftWarps * 32, false);
+                if (exact && (!WIN || t <= last_sum)) bar_sync_and(1, kSoftWarps * 32, false);
                 ok = false;
                 break;
             }
@@ -851,7 +884,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 s[q + 1] = ex2(s[q + 1]);
             }
             if (!mbar_wait_warp_inline(&c.dp_full[h], ph, abort_flag, err)) {
-                if (exact) bar_sync_and(1, kSoftWarps * 32, false);
+                if (exact && (!WIN || t <= last_sum)) bar_sync_and(1, kSoftWarps * 32, false);
                 ok = false;
                 break;
             }
@@ -860,13 +893,22 @@ __global__ void __launch_bounds__(kThreads, 1)
             float* d = reinterpret_cast<float*>(dr);
             tmem_ld32_issue(td, dr);
             tmem_wait_ld32(dr);
-            if (exact) {
+            if (exact && (!WIN || t <= last_sum)) {
                 // every key of the sequence is here: D = sum_j P dP in fp32, for this kernel and the next.  From a bf16 O
                 // it is off by up to 2^-8 of the sum of |dO O|, which with a few keys exceeds the rounding of dS (2 keys: dK off by
                 // 5e-3, so 2e-3).
-                float sum = 0.f;
+                float sum = WIN ? dsum : 0.f;
 #pragma unroll
                 for (int q = 0; q < kCols; ++q) sum += (w >> q) & 1u ? s[q] * d[q] : 0.f;
+                if constexpr (WIN) {
+                    dsum = sum;
+                    if (t < last_sum) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&c.ds_full[h]);
+                        continue;
+                    }
+                }
                 c.dpart[2 * h + cw][r] = sum;
                 if (!bar_sync_and(1, kSoftWarps * 32, true)) {  // a warp gave up
                     ok = false;
@@ -874,6 +916,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 nd = none ? 0.f : -((c.dpart[0][r] + c.dpart[1][r]) + (c.dpart[2][r] + c.dpart[3][r]));
                 if (warp < 4) stats[kTile + r] = nd;
+                if (WIN && ahead > 0) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&c.ds_full[h]);
+                    continue;
+                }
             }
 #pragma unroll
             for (int q = 0; q < kCols; q += 2) {
