@@ -10,7 +10,6 @@
 // integers run at an eighth of that rate.
 
 #include <algorithm>
-#include <type_traits>
 
 #include "gs_paged.h"
 #include "gs_tc_ptx.cuh"
@@ -22,7 +21,7 @@ using u64 = unsigned long long;
 
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kMaxCtas = 8, kResident = 8;  // CTAs of a row; of a multiprocessor
-constexpr int kAhead = 4;                   // 16-byte loads of a lane in flight, of P and of D each
+constexpr int kAhead = 2;                   // 16-byte loads of a lane, of P and of D each, that go together
 constexpr float kHigh = 2097152.f, kLow = 8388608.f, kMagic = 12582912.f;  // 2^21, 2^23, 1.5 * 2^23
 constexpr int kMagicBits = 0x4B400000;
 
@@ -90,27 +89,30 @@ __device__ __forceinline__ void add16(const uint4& a, const uint4& b, int& hi, i
         }
     }
 }
-// Steps of 16 bytes at p (and d), `step` entries apart, kAhead in flight.
+// Steps of 16 bytes at p (and d), `step` entries apart: kAhead on their way while as many are added.
 template <typename T, bool LESS>
 __device__ __forceinline__ long long sum_steps(const T* p, const T* d, int steps, int step) {
     long long sum = 0;
-    int w = 0;
-    auto some = [&](auto n) {
-        constexpr int kN = decltype(n)::value;
-        uint4 a[kN], b[kN];
+    uint4 a[2][kAhead], b[2][kAhead];
+    auto load = [&](uint4(&x)[kAhead], uint4(&y)[kAhead], int w) {
 #pragma unroll
-        for (int u = 0; u < kN; ++u) {
-            a[u] = __ldg(reinterpret_cast<const uint4*>(p + (long long)(w + u) * step));
-            b[u] = LESS ? __ldg(reinterpret_cast<const uint4*>(d + (long long)(w + u) * step)) : make_uint4(0, 0, 0, 0);
+        for (int u = 0; u < kAhead; ++u) {
+            const bool in = w + u < steps;
+            x[u] = in ? __ldg(reinterpret_cast<const uint4*>(p + (long long)(w + u) * step)) : make_uint4(0, 0, 0, 0);
+            y[u] = LESS && in ? __ldg(reinterpret_cast<const uint4*>(d + (long long)(w + u) * step)) : make_uint4(0, 0, 0, 0);
         }
-        int hi = 0, lo = 0;
-#pragma unroll
-        for (int u = 0; u < kN; ++u) add16<T, LESS>(a[u], b[u], hi, lo);
-        sum += units(hi, lo);
-        w += kN;
     };
-    while (w + kAhead <= steps) some(std::integral_constant<int, kAhead>());
-    while (w < steps) some(std::integral_constant<int, 1>());
+    load(a[0], b[0], 0);
+    for (int w = 0; w < steps; w += 2 * kAhead) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            load(a[k ^ 1], b[k ^ 1], w + (k + 1) * kAhead);
+            int hi = 0, lo = 0;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) add16<T, LESS>(a[k][u], b[k][u], hi, lo);
+            sum += units(hi, lo);
+        }
+    }
     return sum;
 }
 // Sum of the weights [j0, j1): entries j0 + first, .. + 16 bytes, then `step` entries on, as long as they lie inside; then those that
@@ -145,12 +147,24 @@ __device__ __forceinline__ u64 sum_piece(const Row& r, int j0, int j1, bool vec)
     return v;
 }
 
-// The first index of [j0, j1) whose running weight is above t (there is one); a warp.  Each lane sums a 32nd, and the one whose part
-// crosses t is cut into 32 again: 8,192 entries take three rounds.
+// The first index of [j0, j1) whose running weight is above t (there is one); a warp.  Runs of 1,024 entries (fp32: 512) are summed as
+// before up to the one that crosses t; then each lane sums a 32nd of that, and the lane's part that crosses t is cut into 32 again.
+// (Lanes with a 32nd of all 8,192 from the start had 32 loads one behind the other: the whole call 33 us.)
 template <typename T>
 __device__ int locate(const Row& r, int j0, int j1, u64 t, bool vec) {
     constexpr int N = 16 / sizeof(T);
     const int lane = threadIdx.x & 31;
+    if (vec) {
+        constexpr int kRun = 4 * 32 * N;
+        for (; j0 + kRun < j1; j0 += kRun) {
+            const u64 v = sum_piece<T>(r, j0, j0 + kRun, true);
+            if (v > t) {
+                j1 = j0 + kRun;
+                break;
+            }
+            t -= v;
+        }
+    }
     for (;;) {
         const int n = j1 - j0;
         int per = (n + 31) / 32;
