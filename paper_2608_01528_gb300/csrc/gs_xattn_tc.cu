@@ -400,7 +400,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (busy) {
                         whole = !a.mask && __all_sync(0xffffffffu, sp.lo <= j0 && sp.hi >= j0 + kTile);
                         if (!whole) {
-                            valid_words(w, a, im.b, j0, im.n);
+                            if (a.mask) {
+                                valid_words(w, a, im.b, j0, im.n);
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) w[i] = 0xffffffffu;  // (a row's span ends with the sequence)
+                            }
 #pragma unroll
                             for (int i = 0; i < 4; ++i) w[i] &= seen_word(sp, j0 + 32 * i);
                             whole = __all_sync(0xffffffffu, (w[0] & w[1] & w[2] & w[3]) == 0xffffffffu);
