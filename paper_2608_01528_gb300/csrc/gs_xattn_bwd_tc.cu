@@ -154,6 +154,11 @@ __device__ __forceinline__ float dot_eight(const uint4& x, const uint4& y, float
     return acc;
 }
 
+// Through a window: a row that sees one key at most has no dS, exactly (its weight is 1 whatever its logit), where P (dP - D) would
+// leave a rounding.  kOneKey in D's place says so; a D that is infinite goes there as NaN.
+constexpr float kOneKey = INFINITY;
+__device__ __forceinline__ float not_one_key(float nd) { return nd == kOneKey ? NAN : nd; }
+
 // The key tiles that some row of a row tile sees through a window: first sinks, then the window.  Where the window's are two or fewer,
 // the dQ kernel sums D = sum_j P dP itself, in a pass of its own ahead (few): with some ten keys a D from a bf16 O adds half as much
 // error to dQ as the rounding of dS does.
@@ -210,7 +215,7 @@ __device__ __forceinline__ void sum_few_seen(const XattnArgs& a, int b, int hk, 
             }
             if (in) sum = fmaf(ex2(fmaf(s, cs, nl2)), dp, sum);
         }
-        if (on && ln == 0) dst[kTile + r] = nl2 == -INFINITY ? 0.f : -sum;
+        if (on && ln == 0) dst[kTile + r] = nl2 == -INFINITY ? 0.f : not_one_key(-sum);
     }
 }
 
@@ -258,23 +263,27 @@ __global__ void __launch_bounds__(256) k_xattn_stats(const XattnArgs a, int nl, 
             const int r = grp + 16 * k;
             const float nl2 = neg_lse2(L[k]);
             dst[r] = nl2;
-            dst[kTile + r] = nl2 == -INFINITY ? 0.f : -acc[k];
+            const float nd = nl2 == -INFINITY ? 0.f : -acc[k];
+            dst[kTile + r] = WIN ? not_one_key(nd) : nd;
         }
     }
     const int n = keys_of(a, b);
     if constexpr (WIN) {
         // whether to look at all, by one warp (by all eight: 20 of 47 us for 2 x 4,096 rows of 32 heads of 128)
-        __shared__ int look;
-        if (threadIdx.x < 32) {
-            bool some = !row_tile(a, b, (int)rt, nl, n).few;  // (else the dQ kernel sums D)
-            if (some && !a.mask) {  // along a tile the number of keys grows, then falls: the first and the last row see the fewest
-                const int first = (int)rt * nl, last = min(first + nl, a.Lq) - 1;
-                some = min(key_span<kWindowKeys>(a, b, first, first, n).count(), key_span<kWindowKeys>(a, b, last, last, n).count()) <= kFewKeys;
-            }
-            if (threadIdx.x == 0) look = some;
+        __shared__ int look;  // 1: for rows of few keys, 2: for rows of one key
+        if (threadIdx.x < 32) {  // (along a tile the number of keys grows, then falls: the first and the last row see the fewest)
+            const int first = (int)rt * nl, last = min(first + nl, a.Lq) - 1;
+            const int least = min(key_span<kWindowKeys>(a, b, first, first, n).count(), key_span<kWindowKeys>(a, b, last, last, n).count());
+            const bool few = !row_tile(a, b, (int)rt, nl, n).few && (a.mask || least <= kFewKeys);  // (else the dQ kernel sums D)
+            if (threadIdx.x == 0) look = (few ? 1 : 0) | (least <= 1 ? 2 : 0);
         }
         __syncthreads();
-        if (look) sum_few_seen(a, b, hk, rt, nl, grp, ln, n, dst);
+        if (look & 1) sum_few_seen(a, b, hk, rt, nl, grp, ln, n, dst);
+        if ((look & 2) && ln == 0)
+            for (int r = grp; r < grp + 16 * kStatRows; r += 16) {
+                const int l = r / a.G, ql = (int)rt * nl + l;
+                if (l < nl && ql < a.Lq && key_span<kWindowKeys>(a, b, ql, ql, n).count() <= 1) dst[kTile + r] = kOneKey;
+            }
         return;
     }
     if (!a.mask || n <= kTile) return;  // (up to a tile's keys: k_xattn_dq_tc sums D)
@@ -579,6 +588,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             float* d = reinterpret_cast<float*>(dr);
             tmem_ld32_issue(td, dr);
             tmem_wait_ld32(dr);
+            bool all = whole;
+            if constexpr (WIN) {
+                see &= ~__ballot_sync(0xffffffffu, c.stats[rp.idx][kTile + kHalf * h + kCols * cw + lane] == kOneKey);
+                all = __all_sync(0xffffffffu, see == 0xffffffffu);
+            }
 #pragma unroll
             for (int q = 0; q < kCols / 4; ++q) {
                 const float4 D = nd[q];
@@ -588,7 +602,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 mul2(x[0], x[1], s[4 * q], s[4 * q + 1]);
                 mul2(x[2], x[3], s[4 * q + 2], s[4 * q + 3]);
             }
-            if (!whole) {
+            if (!all) {
 #pragma unroll
                 for (int q = 0; q < kCols; ++q) d[q] = (WIN ? (see >> q) & 1u : valid) ? d[q] : 0.f;
             }
@@ -849,6 +863,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // D is summed here: by the sequence, not by its padding (other parts have no tile then)
         const bool exact = WIN ? few && nt > 0 : n <= kTile && nt == 1;
         [[maybe_unused]] float dsum = 0.f;
+        const bool one = WIN && mine && mine_sees.count() <= 1;
         [[maybe_unused]] const int last_sum = max(ahead - 1, 0);  // the last tile of D's pass
         if (nt > 0) {
             keep_row(t_q + lane_base, qx, warp >> 2);
@@ -920,6 +935,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     break;
                 }
                 nd = none ? 0.f : -((c.dpart[0][r] + c.dpart[1][r]) + (c.dpart[2][r] + c.dpart[3][r]));
+                if (WIN) nd = one ? kOneKey : not_one_key(nd);
                 if (warp < 4) stats[kTile + r] = nd;
                 if (WIN && ahead > 0) {
                     tc_fence_before();
@@ -938,7 +954,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int q = 0; q < kCols; ++q) d[q] = (w >> q) & 1u ? d[q] : 0.f;
             }
 #pragma unroll
-            for (int q = 0; q < kCols / 2; ++q) pk[q] = none ? 0u : pack_bf16(d[2 * q], d[2 * q + 1]);
+            for (int q = 0; q < kCols / 2; ++q) pk[q] = none || one ? 0u : pack_bf16(d[2 * q], d[2 * q + 1]);
             tmem_st16(td, pk);
             tmem_wait_st();
             tc_fence_before();

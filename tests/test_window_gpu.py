@@ -141,6 +141,20 @@ def test_rows_of_few_keys_take_no_rounded_output(gs, shape):
 
 @pytest.mark.parametrize("path", ["auto", "simt"])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_row_of_one_key_has_no_gradient_but_its_value_s(gs, dtype, path):
+    """Its weight is 1 whatever its logit: dQ and dK are 0, not a rounding's rest, also beside rows of more keys."""
+    for Lq, window, sinks, start, n in ((400, 1, 0, 0, None), (300, 1, 0, 200, (1, 500)), (3, 5, 2, 0, (1, 1)), (200, 1000, 4, 0, (1, 1))):
+        Q, K, V, dO = make(2, Lq, 500, 4, 2, 64, 64, dtype)
+        lens = torch.tensor(n, dtype=torch.int32).cuda() if n else None
+        out, got = check(gs, Q, K, V, dO, window, sinks, start, lens, path=path)
+        assert (got["dQ"] == 0).all() and (got["dK"] == 0).all() and (got["dV"] != 0).any()
+    Q, K, V, dO = make(2, 300, 300, 4, 2, 64, 64, dtype)
+    out, got = check(gs, Q, K, V, dO, 150, 2, 0, path=path)
+    assert (got["dQ"][:, 0] == 0).all() and (got["dQ"][:, 1] != 0).any()
+
+
+@pytest.mark.parametrize("path", ["auto", "simt"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_starts_of_their_own(gs, dtype, path):
     Q, K, V, dO = make(5, 140, 400, 4, 2, 64, 64, dtype)
     start = torch.tensor([0, 260, -7, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32).cuda()
