@@ -4,10 +4,12 @@
 // that rows come in eights (a decoding step of four query heads to a key head fills half of one tile, not an eighth), P goes from
 // one product to the other in registers, and no warp waits for another.  K and V are read once, 16 bytes a lane and copy, three steps
 // in a ring; the table entry of a step is read four steps before it and its rows' addresses are known two before, so a page may end anywhere.
-// A row's reference maximum moves only where it grew by more than 2^8, which spares the reduction over keys in most steps.
+// A row's reference maximum moves only where it grew by more than 2^8, which spares the reduction over keys in most steps.  The weights go
+// to V in two bf16 terms (error of O against 64 bits 2.1e-3 -> 1.7e-3 of its norm, the output's own rounding; 64 single rows 101 -> 103 us,
+// six rows over long histories 272 -> 285).
 //
-// Bound by memory: 16 keys of 128 + 128 columns are 8 KB and 0.18 us of an SM's share of HBM, in which 32 rows take 256 products of
-// 16 x 8 x 16.  A tcgen05 tile has 128 rows, of which a decoding step fills 1 to 32, and would add a pass through TMEM to each step.
+// Bound by memory: 16 keys of 128 + 128 columns are 8 KB and 0.18 us of an SM's share of HBM, in which 32 rows take 96 products of
+// 16 x 8 x 16 (64 x 1 to 4,096 keys, 32 / 8 heads of 128: 5.2 TB/s of calls, 5.9 of the kernel; 8 x 32,769 to 65,537 keys: 5.7 and 6.3).  A tcgen05 tile has 128 rows, of which a decoding step fills 1 to 32, and would add a pass through TMEM to each step.
 //
 // Work.  A unit is a request, a chunk of rows and up to four neighbouring key heads, one to each warp of a CTA, which so read 1 KB of a
 // position together (fewer heads: the warps that are over take runs of their own).  Every worker takes an equal run of the steps of all
@@ -412,7 +414,7 @@ __global__ void __launch_bounds__(kThreads, resident<DK, DV, NR>()) k_paged_mma(
                 }
         }
         // ------------------------------------------------------------- P^T, and V^T P^T
-        uint32_t pb[NR][2];
+        uint32_t pb[NR][2], pl[NR][2];  // the weights in two bf16 terms: the tensor pipe has room, and O keeps fp32's accuracy
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
 #pragma unroll
@@ -422,8 +424,13 @@ __global__ void __launch_bounds__(kThreads, resident<DK, DV, NR>()) k_paged_mma(
                 c[n][2 + e] = ex2(c[n][2 + e] - ms);
                 sum[n][e] += c[n][e] + c[n][2 + e];
             }
-            pb[n][0] = transposed(ptx::pack_bf16(c[n][0], c[n][1]));
-            pb[n][1] = transposed(ptx::pack_bf16(c[n][2], c[n][3]));
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float x = c[n][2 * h], y = c[n][2 * h + 1];
+                const uint32_t u = ptx::pack_bf16(x, y);
+                pb[n][h] = transposed(u);
+                pl[n][h] = transposed(ptx::pack_bf16(x - __uint_as_float(u << 16), y - __uint_as_float(u & 0xffff0000u)));
+            }
         }
         if (wild) {  // what is not finite goes to the rows that see it by itself, and out of the tile
             auto value = [&](int j, int col) { return vs + chunk_at<DV>(j, col >> 3) + 2 * (col & 7); };
@@ -465,7 +472,10 @@ __global__ void __launch_bounds__(kThreads, resident<DK, DV, NR>()) k_paged_mma(
             uint32_t x[4];
             ldmatrix_t(x, vs + chunk_at<DV>((lane & 7) + ((lane >> 4) << 3), 2 * i + ((lane >> 3) & 1)));
 #pragma unroll
-            for (int n = 0; n < NR; ++n) mma(o[i][n], x, pb[n][0], pb[n][1]);
+            for (int n = 0; n < NR; ++n) {
+                mma(o[i][n], x, pb[n][0], pb[n][1]);
+                mma(o[i][n], x, pl[n][0], pl[n][1]);
+            }
         }
         ok0 = ok1;
         ok1 = ok2;
