@@ -91,6 +91,15 @@ __device__ __forceinline__ uint32_t chunk_at(int r, int c) {
 __device__ __forceinline__ bool odd_low(uint32_t x) { return (x & 0x7f80u) == 0x7f80u; }            // an infinity or NaN of a pair
 __device__ __forceinline__ bool odd_high(uint32_t x) { return (x & 0x7f800000u) == 0x7f800000u; }
 
+// Two weights in two bf16 terms: their upper halves, and what these leave, which is above 0 where the weight is (the smallest bf16
+// number, 2^-133, at least), so that an infinite value times either term stays the same infinity.  (With terms to the nearest the second
+// was 0 or negative: infinities that a row sees came out as NaN.)
+__device__ __forceinline__ void two_terms(float x, float y, uint32_t& high, uint32_t& low) {
+    const uint32_t u = __float_as_uint(x) & 0xffff0000u, v = __float_as_uint(y) & 0xffff0000u;
+    high = u >> 16 | v;
+    low = __vmaxu2(ptx::pack_bf16(x - __uint_as_float(u), y - __uint_as_float(v)), __vminu2(high, 0x00010001u));
+}
+
 __device__ __forceinline__ KeySpan unit_span(const XattnArgs& a, int b, int n) {
     return key_span<kPagedKeys>(a, b, 0, a.Lq - 1, n);
 }
@@ -414,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, resident<DK, DV, NR>()) k_paged_mma(
                 }
         }
         // ------------------------------------------------------------- P^T, and V^T P^T
-        uint32_t pb[NR][2], pl[NR][2];  // the weights in two bf16 terms: the tensor pipe has room, and O keeps fp32's accuracy
+        uint32_t pb[NR][2], pl[NR][2];  // the weights in two bf16 terms (16 bits together): the tensor pipe has room, and O keeps fp32's accuracy
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
 #pragma unroll
@@ -427,9 +436,10 @@ __global__ void __launch_bounds__(kThreads, resident<DK, DV, NR>()) k_paged_mma(
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const float x = c[n][2 * h], y = c[n][2 * h + 1];
-                const uint32_t u = ptx::pack_bf16(x, y);
-                pb[n][h] = transposed(u);
-                pl[n][h] = transposed(ptx::pack_bf16(x - __uint_as_float(u << 16), y - __uint_as_float(u & 0xffff0000u)));
+                uint32_t high, low;
+                two_terms(x, y, high, low);
+                pb[n][h] = transposed(high);
+                pl[n][h] = transposed(low);
             }
         }
         if (wild) {  // what is not finite goes to the rows that see it by itself, and out of the tile
