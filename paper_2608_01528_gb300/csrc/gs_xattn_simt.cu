@@ -82,6 +82,8 @@ void xattn_simt_plan(XattnArgs& a, bool backward, int sms, KeyMode mode) {
         a.rsplits = xattn_sink_parts(kt * a.Hkv * a.B, rt, some, rt * keys * a.Hkv * a.B, 2 * sms);
         if (a.rsplits > 1) a.pkeys = (int)std::min<long long>(a.Lk, (a.win.sinks + kTile - 1ll) / kTile * kTile);
     }
+    if (rt == 0) a.splits = 1;   // (nothing to cut, and no sums to launch, although the other axis alone may ask for parts)
+    if (kt == 0) a.rsplits = 1;
     a.stats = xattn_round4(xattn_rows(a));  // D_i
 }
 
