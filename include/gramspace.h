@@ -527,7 +527,9 @@ GS_API gs_status gs_page_slots(const int* lens, const int* added, int B, int Lne
  * Stores new keys and values: row (b, l) of K (B x L x H x dk) and V (B x L x H x dv) to slot slots[b * ld_slots + l] of Kc
  * and Vc (pages x page_size x H x width), all of type dtype.  Rows whose slot lies outside [0, pages * page_size) are
  * skipped, slots that no row names keep what they hold.  Slots must differ: of two rows with one slot, which stays is not defined
- * (each 16 bytes are one's or the other's).  K and V must not overlap the cache.  No workspace.
+ * (each 16 bytes are one's or the other's).  K and V must not overlap the cache.  No workspace.  Requires pages * page_size and
+ * B * L below 2^31, and rows (H * dk and H * dv) of fewer than 2^31 - 1024 elements.
+ * Errors: GS_ERR_INVALID_ARG, GS_ERR_SHAPE, GS_ERR_ALIGNMENT, GS_ERR_CUDA, GS_ERR_UNSUPPORTED.
  */
 GS_API gs_status gs_page_store(int dtype, int B, int L, int H, int dk, int dv, const gs_heads* K, const gs_heads* V,
                                const int* slots, long long ld_slots, int pages, int page_size, const gs_heads* Kc,

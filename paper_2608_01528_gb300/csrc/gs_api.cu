@@ -1241,9 +1241,9 @@ gs_status gs_page_store(int dtype, int B, int L, int H, int dk, int dv, const gs
                         long long ld_slots, int pages, int page_size, const gs_heads* Kc, const gs_heads* Vc, void* stream) {
     if (dtype != GS_F32 && dtype != GS_BF16) return GS_ERR_INVALID_ARG;
     if (!K || !V || !Kc || !Vc) return GS_ERR_INVALID_ARG;
-    const long long limit = 0x7fffffffLL;
+    const long long limit = 0x7fffffffLL, far = limit - 1024;
     if (B < 0 || L < 0 || H < 1 || dk < 1 || dv < 1 || pages < 0 || page_size < 1 || ld_slots < L ||
-        (long long)pages * page_size > limit || (long long)B * L > limit || (long long)H * std::max(dk, dv) > limit)
+        (long long)pages * page_size > limit || (long long)B * L > limit || (long long)H * std::max(dk, dv) > far)
         return GS_ERR_SHAPE;
     if (!valid_heads(K, B, L, H, false) || !valid_heads(V, B, L, H, false) || !valid_heads(Kc, pages, page_size, H, true) ||
         !valid_heads(Vc, pages, page_size, H, true))

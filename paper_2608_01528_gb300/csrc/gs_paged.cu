@@ -102,6 +102,7 @@ __global__ void __launch_bounds__(kThreads) k_page_slots(const SlotArgs a, int p
 
 // ----------------------------------------------------------------- stores
 // A warp moves one token's keys or values, four 16-byte loads of a lane on their way before the first store.  Bound by memory.
+// (A row has fewer than 2^31 - 1024 elements, which leaves room for the last steps' numbers, and up to 2^33 bytes.)
 template <typename T>
 __device__ __forceinline__ void move_row(char* dst, const char* src, int H, int per, long long dh, long long sh) {
     const int lane = threadIdx.x & 31;
@@ -137,9 +138,8 @@ __global__ void __launch_bounds__(kThreads) k_page_store(const StoreArgs a) {
         const HeadView &s = a.src[x], &d = a.dst[x];
         const char* from = s.p + (b * s.b + l * s.l) * a.bytes;
         char* to = d.p + (page * d.b + row * d.l) * a.bytes;
-        const int bytes = a.w[x] * a.bytes;
         if (a.vec[x])
-            move_row<uint4>(to, from, a.H, bytes / 16, d.h * a.bytes, s.h * a.bytes);
+            move_row<uint4>(to, from, a.H, (int)((long long)a.w[x] * a.bytes / 16), d.h * a.bytes, s.h * a.bytes);
         else if (a.bytes == 4)
             move_row<uint32_t>(to, from, a.H, a.w[x], d.h * 4, s.h * 4);
         else
@@ -169,7 +169,7 @@ cudaError_t launch_page_store(const StoreArgs& args, int sms, cudaStream_t s) {
             auto ok = [&](long long stride, int n) { return n <= 1 || stride * a.bytes % 16 == 0; };
             return (uintptr_t)v.p % 16 == 0 && ok(v.b, nb) && ok(v.l, nl) && ok(v.h, H);
         };
-        a.vec[x] = a.w[x] * a.bytes % 16 == 0 && on_16(a.src[x], a.B, a.L) && on_16(a.dst[x], a.pages, a.page);
+        a.vec[x] = (long long)a.w[x] * a.bytes % 16 == 0 && on_16(a.src[x], a.B, a.L) && on_16(a.dst[x], a.pages, a.page);
         flat = flat && (H == 1 || (a.src[x].h == a.w[x] && a.dst[x].h == a.w[x]));
     }
     if (flat) {  // heads lie next to one another: one row of H * w
