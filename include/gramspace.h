@@ -617,8 +617,8 @@ GS_API gs_status gs_sample_scores(const void* S, int s_dtype, long long N, int M
  * Weights are integers in units of 2^-44 (entries that are negative or NaN count as 0, above 1 as 1), their sums exact
  * in any order, so that a draw differs from exact arithmetic's only where U lies that close to a border; the comparison is exact.
  * P and D: GS_F32 or GS_BF16, strides p_batch, p_row, d_batch, d_row in elements (>= 0), unit stride along M <= 2^19.
- * accepted (B) and tokens are optional, not both NULL.  No workspace.
- * Errors: GS_ERR_INVALID_ARG, GS_ERR_SHAPE, GS_ERR_ALIGNMENT, GS_ERR_CUDA, GS_ERR_UNSUPPORTED.
+ * accepted (B) and tokens are optional, not both NULL; neither may overlap an input or the other.  No workspace.
+ * Errors: GS_ERR_INVALID_ARG (a null pointer, overlap), GS_ERR_SHAPE, GS_ERR_ALIGNMENT, GS_ERR_CUDA, GS_ERR_UNSUPPORTED.
  */
 GS_API gs_status gs_verify_drafts(const void* P, const void* D, int dtype, int B, int K, int M, long long p_batch,
                                   long long p_row, long long d_batch, long long d_row, const int* drafts,

@@ -882,6 +882,11 @@ template <typename... P>
 bool on_elements(int bytes, const P*... p) {
     return ((... | (uintptr_t)p) & (uintptr_t)(bytes - 1)) == 0;
 }
+// Whether arrays of so many bytes (0 or less, or null: none) share none of them.
+bool apart(const void* x, long long nx, const void* y, long long ny) {
+    const char *a = (const char*)x, *b = (const char*)y;
+    return !x || !y || nx <= 0 || ny <= 0 || a + nx <= b || b + ny <= a;
+}
 constexpr float kMaxScale = 2e38f;  // scale * log2(e) is an fp32 number
 gs::HeadView view_of(const gs_heads* v) { return {(char*)v->data, v->batch, v->row, v->head}; }
 
@@ -1213,17 +1218,14 @@ gs_status gs_page_slots(const int* lens, const int* added, int B, int Lnew, int 
     if (B > 0 && (!lens || !added || (columns > 0 && !table) || (n_free > 0 && !free_list) || (Lnew > 0 && !slots)))
         return GS_ERR_INVALID_ARG;
     // blocks read the lengths of the requests before theirs while others write: no output lies on an input
-    auto apart = [](const int* x, long long nx, const int* y, long long ny) {
-        return !x || !y || nx <= 0 || ny <= 0 || x + nx <= y || y + ny <= x;
-    };
     const long long cells = B > 0 ? (B - 1) * ld_table + columns : 0, tokens = (long long)B * Lnew;
     const struct { const int* p; long long n; } in[] = {{lens, B}, {added, B}, {free_list, n_free}, {free_from, 1}},
                                                 out[] = {{table, cells}, {slots, tokens}, {new_lens, B}, {taken, 1}};
     for (int i = 0; i < 4; ++i) {
         for (const auto& x : in)
-            if (!apart(x.p, x.n, out[i].p, out[i].n)) return GS_ERR_INVALID_ARG;
+            if (!apart(x.p, 4 * x.n, out[i].p, 4 * out[i].n)) return GS_ERR_INVALID_ARG;
         for (int j = 0; j < i; ++j)
-            if (!apart(out[j].p, out[j].n, out[i].p, out[i].n)) return GS_ERR_INVALID_ARG;
+            if (!apart(out[j].p, 4 * out[j].n, out[i].p, 4 * out[i].n)) return GS_ERR_INVALID_ARG;
     }
     if (B == 0 && !taken) return GS_OK;
     int dev = 0, sms = 0;
@@ -1274,6 +1276,14 @@ gs_status gs_verify_drafts(const void* P, const void* D, int dtype, int B, int K
     if (!P || !U || (!accepted && !tokens) || (K > 0 && !drafts)) return GS_ERR_INVALID_ARG;
     if (!on_elements(dtype == GS_F32 ? 4 : 2, P, D) || !on_elements(4, drafts, draft_lens, U, accepted, tokens))
         return GS_ERR_ALIGNMENT;
+    // a request's tokens are written while other requests' blocks read theirs
+    const long long e = dtype == GS_F32 ? 4 : 2, n = 4LL * B * K, n1 = 4LL * B * (K + 1LL);
+    const struct { const void* p; long long n; } in[] = {{P, e * ((B - 1LL) * p_batch + K * p_row + M)},
+                                                         {K > 0 ? D : nullptr, e * ((B - 1LL) * d_batch + (K - 1LL) * d_row + M)},
+                                                         {drafts, n}, {draft_lens, 4LL * B}, {U, n1}};
+    for (const auto& x : in)
+        if (!apart(x.p, x.n, accepted, 4LL * B) || !apart(x.p, x.n, tokens, n1)) return GS_ERR_INVALID_ARG;
+    if (!apart(accepted, 4LL * B, tokens, n1)) return GS_ERR_INVALID_ARG;
     int dev = 0, sms = 0;
     gs_status st = attn_device(dev, sms);
     if (st != GS_OK) return st;
