@@ -612,10 +612,12 @@ GS_API gs_status gs_sample_scores(const void* S, int s_dtype, long long N, int M
  *     draft x_i is kept while   U[b][i] * D_i(x_i) < P_i(x_i),   i = 0, 1, .. n-1;      a = accepted[b], the drafts kept
  *     w = max(P_a - D_a, 0) if a < n (P_a where that is zero everywhere), w = P_a if a = n
  *     tokens[b] = the kept drafts, then the first index whose running weight in w exceeds U[b][K] times its sum, then -1
- * (B x (K+1), dense; the drawn token is -1 where P_a holds nothing above 0).  U is B x (K+1) numbers of [0, 1), taken as 0 where
+ * (B x (K+1), dense; the drawn token is -1 where P_a holds nothing above 2^-45).  U is B x (K+1) numbers of [0, 1), taken as 0 where
  * negative or NaN and as the largest fp32 below 1 from 1 on.  A draft outside [0, M) is not kept, nor one whose comparison has a NaN.
- * Weights are integers in units of 2^-44 (entries that are negative or NaN count as 0, above 1 as 1), their sums exact
- * in any order, so that a draw differs from exact arithmetic's only where U lies that close to a border; the comparison is exact.
+ * Weights are integers in units of 2^-44 (entries that are negative or NaN count as 0, above 1 as 1), their sums exact in any order;
+ * the comparison is exact.  A weight is off by up to half a unit (a unit in P_a - D_a), so a draw differs from exact arithmetic's only where
+ * U lies within M 2^-44 / sum(w) of a border between entries: M = 2^17 and w = P_a, of sum 1, 7e-9; a rest of sum 1e-4, 7e-5.  An entry
+ * of P_a of 2^-45 or less is never drawn from P_a, and a rest of which no unit is left counts as zero everywhere.
  * P and D: GS_F32 or GS_BF16, strides p_batch, p_row, d_batch, d_row in elements (>= 0), unit stride along M <= 2^19.
  * accepted (B) and tokens are optional, not both NULL; neither may overlap an input or the other.  No workspace.
  * Errors: GS_ERR_INVALID_ARG (a null pointer, overlap), GS_ERR_SHAPE, GS_ERR_ALIGNMENT, GS_ERR_CUDA, GS_ERR_UNSUPPORTED.

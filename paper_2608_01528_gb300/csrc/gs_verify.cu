@@ -5,7 +5,8 @@
 // up to 8 CTAs, a contiguous piece a warp.  The pieces' sums meet in shared memory across the cluster, and the warp whose piece holds the
 // drawn point looks through it again (by then in L1 or L2).
 //
-// Weights are integers in units of 2^-44, rint(p 2^44) - rint(d 2^44), so that every sum is exact in any order.  A conversion in two steps of
+// Weights are integers in units of 2^-44, rint(p 2^44) - rint(d 2^44), so that every sum is exact in any order.  Each is off by a unit at
+// most, M of them shift the drawn point by up to M 2^-44 of their sum: what is lost where little is left of P - D.  A conversion in two steps of
 // fp32, p 2^21 = hi + lo 2^-23 with hi and lo read off the mantissas of sums with 1.5 2^23, costs four FMAs or adds; conversions to 64-bit
 // integers run at an eighth of that rate.
 
