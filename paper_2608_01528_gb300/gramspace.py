@@ -716,7 +716,8 @@ def page_slots(lens, added, table, free, page_size, max_new, pages, free_from=No
     lens, added: int32 CUDA vectors, tokens that each request holds and gets.  table: int32 requests x columns, the block table,
     whose next columns are filled in place.  free: int32 vector, the free pages, taken from entry free_from (an int32 CUDA
     tensor of one; None: 0) on.  max_new: columns of the result, pages: of the cache.  Returns {"slots": requests x max_new, "lens": the
-    requests' new lengths, "taken": pages asked for, one number}, int32."""
+    requests' new lengths, "taken": pages asked for, one number}, int32.  free_from of the next call is free_from + taken, or the list's
+    length where that is less: free_from.add_(taken).clamp_(max=free.numel())."""
     dev = lens.device
     t, B, columns, ld = _table(table, dev)
     _c_int(abs(int(page_size)), abs(int(max_new)), abs(int(pages)), free.numel())
