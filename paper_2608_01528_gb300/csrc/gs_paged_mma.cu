@@ -32,8 +32,14 @@ using xtc::kLog2e;
 using xtc::keys_of;
 
 constexpr int kWarps = 4, kThreads = kWarps * 32, kStep = 16, kStages = 3;
+// A CTA takes whole units where none has more keys than this: 4 x 512 keys, 32 / 8 heads of 128, whole 21.6, in pieces 22.7 us (in a graph), 16 x 512
+// 22.7 / 26.8, 4 x 90 to 300, 8 heads of 64, 14.5 / 21.6, but 256 x 512 128 / 119; 4 x 1,024 30.8 / 24.7.
 constexpr int kWholeKeys = 512;
-constexpr int kLeastSteps = 4;  // of a worker
+// .. or where there are so many units a CTA: what the table has room for does not tell how long requests are, and short ones lose more in
+// pieces than long ones gain: 20,000 of 1 to 60 keys, 4 heads to one of 64, 177 / 286 us, 1,024 of 1 to 2,048, 32 / 8 heads of 128, 786 / 697.
+constexpr long long kWholeUnits = 16;
+// Steps of a worker, at least: one request of 1,500 keys with 1, 2, 4, 8, 16: 44, 32, 28, 30, 38 us; four of them 34, 35, 30, 32, 38.
+constexpr int kLeastSteps = 4;
 constexpr float kGrow = 8.f;    // the maximum moves when it grew by more than 2^kGrow
 
 struct Params {
@@ -670,7 +676,7 @@ Plan plan_of(const XattnArgs& a, int sms) {
     const long long keys = std::min<long long>(a.Lk, (long long)a.win.window + a.win.sinks + a.Lq);
     p.ctas = sms * (p.nr == 1 ? resident_nr<1>(k2, v2) : p.nr == 2 ? resident_nr<2>(k2, v2)
                                                      : p.nr == 3 ? resident_nr<3>(k2, v2) : resident_nr<4>(k2, v2));
-    p.whole = (keys <= kWholeKeys || units >= 16ll * p.ctas) && units <= 0x7fffffffLL;
+    p.whole = (keys <= kWholeKeys || units >= kWholeUnits * p.ctas) && units <= 0x7fffffffLL;
     if (p.whole) {
         p.ctas = (int)units;
         p.heads = 1;

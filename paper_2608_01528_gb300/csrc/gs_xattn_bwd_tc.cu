@@ -20,7 +20,8 @@
 // statistics (-lse log2 e, -D) are laid out per row tile by k_xattn_stats, so that a tile's come with one copy.
 //
 // P and dS go to bf16 for their products (half a step, 2^-8 relative): the other operands, dO, Q and K, are bf16, and the tensor
-// core takes both in one type.  Error of dQ, dK and dV against 64 bits: 2.4e-3 of their norm, 1.7e-3 with fp32 P and dS.
+// core takes both in one type.  Error of dQ, dK and dV against 64 bits: 2.4e-3 of their norm, 1.7e-3 with fp32 P and dS (through windows of 64
+// keys to all of 2,048 2.3e-3 to 2.4e-3, 1.7e-3 the outputs' own rounding).
 //
 // Measured at 2 sequences of 4,096 x 4,096, 32 / 8 heads of 128: dK and dV 0.71 ms, dQ 0.55 ms, statistics 0.03.  dK and dV keep the
 // tensor pipe busy in 77 % of the multiprocessors' active clocks, which are 84 % of the kernel's (512 CTAs on 152 of them), dQ in
@@ -154,8 +155,8 @@ __device__ __forceinline__ float dot_eight(const uint4& x, const uint4& y, float
     return acc;
 }
 
-// Through a window: a row that sees one key at most has no dS, exactly (its weight is 1 whatever its logit), where P (dP - D) would
-// leave a rounding.  kOneKey in D's place says so; a D that is infinite goes there as NaN.
+// Through a window: a row whose span is one key at most has no dS, exactly (its weight is 1 whatever its logit), where P (dP - D) would
+// leave a rounding, as it does where a key mask leaves one key of more.  kOneKey in D's place says so; a D that is infinite goes there as NaN.
 constexpr float kOneKey = INFINITY;
 __device__ __forceinline__ float not_one_key(float nd) { return nd == kOneKey ? NAN : nd; }
 

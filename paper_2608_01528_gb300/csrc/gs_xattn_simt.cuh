@@ -426,7 +426,7 @@ __device__ __forceinline__ void tile_grad(float (&s)[RI][4], float (&dp)[RI][4],
 #pragma unroll
     for (int i = 0; i < RI; ++i) {
         const float L = lse2[ty + 16 * i], D = delta[ty + 16 * i];
-        // (a row that sees one key at most has no dS, exactly: its weight is 1 whatever its logit)
+        // (a row whose span is one key at most has no dS, exactly: its weight is 1 whatever its logit)
         const bool one = WIN && span[i].hi - span[i].lo + min(sinks, span[i].lo) <= 1;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
