@@ -5,11 +5,11 @@
 // one product to the other in registers, and no warp waits for another.  K and V are read once, 16 bytes a lane and copy, three steps
 // in a ring; the table entry of a step is read four steps before it and its rows' addresses are known two before, so a page may end anywhere.
 // A row's reference maximum moves only where it grew by more than 2^8, which spares the reduction over keys in most steps.  The weights go
-// to V in two bf16 terms (error of O against 64 bits 2.1e-3 -> 1.7e-3 of its norm, the output's own rounding; 64 single rows 101 -> 103 us,
-// six rows over long histories 272 -> 285).
+// to V in two bf16 terms (error of O against 64 bits 2.1e-3 -> 1.7e-3 of its norm, the output's own rounding; 64 single rows 101 -> 96 to 103 us,
+// six rows over long histories 272 -> 270 to 305).
 //
 // Bound by memory: 16 keys of 128 + 128 columns are 8 KB and 0.18 us of an SM's share of HBM, in which 32 rows take 96 products of
-// 16 x 8 x 16 (64 x 1 to 4,096 keys, 32 / 8 heads of 128: 5.2 TB/s of calls, 5.9 of the kernel; 8 x 32,769 to 65,537 keys: 5.7 and 6.3).  A tcgen05 tile has 128 rows, of which a decoding step fills 1 to 32, and would add a pass through TMEM to each step.
+// 16 x 8 x 16 (64 x 1 to 4,096 keys, 32 / 8 heads of 128: 5.2 to 5.6 TB/s of calls, 5.9 of the kernel; 8 x 32,769 to 65,537 keys: 5.3 to 5.9 and 5.7).  A tcgen05 tile has 128 rows, of which a decoding step fills 1 to 32, and would add a pass through TMEM to each step.
 //
 // Work.  A unit is a request, a chunk of rows and up to four neighbouring key heads, one to each warp of a CTA, which so read 1 KB of a
 // position together (fewer heads: the warps that are over take runs of their own).  Every worker takes an equal run of the steps of all
