@@ -516,8 +516,8 @@ GS_API gs_status gs_window_attention_backward(const gs_attn* a, const gs_window*
  * n_free), in a captured graph too.  (A request that came short asks again in the next step: without the limit, free_from moves on past
  * the end, and pages that come to the list later are skipped.)  A page that the list has not (too short) is -1 in the table; its tokens
  * have slot -1 and do not count in new_lens; entries of the table or the list outside [0, pages) give slot -1 to tokens that do
- * count.  lens and added count as the nearer end of [0, columns * page_size] and
- * [0, Lnew]; tokens behind the table's last column have no slot.  No output may overlap an input or another output.
+ * count.  lens and added count as the nearer end of [0, columns * page_size] and [0, Lnew]; tokens behind the table's last column
+ * have no slot.  No output may overlap an input or another output.
  * Requires pages * page_size < 2^31, and columns * page_size, B * columns and B * Lnew near it at most.  No workspace.
  * Errors: GS_ERR_INVALID_ARG (a null pointer, overlap), GS_ERR_SHAPE, GS_ERR_ALIGNMENT, GS_ERR_CUDA, GS_ERR_UNSUPPORTED.
  */
