@@ -621,7 +621,8 @@ GS_API gs_status gs_sample_scores(const void* S, int s_dtype, long long N, int M
  * U lies within M 2^-44 / sum(w) of a border between entries: M = 2^17 and w = P_a, of sum 1, 7e-9; a rest of sum 1e-4, 7e-5.  An entry
  * of P_a of 2^-45 or less is never drawn from P_a, and a rest of which no unit is left counts as zero everywhere.
  * P and D: GS_F32 or GS_BF16, strides p_batch, p_row, d_batch, d_row in elements (>= 0), unit stride along M <= 2^19.
- * accepted (B) and tokens are optional, not both NULL; neither may overlap an input or the other.  No workspace.
+ * accepted (B) and tokens are optional, not both NULL; neither may overlap an input or the other (checked
+ * for the dense ones).  No workspace.
  * Errors: GS_ERR_INVALID_ARG (a null pointer, overlap), GS_ERR_SHAPE, GS_ERR_ALIGNMENT, GS_ERR_CUDA, GS_ERR_UNSUPPORTED.
  */
 GS_API gs_status gs_verify_drafts(const void* P, const void* D, int dtype, int B, int K, int M, long long p_batch,
